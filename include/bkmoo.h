@@ -400,6 +400,82 @@ int bkmoo_resolve_launches(int32_t K, int32_t in_dtype, int32_t rule, const int6
 int bkmoo_resolve_path(int32_t K, int32_t in_dtype, int32_t rule, const int64_t* offsets,
                        int64_t n_buckets, uint32_t flags, int32_t* path);
 
+/*
+ * The gated projections of a feed-forward block, with weight gradients kept
+ * apart by language.  The resolve needs one gradient per language.  K backward
+ * passes give them one by one; where the K languages' rows are in one batch, a
+ * linear layer's weight gradients come apart in one pass instead, because each
+ * is a sum over rows: dW_k = sum over language k's rows t of dy_t x_t^T.
+ *
+ * Common to the calls below: matrices are bf16, row-major, rows of `ld*`
+ * elements (>= the width, a multiple of 8) from a 16-byte aligned address;
+ * widths and row counts are arbitrary.  Sums are fp32, each result is rounded
+ * once.  Outputs must not overlap inputs or one another (columns of one wider
+ * matrix may hold different ones).  The kernels wait for nothing but their own
+ * copies and products; a wait that takes more than 2 s all the same gives up
+ * (BKMOO_ERR_TIMEOUT from bkmoo_op_status, the output then undefined).  The
+ * first call on each device comes before any stream capture.
+ */
+typedef enum {
+  BKMOO_SILU = 0,     /* a / (1 + e^-a)                                       */
+  BKMOO_GELU = 1,     /* a Phi(a), Phi the normal distribution                */
+  BKMOO_GELU_TANH = 2 /* a (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))) / 2      */
+} bkmoo_act;
+
+/*
+ * bkmoo_gate_forward -- a = x Wg^T, b = x Wu^T, h = act(a) b, in one kernel.
+ *
+ * x: [T][D]; w_gate, w_up: [F][D], both with rows of ldw.  h, a, b: [T][F]; h
+ * from the unrounded a and b.  a and b (the backward pass's inputs) may both be
+ * NULL; h may be NULL if they are not.  T = 0 queues nothing.
+ */
+int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate, const void* w_up,
+                       int64_t ldw, int64_t T, int64_t D, int64_t F, int32_t act, void* h,
+                       int64_t ldh, void* a, void* b, int64_t ld_ab, void* stream);
+
+/* Bytes of device workspace bkmoo_gate_backward needs (da and db).  Host only. */
+int bkmoo_gate_backward_workspace_size(int64_t T, int64_t F, size_t* bytes);
+
+/*
+ * bkmoo_gate_backward -- from dh, the gradient of h, with a and b as the
+ * forward call gave them: da = dh b act'(a), db = dh act(a), and
+ *   dx = da Wg + db Wu,
+ *   dWg_k = sum_t da_t x_t^T, dWu_k = sum_t db_t x_t^T over language k's rows.
+ *
+ * rows: host, K + 1 row bounds, 0 = rows[0] <= ... <= rows[K] = T; language k
+ * has the rows from rows[k] to rows[k + 1], none if they are equal (its
+ * gradients are then 0).  dx: [T][D], or NULL.  dw_gate, dw_up: host arrays of K
+ * device pointers, each to a contiguous [F][D] of dw_dtype at any element's
+ * address (a place in a flat per-language gradient, say); or both NULL.
+ * accumulate: 0 writes them, 1 adds to what they hold (in fp32, rounded once).
+ * da and db, the operands of bf16 products, are rounded to bf16 between; fp32
+ * gradients are the unrounded fp32 sums of those.  ws: device, 256-byte
+ * aligned, ws_bytes >= bkmoo_gate_backward_workspace_size, not shared by calls
+ * that overlap.
+ */
+int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a, const void* b, int64_t ld_ab,
+                        const void* x, int64_t ldx, const void* w_gate, const void* w_up,
+                        int64_t ldw, int64_t T, int64_t D, int64_t F, int32_t act, int32_t K,
+                        const int64_t* rows, void* dx, int64_t ld_dx, void* const* dw_gate,
+                        void* const* dw_up, int32_t dw_dtype, int32_t accumulate, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/*
+ * bkmoo_language_wgrad -- dW_k = sum over language k's rows t of dy_t x_t^T for
+ * a linear layer y = x W^T: dy [T][M], x [T][N], dW_k [M][N].  rows, dw,
+ * dw_dtype and accumulate as in bkmoo_gate_backward.
+ */
+int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int64_t T,
+                         int64_t M, int64_t N, int32_t K, const int64_t* rows, void* const* dw,
+                         int32_t dw_dtype, int32_t accumulate, void* stream);
+
+/*
+ * bkmoo_op_status -- synchronise `stream` and read the current device's status
+ * word of the gate and weight-gradient calls: BKMOO_OK, or BKMOO_ERR_TIMEOUT if
+ * one of them gave up since it was last read.  Clears it.  Writes *status.
+ */
+int bkmoo_op_status(void* stream, int32_t* status);
+
 /* Static English text for a bkmoo_status value. */
 const char* bkmoo_status_string(int32_t status);
 

@@ -1,0 +1,253 @@
+// The gated projections of a feed-forward block, forward and backward, and the
+// per-language weight gradient of a linear layer (include/bkmoo.h): argument
+// checks, the choice of tiles, and the pass that turns dh into da and db.  The
+// products are tile_gemm.cuh's.
+#include "tile_host.cuh"
+
+namespace bkmoo {
+namespace {
+
+bool act_ok(int32_t act) { return act == BKMOO_SILU || act == BKMOO_GELU || act == BKMOO_GELU_TANH; }
+int32_t up(int64_t n, int64_t by) { return (int32_t)((n + by - 1) / by); }
+
+// act(a) and act'(a) (tile_gemm.cuh: activation).
+__device__ __forceinline__ void activation_slope(int act, float a, float* f, float* df) {
+  if (act == BKMOO_SILU) {
+    const float s = sigmoid(a);
+    *f = a * s;
+    *df = s * (1.0f + a * (1.0f - s));
+  } else if (act == BKMOO_GELU) {
+    const float c = 0.5f * erfcf(-0.70710678f * a);
+    *f = a * c;
+    *df = c + a * 0.39894228f * __expf(-0.5f * a * a);
+  } else {
+    const float q = a * a, s = sigmoid(1.59576912f * a * (1.0f + 0.044715f * q));
+    *f = a * s;
+    *df = s + a * s * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * q);
+  }
+}
+
+struct SlopeArgs {
+  const __nv_bfloat16 *dh, *a, *b;
+  __nv_bfloat16 *da, *db;
+  int64_t ld_dh, ld_ab, ld_d;
+  int64_t rows;
+  int32_t cols, act;
+};
+
+// da = dh b act'(a), db = dh act(a).  Bound by memory: 10 bytes an element, in
+// vectors of 8 (one thread one vector; the last of a row element by element).
+// The products behind it take bf16 operands, so da and db are rounded to bf16
+// here, once, from fp32.
+__global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
+  const int64_t per = (p.cols + 7) / 8, n = p.rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
+       i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t row = n < (1ll << 32) ? (uint32_t)i / (uint32_t)per : i / per;
+    const int col = (int)(i - row * per) * 8;
+    const __nv_bfloat16 *dh = p.dh + row * p.ld_dh + col, *a = p.a + row * p.ld_ab + col,
+                        *b = p.b + row * p.ld_ab + col;
+    __nv_bfloat16 *da = p.da + row * p.ld_d + col, *db = p.db + row * p.ld_d + col;
+    if (col + 8 <= p.cols) {
+      const uint4 xh = __ldg(reinterpret_cast<const uint4*>(dh)), xa = __ldg(reinterpret_cast<const uint4*>(a)),
+                  xb = __ldg(reinterpret_cast<const uint4*>(b));
+      const uint32_t h[4] = {xh.x, xh.y, xh.z, xh.w}, u[4] = {xa.x, xa.y, xa.z, xa.w},
+                     v[4] = {xb.x, xb.y, xb.z, xb.w};
+      uint32_t oa[4], ob[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float f0, d0, f1, d1;
+        const float h0 = __uint_as_float(h[j] << 16), h1 = __uint_as_float(h[j] & 0xffff0000u);
+        activation_slope(p.act, __uint_as_float(u[j] << 16), &f0, &d0);
+        activation_slope(p.act, __uint_as_float(u[j] & 0xffff0000u), &f1, &d1);
+        oa[j] = pack_bf16(h0 * __uint_as_float(v[j] << 16) * d0,
+                          h1 * __uint_as_float(v[j] & 0xffff0000u) * d1);
+        ob[j] = pack_bf16(h0 * f0, h1 * f1);
+      }
+      *reinterpret_cast<uint4*>(da) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+      *reinterpret_cast<uint4*>(db) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+    } else {
+      for (int j = 0; col + j < p.cols; ++j) {
+        float f, d;
+        const float h = __bfloat162float(dh[j]);
+        activation_slope(p.act, __bfloat162float(a[j]), &f, &d);
+        da[j] = __float2bfloat16_rn(h * __bfloat162float(b[j]) * d);
+        db[j] = __float2bfloat16_rn(h * f);
+      }
+    }
+  }
+}
+
+// Whether the CTAs work in pairs.
+int choose_pair(int64_t rows) { return 1; }
+
+// dW_k = dy_k^T x_k for one or two dy (mats), every language.
+int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, int64_t ldx,
+                 int64_t M, int64_t N, int32_t K, const int64_t* rows, void* const* const* dw,
+                 int32_t dw_dtype, int32_t accumulate, cudaStream_t s) {
+  const int cg = choose_pair(M);
+  TileArgs<kWeight> p = {};
+  int r = tile_status_word(s, &p.status);
+  if (r != BKMOO_OK) return r;
+  const int elem = dw_dtype == BKMOO_F32 ? 4 : 2;
+  bool any = false;
+  for (int k = 0; k < K; ++k) {
+    const int64_t n = rows[k + 1] - rows[k], at = rows[k];
+    p.nkt[k] = up(n, kTileK);
+    int j = k;                                  // insertion by falling length
+    while (j > 0 && p.nkt[p.order[j - 1]] < p.nkt[k]) p.order[j] = p.order[j - 1], --j;
+    p.order[j] = k;
+    for (int i = 0; i < mats; ++i) {
+      p.out[i * kMaxK + k] = dw[i][k];
+      p.vec[i * kMaxK + k] = store_width(dw[i][k], N, elem);
+    }
+    any = any || n > 0 || !accumulate;
+    if (n == 0) continue;
+    r = tile_map(&p.b[k], static_cast<const __nv_bfloat16*>(x) + at * ldx, n, N, ldx, kTileK);
+    for (int i = 0; i < mats && r == BKMOO_OK; ++i)
+      r = tile_map(&p.a[i * kMaxK + k], static_cast<const __nv_bfloat16*>(dy[i]) + at * ld_dy, n, M,
+                   ld_dy, kTileK);
+    if (r != BKMOO_OK) return r;
+  }
+  if (!any) return BKMOO_OK;
+  p.rows = (int32_t)M;
+  p.cols = (int32_t)N;
+  p.tiles_m = up(M, kTileM * cg);
+  p.tiles_n = up(N, kTileN);
+  p.mats = mats;
+  p.n_lang = K;
+  p.out_dtype = dw_dtype;
+  p.accumulate = accumulate;
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * mats * K;
+  if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
+  p.tiles = (int32_t)tiles;
+  return tile_launch(tile_weight_fn(cg), cg, &p, tiles, s);
+}
+
+bool grads_ok(void* const* dw, int32_t K, int32_t dtype) {
+  if (!dw) return false;
+  for (int k = 0; k < K; ++k)
+    if (!dw[k] || ((uintptr_t)dw[k] & (dtype == BKMOO_F32 ? 3u : 1u))) return false;
+  return true;
+}
+
+}  // namespace
+}  // namespace bkmoo
+
+using namespace bkmoo;
+
+extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate, const void* w_up,
+                                  int64_t ldw, int64_t T, int64_t D, int64_t F, int32_t act,
+                                  void* h, int64_t ldh, void* a, void* b, int64_t ld_ab,
+                                  void* stream) {
+  if (!act_ok(act) || !operand_ok(w_gate, F, D, ldw) || !operand_ok(w_up, F, D, ldw) || T < 0 ||
+      (a == nullptr) != (b == nullptr))
+    return BKMOO_ERR_INVALID;
+  if (T == 0) return BKMOO_OK;
+  if (!operand_ok(x, T, D, ldx) || (!h && !a) || (h && !operand_ok(h, T, F, ldh)) ||
+      (a && (!operand_ok(a, T, F, ld_ab) || !operand_ok(b, T, F, ld_ab))))
+    return BKMOO_ERR_INVALID;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int cg = choose_pair(T);
+  TileArgs<kGate> p = {};
+  int r = tile_status_word(s, &p.status);
+  if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, 128);
+  if (r == BKMOO_OK) r = tile_map(&p.b[0], w_gate, F, D, ldw, 128);
+  if (r == BKMOO_OK) r = tile_map(&p.b[1], w_up, F, D, ldw, 128);
+  if (r != BKMOO_OK) return r;
+  p.out[0] = {h, ldh, store_width(h, ldh, 2)};
+  p.out[1] = {a, ld_ab, store_width(a, ld_ab, 2)};
+  p.out[2] = {b, ld_ab, store_width(b, ld_ab, 2)};
+  p.rows = (int32_t)T;
+  p.cols = (int32_t)F;
+  p.tiles_m = up(T, kTileM * cg);
+  p.tiles_n = up(F, kTileN / 2);
+  p.nkt = up(D, kTileK);
+  p.act = act;
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
+  p.tiles = (int32_t)tiles;
+  return tile_launch(tile_gate_fn(cg), cg, &p, tiles, s);
+}
+
+extern "C" int bkmoo_gate_backward_workspace_size(int64_t T, int64_t F, size_t* bytes) {
+  if (!bytes || T < 0 || F < 1) return BKMOO_ERR_INVALID;
+  *bytes = 2 * align256((size_t)T * (size_t)((F + 7) / 8 * 8) * 2);
+  return BKMOO_OK;
+}
+
+extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a, const void* b,
+                                   int64_t ld_ab, const void* x, int64_t ldx, const void* w_gate,
+                                   const void* w_up, int64_t ldw, int64_t T, int64_t D, int64_t F,
+                                   int32_t act, int32_t K, const int64_t* rows, void* dx,
+                                   int64_t ld_dx, void* const* dw_gate, void* const* dw_up,
+                                   int32_t dw_dtype, int32_t accumulate, void* ws, size_t ws_bytes,
+                                   void* stream) {
+  const bool weights = dw_gate || dw_up;
+  if (!act_ok(act) || T < 0 || (dw_dtype != BKMOO_F32 && dw_dtype != BKMOO_BF16) ||
+      !operand_ok(w_gate, F, D, ldw) || !operand_ok(w_up, F, D, ldw) || !languages_ok(rows, K, T) ||
+      (!dx && !weights && T > 0) ||
+      (weights && (!grads_ok(dw_gate, K, dw_dtype) || !grads_ok(dw_up, K, dw_dtype))))
+    return BKMOO_ERR_INVALID;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int64_t ld = (F + 7) / 8 * 8;
+  __nv_bfloat16* d[2] = {nullptr, nullptr};
+  if (T > 0) {
+    if (!operand_ok(dh, T, F, ld_dh) || !operand_ok(a, T, F, ld_ab) || !operand_ok(b, T, F, ld_ab) ||
+        !operand_ok(x, T, D, ldx) || (dx && !operand_ok(dx, T, D, ld_dx)) || !ws ||
+        ((uintptr_t)ws & 255u))
+      return BKMOO_ERR_INVALID;
+    size_t need = 0;
+    (void)bkmoo_gate_backward_workspace_size(T, F, &need);
+    if (ws_bytes < need) return BKMOO_ERR_WORKSPACE;
+    d[0] = static_cast<__nv_bfloat16*>(ws);
+    d[1] = d[0] + need / 4;
+    int sms = 0;
+    const int r = tile_sms(&sms);
+    if (r != BKMOO_OK) return r;
+    SlopeArgs q = {static_cast<const __nv_bfloat16*>(dh), static_cast<const __nv_bfloat16*>(a),
+                   static_cast<const __nv_bfloat16*>(b), d[0], d[1], ld_dh, ld_ab, ld, T, (int32_t)F, act};
+    const int64_t blocks = (T * (ld / 8) + 255) / 256, most = (int64_t)sms * 8;
+    gate_slope_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(q);
+    if (cudaGetLastError() != cudaSuccess) return BKMOO_ERR_CUDA;
+  }
+  if (dx && T > 0) {
+    const int cg = choose_pair(T);
+    TileArgs<kInput> p = {};
+    int r = tile_status_word(s, &p.status);
+    const void* w[2] = {w_gate, w_up};
+    for (int i = 0; i < 2 && r == BKMOO_OK; ++i) {
+      r = tile_map(&p.a[i], d[i], T, F, ld, 128);
+      if (r == BKMOO_OK) r = tile_map(&p.b[i], w[i], F, D, ldw, kTileK);
+    }
+    if (r != BKMOO_OK) return r;
+    p.out = {dx, ld_dx, store_width(dx, ld_dx, 2)};
+    p.rows = (int32_t)T;
+    p.cols = (int32_t)D;
+    p.tiles_m = up(T, kTileM * cg);
+    p.tiles_n = up(D, kTileN);
+    p.nkt = up(F, kTileK);
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+    if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
+    p.tiles = (int32_t)tiles;
+    r = tile_launch(tile_input_fn(cg), cg, &p, tiles, s);
+    if (r != BKMOO_OK) return r;
+  }
+  if (!weights) return BKMOO_OK;
+  const void* dy[2] = {d[0], d[1]};
+  void* const* dw[2] = {dw_gate, dw_up};
+  return weight_grads(dy, ld, 2, x, ldx, F, D, K, rows, dw, dw_dtype, accumulate, s);
+}
+
+extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
+                                    int64_t T, int64_t M, int64_t N, int32_t K, const int64_t* rows,
+                                    void* const* dw, int32_t dw_dtype, int32_t accumulate,
+                                    void* stream) {
+  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
+  if (T < 0 || M < 1 || N < 1 || M > kMost || N > kMost || !languages_ok(rows, K, T) ||
+      (dw_dtype != BKMOO_F32 && dw_dtype != BKMOO_BF16) || !grads_ok(dw, K, dw_dtype) ||
+      (T > 0 && (!operand_ok(dy, T, M, ld_dy) || !operand_ok(x, T, N, ldx))))
+    return BKMOO_ERR_INVALID;
+  return weight_grads(&dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate,
+                      static_cast<cudaStream_t>(stream));
+}

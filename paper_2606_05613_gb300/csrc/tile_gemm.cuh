@@ -1,0 +1,458 @@
+// The matrix products of the gated projections and of the per-language weight
+// gradients, on the tensor cores: one persistent kernel in three kinds.
+//
+//   kGate    [a | b] = x [Wg; Wu]^T, h = act(a) b       sum over the input width
+//   kInput   dx = da Wg + db Wu                         sum over the hidden width
+//   kWeight  dW_k = dy_k^T x_k for every language k     sum over its rows
+//
+// A tile is 128 rows (256 with a CTA pair) by 256 columns of fp32 accumulators;
+// for kGate 128 columns of a and the same 128 of b, so that h is formed where
+// both are.  Warp 8 of a CTA copies operand tiles of 64 along the sum into a
+// ring of stages (TMA, 128-byte swizzle, rows and columns beyond the matrix are
+// zeros), one thread of warp 9 issues the products (tcgen05) into one of two
+// accumulators in tensor memory, and warps 0-7 take the other to global memory
+// meanwhile.  Operands whose sum runs across their rows (kInput's W, kWeight's
+// dy and x) are read as they lie: the products take them across, no transposed
+// copy is made.  All sums are fp32; a result is rounded once, when it is stored.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "tensor_core.cuh"
+
+namespace bkmoo {
+
+enum TileKind { kGate = 0, kInput = 1, kWeight = 2 };
+
+constexpr int kTileM = 128;    // rows of a CTA's tile
+constexpr int kTileN = 256;    // accumulator columns
+constexpr int kTileK = 64;     // of the sum per stage: 128 bytes, the swizzle's row
+constexpr int kTileEpilogueWarps = 8;
+constexpr int kTileThreads = 32 * (kTileEpilogueWarps + 2);
+constexpr int kTileGroupM = 8;  // tiles of rows that are worked on together
+
+__host__ __device__ constexpr int tile_stages(int cg) { return cg == 1 ? 4 : 6; }
+__host__ __device__ constexpr int tile_b_bytes(int cg) { return (cg == 1 ? 256 : 128) * kTileK * 2; }
+__host__ __device__ constexpr int tile_stage_bytes(int cg) {
+  return kTileM * kTileK * 2 + tile_b_bytes(cg);
+}
+__host__ __device__ constexpr int tile_smem(int cg) {
+  return tile_stages(cg) * tile_stage_bytes(cg) + 1024;   // stages start on 1024 bytes
+}
+
+// Where a result goes: rows of `ld` elements.  `vec` is the widest store that
+// every row's 32-column pieces allow: 32, 16 or 0 bytes (element by element).
+struct TileOut {
+  void* p;
+  int64_t ld;
+  int32_t vec;
+};
+
+template <int KIND>
+struct TileArgs;
+
+template <>
+struct TileArgs<kGate> {
+  CUtensorMap a, b[2];          // x; Wg, Wu
+  TileOut out[3];               // h, a, b; p = NULL: not wanted
+  int32_t* status;
+  int32_t rows, cols;           // T, F
+  int32_t tiles_m, tiles_n, tiles;
+  int32_t nkt;
+  int32_t act;
+};
+template <>
+struct TileArgs<kInput> {
+  CUtensorMap a[2], b[2];       // da, db; Wg, Wu
+  TileOut out;                  // dx
+  int32_t* status;
+  int32_t rows, cols;           // T, D
+  int32_t tiles_m, tiles_n, tiles;
+  int32_t nkt;                  // of one of the two products
+};
+// Up to two matrices dy (da and db) against one x, for every language.  Empty
+// languages have no map; their gradient is zero.
+template <>
+struct TileArgs<kWeight> {
+  CUtensorMap a[2 * kMaxK], b[kMaxK];
+  void* out[2 * kMaxK];         // [matrix][language], contiguous rows of `cols`
+  int32_t vec[2 * kMaxK];
+  int32_t nkt[kMaxK];
+  int32_t order[kMaxK];         // languages, the longest first
+  int32_t* status;
+  int32_t rows, cols;
+  int32_t tiles_m, tiles_n, tiles;
+  int32_t mats, n_lang;
+  int32_t out_dtype, accumulate;
+};
+
+struct Tile {
+  int g, m0, n0, nkt;   // g: kWeight's matrix * kMaxK + language
+};
+
+template <int KIND, int CG>
+__device__ __forceinline__ Tile tile_at(const TileArgs<KIND>& p, int t) {
+  Tile r;
+  int i = t;
+  r.g = 0;
+  if constexpr (KIND == kWeight) {
+    const int per = p.tiles_m * p.tiles_n;
+    const int unit = t / per;                 // language by language, its matrices in turn
+    i = t - unit * per;
+    const int lang = p.order[unit / p.mats];
+    r.g = (unit % p.mats) * kMaxK + lang;
+    r.nkt = p.nkt[lang];
+  } else if constexpr (KIND == kInput) {
+    r.nkt = 2 * p.nkt;
+  } else {
+    r.nkt = p.nkt;
+  }
+  // kTileGroupM tiles of rows at a time, so that the tiles in flight share both
+  // their rows' and their columns' operands in L2
+  const int band = kTileGroupM * p.tiles_n, b = i / band;
+  const int first = b * kTileGroupM;
+  const int high = p.tiles_m - first < kTileGroupM ? p.tiles_m - first : kTileGroupM;
+  const int j = i - b * band;
+  r.m0 = (first + j % high) * (kTileM * CG);
+  r.n0 = (j / high) * (KIND == kGate ? kTileN / 2 : kTileN);
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&t);
+}
+__device__ __forceinline__ void st_global32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]),
+               "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+// 32 columns of one row, the first n of which exist.
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&v)[32], int n, int vec) {
+  if (vec != 0 && n >= 32) {
+    uint32_t w[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    if (vec == 32) {
+      st_global32(p, w);
+      st_global32(p + 16, w + 8);
+    } else {
+      uint4* q = reinterpret_cast<uint4*>(p);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < n) p[j] = __float2bfloat16_rn(v[j]);
+}
+__device__ __forceinline__ void store_row(float* p, const float (&v)[32], int n, int vec) {
+  if (vec != 0 && n >= 32) {
+    float4* q = reinterpret_cast<float4*>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < n) p[j] = v[j];
+}
+__device__ __forceinline__ void add_row(const __nv_bfloat16* p, float (&v)[32], int n, int vec) {
+  if (vec != 0 && n >= 32) {
+    const uint4* q = reinterpret_cast<const uint4*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint4 x = q[j];
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[8 * j + 2 * i] += __uint_as_float(w[i] << 16);
+        v[8 * j + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < n) v[j] += __bfloat162float(p[j]);
+}
+__device__ __forceinline__ void add_row(const float* p, float (&v)[32], int n, int vec) {
+  if (vec != 0 && n >= 32) {
+    const float4* q = reinterpret_cast<const float4*>(p);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float4 x = q[j];
+      v[4 * j] += x.x;
+      v[4 * j + 1] += x.y;
+      v[4 * j + 2] += x.z;
+      v[4 * j + 3] += x.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 32; ++j)
+    if (j < n) v[j] += p[j];
+}
+
+__device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int col,
+                                           const float (&v)[32], int n) {
+  if (o.p) store_row(static_cast<__nv_bfloat16*>(o.p) + row * o.ld + col, v, n, o.vec);
+}
+
+// act(a).  silu a / (1 + e^-a); gelu a Phi(a) with Phi(a) = erfc(-a / sqrt 2) / 2;
+// gelu_tanh a / (1 + e^(-2 z)), z = sqrt(2/pi) (a + 0.044715 a^3), which is
+// a (1 + tanh z) / 2 without its cancellation.  The fast exponential and
+// quotient are good to about 2^-20 of the result, a 2^11th of a bf16 rounding.
+__device__ __forceinline__ float sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }
+__device__ __forceinline__ float activation(int act, float a) {
+  if (act == BKMOO_SILU) return a * sigmoid(a);
+  if (act == BKMOO_GELU) return a * 0.5f * erfcf(-0.70710678f * a);
+  return a * sigmoid(1.59576912f * (a + 0.044715f * a * a * a));
+}
+
+template <int CG>
+struct TileShared {
+  uint64_t full[tile_stages(CG)], empty[tile_stages(CG)];   // full: the first CTA's, for both
+  uint64_t tfull[2], tempty[2];                             // tempty: the first CTA's, for both
+  uint64_t drain;
+  uint32_t tmem;
+  int abort;
+};
+
+// Operand tiles of one step of the sum.
+template <int KIND, int CG>
+__device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t, int kt,
+                                          unsigned rank, unsigned char* a, unsigned char* b,
+                                          uint32_t bar) {
+  const int m = t.m0 + (int)rank * kTileM;
+  if constexpr (KIND == kGate) {
+    tile_load<CG>(a, &p.a, kt * kTileK, m, bar);
+    if (CG == 1) {
+      tile_load<CG>(b, &p.b[0], kt * kTileK, t.n0, bar);
+      tile_load<CG>(b + 128 * kTileK * 2, &p.b[1], kt * kTileK, t.n0, bar);
+    } else {
+      tile_load<CG>(b, &p.b[rank], kt * kTileK, t.n0, bar);
+    }
+  } else {
+    const CUtensorMap* bm;
+    int y;
+    if constexpr (KIND == kInput) {
+      const int second = kt >= p.nkt;
+      y = (kt - (second ? p.nkt : 0)) * kTileK;
+      tile_load<CG>(a, &p.a[second], y, m, bar);
+      bm = &p.b[second];
+    } else {
+      y = kt * kTileK;
+      tile_load<CG>(a, &p.a[t.g], m, y, bar);
+      tile_load<CG>(a + 64 * kTileK * 2, &p.a[t.g], m + 64, y, bar);
+      bm = &p.b[t.g % kMaxK];
+    }
+    const int n = t.n0 + (int)rank * 128;
+#pragma unroll
+    for (int c = 0; c < (CG == 1 ? 4 : 2); ++c)
+      tile_load<CG>(b + c * 64 * kTileK * 2, bm, n + 64 * c, y, bar);
+  }
+}
+
+// One warp's share of a finished tile: rows of its quarter, columns of its half.
+// `acc`: the accumulator's tensor-memory address for this warp's lanes; `empty`:
+// the tile's sum is empty and the accumulator was not written.
+template <int KIND>
+__device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t, int row, int half,
+                                          uint32_t acc, bool empty) {
+  const bool live = row < p.rows;
+  if constexpr (KIND == kGate) {
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+      const int at = 64 * half + 32 * c, n = p.cols - (t.n0 + at);
+      uint32_t ra[32], rb[32];
+      tc_load32(ra, acc + at);
+      tc_load32(rb, acc + 128 + at);
+      tc_landed(ra);
+      tc_landed(rb);
+      if (live && n > 0) {
+        float a[32], b[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+          a[j] = __uint_as_float(ra[j]);
+          b[j] = __uint_as_float(rb[j]);
+        }
+        store_bf16(p.out[1], row, t.n0 + at, a, n);
+        store_bf16(p.out[2], row, t.n0 + at, b, n);
+        if (p.out[0].p) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) a[j] = activation(p.act, a[j]) * b[j];
+          store_bf16(p.out[0], row, t.n0 + at, a, n);
+        }
+      }
+      __syncwarp();   // the loads are the whole warp's
+    }
+  } else {
+#pragma unroll 1
+    for (int c = 0; c < 4; ++c) {
+      const int at = 128 * half + 32 * c, n = p.cols - (t.n0 + at);
+      uint32_t r[32];
+      if (!empty) {
+        tc_load32(r, acc + at);
+        tc_landed(r);
+      }
+      if (live && n > 0) {
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[j]);
+        if constexpr (KIND == kInput) {
+          store_bf16(p.out, row, t.n0 + at, v, n);
+        } else if (!(empty && p.accumulate)) {
+          const int64_t to = (int64_t)row * p.cols + t.n0 + at;
+          if (p.out_dtype == BKMOO_BF16) {
+            __nv_bfloat16* q = static_cast<__nv_bfloat16*>(p.out[t.g]) + to;
+            if (p.accumulate) add_row(q, v, n, p.vec[t.g]);
+            store_row(q, v, n, p.vec[t.g]);
+          } else {
+            float* q = static_cast<float*>(p.out[t.g]) + to;
+            if (p.accumulate) add_row(q, v, n, p.vec[t.g]);
+            store_row(q, v, n, p.vec[t.g]);
+          }
+        }
+      }
+      __syncwarp();   // the loads are the whole warp's
+    }
+  }
+}
+
+template <int KIND, int CG>
+__global__ void __launch_bounds__(kTileThreads, 1)
+    tile_gemm_kernel(const __grid_constant__ TileArgs<KIND> p) {
+  constexpr int S = tile_stages(CG), A_BYTES = kTileM * kTileK * 2;
+  constexpr bool A_ACROSS = KIND == kWeight, B_ACROSS = KIND != kGate;
+  extern __shared__ unsigned char raw[];
+  __shared__ TileShared<CG> sh;
+  unsigned char* ring = raw + ((1024 - (st_smem(raw) & 1023)) & 1023);
+  const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned rank = CG == 1 ? 0 : cluster_rank();
+  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      bar_init(&sh.full[i], 1);
+      bar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(&sh.tfull[i], 1);
+      bar_init(&sh.tempty[i], CG * kTileEpilogueWarps);
+    }
+    bar_init(&sh.drain, 1);
+    sh.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (wid == kTileEpilogueWarps + 1) {
+    tmem_alloc<CG>(&sh.tmem, 512);
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (CG == 2) cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = sh.tmem;
+  volatile int* abort = &sh.abort;
+
+  if (wid == kTileEpilogueWarps) {
+    if (elect_one()) {
+      int s = 0, laps = 0;
+      for (int i = first; i < p.tiles && !*abort; i += stride) {
+        const Tile t = tile_at<KIND, CG>(p, i);
+        for (int kt = 0; kt < t.nkt; ++kt) {
+          if (!bar_wait<CG>(&sh.empty[s], (laps & 1) ^ 1, abort)) break;
+          unsigned char* a = ring + s * tile_stage_bytes(CG);
+          const uint32_t bar = CG == 1 ? st_smem(&sh.full[s]) : peer_smem(&sh.full[s], 0);
+          if (rank == 0) bar_arrive_tx(&sh.full[s], CG * tile_stage_bytes(CG));
+          load_step<KIND, CG>(p, t, kt, rank, a, a + A_BYTES, bar);
+          if (++s == S) s = 0, ++laps;
+        }
+      }
+      // every copy has landed and been used before the CTA ends
+      for (int i = 0; i < S; ++i) {
+        if (!bar_wait<CG>(&sh.empty[s], (laps & 1) ^ 1, abort) && rank == 0 && laps > 0) {
+          int none = 0;
+          bar_wait<CG>(&sh.full[s], (laps & 1) ^ 1, &none);
+        }
+        if (++s == S) s = 0, ++laps;
+      }
+    }
+  } else if (wid == kTileEpilogueWarps + 1) {
+    if (rank == 0 && elect_one()) {
+      constexpr uint32_t desc = product_desc(kTileM * CG, kTileN, A_ACROSS, B_ACROSS);
+      constexpr uint32_t chunk = 64 * kTileK * 2;
+      // 16 of the sum: 32 bytes along a swizzled row, or 16 rows of 128 bytes
+      constexpr uint32_t a_step = A_ACROSS ? 2048 : 32, b_step = B_ACROSS ? 2048 : 32;
+      int s = 0, laps = 0, n = 0;
+      for (int i = first; i < p.tiles && !*abort; i += stride) {
+        const Tile t = tile_at<KIND, CG>(p, i);
+        if (t.nkt == 0) continue;
+        const int acc = n & 1;
+        if (!bar_wait<CG>(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort)) break;
+        tc_fence_after();
+        const uint32_t d = tmem + acc * kTileN;
+        for (int kt = 0; kt < t.nkt; ++kt) {
+          if (!bar_wait<CG>(&sh.full[s], laps & 1, abort)) break;
+          tc_fence_after();
+          const uint32_t a = st_smem(ring + s * tile_stage_bytes(CG)), b = a + A_BYTES;
+#pragma unroll
+          for (int k = 0; k < kTileK / 16; ++k)
+            tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
+                             desc, kt > 0 || k > 0);
+          products_arrive<CG>(&sh.empty[s]);
+          if (++s == S) s = 0, ++laps;
+        }
+        products_arrive<CG>(&sh.tfull[acc]);
+        ++n;
+      }
+      if (*abort) {
+        // no product is in flight when tensor memory is handed back
+        int none = 0;
+        products_arrive<CG>(&sh.drain);
+        bar_wait<CG>(&sh.drain, 0, &none);
+      }
+    }
+  } else {
+    const int quarter = wid & 3, half = wid >> 2;
+    int n = 0;
+    for (int i = first; i < p.tiles; i += stride) {
+      const Tile t = tile_at<KIND, CG>(p, i);
+      const int acc = n & 1;
+      bool ok = true;
+      if (t.nkt > 0) {
+        ok = bar_wait<CG>(&sh.tfull[acc], (n >> 1) & 1, abort);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
+      take_tile<KIND>(p, t, row, half, tmem + ((uint32_t)(quarter * 32) << 16) + acc * kTileN, t.nkt == 0);
+      if (t.nkt > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank == 0) bar_arrive(&sh.tempty[acc]);
+          else bar_arrive_at(peer_smem(&sh.tempty[acc], 0));
+        }
+        ++n;
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (CG == 2) cluster_sync();
+  tc_fence_after();
+  if (wid == kTileEpilogueWarps + 1) tmem_free<CG>(tmem, 512);
+  if (threadIdx.x == 0 && sh.abort) atomicCAS(p.status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
+}
+
+// The kernels, one translation unit each (nvcc runs them side by side).
+const void* tile_gate_fn(int cg);
+const void* tile_input_fn(int cg);
+const void* tile_weight_fn(int cg);
+
+}  // namespace bkmoo

@@ -1,0 +1,38 @@
+// Host helpers of the tile kernels' entry points: tensor maps, launches and the
+// device word that notes a wait that gave up.
+#pragma once
+
+#include "tile_gemm.cuh"
+
+namespace bkmoo {
+
+// A bf16 matrix that the tile kernels read: rows of `ld` elements.
+inline bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) {
+  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;   // coordinates are 32 bits
+  return p && ((uintptr_t)p & 15u) == 0 && rows >= 0 && rows <= kMost && cols >= 1 &&
+         cols <= kMost && ld >= cols && ld % 8 == 0 && ld <= ((int64_t)1 << 38);
+}
+// Language bounds: 0 = rows[0] <= rows[1] <= ... <= rows[K] = T.
+inline bool languages_ok(const int64_t* rows, int32_t K, int64_t T) {
+  if (!rows || K < 1 || K > kMaxK || rows[0] != 0 || rows[K] != T) return false;
+  for (int k = 0; k < K; ++k)
+    if (rows[k + 1] < rows[k]) return false;
+  return true;
+}
+// Widest store that 32-column pieces of every row allow (tile_gemm.cuh).
+inline int store_width(const void* p, int64_t ld, int elem) {
+  const uintptr_t at = (uintptr_t)p | (uintptr_t)(ld * elem);
+  return (at & 31u) == 0 ? 32 : (at & 15u) == 0 ? 16 : 0;
+}
+
+// Map of a matrix (rows x cols bf16, rows of ld elements) read in boxes of 64
+// columns by box_rows rows.
+int tile_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows);
+// SMs of the current device.
+int tile_sms(int* sms);
+// The device's status word for kernels that may give up.
+int tile_status_word(cudaStream_t s, int32_t** word);
+// Queues a tile kernel over `tiles` tiles, by CTAs or pairs of CTAs.
+int tile_launch(const void* fn, int cg, void* args, int64_t tiles, cudaStream_t s);
+
+}  // namespace bkmoo

@@ -34,10 +34,12 @@ BKMOO_FLAG_FUSED = 0x4
 BKMOO_FLAG_THREE_PASS = 0x8
 BKMOO_FLAG_TEST_WITHHOLD = 0x100
 BKMOO_FLAG_TEST_WITHHOLD_EXCHANGE = 0x200
+BKMOO_SILU, BKMOO_GELU, BKMOO_GELU_TANH = 0, 1, 2
 BKMOO_NOALLOC_SCRATCH_BYTES = 32 << 20
 BKMOO_NOALLOC_MAX_BUCKETS = 4096
 
 RULES = {"mgda": BKMOO_MGDA, "pcgrad": BKMOO_PCGRAD, "cagrad": BKMOO_CAGRAD, "mean": BKMOO_MEAN}
+ACTS = {"silu": BKMOO_SILU, "gelu": BKMOO_GELU, "gelu_tanh": BKMOO_GELU_TANH}
 
 _lock = threading.Lock()
 _lib = None
@@ -114,6 +116,20 @@ def load():
                                                ctypes.POINTER(ctypes.c_int32)]
         lib.bkmoo_selftest_fp64.restype = ctypes.c_int
         lib.bkmoo_selftest_fp64.argtypes = [i32, vp, vp, vp, i64, vp]
+        lib.bkmoo_gate_forward.restype = ctypes.c_int
+        lib.bkmoo_gate_forward.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, i32, vp, i64, vp,
+                                           vp, i64, vp]
+        lib.bkmoo_gate_backward_workspace_size.restype = ctypes.c_int
+        lib.bkmoo_gate_backward_workspace_size.argtypes = [i64, i64, ctypes.POINTER(sz)]
+        lib.bkmoo_gate_backward.restype = ctypes.c_int
+        lib.bkmoo_gate_backward.argtypes = [vp, i64, vp, vp, i64, vp, i64, vp, vp, i64, i64, i64,
+                                            i64, i32, i32, vp, vp, i64, vp, vp, i32, i32, vp, sz,
+                                            vp]
+        lib.bkmoo_language_wgrad.restype = ctypes.c_int
+        lib.bkmoo_language_wgrad.argtypes = [vp, i64, vp, i64, i64, i64, i64, i32, vp, vp, i32,
+                                             i32, vp]
+        lib.bkmoo_op_status.restype = ctypes.c_int
+        lib.bkmoo_op_status.argtypes = [vp, ctypes.POINTER(i32)]
         _lib = lib
         return lib
 
@@ -330,6 +346,151 @@ def bkmoo_selftest_fp64(op: int, a, b, out, stream=None):
     _check(load().bkmoo_selftest_fp64(op, a.data_ptr(), b.data_ptr() if b is not None else None,
                                       out.data_ptr(), int(out.numel()),
                                       _stream_handle(stream, out.device)), "bkmoo_selftest_fp64")
+
+
+def _matrix(t, rows: int, cols: int, what: str):
+    """(address, row stride) of a bf16 CUDA matrix the tile kernels take."""
+    import torch
+    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError("%s must be a bfloat16 CUDA matrix of %d x %d" % (what, rows, cols))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    ld = t.stride(0) if rows > 1 else (cols + 7) // 8 * 8
+    if ld < cols or ld % 8 or t.data_ptr() % 16:
+        raise ValueError("%s: rows must start on 16 bytes (pad them to a multiple of 8 elements)"
+                         % what)
+    return t.data_ptr(), ld
+
+
+def _language_rows(rows, T: int):
+    r = _offsets_array(rows)
+    if r.ndim != 1 or not 2 <= len(r) <= 17 or r[0] != 0 or r[-1] != T or (np.diff(r) < 0).any():
+        raise ValueError("rows must be K + 1 bounds from 0 to the number of rows, 1 <= K <= 16")
+    return r
+
+
+def _weight_grads(dw, K: int, rows: int, cols: int, device, what: str):
+    """(array of K addresses, dtype code) of a list of per-language gradients."""
+    dw = list(dw)
+    if len(dw) != K:
+        raise ValueError("%s: one gradient per language, %d" % (what, K))
+    for g in dw:
+        if tuple(g.shape) != (rows, cols) or not g.is_contiguous() or g.device != device or \
+                g.dtype != dw[0].dtype:
+            raise ValueError("%s must be contiguous %d x %d matrices of one dtype on %s"
+                             % (what, rows, cols, device))
+    return (ctypes.c_void_p * K)(*[g.data_ptr() for g in dw]), _dtype_code(dw[0])
+
+
+def _one_device(*tensors):
+    devs = {t.device for t in tensors if t is not None}
+    if len(devs) != 1:
+        raise ValueError("all tensors must be on one device, got %s" % sorted(map(str, devs)))
+
+
+def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None):
+    """h = act(x w_gate^T) * (x w_up^T), and a = x w_gate^T, b = x w_up^T for the
+    backward pass where given.  x [T, D], weights [F, D], outputs [T, F], all
+    bfloat16, rows on 16 bytes."""
+    import torch
+    T, D, F = int(x.shape[0]), int(x.shape[1]), int(w_gate.shape[0])
+    if isinstance(act, str):
+        act = ACTS[act]
+    _one_device(x, w_gate, w_up, h, a, b)
+    px, ldx = _matrix(x, T, D, "x")
+    pg, ldw = _matrix(w_gate, F, D, "w_gate")
+    pu, ldu = _matrix(w_up, F, D, "w_up")
+    if ldu != ldw:
+        raise ValueError("w_gate and w_up must have one row stride")
+    ph, ldh = _matrix(h, T, F, "h") if h is not None else (None, 0)
+    pa, lda = _matrix(a, T, F, "a") if a is not None else (None, 0)
+    pb, ldb = _matrix(b, T, F, "b") if b is not None else (None, 0)
+    if lda != ldb:
+        raise ValueError("a and b must have one row stride")
+    with torch.cuda.device(x.device):
+        _check(load().bkmoo_gate_forward(px, ldx, pg, pu, ldw, T, D, F, act, ph, ldh, pa, pb, lda,
+                                         _stream_handle(stream, x.device)), "bkmoo_gate_forward")
+
+
+def bkmoo_gate_backward_workspace_size(T: int, F: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().bkmoo_gate_backward_workspace_size(T, F, ctypes.byref(n)),
+           "bkmoo_gate_backward_workspace_size")
+    return int(n.value)
+
+
+def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=None, dw_up=None,
+                        accumulate=False, ws=None, stream=None):
+    """From dh, with the forward pass's a and b: dx (may be None), and for every
+    language k (rows[k] to rows[k + 1] of the batch) its own dw_gate[k], dw_up[k]
+    (contiguous [F, D], float32 or bfloat16; both lists may be None).  ws: a CUDA
+    byte tensor of bkmoo_gate_backward_workspace_size; allocated (torch, on
+    `stream`) where None."""
+    import torch
+    T, D, F = int(x.shape[0]), int(x.shape[1]), int(w_gate.shape[0])
+    if isinstance(act, str):
+        act = ACTS[act]
+    _one_device(dh, a, b, x, w_gate, w_up, dx)
+    r = _language_rows(rows, T)
+    K = len(r) - 1
+    pd, ldd = _matrix(dh, T, F, "dh")
+    pa, lda = _matrix(a, T, F, "a")
+    pb, ldb = _matrix(b, T, F, "b")
+    px, ldx = _matrix(x, T, D, "x")
+    pg, ldw = _matrix(w_gate, F, D, "w_gate")
+    pu, ldu = _matrix(w_up, F, D, "w_up")
+    if ldu != ldw or lda != ldb:
+        raise ValueError("w_gate and w_up, and a and b, must have one row stride")
+    pdx, lddx = _matrix(dx, T, D, "dx") if dx is not None else (None, 0)
+    gg = gu = None
+    dt = BKMOO_BF16
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("dw_gate and dw_up come together")
+    if dw_gate is not None:
+        gg, dt = _weight_grads(dw_gate, K, F, D, x.device, "dw_gate")
+        gu, du = _weight_grads(dw_up, K, F, D, x.device, "dw_up")
+        if dt != du:
+            raise ValueError("dw_gate and dw_up must have one dtype")
+    if stream is None:
+        stream = torch.cuda.current_stream(x.device)
+    with torch.cuda.device(x.device):
+        if ws is None:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8,
+                                 device=x.device)
+        _check(load().bkmoo_gate_backward(pd, ldd, pa, pb, lda, px, ldx, pg, pu, ldw, T, D, F, act,
+                                          K, r.ctypes.data, pdx, lddx, gg, gu, dt,
+                                          1 if accumulate else 0, ws.data_ptr(),
+                                          ws.numel() * ws.element_size(),
+                                          _stream_handle(stream, x.device)), "bkmoo_gate_backward")
+
+
+def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
+    """dw[k] = dy[rows[k]:rows[k + 1]]^T x[rows[k]:rows[k + 1]] for every language:
+    dy [T, M] and x [T, N] bfloat16, dw[k] contiguous [M, N], float32 or bfloat16."""
+    import torch
+    T, M, N = int(dy.shape[0]), int(dy.shape[1]), int(x.shape[1])
+    _one_device(dy, x)
+    r = _language_rows(rows, T)
+    K = len(r) - 1
+    pd, ldd = _matrix(dy, T, M, "dy")
+    px, ldx = _matrix(x, T, N, "x")
+    g, dt = _weight_grads(dw, K, M, N, x.device, "dw")
+    with torch.cuda.device(x.device):
+        _check(load().bkmoo_language_wgrad(pd, ldd, px, ldx, T, M, N, K, r.ctypes.data, g, dt,
+                                           1 if accumulate else 0,
+                                           _stream_handle(stream, x.device)),
+               "bkmoo_language_wgrad")
+
+
+def bkmoo_op_status(device=None, stream=None) -> int:
+    """Status word of the gate and weight-gradient calls on `device`; cleared."""
+    import torch
+    st = ctypes.c_int32(0)
+    with torch.cuda.device(device):
+        _check(load().bkmoo_op_status(_stream_handle(stream, device), ctypes.byref(st)),
+               "bkmoo_op_status")
+    return int(st.value)
 
 
 class Resolver:

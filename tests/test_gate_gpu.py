@@ -1,0 +1,370 @@
+"""The gated projections and the per-language weight gradients on the GPU,
+against the formulas in 64 bits.
+
+Tolerances, element by element.  A bf16 result is off by at most half an ulp,
+2^-8 of it.  An fp32 sum of n products in steps of 16 is off by at most
+(n/16 + 16) 2^-23 of the sum of their magnitudes (a rounding a step, and within
+a step).  The activations' fast exponential and quotient are good to 2^-18.
+da and db are rounded to bf16 before they are summed: 2^-8 of each magnitude.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_05613_gb300 import native as bk
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+ACTS = ["silu", "gelu", "gelu_tanh"]
+HALF = 2.0 ** -8
+
+
+def _step(n):
+    return (n / 16 + 16) * 2.0 ** -23
+
+
+def _mat(gen, rows, cols, scale=1.0, pad=0, lead=0):
+    """bf16 matrix in the middle of a wider one full of NaN: reading past an edge
+    shows in every sum."""
+    ld = (lead + cols + pad + 7) // 8 * 8
+    m = torch.full((rows, ld), float("nan"), dtype=torch.bfloat16, device=DEV)
+    m[:, lead:lead + cols] = (torch.randn(rows, cols, generator=gen, device=DEV) * scale).bfloat16()
+    return m[:, lead:lead + cols]
+
+
+def _copy(t):
+    """The same values in rows that start on 16 bytes."""
+    m = torch.empty(t.shape[0], (t.shape[1] + 7) // 8 * 8, dtype=t.dtype, device=t.device)[:, :t.shape[1]]
+    return m.copy_(t)
+
+
+def _room(rows, cols, pad=0, lead=0):
+    """An output with a frame of 7s around it."""
+    ld = (lead + cols + pad + 7) // 8 * 8
+    whole = torch.full((rows + 1, ld), 7.0, dtype=torch.bfloat16, device=DEV)
+    return whole, whole[:rows, lead:lead + cols]
+
+
+def _framed(whole, view, lead):
+    w = whole.clone()
+    w[:view.shape[0], lead:lead + view.shape[1]] = 7.0
+    return bool((w == 7.0).all())
+
+
+def _act(name, a):
+    if name == "silu":
+        s = torch.sigmoid(a)
+        return a * s, s * (1 + a * (1 - s))
+    if name == "gelu":
+        c = torch.special.ndtr(a)
+        return a * c, c + a * torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+    z = math.sqrt(2 / math.pi) * (a + 0.044715 * a ** 3)
+    s = torch.sigmoid(2 * z)
+    return a * s, s + 2 * a * s * (1 - s) * math.sqrt(2 / math.pi) * (1 + 3 * 0.044715 * a ** 2)
+
+
+def _check(out, ref, tol, what):
+    off = (out.double() - ref).abs()
+    bad = ~(off <= tol)
+    assert not bool(bad.any()), (what, int(bad.sum()), float((off - tol).nan_to_num(nan=1e9).max()),
+                                 [int(i) for i in bad.nonzero()[0]])
+
+
+def _forward_ref(x, wg, wu, act):
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    a, b = x @ wg.T, x @ wu.T
+    ea, eb = (_step(x.shape[1]) * (x.abs() @ w.abs().T) for w in (wg, wu))
+    f, _ = _act(act, a)
+    h = f * b
+    eh = 1.2 * ea * b.abs() + f.abs() * eb + 1.2 * ea * eb + 2.0 ** -18 * h.abs()
+    return (h, HALF * h.abs() + 1.01 * eh), (a, HALF * a.abs() + 1.01 * ea), (b, HALF * b.abs() + 1.01 * eb)
+
+
+SHAPES = [(1, 64, 128), (1, 8, 1), (1, 2048, 8192), (2, 200, 24), (3, 72, 41), (5, 1003, 300),
+          (8, 512, 640), (9, 512, 640), (16, 136, 3), (17, 2048, 1000), (37, 1003, 2731), (64, 256, 512), (65, 264, 520),
+          (127, 65, 129), (128, 64, 128), (129, 130, 257), (256, 1024, 512), (257, 520, 384),
+          (511, 192, 1152), (1000, 768, 2048)]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,D,F", SHAPES)
+def test_forward(T, D, F, act):
+    gen = torch.Generator(device=DEV).manual_seed(T * 7 + D + F)
+    x, wg, wu = _mat(gen, T, D, pad=3), _mat(gen, F, D, 1.5 / math.sqrt(D)), _mat(gen, F, D, 1 / math.sqrt(D))
+    refs = _forward_ref(x, wg, wu, act)
+    for save in (False, True):
+        (wh, h), (wa, a), (wb, b) = _room(T, F, pad=8), _room(T, F, lead=8), _room(T, F, lead=8)
+        bk.bkmoo_gate_forward(x, wg, wu, act, h, a if save else None, b if save else None)
+        for out, ref, name in zip((h, a, b) if save else (h,), refs, ("h", "a", "b")):
+            _check(out, ref[0], ref[1], (name, save))
+        assert _framed(wh, h, 0) and _framed(wa, a, 8) and _framed(wb, b, 8)
+    # only a and b
+    (wa2, a2), (wb2, b2) = _room(T, F), _room(T, F)
+    bk.bkmoo_gate_forward(x, wg, wu, act, None, a2, b2)
+    assert torch.equal(a, a2) and torch.equal(b, b2)
+    assert bk.bkmoo_op_status(DEV) == 0
+
+
+@pytest.mark.parametrize("T", [1, 7, 33, 200])
+def test_forward_of_one_wide_weight_into_one_wide_output(T):
+    """Gate and up as halves of one matrix, a and b as halves of another."""
+    D, F = 256, 384
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    x, w = _mat(gen, T, D), _mat(gen, 2 * F, D, 0.1)
+    ab = torch.empty(T, 2 * F, dtype=torch.bfloat16, device=DEV)
+    h = torch.empty(T, F, dtype=torch.bfloat16, device=DEV)
+    bk.bkmoo_gate_forward(x, w[:F], w[F:], "silu", h, ab[:, :F], ab[:, F:])
+    refs = _forward_ref(x, w[:F], w[F:], "silu")
+    for out, ref in zip((h, ab[:, :F], ab[:, F:]), refs):
+        _check(out, ref[0], ref[1], "halves")
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_forward_large_and_non_finite_values(T):
+    """Large gates saturate, an infinity or a NaN stays in its own row."""
+    D, F = 128, 256
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    x, wg, wu = _mat(gen, T, D, 30.0), _mat(gen, F, D, 1.0), _mat(gen, F, D, 0.1)
+    row = T // 2
+    clean = x.clone()
+    h0 = torch.empty(T, F, dtype=torch.bfloat16, device=DEV)
+    bk.bkmoo_gate_forward(clean, wg, wu, "silu", h0)
+    ref = _forward_ref(clean, wg, wu, "silu")[0]
+    _check(h0, ref[0], ref[1], "large")
+    for bad in (float("nan"), float("inf")):
+        y = clean.clone()
+        y[row, 5] = bad
+        h = torch.empty_like(h0)
+        bk.bkmoo_gate_forward(y, wg, wu, "silu", h)
+        keep = torch.arange(T, device=DEV) != row
+        assert torch.equal(h[keep], h0[keep])
+        assert not torch.isfinite(h[row]).all()
+
+
+def _languages(T, K, how):
+    if how == "even":
+        return [T * k // K for k in range(K + 1)]
+    if how == "first":
+        return [0] + [T] * K
+    if how == "last":
+        return [0] * K + [T]
+    rng = np.random.default_rng(K * 1000 + T)
+    inner = np.sort(rng.integers(0, T + 1, K - 1))
+    if K > 2:
+        inner[1] = inner[0]                      # an empty language in the middle
+    return [0] + [int(i) for i in inner] + [T]
+
+
+def _grads(K, M, N, dtype, odd, fill=0.0):
+    """K gradients as places in K flat buffers, at an odd element where `odd`."""
+    flat = [torch.full((M * N + 16,), 5.0, dtype=dtype, device=DEV) for _ in range(K)]
+    at = 3 if odd else 0
+    views = [f[at:at + M * N].view(M, N) for f in flat]
+    for v in views:
+        v.fill_(fill)
+    return flat, views, at
+
+
+def _wgrad_ref(dy, x, rows):
+    d, e = [], []
+    for i, j in zip(rows, rows[1:]):
+        u, v = dy[i:j].double(), x[i:j].double()
+        d.append(u.T @ v)
+        e.append(_step(j - i) * (u.abs().T @ v.abs()))
+    return d, e
+
+
+WGRADS = [(1, 8, 8, 1, "even"), (1, 130, 70, 3, "last"), (5, 64, 256, 2, "even"), (64, 128, 256, 1, "even"),
+          (65, 129, 257, 4, "uneven"), (200, 771, 517, 3, "uneven"), (333, 256, 512, 16, "uneven"),
+          (1000, 384, 640, 8, "uneven"), (700, 1, 300, 2, "even"), (129, 300, 1, 5, "uneven"),
+          (512, 512, 512, 4, "first"), (2050, 256, 256, 2, "even")]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,M,N,K,how", WGRADS)
+def test_language_wgrad(T, M, N, K, how, dtype):
+    gen = torch.Generator(device=DEV).manual_seed(T + M + N)
+    dy, x = _mat(gen, T, M, 0.1, pad=5), _mat(gen, T, N)
+    rows = _languages(T, K, how)
+    ref, err = _wgrad_ref(dy, x, rows)
+    half = HALF if dtype == torch.bfloat16 else 2.0 ** -23
+    for odd in (False, True):
+        flat, dw, at = _grads(K, M, N, dtype, odd)
+        bk.bkmoo_language_wgrad(dy, x, rows, dw)
+        for k in range(K):
+            _check(dw[k], ref[k], half * ref[k].abs() + 1.01 * err[k], ("dw", k, odd))
+            assert bool((flat[k][:at] == 5).all()) and bool((flat[k][at + M * N:] == 5).all())
+        flat, more, at = _grads(K, M, N, dtype, odd, fill=0.75)
+        bk.bkmoo_language_wgrad(dy, x, rows, more, accumulate=True)
+        for k in range(K):
+            if rows[k] == rows[k + 1]:
+                assert bool((more[k] == 0.75).all())
+            total = ref[k] + 0.75
+            _check(more[k], total, half * total.abs() + 1.02 * err[k] + 2.0 ** -23 * total.abs(), ("sum", k, odd))
+    assert bk.bkmoo_op_status(DEV) == 0
+
+
+def test_languages_do_not_see_one_another():
+    """A NaN or infinity in one language's rows reaches no other language's gradient, also where
+    the bounds lie inside a tile of rows."""
+    T, M, N, rows = 150, 200, 300, [0, 37, 101, 150]
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    dy, x = _mat(gen, T, M), _mat(gen, T, N)
+    _, clean, _ = _grads(3, M, N, torch.float32, False)
+    bk.bkmoo_language_wgrad(dy, x, rows, clean)
+    for k, t in ((0, 36), (1, 37), (1, 100), (2, 101)):
+        for which in (0, 1):
+            u, v = _copy(dy), _copy(x)
+            (u, v)[which][t, :] = float("nan") if which else float("inf")
+            _, dw, _ = _grads(3, M, N, torch.float32, False)
+            bk.bkmoo_language_wgrad(u, v, rows, dw)
+            for j in range(3):
+                assert torch.equal(dw[j], clean[j]) == (j != k)
+
+
+def _backward_ref(dh, a, b, x, wg, wu, act, rows):
+    dh, a, b, x, wg, wu = (t.double() for t in (dh, a, b, x, wg, wu))
+    f, df = _act(act, a)
+    da, db = dh * b * df, dh * f
+    # rounding to bf16, and the fast activation (the slope is a sum of terms up to 1.2)
+    ra, rb = HALF * da.abs() + 2.0 ** -17 * (dh * b).abs(), HALF * db.abs() + 2.0 ** -17 * dh.abs() * a.abs()
+    step = _step(2 * wg.shape[0])
+    dx = da @ wg + db @ wu
+    ex = (ra + step * da.abs()) @ wg.abs() + (rb + step * db.abs()) @ wu.abs()
+    out = []
+    for d, r in ((da, ra), (db, rb)):
+        for i, j in zip(rows, rows[1:]):
+            out.append((d[i:j].T @ x[i:j], (r[i:j] + _step(j - i) * d[i:j].abs()).T @ x[i:j].abs()))
+    K = len(rows) - 1
+    return (dx, ex), out[:K], out[K:]
+
+
+BACKWARDS = [(1, 64, 128, 1, "even"), (1, 8, 1, 2, "last"), (7, 72, 41, 3, "uneven"), (64, 256, 256, 2, "even"),
+             (130, 520, 384, 4, "uneven"), (300, 1003, 771, 3, "uneven"), (513, 257, 640, 16, "uneven"),
+             (1357, 768, 2048, 4, "uneven"), (260, 128, 64, 3, "first")]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("T,D,F,K,how", BACKWARDS)
+def test_backward(T, D, F, K, how, act):
+    gen = torch.Generator(device=DEV).manual_seed(T + D + F)
+    x, wg, wu = _mat(gen, T, D), _mat(gen, F, D, 1 / math.sqrt(D)), _mat(gen, F, D, 1 / math.sqrt(D), pad=0)
+    a, b, dh = _mat(gen, T, F, 1.5, lead=8), _mat(gen, T, F, lead=8), _mat(gen, T, F, 0.1, pad=9)
+    rows = _languages(T, K, how)
+    (dx_ref, dx_err), g_ref, u_ref = _backward_ref(dh, a, b, x, wg, wu, act, rows)
+    for dtype in (torch.bfloat16, torch.float32):
+        half = HALF if dtype == torch.bfloat16 else 2.0 ** -23
+        wdx, dx = _room(T, D, pad=8)
+        (fg, dg, at), (fu, du, _) = _grads(K, F, D, dtype, True), _grads(K, F, D, dtype, True)
+        bk.bkmoo_gate_backward(dh, a, b, x, wg, wu, act, rows, dx, dg, du)
+        _check(dx, dx_ref, HALF * dx_ref.abs() + 1.02 * dx_err, "dx")
+        assert _framed(wdx, dx, 0)
+        for k in range(K):
+            for out, (ref, err) in ((dg[k], g_ref[k]), (du[k], u_ref[k])):
+                _check(out, ref, half * ref.abs() + 1.02 * err, ("dw", k))
+            assert bool((fg[k][:at] == 5).all()) and bool((fu[k][at + F * D:] == 5).all())
+    # dx alone, and the weights alone: the same bits
+    dx2 = torch.empty(T, (D + 7) // 8 * 8, dtype=torch.bfloat16, device=DEV)[:, :D]
+    bk.bkmoo_gate_backward(dh, a, b, x, wg, wu, act, rows, dx2)
+    assert torch.equal(dx, dx2)
+    _, dg2, _ = _grads(K, F, D, torch.float32, False)
+    _, du2, _ = _grads(K, F, D, torch.float32, False)
+    ws = torch.empty(bk.bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8, device=DEV)
+    bk.bkmoo_gate_backward(dh, a, b, x, wg, wu, act, rows, None, dg2, du2, ws=ws)
+    assert all(torch.equal(p, q) for p, q in zip(dg + du, dg2 + du2))
+    assert bk.bkmoo_op_status(DEV) == 0
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradient_against_differences(act):
+    """dx and dW of L = <h, dh> against central differences of the forward formula in 64 bits, along
+    random directions.  The formula's own slope along a direction is exact to 1e-6; what the kernels add
+    is the rounding of their results and of da and db, summed over the direction's elements."""
+    T, D, F, K = 24, 32, 40, 2
+    rows = [0, 10, 24]
+    gen = torch.Generator(device=DEV).manual_seed(12)
+    x, wg, wu, dh = _mat(gen, T, D), _mat(gen, F, D, 0.3), _mat(gen, F, D, 0.3), _mat(gen, T, F)
+    X, G, U, H = (t.double() for t in (x, wg, wu, dh))
+
+    def loss(X, G, U, lang=None):
+        h = _act(act, X @ G.T)[0] * (X @ U.T) * H
+        return (h if lang is None else h[rows[lang]:rows[lang + 1]]).sum()
+
+    a, b = (torch.empty(T, F, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    bk.bkmoo_gate_forward(x, wg, wu, act, None, a, b)
+    dx = torch.empty(T, D, dtype=torch.bfloat16, device=DEV)
+    _, dg, _ = _grads(K, F, D, torch.float32, False)
+    _, du, _ = _grads(K, F, D, torch.float32, False)
+    bk.bkmoo_gate_backward(dh, a, b, x, wg, wu, act, rows, dx, dg, du)
+    eps = 1e-4
+    # a, b, da, db and dx are bf16: five roundings of 2^-8 of the magnitudes that are summed, slope and
+    # curvature of the activations at most 1.2
+    f, df = _act(act, X @ G.T)
+    size = (H * (X @ U.T)).abs() * 1.2 + (H * f).abs() + (H * (X @ G.T)).abs() * 1.2
+    for _ in range(5):
+        v = torch.randn(T, D, generator=gen, device=DEV).double()
+        slope = (loss(X + eps * v, G, U) - loss(X - eps * v, G, U)) / (2 * eps)
+        bound = 5 * HALF * ((size @ (G.abs() + U.abs())) * v.abs()).sum()
+        assert abs(float((dx.double() * v).sum() - slope)) <= float(bound)
+        w = torch.randn(F, D, generator=gen, device=DEV).double()
+        for k in range(K):
+            r = slice(rows[k], rows[k + 1])
+            bound = 5 * HALF * ((size[r].T @ X[r].abs()) * w.abs()).sum()
+            slope = (loss(X, G + eps * w, U, k) - loss(X, G - eps * w, U, k)) / (2 * eps)
+            assert abs(float((dg[k].double() * w).sum() - slope)) <= float(bound)
+            slope = (loss(X, G, U + eps * w, k) - loss(X, G, U - eps * w, k)) / (2 * eps)
+            assert abs(float((du[k].double() * w).sum() - slope)) <= float(bound)
+
+
+def test_no_rows():
+    D, F, K = 64, 128, 3
+    x = torch.empty(0, D, dtype=torch.bfloat16, device=DEV)
+    e = torch.empty(0, F, dtype=torch.bfloat16, device=DEV)
+    w = torch.randn(F, D, device=DEV).bfloat16()
+    bk.bkmoo_gate_forward(x, w, w, "silu", e, e, e)
+    _, dg, _ = _grads(K, F, D, torch.bfloat16, True, fill=2.0)
+    _, du, _ = _grads(K, F, D, torch.bfloat16, True, fill=2.0)
+    bk.bkmoo_gate_backward(e, e, e, x, w, w, "silu", [0] * (K + 1), x, dg, du, accumulate=True)
+    assert all(bool((g == 2).all()) for g in dg + du)
+    bk.bkmoo_gate_backward(e, e, e, x, w, w, "silu", [0] * (K + 1), x, dg, du)
+    assert all(bool((g == 0).all()) for g in dg + du)
+    _, dw, _ = _grads(K, F, D, torch.float32, False, fill=2.0)
+    bk.bkmoo_language_wgrad(e, x, [0] * (K + 1), dw)
+    assert all(bool((g == 0).all()) for g in dw)
+
+
+def test_same_bits_again_on_streams_and_in_a_graph():
+    T, D, F, K = 300, 512, 640, 3
+    rows = [0, 90, 200, 300]
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    x, wg, wu, dh = _mat(gen, T, D), _mat(gen, F, D, 0.05), _mat(gen, F, D, 0.05), _mat(gen, T, F)
+
+    def room():
+        return {"h": torch.empty(T, F, dtype=torch.bfloat16, device=DEV), "a": torch.empty(T, F, dtype=torch.bfloat16, device=DEV),
+                "b": torch.empty(T, F, dtype=torch.bfloat16, device=DEV), "dx": torch.empty(T, D, dtype=torch.bfloat16, device=DEV),
+                "g": torch.empty(K, F, D, device=DEV), "u": torch.empty(K, F, D, device=DEV),
+                "ws": torch.empty(bk.bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8, device=DEV)}
+
+    def go(o, stream=None):
+        bk.bkmoo_gate_forward(x, wg, wu, "silu", o["h"], o["a"], o["b"], stream=stream)
+        bk.bkmoo_gate_backward(dh, o["a"], o["b"], x, wg, wu, "silu", rows, o["dx"], o["g"].unbind(0),
+                               o["u"].unbind(0), ws=o["ws"], stream=stream)
+
+    first = room()
+    go(first)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [room() for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, o in zip(streams, outs):
+            go(o, s)
+    torch.cuda.synchronize()
+    graph, o = torch.cuda.CUDAGraph(), room()
+    with torch.cuda.graph(graph):
+        go(o)
+    graph.replay()
+    torch.cuda.synchronize()
+    for o in outs + [o]:
+        assert all(torch.equal(o[k], first[k]) for k in first if k != "ws")
