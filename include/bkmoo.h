@@ -66,7 +66,11 @@ typedef enum {
   BKMOO_MEAN = 3    /* the averaged gradient of plain fine-tuning          */
 } bkmoo_rule;
 
-typedef enum { BKMOO_F32 = 0, BKMOO_BF16 = 1 } bkmoo_dtype;
+typedef enum {
+  BKMOO_F32 = 0,
+  BKMOO_BF16 = 1,
+  BKMOO_E4M3 = 2 /* moments of bkmoo_adamw only                             */
+} bkmoo_dtype;
 
 /* bkmoo_params.flags */
 #define BKMOO_FLAG_CLOSED_FORM_K2 0x1u /* K = 2 MGDA by its closed form      */
@@ -475,6 +479,72 @@ int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t l
  * one of them gave up since it was last read.  Clears it.  Writes *status.
  */
 int bkmoo_op_status(void* stream, int32_t* status);
+
+/*
+ * bkmoo_grad_norm -- the 2-norm of a flat gradient (the direction), n elements
+ * of fp32 or bf16, 16-byte aligned.  out_norm: device fp32, one value.  Squares
+ * are summed in fp32 over at most 64 elements, then in fp64, in an order fixed
+ * by n: deterministic.  Infinite where a square or the sum leaves fp32, NaN with
+ * a NaN.  ws: device, 256-byte aligned, BKMOO_NORM_WS_BYTES, not shared by calls
+ * that overlap.
+ */
+#define BKMOO_NORM_WS_BYTES 16384
+int bkmoo_grad_norm(const void* grad, int32_t dtype, int64_t n, float* out_norm, void* ws,
+                    size_t ws_bytes, void* stream);
+
+typedef struct {
+  double lr;       /* finite                                                  */
+  double beta1;    /* in [0, 1)                                               */
+  double beta2;    /* in [0, 1)                                               */
+  double eps;      /* >= 0                                                    */
+  double max_norm; /* > 0: g is multiplied by min(1, max_norm / (norm + 1e-6)),
+                      norm being *grad_norm; 0: not clipped                   */
+  int64_t step;    /* 1, 2, ...: bias corrections and the key of the rounding */
+  uint64_t seed;   /* of the rounding to 8 bits                               */
+} bkmoo_adamw_params;
+
+/* Fill *p with lr 1e-3, beta1 0.9, beta2 0.999, eps 1e-8, max_norm 0, step 1,
+ * seed 0. */
+void bkmoo_adamw_default_params(bkmoo_adamw_params* p);
+
+/*
+ * bkmoo_adamw -- one AdamW step of every tensor with the direction as gradient,
+ * the optimizer step of Algorithm 1:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - lr weight_decay) p
+ *       - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps).
+ *
+ * params[n_params]: host array of device pointers, tensors of sizes[i] elements
+ *   of param_dtype (fp32 or bf16), in the order in which the flat buffers hold
+ *   them (a bkmoo_plan layout: last registered first); any element-aligned
+ *   address, empty ones allowed.  weight_decay: host, one per tensor, or NULL.
+ * grad: the flat gradient, N = sum of sizes, fp32 or bf16.
+ * master: NULL, or flat fp32 [N], with bf16 params only: the weights that the
+ *   step reads and writes; the tensors then receive them rounded to nearest.
+ *   Without it bf16 weights are widened, stepped and rounded to nearest.
+ * state_dtype BKMOO_F32: m, v flat fp32 [N]; m_scale, v_scale unused.
+ * state_dtype BKMOO_E4M3: m, v flat bytes [N], one fp32 scale for every 256 flat
+ *   elements in m_scale, v_scale [(N + 255) / 256]: m = m_scale e4m3(byte), and
+ *   v's bytes hold its ROOT, sqrt(v) = v_scale e4m3(byte), which spans half as
+ *   many powers of two.  A scale is the largest magnitude of its elements / 448
+ *   (0 below 2^-100).  Values are rounded up with the chance that their rest
+ *   gives, else down: by nearest, a beta2 of 0.999 moves no value of 4 bits'
+ *   precision.  A root that is not 0 never becomes 0.  The chance of flat element
+ *   i is u / 65536 with u the low (m) or high (v) 16 bits of the low (i even) or
+ *   high (i odd) half of mix64(mix64(seed + (step + 1) G) + (i / 2 + 1) G), with
+ *   mix64 and G of bkmoo_resolve.  All zeros is the state before the first step.
+ * grad, m, v, master: 16-byte aligned; none may overlap another or a tensor.
+ * grad_norm: device, as bkmoo_grad_norm gives it, needed where max_norm > 0.
+ *   Where it is given and not finite, nothing is changed: the step is skipped.
+ *   Without it a NaN or infinity in g reaches the state (an infinity in 8 bits
+ *   its whole block).
+ * Moments are computed in fp32.  Up to 1024 tensors take one launch.
+ */
+int bkmoo_adamw(void* const* params, const int64_t* sizes, const float* weight_decay,
+                int32_t n_params, int32_t param_dtype, const void* grad, int32_t grad_dtype,
+                float* master, void* m, void* v, float* m_scale, float* v_scale,
+                int32_t state_dtype, const bkmoo_adamw_params* p, const float* grad_norm,
+                void* stream);
 
 /* Static English text for a bkmoo_status value. */
 const char* bkmoo_status_string(int32_t status);

@@ -27,13 +27,14 @@ BKMOO_ERR_BUFFER_TOO_SMALL = 6
 BKMOO_ERR_NOT_CONVERGED = 7
 
 BKMOO_MGDA, BKMOO_PCGRAD, BKMOO_CAGRAD, BKMOO_MEAN = 0, 1, 2, 3
-BKMOO_F32, BKMOO_BF16 = 0, 1
+BKMOO_F32, BKMOO_BF16, BKMOO_E4M3 = 0, 1, 2
 BKMOO_FLAG_CLOSED_FORM_K2 = 0x1
 BKMOO_FLAG_POLISH = 0x2
 BKMOO_FLAG_FUSED = 0x4
 BKMOO_FLAG_THREE_PASS = 0x8
 BKMOO_FLAG_TEST_WITHHOLD = 0x100
 BKMOO_FLAG_TEST_WITHHOLD_EXCHANGE = 0x200
+BKMOO_NORM_WS_BYTES = 16384
 BKMOO_SILU, BKMOO_GELU, BKMOO_GELU_TANH = 0, 1, 2
 BKMOO_NOALLOC_SCRATCH_BYTES = 32 << 20
 BKMOO_NOALLOC_MAX_BUCKETS = 4096
@@ -60,6 +61,18 @@ class bkmoo_params(ctypes.Structure):
         ("step", ctypes.c_uint64),
         ("flags", ctypes.c_uint32),
         ("events", ctypes.c_void_p),
+    ]
+
+
+class bkmoo_adamw_params(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double),
+        ("beta1", ctypes.c_double),
+        ("beta2", ctypes.c_double),
+        ("eps", ctypes.c_double),
+        ("max_norm", ctypes.c_double),
+        ("step", ctypes.c_int64),
+        ("seed", ctypes.c_uint64),
     ]
 
 
@@ -130,6 +143,13 @@ def load():
                                              i32, vp]
         lib.bkmoo_op_status.restype = ctypes.c_int
         lib.bkmoo_op_status.argtypes = [vp, ctypes.POINTER(i32)]
+        lib.bkmoo_grad_norm.restype = ctypes.c_int
+        lib.bkmoo_grad_norm.argtypes = [vp, i32, i64, vp, vp, sz, vp]
+        lib.bkmoo_adamw_default_params.restype = None
+        lib.bkmoo_adamw_default_params.argtypes = [ctypes.POINTER(bkmoo_adamw_params)]
+        lib.bkmoo_adamw.restype = ctypes.c_int
+        lib.bkmoo_adamw.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32,
+                                    ctypes.POINTER(bkmoo_adamw_params), vp, vp]
         _lib = lib
         return lib
 
@@ -491,6 +511,89 @@ def bkmoo_op_status(device=None, stream=None) -> int:
         _check(load().bkmoo_op_status(_stream_handle(stream, device), ctypes.byref(st)),
                "bkmoo_op_status")
     return int(st.value)
+
+
+def bkmoo_grad_norm(grad, out_norm, ws=None, stream=None):
+    """The 2-norm of a flat gradient into out_norm (a float32 CUDA tensor of one
+    element).  ws: a CUDA byte tensor of BKMOO_NORM_WS_BYTES; allocated (torch,
+    on `stream`) where None."""
+    import torch
+    if not grad.is_cuda or not grad.is_contiguous():
+        raise ValueError("the gradient must be a contiguous CUDA tensor")
+    if out_norm.dtype != torch.float32 or out_norm.numel() != 1 or out_norm.device != grad.device:
+        raise ValueError("out_norm must be one float32 on the gradient's device")
+    if stream is None:
+        stream = torch.cuda.current_stream(grad.device)
+    with torch.cuda.device(grad.device):
+        if ws is None:
+            with torch.cuda.stream(stream):
+                ws = torch.empty(BKMOO_NORM_WS_BYTES, dtype=torch.uint8, device=grad.device)
+        _check(load().bkmoo_grad_norm(grad.data_ptr(), _dtype_code(grad), grad.numel(),
+                                      out_norm.data_ptr(), ws.data_ptr(),
+                                      ws.numel() * ws.element_size(),
+                                      _stream_handle(stream, grad.device)), "bkmoo_grad_norm")
+
+
+def bkmoo_adamw_default_params() -> bkmoo_adamw_params:
+    p = bkmoo_adamw_params()
+    load().bkmoo_adamw_default_params(ctypes.byref(p))
+    return p
+
+
+def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None, m_scale=None,
+                v_scale=None, grad_norm=None, stream=None):
+    """One AdamW step of `tensors` (contiguous CUDA tensors of one dtype, in the
+    order of the flat buffers) with the flat gradient.  m, v: flat float32, or
+    flat float8_e4m3fn with one float32 scale per 256 elements (v then holds the
+    root of the second moment); master: flat float32 weights of bfloat16
+    tensors, or None.  weight_decay: one number per tensor, or one for all."""
+    import torch
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("need at least one tensor")
+    dev, dt = grad.device, tensors[0].dtype
+    for t in tensors:
+        if t.device != dev or t.dtype != dt or not t.is_contiguous():
+            raise ValueError("the tensors must be contiguous, of one dtype and on the gradient's device")
+    sizes = np.fromiter((t.numel() for t in tensors), np.int64, len(tensors))
+    N = int(sizes.sum())
+    eight = m.dtype == torch.float8_e4m3fn
+    flat = [("grad", grad, None), ("m", m, torch.float8_e4m3fn if eight else torch.float32),
+            ("v", v, m.dtype)]
+    if master is not None:
+        if dt != torch.bfloat16:
+            raise ValueError("a master copy goes with bfloat16 tensors")
+        flat.append(("master", master, torch.float32))
+    for name, t, want in flat:
+        if not t.is_cuda or t.device != dev or not t.is_contiguous() or t.numel() != N or \
+                (want is not None and t.dtype != want):
+            raise ValueError("%s must be a flat CUDA tensor of the tensors' %d elements%s"
+                             % (name, N, "" if want is None else ", %s" % want))
+    if eight:
+        for name, t in (("m_scale", m_scale), ("v_scale", v_scale)):
+            if t is None or t.dtype != torch.float32 or t.device != dev or \
+                    not t.is_contiguous() or t.numel() != (N + 255) // 256:
+                raise ValueError("%s must hold one float32 per 256 elements" % name)
+    if grad_norm is not None and (grad_norm.dtype != torch.float32 or grad_norm.device != dev or
+                                  grad_norm.numel() != 1):
+        raise ValueError("grad_norm must be one float32 on the gradient's device")
+    if weight_decay is not None:
+        weight_decay = np.ascontiguousarray(np.broadcast_to(
+            np.asarray(weight_decay, dtype=np.float32), (len(tensors),)))
+    ptrs = (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+    p = params if params is not None else bkmoo_adamw_default_params()
+
+    def ptr(t):
+        return t.data_ptr() if t is not None else None
+
+    with torch.cuda.device(dev):
+        _check(load().bkmoo_adamw(ptrs, sizes.ctypes.data,
+                                  weight_decay.ctypes.data if weight_decay is not None else None,
+                                  len(tensors), _dtype_code(tensors[0]), grad.data_ptr(),
+                                  _dtype_code(grad), ptr(master), m.data_ptr(), v.data_ptr(),
+                                  ptr(m_scale) if eight else None, ptr(v_scale) if eight else None,
+                                  BKMOO_E4M3 if eight else BKMOO_F32, ctypes.byref(p),
+                                  ptr(grad_norm), _stream_handle(stream, dev)), "bkmoo_adamw")
 
 
 class Resolver:
