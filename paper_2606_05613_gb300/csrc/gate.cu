@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
 }
 
 // Whether the CTAs work in pairs.
-int choose_pair(int64_t rows) { return 1; }
+int choose_pair(int64_t rows) { return rows > kTileM ? 2 : 1; }
 
 // dW_k = dy_k^T x_k for one or two dy (mats), every language.
 int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, int64_t ldx,
