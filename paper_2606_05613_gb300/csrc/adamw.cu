@@ -6,9 +6,9 @@
 // flat elements at a time, whatever tensors they lie in: each lane 4 and 4 more
 // 128 further on, so that every access of the flat buffers is a whole vector and
 // a warp's accesses are contiguous.  256 is also the block of elements that share
-// a scale in 8 bits, so its largest value is a matter of one warp.  Which tensor
-// an element belongs to comes from a table in the kernel's parameters (a binary
-// search per four blocks, then steps).
+// a scale in 8 bits, so its largest value is a matter of one warp.  The grid
+// goes through them side by side.  Which tensor an element belongs to comes from a
+// table in the kernel's parameters (one binary search a warp, then steps).
 //
 // Bound by memory: per element the direction, the weight and both moments (and
 // the master copy) are read once and written once.
@@ -17,6 +17,7 @@
 #include <cuda_fp8.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "common.cuh"
 
@@ -26,8 +27,7 @@ namespace {
 constexpr int kBlock = 256;          // elements per scale, and per warp and turn
 constexpr int kAdamTable = 1024;     // tensors a launch knows
 constexpr int kAdamThreads = 256;
-constexpr int kAdamTurns = 4;        // consecutive blocks of a warp
-constexpr int64_t kAdamSpan = (int64_t)(kAdamThreads / 32) * kAdamTurns;   // blocks of a CTA
+constexpr int64_t kAdamWarps = kAdamThreads / 32;
 
 struct AdamArgs {
   const void* grad;
@@ -56,56 +56,87 @@ __host__ __device__ inline uint64_t mix_word(uint64_t z) {
 }
 constexpr uint64_t kGold = 0x9E3779B97F4A7C15ull;
 
-// Four consecutive elements, of which the first n exist (16-byte aligned base,
-// index a multiple of 4).
-__device__ __forceinline__ void load4(const float* p, int64_t i, int n, float (&x)[4]) {
-  if (n >= 4) {
-    const float4 t = __ldcs(reinterpret_cast<const float4*>(p + i));
-    x[0] = t.x, x[1] = t.y, x[2] = t.z, x[3] = t.w;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? p[i + j] : 0.0f;
-  }
+// Four consecutive elements as they are loaded, and widened to fp32 (8-bit ones
+// times their scale).
+template <class T>
+struct Raw;
+template <>
+struct Raw<float> {
+  float4 x;
+};
+template <>
+struct Raw<__nv_bfloat16> {
+  uint2 x;
+};
+template <>
+struct Raw<uint8_t> {
+  uint32_t x;
+};
+template <bool E4M3>
+struct State {
+  using T = typename std::conditional<E4M3, uint8_t, float>::type;
+};
+
+__device__ __forceinline__ Raw<float> load_raw(const float* p) {
+  return {__ldcs(reinterpret_cast<const float4*>(p))};
 }
-__device__ __forceinline__ void load4(const __nv_bfloat16* p, int64_t i, int n, float (&x)[4]) {
-  if (n >= 4) {
-    const uint2 t = __ldcs(reinterpret_cast<const uint2*>(p + i));
-    x[0] = __uint_as_float(t.x << 16), x[1] = __uint_as_float(t.x & 0xffff0000u);
-    x[2] = __uint_as_float(t.y << 16), x[3] = __uint_as_float(t.y & 0xffff0000u);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = j < n ? __bfloat162float(p[i + j]) : 0.0f;
-  }
+__device__ __forceinline__ Raw<__nv_bfloat16> load_raw(const __nv_bfloat16* p) {
+  return {__ldcs(reinterpret_cast<const uint2*>(p))};
 }
-__device__ __forceinline__ void store4(float* p, int64_t i, int n, const float (&x)[4]) {
-  if (n >= 4) {
-    __stcs(reinterpret_cast<float4*>(p + i), make_float4(x[0], x[1], x[2], x[3]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[i + j] = x[j];
-  }
+__device__ __forceinline__ Raw<uint8_t> load_raw(const uint8_t* p) {
+  return {__ldcs(reinterpret_cast<const uint32_t*>(p))};
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, int64_t i, int n, const float (&x)[4]) {
-  if (n >= 4) {
-    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-    __stcs(reinterpret_cast<uint2*>(p + i),
-           make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
-  } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[i + j] = __float2bfloat16_rn(x[j]);
-  }
+// The first n of the four, the others 0.
+__device__ __forceinline__ Raw<float> load_part(const float* p, int n) {
+  return {make_float4(n > 0 ? p[0] : 0.0f, n > 1 ? p[1] : 0.0f, n > 2 ? p[2] : 0.0f, n > 3 ? p[3] : 0.0f)};
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t i, int n) {
-  if (n >= 4) return __ldcs(reinterpret_cast<const uint32_t*>(p + i));
+__device__ __forceinline__ Raw<__nv_bfloat16> load_part(const __nv_bfloat16* p, int n) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = j < n ? __bfloat16_as_ushort(p[j]) : 0u;
+  return {make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16)};
+}
+__device__ __forceinline__ Raw<uint8_t> load_part(const uint8_t* p, int n) {
   uint32_t w = 0;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (j < n) w |= (uint32_t)p[i + j] << (8 * j);
-  return w;
+    if (j < n) w |= (uint32_t)p[j] << (8 * j);
+  return {w};
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int n, uint32_t w) {
+__device__ __forceinline__ void widen(const Raw<float>& r, float (&x)[4], float) {
+  x[0] = r.x.x, x[1] = r.x.y, x[2] = r.x.z, x[3] = r.x.w;
+}
+__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float (&x)[4], float) {
+  x[0] = __uint_as_float(r.x.x << 16), x[1] = __uint_as_float(r.x.x & 0xffff0000u);
+  x[2] = __uint_as_float(r.x.y << 16), x[3] = __uint_as_float(r.x.y & 0xffff0000u);
+}
+__device__ __forceinline__ void widen(const Raw<uint8_t>& r, float (&x)[4], float scale) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(r.x >> (16 * j)), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    x[2 * j] = __fmul_rn(f.x, scale);
+    x[2 * j + 1] = __fmul_rn(f.y, scale);
+  }
+}
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+}
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+  __stcs(reinterpret_cast<uint2*>(p),
+         make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
+}
+__device__ __forceinline__ void store_part(float* p, int64_t n, const float (&x)[4]) {
+  if (n >= 4) {
+    store4(p, x);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = x[j];
+  }
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, uint32_t w) {
   if (n >= 4) {
     __stcs(reinterpret_cast<uint32_t*>(p + i), w);
   } else {
@@ -114,215 +145,311 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int n, uint32
       if (j < n) p[i + j] = (uint8_t)(w >> (8 * j));
   }
 }
-__device__ __forceinline__ void decode4(uint32_t w, float scale, float (&x)[4]) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> (16 * j)), __NV_E4M3);
-    const float2 f = __half22float2(__half2(h));
-    x[2 * j] = f.x * scale;
-    x[2 * j + 1] = f.y * scale;
-  }
-}
 
-// |x| / scale as an e4m3 code, rounded up with the chance that the rest gives:
-// u, 16 bits, stands for u / 65536.  2^-120 takes e4m3's smallest normal number,
-// 2^-6, to fp32's, 2^-126, so the product's bits above the 20th are the code, of
-// subnormal values too, and what is below them is the rest.
-__device__ __forceinline__ uint32_t encode(float x, float inv, uint32_t u, bool positive) {
-  const uint32_t bits = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x), inv), 0x1p-120f));
-  uint32_t c = min((bits + (u << 4)) >> 20, 0x7eu);
-  if (positive && c == 0 && bits > 0) c = 1;
-  if (bits > 0x7f800000u) c = 0x7f;    // NaN stays NaN
+// Four values / their scale as e4m3 bytes, each rounded away from 0 with the
+// chance that its rest gives: u, 16 bits in bits 4 to 19, stands for u / 2^20.
+// `inv` is 2^-120 / scale, and 2^-120 takes e4m3's smallest normal number, 2^-6,
+// to fp32's, 2^-126: the product's bits from the 20th on are the code, of
+// subnormal values too, and what is below them is the rest.  Without SIGNED
+// (roots, which are not negative) what is not 0 does not become 0: 1 + 0xfffff
+// is code 1, 0 + 0xfffff is code 0.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t encode4(const float (&x)[4], float inv, const uint32_t (&u)[4]) {
+  uint32_t s[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t bits = __float_as_uint(__fmul_rn(fabsf(x[j]), inv));
+    s[j] = __viaddmin_u32(bits, u[j], 0x7efffffu);
+    if (!SIGNED) s[j] = max(s[j], __viaddmin_u32(bits, 0xfffffu, 0x100000u));
+    s[j] <<= 4;                   // the code is the top byte
+  }
+  uint32_t c = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
+  if (SIGNED) {
+    const uint32_t g = __byte_perm(
+        __byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
+        __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
+    c |= g & 0x80808080u;
+  }
+  return c;
+}
+// The same where 2^-120 / scale is no normal number (a scale above 2^6) or the
+// block has a NaN or an infinity: `inv` is 1 / scale, and a NaN stays one.
+template <bool SIGNED>
+__device__ __noinline__ uint32_t encode4_any(float x0, float x1, float x2, float x3, float inv, uint32_t u0,
+                                             uint32_t u1, uint32_t u2, uint32_t u3) {
+  const float x[4] = {x0, x1, x2, x3};
+  const uint32_t u[4] = {u0, u1, u2, u3};
+  uint32_t c = 0;
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t bits = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x[j]), inv), 0x1p-120f));
+    uint32_t k = min((bits + u[j]) >> 20, 0x7eu);
+    if (!SIGNED) k = max(k, min(bits, 1u));
+    if (bits > 0x7f800000u) k = 0x7f;
+    if (SIGNED) k |= (__float_as_uint(x[j]) >> 24) & 0x80u;
+    c |= k << (8 * j);
+  }
   return c;
 }
 
-// The weights of four consecutive flat elements.
-template <class P>
-struct Weights {
-  P* p;        // of the first element
-  int t;       // its tensor
-  int n;       // how many of the four lie in it
-  float keep;
-};
-template <class P>
-__device__ __forceinline__ Weights<P> find(const AdamArgs& a, int t, int64_t e) {
+// The tensor of a flat element, from one at or before it on.
+__device__ __forceinline__ int tensor_of(const AdamArgs& a, int t, int64_t e) {
   while (t + 1 < a.tensors && a.start[t + 1] <= e) ++t;
-  Weights<P> w;
-  const int64_t s = a.start[t], left = a.start[t + 1] - e;
-  w.p = static_cast<P*>(a.p[t]) + (e - s);
-  w.t = t;
-  w.n = left < 4 ? (int)left : 4;
-  w.keep = a.keep[t];
-  return w;
+  return t;
 }
+
+// What a lane has loaded of a block: 4 elements and 4 more 128 further on.
+template <class P, class G, bool E4M3>
+struct Loaded {
+  Raw<G> g[2];
+  Raw<typename State<E4M3>::T> m[2], v[2];
+  Raw<P> w[2];           // where the weights are read as whole vectors
+  float ms, vs;
+  P* p;                  // the lane's first weight, NULL: element by element
+  float keep;
+  int t;                 // the tensor of the block's first element
+};
+
+// Both to about 2^-23; below fp32's normal numbers (a gradient below 1e-19) 0 and
+// infinity.
+__device__ __forceinline__ float root_of(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// x[j] without an address of its own.
+__device__ __forceinline__ float pick(const float (&x)[4], int j) {
+  return j < 2 ? (j ? x[1] : x[0]) : (j == 2 ? x[2] : x[3]);
+}
+__device__ __forceinline__ void put(float (&x)[4], int j, float y) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = i == j ? y : x[i];
+}
+
+// One element's step: moments in place (v as its root in 8 bits), the new weight
+// returned.  The moments round as written, product by product: in 8 bits a last
+// bit can move a code.
+template <bool E4M3>
+struct Step {
+  float b1, one_b1, b2, one_b2, rate, root, eps, clip;
+  __device__ __forceinline__ float operator()(float g, float keep, float w, float& m, float& v) const {
+    const float gj = __fmul_rn(g, clip);
+    const float old = E4M3 ? __fmul_rn(v, v) : v;
+    m = __fadd_rn(__fmul_rn(m, b1), __fmul_rn(gj, one_b1));
+    const float vj = __fadd_rn(__fmul_rn(old, b2), __fmul_rn(__fmul_rn(gj, gj), one_b2));
+    const float r = root_of(vj);
+    v = E4M3 ? r : vj;
+    return fmaf(-rate * m, reciprocal(fmaf(r, root, eps)), w * keep);
+  }
+  __device__ __forceinline__ float operator()(float g, float keep, float w, float (&m)[4], float (&v)[4],
+                                              int j) const {
+    float mj = pick(m, j), vj = pick(v, j);
+    const float r = (*this)(g, keep, w, mj, vj);
+    put(m, j, mj);
+    put(v, j, vj);
+    return r;
+  }
+};
 
 template <class P, class G, bool E4M3, bool MASTER>
 __global__ void __launch_bounds__(kAdamThreads)
     adamw_kernel(const __grid_constant__ AdamArgs a) {
+  using S = typename State<E4M3>::T;
+  using W = typename std::conditional<MASTER, float, P>::type;    // what the step reads
   const int lane = threadIdx.x & 31;
-  const int64_t b0 = a.first + blockIdx.x * kAdamSpan + (threadIdx.x >> 5) * kAdamTurns;
-  const int64_t end = a.first + a.blocks;
-  if (b0 >= end) return;
-  float clip = 1.0f;
+  const int64_t end = a.first + a.blocks, stride = (int64_t)gridDim.x * kAdamWarps;
+  int64_t blk = a.first + (int64_t)blockIdx.x * kAdamWarps + (threadIdx.x >> 5);
+  if (blk >= end) return;
+  Step<E4M3> step = {a.b1, a.one_b1, a.b2, a.one_b2, a.rate, a.root, a.eps, 1.0f};
   if (a.norm) {
     const float norm = *a.norm;
     if (!(fabsf(norm) <= 3.4028235e38f)) return;      // not a step to take
-    if (a.max_norm > 0.0f) clip = fminf(1.0f, __fdiv_rn(a.max_norm, __fadd_rn(norm, 1e-6f)));
+    if (a.max_norm > 0.0f) step.clip = fminf(1.0f, __fdiv_rn(a.max_norm, __fadd_rn(norm, 1e-6f)));
   }
-  int t = 0;                        // the tensor of the first element
-  {
-    int hi = a.tensors;
-    while (hi - t > 1) {
-      const int mid = (t + hi) >> 1;
-      if (a.start[mid] <= b0 * kBlock) t = mid;
-      else hi = mid;
-    }
+  int t = 0;                        // the tensor of the block's first element
+  for (int hi = a.tensors; hi - t > 1;) {
+    const int mid = (t + hi) >> 1;
+    if (a.start[mid] <= blk * kBlock) t = mid;
+    else hi = mid;
   }
-#pragma unroll 1
-  for (int turn = 0; turn < kAdamTurns; ++turn) {
-    const int64_t blk = b0 + turn;
-    if (blk >= end) break;
-    float g[2][4], m[2][4], v[2][4];
-    uint32_t mc[2], vc[2];
-    int64_t e[2];
-    int n[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      e[h] = blk * kBlock + 128 * h + 4 * lane;
-      const int64_t left = a.n - e[h];
-      n[h] = left < 4 ? (left < 0 ? 0 : (int)left) : 4;
-      load4(static_cast<const G*>(a.grad), e[h], n[h], g[h]);
-      if (E4M3) {
-        mc[h] = load_codes(static_cast<const uint8_t*>(a.m), e[h], n[h]);
-        vc[h] = load_codes(static_cast<const uint8_t*>(a.v), e[h], n[h]);
-      } else {
-        load4(static_cast<const float*>(a.m), e[h], n[h], m[h]);
-        load4(static_cast<const float*>(a.v), e[h], n[h], v[h]);
-      }
-    }
-    float ms = 0.0f, vs = 0.0f;
-    if (E4M3) ms = a.m_scale[blk], vs = a.v_scale[blk];
-    float mtop = 0.0f, rtop = 0.0f;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (E4M3) {
-        decode4(mc[h], ms, m[h]);
-        decode4(vc[h], vs, v[h]);
-      }
-      // p is fetched here, behind the flat loads of both halves
-      float w[4], keep[4];
-      Weights<P> at = {};
-      const bool any = n[h] > 0;
-      bool whole = false;
-      if (any) {
-        at = find<P>(a, t, e[h]);
-        whole = at.n == 4;
-        if (MASTER) {
-          load4(a.master, e[h], n[h], w);
-        } else if (whole) {
-          if (((uintptr_t)at.p & (4 * sizeof(P) - 1)) == 0) {
-            load4(at.p, 0, 4, w);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = (float)at.p[j];
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) keep[j] = at.keep;
-      P* q[4];
-      if (any && !whole) {          // a tensor ends here: element by element
-        int tj = at.t;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (j < n[h]) {
-            const Weights<P> x = find<P>(a, tj, e[h] + j);
-            tj = x.t;
-            q[j] = x.p;
-            keep[j] = x.keep;
-            if (!MASTER) w[j] = (float)*x.p;
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float gj = __fmul_rn(g[h][j], clip);
-        const float old = E4M3 ? __fmul_rn(v[h][j], v[h][j]) : v[h][j];
-        m[h][j] = __fadd_rn(__fmul_rn(m[h][j], a.b1), __fmul_rn(gj, a.one_b1));
-        const float vj = __fadd_rn(__fmul_rn(old, a.b2), __fmul_rn(__fmul_rn(gj, gj), a.one_b2));
-        const float r = __fsqrt_rn(vj);
-        v[h][j] = E4M3 ? r : vj;
-        if (E4M3) {
-          mtop = fmaxf(mtop, fabsf(m[h][j]));
-          rtop = fmaxf(rtop, r);
-        }
-        w[j] = w[j] * keep[j] - __fdividef(m[h][j], r * a.root + a.eps) * a.rate;
-      }
-      if (any) {
-        if (MASTER) store4(a.master, e[h], n[h], w);
-        if (whole) {
-          if (((uintptr_t)at.p & (4 * sizeof(P) - 1)) == 0) {
-            store4(at.p, 0, 4, w);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) at.p[j] = (P)w[j];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (j < n[h]) *q[j] = (P)w[j];
-        }
-      }
-      if (!E4M3 && any) {
-        store4(static_cast<float*>(a.m), e[h], n[h], m[h]);
-        store4(static_cast<float*>(a.v), e[h], n[h], v[h]);
-      }
-    }
-    if (E4M3) {
-      // largest magnitudes of the block, as bits (they are not negative)
-      float mt = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mtop)));
-      float rt = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(rtop)));
-      if (mt < 0x1p-100f) mt = 0.0f;
-      if (rt < 0x1p-100f) rt = 0.0f;
-      const float mi = mt > 0.0f ? __fdiv_rn(448.0f, mt) : 0.0f;
-      const float ri = rt > 0.0f ? __fdiv_rn(448.0f, rt) : 0.0f;
-      if (lane == 0) {
-        a.m_scale[blk] = __fdiv_rn(mt, 448.0f);
-        a.v_scale[blk] = __fdiv_rn(rt, 448.0f);
-      }
+  // of that tensor: its end, where its weight 0 of the flat buffers would lie, and
+  // whether whole vectors of it are aligned
+  int64_t stop = 0;
+  P* base = nullptr;
+  float keep = 0.0f;
+  bool straight = false;
+  auto enter = [&](int tensor) {
+    t = tensor;
+    stop = a.start[t + 1];
+    base = static_cast<P*>(a.p[t]) - a.start[t];
+    keep = a.keep[t];
+    straight = ((uintptr_t)base & (4 * sizeof(P) - 1)) == 0;
+  };
+  enter(t);
+
+  // Everything of a block that can be loaded at once.
+  auto load = [&](int64_t b, Loaded<W, G, E4M3>& x) {
+    const int64_t e0 = b * kBlock, e = e0 + 4 * lane;
+    if (e0 >= stop) enter(tensor_of(a, t, e0));
+    x.t = t;
+    x.keep = keep;
+    x.p = straight && e0 + kBlock <= stop ? reinterpret_cast<W*>(base + e) : nullptr;
+    if (E4M3) x.ms = __ldcs(a.m_scale + b), x.vs = __ldcs(a.v_scale + b);
+    if (e0 + kBlock <= a.n) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint32_t cm = 0, cr = 0;
+        x.g[h] = load_raw(static_cast<const G*>(a.grad) + e + 128 * h);
+        x.m[h] = load_raw(static_cast<const S*>(a.m) + e + 128 * h);
+        x.v[h] = load_raw(static_cast<const S*>(a.v) + e + 128 * h);
+        if (MASTER) x.w[h] = load_raw(reinterpret_cast<const W*>(a.master) + e + 128 * h);
+        else if (x.p) x.w[h] = load_raw(x.p + 128 * h);
+      }
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const uint64_t z = mix_word(a.key + (uint64_t)((e[h] + j) / 2 + 1) * kGold);
+      for (int h = 0; h < 2; ++h) {
+        const int64_t left = a.n - (e + 128 * h);
+        const int n = left < 4 ? (left < 0 ? 0 : (int)left) : 4;
+        x.g[h] = load_part(static_cast<const G*>(a.grad) + e + 128 * h, n);
+        x.m[h] = load_part(static_cast<const S*>(a.m) + e + 128 * h, n);
+        x.v[h] = load_part(static_cast<const S*>(a.v) + e + 128 * h, n);
+        if (MASTER) x.w[h] = load_part(reinterpret_cast<const W*>(a.master) + e + 128 * h, n);
+      }
+    }
+  };
+
+  // 8-bit moments are little data for the work: the next block is fetched ahead
+  // of the present one's step.  32-bit ones fill the memory pipe without.
+  constexpr bool AHEAD = E4M3;
+  // 64-bit words of the lane's pairs of elements: 0 and 1, 64 and 65 from here
+  uint64_t word = E4M3 ? a.key + (uint64_t)(blk * (kBlock / 2) + 2 * lane + 1) * kGold : 0;
+  const uint64_t word_step = (uint64_t)(stride * (kBlock / 2)) * kGold;
+  Loaded<W, G, E4M3> x;
+  load(blk, x);
+  for (;;) {
+    const int64_t next = blk + stride;
+    Loaded<W, G, E4M3> y;
+    if (AHEAD && next < end) load(next, y);
+    const int64_t e = blk * kBlock + 4 * lane;
+    float m[2][4], v[2][4];
+    uint32_t mtop = 0, rtop = 0;
+    if (x.p) {
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint32_t u = (uint32_t)(z >> (32 * i));
-            const float x = m[h][j + i];
-            const uint32_t c = encode(x, mi, u & 0xffffu, false) | (x < 0.0f ? 0x80u : 0u);
-            cm |= c << (8 * (j + i));
-            cr |= encode(v[h][j + i], ri, u >> 16, true) << (8 * (j + i));
-          }
+      for (int h = 0; h < 2; ++h) {
+        float g[4], w[4];
+        widen(x.g[h], g, 1.0f);
+        widen(x.m[h], m[h], x.ms);
+        widen(x.v[h], v[h], x.vs);
+        widen(x.w[h], w, 1.0f);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = step(g[j], x.keep, w[j], m[h][j], v[h][j]);
+        if (MASTER) {
+          store4(a.master + e + 128 * h, w);
+          store4(static_cast<P*>(a.p[x.t]) + (e - a.start[x.t]) + 128 * h, w);
+        } else {
+          store4(reinterpret_cast<P*>(x.p) + 128 * h, w);
         }
-        if (n[h] > 0) {
-          store_codes(static_cast<uint8_t*>(a.m), e[h], n[h], cm);
-          store_codes(static_cast<uint8_t*>(a.v), e[h], n[h], cr);
+      }
+    } else {
+      // a tensor ends in the block, or its weights lie askew: one by one
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float g[4], w[4] = {};
+        widen(x.g[h], g, 1.0f);
+        widen(x.m[h], m[h], x.ms);
+        widen(x.v[h], v[h], x.vs);
+        if (MASTER) widen(x.w[h], w, 1.0f);
+        int tj = x.t;
+#pragma unroll 1
+        for (int j = 0; j < 4; ++j) {
+          const int64_t i = e + 128 * h + j;
+          if (i >= a.n) break;
+          tj = tensor_of(a, tj, i);
+          P* p = static_cast<P*>(a.p[tj]) + (i - a.start[tj]);
+          const float wj = step(pick(g, j), a.keep[tj], MASTER ? pick(w, j) : (float)*p, m[h], v[h], j);
+          *p = (P)wj;
+          if (MASTER) a.master[i] = wj;
         }
       }
     }
+    const int64_t left = a.n - e;
+    if (E4M3) {
+      // largest magnitudes of the block, as bits (a NaN is above all)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          mtop = max(mtop, __float_as_uint(m[h][j]) & 0x7fffffffu);
+          rtop = max(rtop, __float_as_uint(v[h][j]));
+        }
+      mtop = __reduce_max_sync(0xffffffffu, mtop);
+      rtop = __reduce_max_sync(0xffffffffu, rtop);
+      if (mtop < 0x0d800000u) mtop = 0;               // below 2^-100
+      if (rtop < 0x0d800000u) rtop = 0;
+      // one division for all four quotients: lanes 0 and 1 448 / top, 2 and 3 the
+      // scales top / 448
+      const float top = __uint_as_float((lane & 1) ? rtop : mtop);
+      const float q = __fdiv_rn((lane & 2) ? top : 448.0f, (lane & 2) ? 448.0f : top);
+      float mi = mtop != 0 ? __shfl_sync(0xffffffffu, q, 0) : 0.0f;
+      float ri = rtop != 0 ? __shfl_sync(0xffffffffu, q, 1) : 0.0f;
+      if (lane == 2) a.m_scale[blk] = q;
+      if (lane == 3) a.v_scale[blk] = q;
+      constexpr uint32_t kMost = 0x46e00000u;         // 28672 = 448 2^6
+      const bool plain = mtop <= kMost && rtop <= kMost;
+      if (plain) mi *= 0x1p-120f, ri *= 0x1p-120f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t um[4], ur[4];
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const uint64_t z = mix_word(word + (uint64_t)(64 * h + j / 2) * kGold);
+          const uint32_t lo = (uint32_t)z, hi = (uint32_t)(z >> 32);
+          um[j] = (lo << 4) & 0xffff0u;
+          ur[j] = (lo >> 12) & 0xffff0u;
+          um[j + 1] = (hi << 4) & 0xffff0u;
+          ur[j + 1] = (hi >> 12) & 0xffff0u;
+        }
+        uint32_t cm, cr;
+        if (plain) {
+          cm = encode4<true>(m[h], mi, um);
+          cr = encode4<false>(v[h], ri, ur);
+        } else {
+          cm = encode4_any<true>(m[h][0], m[h][1], m[h][2], m[h][3], mi, um[0], um[1], um[2], um[3]);
+          cr = encode4_any<false>(v[h][0], v[h][1], v[h][2], v[h][3], ri, ur[0], ur[1], ur[2], ur[3]);
+        }
+        store_codes(static_cast<uint8_t*>(a.m), e + 128 * h, left - 128 * h, cm);
+        store_codes(static_cast<uint8_t*>(a.v), e + 128 * h, left - 128 * h, cr);
+      }
+      word += word_step;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        store_part(static_cast<float*>(a.m) + e + 128 * h, left - 128 * h, m[h]);
+        store_part(static_cast<float*>(a.v) + e + 128 * h, left - 128 * h, v[h]);
+      }
+    }
+    if (next >= end) break;
+    blk = next;
+    if (AHEAD) x = y;
+    else load(blk, x);
   }
 }
 
+// A master copy goes with bf16 weights.
+template <class G, bool E4M3>
+const void* adamw_fn(bool f32_params, bool master) {
+  if (f32_params) return (const void*)adamw_kernel<float, G, E4M3, false>;
+  return master ? (const void*)adamw_kernel<__nv_bfloat16, G, E4M3, true>
+                : (const void*)adamw_kernel<__nv_bfloat16, G, E4M3, false>;
+}
 const void* adamw_fn(int pd, int gd, bool e4m3, bool master) {
-#define BKMOO_ADAM(P, G)                                                                    \
-  (e4m3 ? (master ? (const void*)adamw_kernel<P, G, true, true>                             \
-                  : (const void*)adamw_kernel<P, G, true, false>)                           \
-        : (master ? (const void*)adamw_kernel<P, G, false, true>                            \
-                  : (const void*)adamw_kernel<P, G, false, false>))
-  if (pd == BKMOO_F32) return gd == BKMOO_F32 ? BKMOO_ADAM(float, float) : BKMOO_ADAM(float, __nv_bfloat16);
-  return gd == BKMOO_F32 ? BKMOO_ADAM(__nv_bfloat16, float) : BKMOO_ADAM(__nv_bfloat16, __nv_bfloat16);
-#undef BKMOO_ADAM
+  const bool f = pd == BKMOO_F32;
+  if (gd == BKMOO_F32) return e4m3 ? adamw_fn<float, true>(f, master) : adamw_fn<float, false>(f, master);
+  return e4m3 ? adamw_fn<__nv_bfloat16, true>(f, master) : adamw_fn<__nv_bfloat16, false>(f, master);
 }
 
 // ---- norm ------------------------------------------------------------------
@@ -446,7 +573,7 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
         (weight_decay && !(weight_decay[i] >= 0.0f && std::isfinite(weight_decay[i]))))
       return BKMOO_ERR_INVALID;
     n += sizes[i];
-    if (n > ((int64_t)1 << 42)) return BKMOO_ERR_INVALID;   // one grid holds it
+    if (n > ((int64_t)1 << 48)) return BKMOO_ERR_INVALID;
   }
   if (n == 0) return BKMOO_OK;
   if (!at(grad, 16) || !at(m, 16) || !at(v, 16) || (master && !at(master, 16)) ||
@@ -472,6 +599,12 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
   a.n = n;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const void* fn = adamw_fn(param_dtype, grad_dtype, e4m3, master != nullptr);
+  int dev = 0, sms = 0, per_sm = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, kAdamThreads, 0) != cudaSuccess)
+    return BKMOO_ERR_CUDA;
+  const int64_t grid = (int64_t)sms * (per_sm < 1 ? 1 : per_sm);
   // a launch knows kAdamTable tensors; the blocks that lie in them whole are its
   // own, and the next launch begins with the tensor of the first block left
   const int64_t all = (n + kBlock - 1) / kBlock;
@@ -493,9 +626,10 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
     a.tensors = k;
     a.first = first;
     a.blocks = (end >= n ? all : end / kBlock) - first;
+    int64_t ctas = (a.blocks + kAdamWarps - 1) / kAdamWarps;
+    if (ctas > grid) ctas = grid;
     void* list[] = {&a};
-    if (cudaLaunchKernel(fn, dim3((unsigned)((a.blocks + kAdamSpan - 1) / kAdamSpan)),
-                         dim3(kAdamThreads), list, 0, s) != cudaSuccess)
+    if (cudaLaunchKernel(fn, dim3((unsigned)ctas), dim3(kAdamThreads), list, 0, s) != cudaSuccess)
       return BKMOO_ERR_CUDA;
     first += a.blocks;
   }
