@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kBlock = 256;          // elements per scale, and per warp and turn
 constexpr int kAdamTable = 1024;     // tensors a launch knows
-constexpr int kAdamThreads = 256;
+constexpr int kAdamThreads = 128;
 constexpr int64_t kAdamWarps = kAdamThreads / 32;
 
 struct AdamArgs {
@@ -103,37 +103,35 @@ __device__ __forceinline__ Raw<uint8_t> load_part(const uint8_t* p, int n) {
     if (j < n) w |= (uint32_t)p[j] << (8 * j);
   return {w};
 }
-__device__ __forceinline__ void widen(const Raw<float>& r, float (&x)[4], float) {
-  x[0] = r.x.x, x[1] = r.x.y, x[2] = r.x.z, x[3] = r.x.w;
+__device__ __forceinline__ void widen(const Raw<float>& r, float2 (&x)[2], float) {
+  x[0] = make_float2(r.x.x, r.x.y), x[1] = make_float2(r.x.z, r.x.w);
 }
-__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float (&x)[4], float) {
-  x[0] = __uint_as_float(r.x.x << 16), x[1] = __uint_as_float(r.x.x & 0xffff0000u);
-  x[2] = __uint_as_float(r.x.y << 16), x[3] = __uint_as_float(r.x.y & 0xffff0000u);
+__device__ __forceinline__ void widen(const Raw<__nv_bfloat16>& r, float2 (&x)[2], float) {
+  x[0] = make_float2(__uint_as_float(r.x.x << 16), __uint_as_float(r.x.x & 0xffff0000u));
+  x[1] = make_float2(__uint_as_float(r.x.y << 16), __uint_as_float(r.x.y & 0xffff0000u));
 }
-__device__ __forceinline__ void widen(const Raw<uint8_t>& r, float (&x)[4], float scale) {
+__device__ __forceinline__ void widen(const Raw<uint8_t>& r, float2 (&x)[2], float scale) {
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(r.x >> (16 * j)), __NV_E4M3);
-    const float2 f = __half22float2(__half2(h));
-    x[2 * j] = __fmul_rn(f.x, scale);
-    x[2 * j + 1] = __fmul_rn(f.y, scale);
+    x[j] = __fmul2_rn(__half22float2(__half2(h)), make_float2(scale, scale));
   }
 }
-__device__ __forceinline__ void store4(float* p, const float (&x)[4]) {
-  __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3]));
+__device__ __forceinline__ void store4(float* p, const float2 (&x)[2]) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(x[0].x, x[0].y, x[1].x, x[1].y));
 }
-__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
-  const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float2 (&x)[2]) {
+  const __nv_bfloat162 a = __float22bfloat162_rn(x[0]), b = __float22bfloat162_rn(x[1]);
   __stcs(reinterpret_cast<uint2*>(p),
          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b)));
 }
-__device__ __forceinline__ void store_part(float* p, int64_t n, const float (&x)[4]) {
+__device__ __forceinline__ void store_part(float* p, int64_t n, const float2 (&x)[2]) {
   if (n >= 4) {
     store4(p, x);
   } else {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < n) p[j] = x[j];
+    if (n > 0) p[0] = x[0].x;
+    if (n > 1) p[1] = x[0].y;
+    if (n > 2) p[2] = x[1].x;
   }
 }
 __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, uint32_t w) {
@@ -147,27 +145,31 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, ui
 }
 
 // Four values / their scale as e4m3 bytes, each rounded away from 0 with the
-// chance that its rest gives: u, 16 bits in bits 4 to 19, stands for u / 2^20.
-// `inv` is 2^-120 / scale, and 2^-120 takes e4m3's smallest normal number, 2^-6,
-// to fp32's, 2^-126: the product's bits from the 20th on are the code, of
-// subnormal values too, and what is below them is the rest.  Without SIGNED
-// (roots, which are not negative) what is not 0 does not become 0: 1 + 0xfffff
-// is code 1, 0 + 0xfffff is code 0.
-template <bool SIGNED>
-__device__ __forceinline__ uint32_t encode4(const float (&x)[4], float inv, const uint32_t (&u)[4]) {
+// chance that its rest gives.  `inv` is 2^-120 / scale, and 2^-120 takes e4m3's
+// smallest normal number, 2^-6, to fp32's, 2^-126: the product's bits from the
+// 20th on are the code, of subnormal values too, and what is below them is the
+// rest, of which the upper 16 bits meet the chance's (all 16 places up: the code
+// is the top byte; the block's largest value has an empty rest, so no code is
+// passed).  w: a word for each value, the chance in its low half (SIGNED) or its
+// high half.  FLOOR: what is not 0 does not become 0.
+template <bool SIGNED, bool FLOOR>
+__device__ __forceinline__ uint32_t encode4(const float2 (&x)[2], float inv, const uint32_t (&w)[4]) {
   uint32_t s[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t bits = __float_as_uint(__fmul_rn(fabsf(x[j]), inv));
-    s[j] = __viaddmin_u32(bits, u[j], 0x7efffffu);
-    if (!SIGNED) s[j] = max(s[j], __viaddmin_u32(bits, 0xfffffu, 0x100000u));
-    s[j] <<= 4;                   // the code is the top byte
+  for (int j = 0; j < 2; ++j) {
+    const float2 y = __fmul2_rn(x[j], make_float2(inv, inv));
+    const uint32_t bits[2] = {__float_as_uint(y.x), __float_as_uint(y.y)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s[2 * j + i] = bits[i] * 16 + __byte_perm(w[2 * j + i], 0, SIGNED ? 0x4104 : 0x4324);
+      if (FLOOR && bits[i] != 0) s[2 * j + i] = max(s[2 * j + i], 0x1000000u);
+    }
   }
   uint32_t c = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
   if (SIGNED) {
     const uint32_t g = __byte_perm(
-        __byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0073),
-        __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0073), 0x5410);
+        __byte_perm(__float_as_uint(x[0].x), __float_as_uint(x[0].y), 0x0073),
+        __byte_perm(__float_as_uint(x[1].x), __float_as_uint(x[1].y), 0x0073), 0x5410);
     c |= g & 0x80808080u;
   }
   return c;
@@ -175,14 +177,14 @@ __device__ __forceinline__ uint32_t encode4(const float (&x)[4], float inv, cons
 // The same where 2^-120 / scale is no normal number (a scale above 2^6) or the
 // block has a NaN or an infinity: `inv` is 1 / scale, and a NaN stays one.
 template <bool SIGNED>
-__device__ __noinline__ uint32_t encode4_any(float x0, float x1, float x2, float x3, float inv, uint32_t u0,
-                                             uint32_t u1, uint32_t u2, uint32_t u3) {
-  const float x[4] = {x0, x1, x2, x3};
-  const uint32_t u[4] = {u0, u1, u2, u3};
+__device__ __noinline__ uint32_t encode4_any(float2 x01, float2 x23, float inv, uint32_t w0, uint32_t w1,
+                                             uint32_t w2, uint32_t w3) {
+  const float x[4] = {x01.x, x01.y, x23.x, x23.y};
+  const uint32_t w[4] = {w0, w1, w2, w3};
   uint32_t c = 0;
   for (int j = 0; j < 4; ++j) {
     const uint32_t bits = __float_as_uint(__fmul_rn(__fmul_rn(fabsf(x[j]), inv), 0x1p-120f));
-    uint32_t k = min((bits + u[j]) >> 20, 0x7eu);
+    uint32_t k = min(((bits >> 4) + (SIGNED ? w[j] & 0xffffu : w[j] >> 16)) >> 16, 0x7eu);
     if (!SIGNED) k = max(k, min(bits, 1u));
     if (bits > 0x7f800000u) k = 0x7f;
     if (SIGNED) k |= (__float_as_uint(x[j]) >> 24) & 0x80u;
@@ -222,42 +224,31 @@ __device__ __forceinline__ float reciprocal(float x) {
   return r;
 }
 
-// x[j] without an address of its own.
-__device__ __forceinline__ float pick(const float (&x)[4], int j) {
-  return j < 2 ? (j ? x[1] : x[0]) : (j == 2 ? x[2] : x[3]);
-}
-__device__ __forceinline__ void put(float (&x)[4], int j, float y) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = i == j ? y : x[i];
-}
-
-// One element's step: moments in place (v as its root in 8 bits), the new weight
+// Two elements' step: moments in place (v as its root in 8 bits), the new weights
 // returned.  The moments round as written, product by product: in 8 bits a last
 // bit can move a code.
 template <bool E4M3>
 struct Step {
   float b1, one_b1, b2, one_b2, rate, root, eps, clip;
-  __device__ __forceinline__ float operator()(float g, float keep, float w, float& m, float& v) const {
-    const float gj = __fmul_rn(g, clip);
-    const float old = E4M3 ? __fmul_rn(v, v) : v;
-    m = __fadd_rn(__fmul_rn(m, b1), __fmul_rn(gj, one_b1));
-    const float vj = __fadd_rn(__fmul_rn(old, b2), __fmul_rn(__fmul_rn(gj, gj), one_b2));
-    const float r = root_of(vj);
+  __device__ __forceinline__ float2 operator()(float2 g, float2 keep, float2 w, float2& m, float2& v) const {
+    auto both = [](float x) { return make_float2(x, x); };
+    const float2 gj = __fmul2_rn(g, both(clip));
+    const float2 old = E4M3 ? __fmul2_rn(v, v) : v;
+    m = __fadd2_rn(__fmul2_rn(m, both(b1)), __fmul2_rn(gj, both(one_b1)));
+    const float2 vj = __fadd2_rn(__fmul2_rn(old, both(b2)), __fmul2_rn(__fmul2_rn(gj, gj), both(one_b2)));
+    const float2 r = make_float2(root_of(vj.x), root_of(vj.y));
     v = E4M3 ? r : vj;
-    return fmaf(-rate * m, reciprocal(fmaf(r, root, eps)), w * keep);
-  }
-  __device__ __forceinline__ float operator()(float g, float keep, float w, float (&m)[4], float (&v)[4],
-                                              int j) const {
-    float mj = pick(m, j), vj = pick(v, j);
-    const float r = (*this)(g, keep, w, mj, vj);
-    put(m, j, mj);
-    put(v, j, vj);
-    return r;
+    const float2 den = __ffma2_rn(r, both(root), both(eps));
+    const float2 q = make_float2(reciprocal(den.x), reciprocal(den.y));
+    return __ffma2_rn(__fmul2_rn(m, both(-rate)), q, __fmul2_rn(w, keep));
   }
 };
+__device__ __forceinline__ uint32_t top_of(uint32_t t, float a, float b) {
+  return __vimax3_u32(t, __float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu);
+}
 
 template <class P, class G, bool E4M3, bool MASTER>
-__global__ void __launch_bounds__(kAdamThreads)
+__global__ void __launch_bounds__(kAdamThreads, E4M3 ? 6 : 7)
     adamw_kernel(const __grid_constant__ AdamArgs a) {
   using S = typename State<E4M3>::T;
   using W = typename std::conditional<MASTER, float, P>::type;    // what the step reads
@@ -335,18 +326,19 @@ __global__ void __launch_bounds__(kAdamThreads)
     Loaded<W, G, E4M3> y;
     if (AHEAD && next < end) load(next, y);
     const int64_t e = blk * kBlock + 4 * lane;
-    float m[2][4], v[2][4];
-    uint32_t mtop = 0, rtop = 0;
+    float2 m[2][2], v[2][2];
+    uint32_t mtop = 0, rtop = 0, rlow = 0xffffffffu;
     if (x.p) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float g[4], w[4];
+        float2 g[2], w[2];
         widen(x.g[h], g, 1.0f);
         widen(x.m[h], m[h], x.ms);
         widen(x.v[h], v[h], x.vs);
         widen(x.w[h], w, 1.0f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = step(g[j], x.keep, w[j], m[h][j], v[h][j]);
+        for (int j = 0; j < 2; ++j)
+          w[j] = step(g[j], make_float2(x.keep, x.keep), w[j], m[h][j], v[h][j]);
         if (MASTER) {
           store4(a.master + e + 128 * h, w);
           store4(static_cast<P*>(a.p[x.t]) + (e - a.start[x.t]) + 128 * h, w);
@@ -358,21 +350,38 @@ __global__ void __launch_bounds__(kAdamThreads)
       // a tensor ends in the block, or its weights lie askew: one by one
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float g[4], w[4] = {};
+        float2 g[2], w[2] = {};
         widen(x.g[h], g, 1.0f);
         widen(x.m[h], m[h], x.ms);
         widen(x.v[h], v[h], x.vs);
         if (MASTER) widen(x.w[h], w, 1.0f);
+        P* p[4] = {};
+        float keeps[4] = {};
         int tj = x.t;
-#pragma unroll 1
+#pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int64_t i = e + 128 * h + j;
-          if (i >= a.n) break;
-          tj = tensor_of(a, tj, i);
-          P* p = static_cast<P*>(a.p[tj]) + (i - a.start[tj]);
-          const float wj = step(pick(g, j), a.keep[tj], MASTER ? pick(w, j) : (float)*p, m[h], v[h], j);
-          *p = (P)wj;
-          if (MASTER) a.master[i] = wj;
+          if (i < a.n) {
+            tj = tensor_of(a, tj, i);
+            p[j] = static_cast<P*>(a.p[tj]) + (i - a.start[tj]);
+            keeps[j] = a.keep[tj];
+            if (!MASTER) (j & 1 ? w[j / 2].y : w[j / 2].x) = (float)*p[j];
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          float2 m2 = m[h][j], v2 = v[h][j];
+          w[j] = step(g[j], make_float2(keeps[2 * j], keeps[2 * j + 1]), w[j], m2, v2);
+          if (p[2 * j]) {
+            *p[2 * j] = (P)w[j].x;
+            if (MASTER) a.master[e + 128 * h + 2 * j] = w[j].x;
+            m[h][j].x = m2.x, v[h][j].x = v2.x;
+          }
+          if (p[2 * j + 1]) {
+            *p[2 * j + 1] = (P)w[j].y;
+            if (MASTER) a.master[e + 128 * h + 2 * j + 1] = w[j].y;
+            m[h][j].y = m2.y, v[h][j].y = v2.y;
+          }
         }
       }
     }
@@ -382,12 +391,14 @@ __global__ void __launch_bounds__(kAdamThreads)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          mtop = max(mtop, __float_as_uint(m[h][j]) & 0x7fffffffu);
-          rtop = max(rtop, __float_as_uint(v[h][j]));
+        for (int j = 0; j < 2; ++j) {
+          mtop = top_of(mtop, m[h][j].x, m[h][j].y);
+          rtop = __vimax3_u32(rtop, __float_as_uint(v[h][j].x), __float_as_uint(v[h][j].y));
+          rlow = __vimin3_u32(rlow, __float_as_uint(v[h][j].x), __float_as_uint(v[h][j].y));
         }
       mtop = __reduce_max_sync(0xffffffffu, mtop);
       rtop = __reduce_max_sync(0xffffffffu, rtop);
+      rlow = __reduce_min_sync(0xffffffffu, rlow);
       if (mtop < 0x0d800000u) mtop = 0;               // below 2^-100
       if (rtop < 0x0d800000u) rtop = 0;
       // one division for all four quotients: lanes 0 and 1 448 / top, 2 and 3 the
@@ -401,25 +412,23 @@ __global__ void __launch_bounds__(kAdamThreads)
       constexpr uint32_t kMost = 0x46e00000u;         // 28672 = 448 2^6
       const bool plain = mtop <= kMost && rtop <= kMost;
       if (plain) mi *= 0x1p-120f, ri *= 0x1p-120f;
+      // no root is as small as a code of 0
+      const bool above = __float_as_uint(__uint_as_float(rlow) * ri) >= 0x100000u;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint32_t um[4], ur[4];
+        uint32_t u[4], cm, cr;
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-          const uint64_t z = mix_word(word + (uint64_t)(64 * h + j / 2) * kGold);
-          const uint32_t lo = (uint32_t)z, hi = (uint32_t)(z >> 32);
-          um[j] = (lo << 4) & 0xffff0u;
-          ur[j] = (lo >> 12) & 0xffff0u;
-          um[j + 1] = (hi << 4) & 0xffff0u;
-          ur[j + 1] = (hi >> 12) & 0xffff0u;
+        for (int j = 0; j < 2; ++j) {
+          const uint64_t z = mix_word(word + (uint64_t)(64 * h + j) * kGold);
+          u[2 * j] = (uint32_t)z;
+          u[2 * j + 1] = (uint32_t)(z >> 32);
         }
-        uint32_t cm, cr;
         if (plain) {
-          cm = encode4<true>(m[h], mi, um);
-          cr = encode4<false>(v[h], ri, ur);
+          cm = encode4<true, false>(m[h], mi, u);
+          cr = above ? encode4<false, false>(v[h], ri, u) : encode4<false, true>(v[h], ri, u);
         } else {
-          cm = encode4_any<true>(m[h][0], m[h][1], m[h][2], m[h][3], mi, um[0], um[1], um[2], um[3]);
-          cr = encode4_any<false>(v[h][0], v[h][1], v[h][2], v[h][3], ri, ur[0], ur[1], ur[2], ur[3]);
+          cm = encode4_any<true>(m[h][0], m[h][1], mi, u[0], u[1], u[2], u[3]);
+          cr = encode4_any<false>(v[h][0], v[h][1], ri, u[0], u[1], u[2], u[3]);
         }
         store_codes(static_cast<uint8_t*>(a.m), e + 128 * h, left - 128 * h, cm);
         store_codes(static_cast<uint8_t*>(a.v), e + 128 * h, left - 128 * h, cr);
