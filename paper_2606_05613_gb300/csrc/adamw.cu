@@ -250,6 +250,7 @@ __device__ __forceinline__ uint32_t top_of(uint32_t t, float a, float b) {
 template <class P, class G, bool E4M3, bool MASTER>
 __global__ void __launch_bounds__(kAdamThreads, E4M3 ? 6 : 7)
     adamw_kernel(const __grid_constant__ AdamArgs a) {
+  grid_wait();
   using S = typename State<E4M3>::T;
   using W = typename std::conditional<MASTER, float, P>::type;    // what the step reads
   const int lane = threadIdx.x & 31;
@@ -471,6 +472,7 @@ static_assert(kNormCtas * sizeof(double) <= BKMOO_NORM_WS_BYTES, "workspace");
 // CTA's by a fixed tree.  The order is fixed by n alone.
 template <class G>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const G* g, int64_t n, double* part) {
+  grid_wait();
   constexpr int V = 16 / sizeof(G);
   const int64_t vecs = n / V, stride = (int64_t)gridDim.x * kNormThreads;
   const uint4* q = reinterpret_cast<const uint4*>(g);
@@ -511,6 +513,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const G* g, int64_t 
   if (threadIdx.x == 0) part[blockIdx.x] = sh[0];
 }
 __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(const double* part, int n, float* out) {
+  grid_wait();
   double sum = 0.0;
   for (int i = threadIdx.x; i < n; i += kNormThreads) sum += part[i];
   __shared__ double sh[kNormThreads];
@@ -552,13 +555,16 @@ extern "C" int bkmoo_grad_norm(const void* grad, int32_t dtype, int64_t n, float
   int64_t ctas = (n + per - 1) / per;
   ctas = ctas < 1 ? 1 : ctas > kNormCtas ? kNormCtas : ctas;
   double* part = static_cast<double*>(ws);
-  if (dtype == BKMOO_F32)
-    norm_kernel<float><<<(unsigned)ctas, kNormThreads, 0, s>>>(static_cast<const float*>(grad), n, part);
-  else
-    norm_kernel<__nv_bfloat16><<<(unsigned)ctas, kNormThreads, 0, s>>>(
-        static_cast<const __nv_bfloat16*>(grad), n, part);
-  norm_sum_kernel<<<1, kNormThreads, 0, s>>>(part, (int)ctas, out_norm);
-  return cudaGetLastError() == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
+  int parts = (int)ctas;
+  void* first[] = {&grad, &n, &part};
+  void* second[] = {&part, &parts, &out_norm};
+  const void* fn = dtype == BKMOO_F32 ? (const void*)norm_kernel<float>
+                                      : (const void*)norm_kernel<__nv_bfloat16>;
+  if (launch_behind(fn, dim3(parts), dim3(kNormThreads), first, 0, s, true) != cudaSuccess ||
+      launch_behind((const void*)norm_sum_kernel, dim3(1), dim3(kNormThreads), second, 0, s, true) !=
+          cudaSuccess)
+    return BKMOO_ERR_CUDA;
+  return BKMOO_OK;
 }
 
 extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const float* weight_decay,
@@ -638,7 +644,7 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
     int64_t ctas = (a.blocks + kAdamWarps - 1) / kAdamWarps;
     if (ctas > grid) ctas = grid;
     void* list[] = {&a};
-    if (cudaLaunchKernel(fn, dim3((unsigned)ctas), dim3(kAdamThreads), list, 0, s) != cudaSuccess)
+    if (launch_behind(fn, dim3((unsigned)ctas), dim3(kAdamThreads), list, 0, s, true) != cudaSuccess)
       return BKMOO_ERR_CUDA;
     first += a.blocks;
   }

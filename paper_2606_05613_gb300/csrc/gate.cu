@@ -2,6 +2,7 @@
 // per-language weight gradient of a linear layer (include/bkmoo.h): argument
 // checks, the choice of tiles, and the pass that turns dh into da and db.  The
 // products are tile_gemm.cuh's.
+#include "gate_few.cuh"
 #include "tile_host.cuh"
 
 namespace bkmoo {
@@ -40,6 +41,7 @@ struct SlopeArgs {
 // The products behind it take bf16 operands, so da and db are rounded to bf16
 // here, once, from fp32.
 __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
+  grid_wait();
   const int64_t per = (p.cols + 7) / 8, n = p.rows * per;
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n;
        i += (int64_t)gridDim.x * blockDim.x) {
@@ -78,16 +80,13 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
   }
 }
 
-// Whether the CTAs work in pairs.
-int choose_pair(int64_t rows) { return rows > kTileM ? 2 : 1; }
-
 // dW_k = dy_k^T x_k for one or two dy (mats), every language.
 int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, int64_t ldx,
                  int64_t M, int64_t N, int32_t K, const int64_t* rows, void* const* const* dw,
                  int32_t dw_dtype, int32_t accumulate, cudaStream_t s) {
-  const int cg = choose_pair(M);
   TileArgs<kWeight> p = {};
-  int r = tile_status_word(s, &p.status);
+  int sms = 0, r = tile_sms(&sms);
+  if (r == BKMOO_OK) r = tile_status_word(s, &p.status);
   if (r != BKMOO_OK) return r;
   const int elem = dw_dtype == BKMOO_F32 ? 4 : 2;
   bool any = false;
@@ -112,8 +111,9 @@ int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, 
   if (!any) return BKMOO_OK;
   p.rows = (int32_t)M;
   p.cols = (int32_t)N;
-  p.tiles_m = up(M, kTileM * cg);
-  p.tiles_n = up(N, kTileN);
+  const TileShape shape = tile_shape(M, N, false, p.nkt, K, mats, sms);
+  p.tiles_m = up(M, kTileM * shape.cg);
+  p.tiles_n = up(N, shape.bn);
   p.mats = mats;
   p.n_lang = K;
   p.out_dtype = dw_dtype;
@@ -121,7 +121,7 @@ int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, 
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * mats * K;
   if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
   p.tiles = (int32_t)tiles;
-  return tile_launch(tile_weight_fn(cg), cg, &p, tiles, s);
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, tiles, s);
 }
 
 bool grads_ok(void* const* dw, int32_t K, int32_t dtype) {
@@ -148,26 +148,36 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
       (a && (!operand_ok(a, T, F, ld_ab) || !operand_ok(b, T, F, ld_ab))))
     return BKMOO_ERR_INVALID;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int cg = choose_pair(T);
+  int sms = 0, r = tile_sms(&sms);
+  if (r != BKMOO_OK) return r;
+  if (T <= kFewRows) {
+    const FewArgs q = {static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w_gate),
+                       static_cast<const __nv_bfloat16*>(w_up), static_cast<__nv_bfloat16*>(h),
+                       static_cast<__nv_bfloat16*>(a), static_cast<__nv_bfloat16*>(b), ldx, ldw, ldh,
+                       ld_ab, (int32_t)T, (int32_t)D, (int32_t)F, act};
+    return launch_gate_few(q, sms, s) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
+  }
+  const int32_t nkt = up(D, kTileK);
+  const TileShape shape = tile_shape(T, F, true, &nkt, 1, 1, sms);
   TileArgs<kGate> p = {};
-  int r = tile_status_word(s, &p.status);
-  if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, 128);
-  if (r == BKMOO_OK) r = tile_map(&p.b[0], w_gate, F, D, ldw, 128);
-  if (r == BKMOO_OK) r = tile_map(&p.b[1], w_up, F, D, ldw, 128);
+  r = tile_status_word(s, &p.status);
+  if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, kTileM);
+  if (r == BKMOO_OK) r = tile_map(&p.b[0], w_gate, F, D, ldw, shape.bn / 2);
+  if (r == BKMOO_OK) r = tile_map(&p.b[1], w_up, F, D, ldw, shape.bn / 2);
   if (r != BKMOO_OK) return r;
   p.out[0] = {h, ldh, store_width(h, ldh, 2)};
   p.out[1] = {a, ld_ab, store_width(a, ld_ab, 2)};
   p.out[2] = {b, ld_ab, store_width(b, ld_ab, 2)};
   p.rows = (int32_t)T;
   p.cols = (int32_t)F;
-  p.tiles_m = up(T, kTileM * cg);
-  p.tiles_n = up(F, kTileN / 2);
-  p.nkt = up(D, kTileK);
+  p.tiles_m = up(T, kTileM * shape.cg);
+  p.tiles_n = up(F, shape.bn / 2);
+  p.nkt = nkt;
   p.act = act;
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
   if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
   p.tiles = (int32_t)tiles;
-  return tile_launch(tile_gate_fn(cg), cg, &p, tiles, s);
+  return tile_launch(tile_gate_fn(shape.cg, shape.bn), shape, &p, tiles, s);
 }
 
 extern "C" int bkmoo_gate_backward_workspace_size(int64_t T, int64_t F, size_t* bytes) {
@@ -192,6 +202,8 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int64_t ld = (F + 7) / 8 * 8;
   __nv_bfloat16* d[2] = {nullptr, nullptr};
+  int sms = 0, r = tile_sms(&sms);
+  if (r != BKMOO_OK) return r;
   if (T > 0) {
     if (!operand_ok(dh, T, F, ld_dh) || !operand_ok(a, T, F, ld_ab) || !operand_ok(b, T, F, ld_ab) ||
         !operand_ok(x, T, D, ldx) || (dx && !operand_ok(dx, T, D, ld_dx)) || !ws ||
@@ -202,35 +214,35 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     if (ws_bytes < need) return BKMOO_ERR_WORKSPACE;
     d[0] = static_cast<__nv_bfloat16*>(ws);
     d[1] = d[0] + need / 4;
-    int sms = 0;
-    const int r = tile_sms(&sms);
-    if (r != BKMOO_OK) return r;
     SlopeArgs q = {static_cast<const __nv_bfloat16*>(dh), static_cast<const __nv_bfloat16*>(a),
                    static_cast<const __nv_bfloat16*>(b), d[0], d[1], ld_dh, ld_ab, ld, T, (int32_t)F, act};
     const int64_t blocks = (T * (ld / 8) + 255) / 256, most = (int64_t)sms * 8;
-    gate_slope_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(q);
-    if (cudaGetLastError() != cudaSuccess) return BKMOO_ERR_CUDA;
+    void* list[] = {&q};
+    if (launch_behind((const void*)gate_slope_kernel, dim3((unsigned)(blocks < most ? blocks : most)),
+                      dim3(256), list, 0, s, true) != cudaSuccess)
+      return BKMOO_ERR_CUDA;
   }
   if (dx && T > 0) {
-    const int cg = choose_pair(T);
+    const int32_t nkt = 2 * up(F, kTileK);
+    const TileShape shape = tile_shape(T, D, false, &nkt, 1, 1, sms);
     TileArgs<kInput> p = {};
-    int r = tile_status_word(s, &p.status);
+    r = tile_status_word(s, &p.status);
     const void* w[2] = {w_gate, w_up};
     for (int i = 0; i < 2 && r == BKMOO_OK; ++i) {
-      r = tile_map(&p.a[i], d[i], T, F, ld, 128);
+      r = tile_map(&p.a[i], d[i], T, F, ld, kTileM);
       if (r == BKMOO_OK) r = tile_map(&p.b[i], w[i], F, D, ldw, kTileK);
     }
     if (r != BKMOO_OK) return r;
     p.out = {dx, ld_dx, store_width(dx, ld_dx, 2)};
     p.rows = (int32_t)T;
     p.cols = (int32_t)D;
-    p.tiles_m = up(T, kTileM * cg);
-    p.tiles_n = up(D, kTileN);
-    p.nkt = up(F, kTileK);
+    p.tiles_m = up(T, kTileM * shape.cg);
+    p.tiles_n = up(D, shape.bn);
+    p.nkt = nkt / 2;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
     if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
     p.tiles = (int32_t)tiles;
-    r = tile_launch(tile_input_fn(cg), cg, &p, tiles, s);
+    r = tile_launch(tile_input_fn(shape.cg, shape.bn), shape, &p, tiles, s);
     if (r != BKMOO_OK) return r;
   }
   if (!weights) return BKMOO_OK;

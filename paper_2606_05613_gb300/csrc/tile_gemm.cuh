@@ -5,9 +5,9 @@
 //   kInput   dx = da Wg + db Wu                         sum over the hidden width
 //   kWeight  dW_k = dy_k^T x_k for every language k     sum over its rows
 //
-// A tile is 128 rows (256 with a CTA pair) by 256 columns of fp32 accumulators;
-// for kGate 128 columns of a and the same 128 of b, so that h is formed where
-// both are.  Warp 8 of a CTA copies operand tiles of 64 along the sum into a
+// A tile is 128 rows (256 with a CTA pair) by BN = 64, 128 or 256 columns of fp32
+// accumulators; for kGate half of them columns of a and half the same ones of b, so
+// that h is formed where both are.  Warp 8 of a CTA copies operand tiles of 64 along the sum into a
 // ring of stages (TMA, 128-byte swizzle, rows and columns beyond the matrix are
 // zeros), one thread of warp 9 issues the products (tcgen05) into one of two
 // accumulators in tensor memory, and warps 0-7 take the other to global memory
@@ -25,23 +25,27 @@ namespace bkmoo {
 enum TileKind { kGate = 0, kInput = 1, kWeight = 2 };
 
 constexpr int kTileM = 128;    // rows of a CTA's tile
-constexpr int kTileN = 256;    // accumulator columns
 constexpr int kTileK = 64;     // of the sum per stage: 128 bytes, the swizzle's row
 constexpr int kTileEpilogueWarps = 8;
 constexpr int kTileThreads = 32 * (kTileEpilogueWarps + 2);
 constexpr int kTileGroupM = 8;  // tiles of rows that are worked on together
 
-__host__ __device__ constexpr int tile_stages(int cg) { return cg == 1 ? 4 : 6; }
-__host__ __device__ constexpr int tile_b_bytes(int cg) { return (cg == 1 ? 256 : 128) * kTileK * 2; }
-__host__ __device__ constexpr int tile_stage_bytes(int cg) {
-  return kTileM * kTileK * 2 + tile_b_bytes(cg);
+// cg: CTAs that share a tile, bn: its columns.
+__host__ __device__ constexpr int tile_stage_bytes(int cg, int bn) {
+  return (kTileM + bn / cg) * kTileK * 2;
 }
-__host__ __device__ constexpr int tile_smem(int cg) {
-  return tile_stages(cg) * tile_stage_bytes(cg) + 1024;   // stages start on 1024 bytes
+__host__ __device__ constexpr int tile_stages(int cg, int bn) {
+  return 196608 / tile_stage_bytes(cg, bn);
+}
+// Where a warp turns 32 x 32 results from rows of lanes to rows of memory.
+constexpr int kTurnBytes = 32 * 33 * 4;
+__host__ __device__ constexpr int tile_smem(int cg, int bn) {
+  return tile_stages(cg, bn) * tile_stage_bytes(cg, bn) + 1024 +   // stages start on 1024 bytes
+         kTileEpilogueWarps * kTurnBytes;
 }
 
 // Where a result goes: rows of `ld` elements.  `vec` is the widest store that
-// every row's 32-column pieces allow: 32, 16 or 0 bytes (element by element).
+// every row's 32-column pieces allow: 32, 16 or 0 bytes (kWeight only).
 struct TileOut {
   void* p;
   int64_t ld;
@@ -90,7 +94,7 @@ struct Tile {
   int g, m0, n0, nkt;   // g: kWeight's matrix * kMaxK + language
 };
 
-template <int KIND, int CG>
+template <int KIND, int CG, int BN>
 __device__ __forceinline__ Tile tile_at(const TileArgs<KIND>& p, int t) {
   Tile r;
   int i = t;
@@ -114,7 +118,7 @@ __device__ __forceinline__ Tile tile_at(const TileArgs<KIND>& p, int t) {
   const int high = p.tiles_m - first < kTileGroupM ? p.tiles_m - first : kTileGroupM;
   const int j = i - b * band;
   r.m0 = (first + j % high) * (kTileM * CG);
-  r.n0 = (j / high) * (KIND == kGate ? kTileN / 2 : kTileN);
+  r.n0 = (j / high) * (KIND == kGate ? BN / 2 : BN);
   return r;
 }
 
@@ -128,39 +132,30 @@ __device__ __forceinline__ void st_global32(void* p, const uint32_t* w) {
                : "memory");
 }
 
-// 32 columns of one row, the first n of which exist.
+// 32 columns of one row, the first n of which exist, 16-byte aligned.
 __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&v)[32], int n, int vec) {
-  if (vec != 0 && n >= 32) {
-    uint32_t w[16];
+  uint32_t w[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-    if (vec == 32) {
-      st_global32(p, w);
-      st_global32(p + 16, w + 8);
+  for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  if (vec == 32 && n >= 32) {
+    st_global32(p, w);
+    st_global32(p + 16, w + 8);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (n >= 8 * j + 8) {
+      reinterpret_cast<uint4*>(p)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
     } else {
-      uint4* q = reinterpret_cast<uint4*>(p);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) q[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+      for (int i = 0; i < 8; ++i)
+        if (8 * j + i < n) p[8 * j + i] = __float2bfloat16_rn(v[8 * j + i]);
     }
-    return;
   }
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < n) p[j] = __float2bfloat16_rn(v[j]);
 }
-__device__ __forceinline__ void store_row(float* p, const float (&v)[32], int n, int vec) {
-  if (vec != 0 && n >= 32) {
-    float4* q = reinterpret_cast<float4*>(p);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < n) p[j] = v[j];
-}
-__device__ __forceinline__ void add_row(const __nv_bfloat16* p, float (&v)[32], int n, int vec) {
-  if (vec != 0 && n >= 32) {
+// The same of whole pieces (n = 32), added to what is there where `add`.
+__device__ __forceinline__ void put_row(__nv_bfloat16* p, float (&v)[32], int vec, bool add) {
+  if (add) {
     const uint4* q = reinterpret_cast<const uint4*>(p);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -172,28 +167,47 @@ __device__ __forceinline__ void add_row(const __nv_bfloat16* p, float (&v)[32], 
         v[8 * j + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
       }
     }
-    return;
   }
-#pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < n) v[j] += __bfloat162float(p[j]);
+  store_row(p, v, 32, vec);
 }
-__device__ __forceinline__ void add_row(const float* p, float (&v)[32], int n, int vec) {
-  if (vec != 0 && n >= 32) {
-    const float4* q = reinterpret_cast<const float4*>(p);
+__device__ __forceinline__ void put_row(float* p, float (&v)[32], int, bool add) {
+  float4* q = reinterpret_cast<float4*>(p);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 x = q[j];
-      v[4 * j] += x.x;
-      v[4 * j + 1] += x.y;
-      v[4 * j + 2] += x.z;
-      v[4 * j + 3] += x.w;
+  for (int j = 0; j < 8; ++j) {
+    float4 x = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    if (add) {
+      const float4 y = q[j];
+      x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
     }
-    return;
+    q[j] = x;
   }
+}
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ void as_type(float* p, float x) { *p = x; }
+__device__ __forceinline__ void as_type(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// The warp's 32 rows of 32 columns, of which the first `rows` and n exist, where
+// they are not aligned for vectors: turned in shared memory, so that the warp
+// writes a row at a time, 32 neighbours, instead of one element of 32 rows (771 x
+// 517 in fp32, 3 languages: 37 us so).
+template <class T>
+__device__ __forceinline__ void put_turned(T* p, int64_t ld, const float (&v)[32], int rows, int n,
+                                           bool add, float* turn) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int j = 0; j < 32; ++j)
-    if (j < n) v[j] += p[j];
+  for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
+  __syncwarp();
+  if (lane < n) {
+#pragma unroll 8
+    for (int r = 0; r < 32; ++r) {
+      if (r >= rows) break;
+      T* q = p + r * ld + lane;
+      const float x = turn[r * 33 + lane];
+      as_type(q, add ? x + as_float(*q) : x);
+    }
+  }
+  __syncwarp();
 }
 
 __device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int col,
@@ -212,17 +226,17 @@ __device__ __forceinline__ float activation(int act, float a) {
   return a * sigmoid(1.59576912f * (a + 0.044715f * a * a * a));
 }
 
-template <int CG>
+template <int CG, int BN>
 struct TileShared {
-  uint64_t full[tile_stages(CG)], empty[tile_stages(CG)];   // full: the first CTA's, for both
-  uint64_t tfull[2], tempty[2];                             // tempty: the first CTA's, for both
+  uint64_t full[tile_stages(CG, BN)], empty[tile_stages(CG, BN)];  // full: the first CTA's, for both
+  uint64_t tfull[2], tempty[2];                                    // tempty: the first CTA's, for both
   uint64_t drain;
   uint32_t tmem;
   int abort;
 };
 
 // Operand tiles of one step of the sum.
-template <int KIND, int CG>
+template <int KIND, int CG, int BN>
 __device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t, int kt,
                                           unsigned rank, unsigned char* a, unsigned char* b,
                                           uint32_t bar) {
@@ -231,7 +245,7 @@ __device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t
     tile_load<CG>(a, &p.a, kt * kTileK, m, bar);
     if (CG == 1) {
       tile_load<CG>(b, &p.b[0], kt * kTileK, t.n0, bar);
-      tile_load<CG>(b + 128 * kTileK * 2, &p.b[1], kt * kTileK, t.n0, bar);
+      tile_load<CG>(b + BN / 2 * kTileK * 2, &p.b[1], kt * kTileK, t.n0, bar);
     } else {
       tile_load<CG>(b, &p.b[rank], kt * kTileK, t.n0, bar);
     }
@@ -249,27 +263,40 @@ __device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t
       tile_load<CG>(a + 64 * kTileK * 2, &p.a[t.g], m + 64, y, bar);
       bm = &p.b[t.g % kMaxK];
     }
-    const int n = t.n0 + (int)rank * 128;
+    const int n = t.n0 + (int)rank * (BN / CG);
 #pragma unroll
-    for (int c = 0; c < (CG == 1 ? 4 : 2); ++c)
+    for (int c = 0; c < BN / CG / 64; ++c)
       tile_load<CG>(b + c * 64 * kTileK * 2, bm, n + 64 * c, y, bar);
+  }
+}
+
+// A warp's 32 rows (this thread's: `row`) by 32 columns of a gradient.
+template <class T>
+__device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile& t, int row, int at,
+                                          float (&v)[32], int n, float* turn) {
+  T* q = static_cast<T*>(p.out[t.g]) + (int64_t)row * p.cols + t.n0 + at;
+  if (p.vec[t.g] != 0 && n >= 32) {
+    if (row < p.rows) put_row(q, v, p.vec[t.g], p.accumulate);
+  } else {
+    const int lane = threadIdx.x & 31;
+    put_turned(q - (int64_t)lane * p.cols, p.cols, v, p.rows - (row - lane), n, p.accumulate, turn);
   }
 }
 
 // One warp's share of a finished tile: rows of its quarter, columns of its half.
 // `acc`: the accumulator's tensor-memory address for this warp's lanes; `empty`:
 // the tile's sum is empty and the accumulator was not written.
-template <int KIND>
+template <int KIND, int BN>
 __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t, int row, int half,
-                                          uint32_t acc, bool empty) {
+                                          uint32_t acc, bool empty, float* turn) {
   const bool live = row < p.rows;
   if constexpr (KIND == kGate) {
 #pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
-      const int at = 64 * half + 32 * c, n = p.cols - (t.n0 + at);
+    for (int at = 32 * half; at < BN / 2; at += 64) {
+      const int n = p.cols - (t.n0 + at);
       uint32_t ra[32], rb[32];
       tc_load32(ra, acc + at);
-      tc_load32(rb, acc + 128 + at);
+      tc_load32(rb, acc + BN / 2 + at);
       tc_landed(ra);
       tc_landed(rb);
       if (live && n > 0) {
@@ -291,30 +318,22 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
     }
   } else {
 #pragma unroll 1
-    for (int c = 0; c < 4; ++c) {
-      const int at = 128 * half + 32 * c, n = p.cols - (t.n0 + at);
+    for (int at = 32 * half; at < BN; at += 64) {
+      const int n = p.cols - (t.n0 + at);
       uint32_t r[32];
       if (!empty) {
         tc_load32(r, acc + at);
         tc_landed(r);
       }
-      if (live && n > 0) {
+      if (n > 0) {
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[j]);
         if constexpr (KIND == kInput) {
-          store_bf16(p.out, row, t.n0 + at, v, n);
+          if (live) store_bf16(p.out, row, t.n0 + at, v, n);
         } else if (!(empty && p.accumulate)) {
-          const int64_t to = (int64_t)row * p.cols + t.n0 + at;
-          if (p.out_dtype == BKMOO_BF16) {
-            __nv_bfloat16* q = static_cast<__nv_bfloat16*>(p.out[t.g]) + to;
-            if (p.accumulate) add_row(q, v, n, p.vec[t.g]);
-            store_row(q, v, n, p.vec[t.g]);
-          } else {
-            float* q = static_cast<float*>(p.out[t.g]) + to;
-            if (p.accumulate) add_row(q, v, n, p.vec[t.g]);
-            store_row(q, v, n, p.vec[t.g]);
-          }
+          if (p.out_dtype == BKMOO_BF16) put_piece<__nv_bfloat16>(p, t, row, at, v, n, turn);
+          else put_piece<float>(p, t, row, at, v, n, turn);
         }
       }
       __syncwarp();   // the loads are the whole warp's
@@ -322,14 +341,15 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
   }
 }
 
-template <int KIND, int CG>
+template <int KIND, int CG, int BN>
 __global__ void __launch_bounds__(kTileThreads, 1)
     tile_gemm_kernel(const __grid_constant__ TileArgs<KIND> p) {
-  constexpr int S = tile_stages(CG), A_BYTES = kTileM * kTileK * 2;
+  constexpr int S = tile_stages(CG, BN), A_BYTES = kTileM * kTileK * 2;
   constexpr bool A_ACROSS = KIND == kWeight, B_ACROSS = KIND != kGate;
   extern __shared__ unsigned char raw[];
-  __shared__ TileShared<CG> sh;
+  __shared__ TileShared<CG, BN> sh;
   unsigned char* ring = raw + ((1024 - (st_smem(raw) & 1023)) & 1023);
+  float* turn = reinterpret_cast<float*>(ring + S * tile_stage_bytes(CG, BN));
   const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const unsigned rank = CG == 1 ? 0 : cluster_rank();
   const int first = blockIdx.x / CG, stride = gridDim.x / CG;
@@ -348,12 +368,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (wid == kTileEpilogueWarps + 1) {
-    tmem_alloc<CG>(&sh.tmem, 512);
+    tmem_alloc<CG>(&sh.tmem, 2 * BN);
     tc_fence_before();
   }
   __syncthreads();
   if (CG == 2) cluster_sync();
   tc_fence_after();
+  grid_wait();
   const uint32_t tmem = sh.tmem;
   volatile int* abort = &sh.abort;
 
@@ -361,13 +382,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     if (elect_one()) {
       int s = 0, laps = 0;
       for (int i = first; i < p.tiles && !*abort; i += stride) {
-        const Tile t = tile_at<KIND, CG>(p, i);
+        const Tile t = tile_at<KIND, CG, BN>(p, i);
         for (int kt = 0; kt < t.nkt; ++kt) {
           if (!bar_wait<CG>(&sh.empty[s], (laps & 1) ^ 1, abort)) break;
-          unsigned char* a = ring + s * tile_stage_bytes(CG);
+          unsigned char* a = ring + s * tile_stage_bytes(CG, BN);
           const uint32_t bar = CG == 1 ? st_smem(&sh.full[s]) : peer_smem(&sh.full[s], 0);
-          if (rank == 0) bar_arrive_tx(&sh.full[s], CG * tile_stage_bytes(CG));
-          load_step<KIND, CG>(p, t, kt, rank, a, a + A_BYTES, bar);
+          if (rank == 0) bar_arrive_tx(&sh.full[s], CG * tile_stage_bytes(CG, BN));
+          load_step<KIND, CG, BN>(p, t, kt, rank, a, a + A_BYTES, bar);
           if (++s == S) s = 0, ++laps;
         }
       }
@@ -382,22 +403,22 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
   } else if (wid == kTileEpilogueWarps + 1) {
     if (rank == 0 && elect_one()) {
-      constexpr uint32_t desc = product_desc(kTileM * CG, kTileN, A_ACROSS, B_ACROSS);
+      constexpr uint32_t desc = product_desc(kTileM * CG, BN, A_ACROSS, B_ACROSS);
       constexpr uint32_t chunk = 64 * kTileK * 2;
       // 16 of the sum: 32 bytes along a swizzled row, or 16 rows of 128 bytes
       constexpr uint32_t a_step = A_ACROSS ? 2048 : 32, b_step = B_ACROSS ? 2048 : 32;
       int s = 0, laps = 0, n = 0;
       for (int i = first; i < p.tiles && !*abort; i += stride) {
-        const Tile t = tile_at<KIND, CG>(p, i);
+        const Tile t = tile_at<KIND, CG, BN>(p, i);
         if (t.nkt == 0) continue;
         const int acc = n & 1;
         if (!bar_wait<CG>(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort)) break;
         tc_fence_after();
-        const uint32_t d = tmem + acc * kTileN;
+        const uint32_t d = tmem + acc * BN;
         for (int kt = 0; kt < t.nkt; ++kt) {
           if (!bar_wait<CG>(&sh.full[s], laps & 1, abort)) break;
           tc_fence_after();
-          const uint32_t a = st_smem(ring + s * tile_stage_bytes(CG)), b = a + A_BYTES;
+          const uint32_t a = st_smem(ring + s * tile_stage_bytes(CG, BN)), b = a + A_BYTES;
 #pragma unroll
           for (int k = 0; k < kTileK / 16; ++k)
             tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
@@ -419,7 +440,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     const int quarter = wid & 3, half = wid >> 2;
     int n = 0;
     for (int i = first; i < p.tiles; i += stride) {
-      const Tile t = tile_at<KIND, CG>(p, i);
+      const Tile t = tile_at<KIND, CG, BN>(p, i);
       const int acc = n & 1;
       bool ok = true;
       if (t.nkt > 0) {
@@ -429,7 +450,8 @@ __global__ void __launch_bounds__(kTileThreads, 1)
         tc_fence_after();
       }
       const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
-      take_tile<KIND>(p, t, row, half, tmem + ((uint32_t)(quarter * 32) << 16) + acc * kTileN, t.nkt == 0);
+      take_tile<KIND, BN>(p, t, row, half, tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN, t.nkt == 0,
+                          turn + wid * (kTurnBytes / 4));
       if (t.nkt > 0) {
         tc_fence_before();
         __syncwarp();
@@ -446,13 +468,13 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   __syncthreads();
   if (CG == 2) cluster_sync();
   tc_fence_after();
-  if (wid == kTileEpilogueWarps + 1) tmem_free<CG>(tmem, 512);
+  if (wid == kTileEpilogueWarps + 1) tmem_free<CG>(tmem, 2 * BN);
   if (threadIdx.x == 0 && sh.abort) atomicCAS(p.status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
 }
 
 // The kernels, one translation unit each (nvcc runs them side by side).
-const void* tile_gate_fn(int cg);
-const void* tile_input_fn(int cg);
-const void* tile_weight_fn(int cg);
+const void* tile_gate_fn(int cg, int bn);
+const void* tile_input_fn(int cg, int bn);
+const void* tile_weight_fn(int cg, int bn);
 
 }  // namespace bkmoo

@@ -2,6 +2,7 @@
 // bkmoo_op_status.
 #include "tile_host.cuh"
 
+#include <cmath>
 #include <mutex>
 
 namespace bkmoo {
@@ -15,7 +16,7 @@ __device__ int32_t g_status;
 struct PerDevice {
   void* status = nullptr;
   int sms = 0;
-  const void* sized[8] = {};    // kernels whose shared-memory limit is raised
+  const void* sized[16] = {};    // kernels whose shared-memory limit is raised
 };
 std::mutex g_mu;
 PerDevice g_dev[kMaxDevices];
@@ -91,7 +92,47 @@ int tile_status_word(cudaStream_t s, int32_t** word) {
   return BKMOO_OK;
 }
 
-int tile_launch(const void* fn, int cg, void* args, int64_t tiles, cudaStream_t s) {
+// Time of a tile (us) from three sweeps on GB300 (forward 9 to 4000 rows, input
+// gradient 16 to 4000, weight gradients of 64 to 8192 rows in 1 and 4 languages,
+// widths 256 to 12288): a step of the sum where the SMs are full, a tile's way to
+// memory (under the next tile's sum if that is longer), and a launch with its first
+// and last tile.  Measured against the rule, us (64 / 128 / 256 columns / pair of
+// 256): forward 2048 -> 8192, 64 rows 18.7 / 17.0 / 18.5 / 18.5, 2000 rows 156 /
+// 109 / 94 / 79; 4096 -> 12288, 64 rows 42.5 / 42.8 / 37.4 / 48.9; input gradient
+// 768 <- 2048, 1000 rows 17.8 / 18.1 / 26.1 / 26.6, 4000 rows 48 / 38 / 36 / 35;
+// weight gradient 2048 x 768, 4 languages of 256 rows 11.3 / 8.6 / 9.1 / 10.9, of
+// 2048 36 / 22 / 25 / 25.
+TileShape tile_shape(int64_t rows, int64_t cols, bool gate, const int32_t* nkt, int groups, int mats,
+                     int sms) {
+  struct Cost {
+    TileShape s;
+    double step, out, launch;
+  };
+  static const Cost costs[4] = {{{1, 64}, 0.165, 0.8, 4.0},
+                                {{1, 128}, 0.217, 1.2, 4.7},
+                                {{1, 256}, 0.376, 2.2, 5.8},
+                                {{2, 256}, 0.320, 2.9, 7.0}};
+  TileShape best = costs[0].s;
+  double least = 0.0;
+  for (int i = 0; i < 4; ++i) {
+    const Cost& c = costs[i];
+    const int64_t m = kTileM * c.s.cg, n = gate ? c.s.bn / 2 : c.s.bn, units = sms / c.s.cg;
+    const double each = (double)((rows + m - 1) / m) * ((cols + n - 1) / n) * mats;
+    double longest = 0.0, sum = 0.0;
+    for (int g = 0; g < groups; ++g) {
+      const double t = nkt[g] * c.step > c.out ? nkt[g] * c.step : c.out;
+      longest = t > longest ? t : longest;
+      sum += t;
+    }
+    const double waves = std::ceil(each * groups / units) * (sum / groups);
+    const double t = c.launch + (waves > longest ? waves : longest);
+    if (i == 0 || t < least) least = t, best = c.s;
+  }
+  return best;
+}
+
+int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s) {
+  const int cg = shape.cg, smem = tile_smem(cg, shape.bn);
   int dev = 0, sms = 0;
   int r = current_device(&dev);
   if (r == BKMOO_OK) r = tile_sms(&sms);
@@ -100,26 +141,29 @@ int tile_launch(const void* fn, int cg, void* args, int64_t tiles, cudaStream_t 
     std::lock_guard<std::mutex> lk(g_mu);
     const void** known = g_dev[dev].sized;
     int i = 0;
-    while (i < 8 && known[i] && known[i] != fn) ++i;
-    if (i == 8 || !known[i]) {
-      if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, tile_smem(cg)) !=
+    while (i < 16 && known[i] && known[i] != fn) ++i;
+    if (i == 16 || !known[i]) {
+      if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
           cudaSuccess)
         return BKMOO_ERR_CUDA;
-      if (i < 8) known[i] = fn;
+      if (i < 16) known[i] = fn;
     }
   }
   const int64_t units = sms / cg;
   cudaLaunchConfig_t cfg = {};
-  cudaLaunchAttribute attr[1];
+  // (the kernel waits at its top for the one ahead of it: launch_behind)
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cg;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.gridDim = dim3((unsigned)((tiles < units ? tiles : units) * cg));
   cfg.blockDim = dim3(kTileThreads);
-  cfg.dynamicSmemBytes = tile_smem(cg);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   void* list[] = {args};
   return cudaLaunchKernelExC(&cfg, fn, list) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
 }

@@ -32,7 +32,15 @@ int tile_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int64_t 
 int tile_sms(int* sms);
 // The device's status word for kernels that may give up.
 int tile_status_word(cudaStream_t s, int32_t** word);
-// Queues a tile kernel over `tiles` tiles, by CTAs or pairs of CTAs.
-int tile_launch(const void* fn, int cg, void* args, int64_t tiles, cudaStream_t s);
+// A tile's shape: CTAs that share it and its columns.
+struct TileShape {
+  int cg, bn;
+};
+// The shape for rows x cols results (gate: cols of h, of which a tile has bn / 2)
+// of `mats` products each with `groups` sums of nkt steps.
+TileShape tile_shape(int64_t rows, int64_t cols, bool gate, const int32_t* nkt, int groups, int mats,
+                     int sms);
+// Queues a tile kernel over `tiles` tiles.
+int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s);
 
 }  // namespace bkmoo

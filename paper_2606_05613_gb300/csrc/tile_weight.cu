@@ -3,8 +3,11 @@
 
 namespace bkmoo {
 
-const void* tile_weight_fn(int cg) {
-  return cg == 1 ? (const void*)tile_gemm_kernel<kWeight, 1> : (const void*)tile_gemm_kernel<kWeight, 2>;
+const void* tile_weight_fn(int cg, int bn) {
+  if (cg == 2) return (const void*)tile_gemm_kernel<kWeight, 2, 256>;
+  if (bn == 256) return (const void*)tile_gemm_kernel<kWeight, 1, 256>;
+  if (bn == 128) return (const void*)tile_gemm_kernel<kWeight, 1, 128>;
+  return (const void*)tile_gemm_kernel<kWeight, 1, 64>;
 }
 
 }  // namespace bkmoo

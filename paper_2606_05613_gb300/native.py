@@ -368,25 +368,70 @@ def bkmoo_selftest_fp64(op: int, a, b, out, stream=None):
                                       _stream_handle(stream, out.device)), "bkmoo_selftest_fp64")
 
 
-def _matrix(t, rows: int, cols: int, what: str):
-    """(address, row stride) of a bf16 CUDA matrix the tile kernels take."""
+def _matrix(t, rows: int, cols: int, device, what: str):
+    """(address, row stride) of a bf16 matrix the tile kernels take."""
     import torch
-    if not t.is_cuda or t.dtype != torch.bfloat16 or t.dim() != 2 or tuple(t.shape) != (rows, cols):
-        raise ValueError("%s must be a bfloat16 CUDA matrix of %d x %d" % (what, rows, cols))
-    if cols > 1 and t.stride(1) != 1:
+    if t.dtype is not torch.bfloat16 or t.shape != (rows, cols) or t.device != device:
+        raise ValueError("%s must be a bfloat16 matrix of %d x %d on %s, got %s %s on %s"
+                         % (what, rows, cols, device, t.dtype, tuple(t.shape), t.device))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % what)
-    ld = t.stride(0) if rows > 1 else (cols + 7) // 8 * 8
-    if ld < cols or ld % 8 or t.data_ptr() % 16:
+    if rows < 2:
+        ld = (cols + 7) // 8 * 8         # no second row: any stride does
+    p = t.data_ptr()
+    if ld < cols or ld % 8 or p % 16:
         raise ValueError("%s: rows must start on 16 bytes (pad them to a multiple of 8 elements)"
                          % what)
-    return t.data_ptr(), ld
+    return p, ld
+
+
+def _pair(t, u, rows: int, cols: int, device, what: str):
+    """Addresses and the one row stride of two matrices of a kind."""
+    p, ld = _matrix(t, rows, cols, device, what)
+    q, lu = _matrix(u, rows, cols, device, what)
+    if ld != lu:
+        raise ValueError("%s: both must have one row stride" % what)
+    return p, q, ld
+
+
+def _cuda_device(t, what: str):
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError("%s must be a CUDA matrix" % what)
+    return t.device
+
+
+class _Current:
+    """Makes `device` current where it is not."""
+
+    def __init__(self, device):
+        import torch
+        self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        if self.ctx is not None:
+            self.ctx.__exit__(*exc)
+
+
+def _scratch(nbytes: int, device, stream):
+    """A byte tensor for work on `stream` (None: the current one)."""
+    import torch
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
 def _language_rows(rows, T: int):
-    r = _offsets_array(rows)
-    if r.ndim != 1 or not 2 <= len(r) <= 17 or r[0] != 0 or r[-1] != T or (np.diff(r) < 0).any():
+    """(K, array) of the language bounds."""
+    r = [int(i) for i in rows]
+    if not 2 <= len(r) <= 17 or r[0] != 0 or r[-1] != T or any(j < i for i, j in zip(r, r[1:])):
         raise ValueError("rows must be K + 1 bounds from 0 to the number of rows, 1 <= K <= 16")
-    return r
+    return len(r) - 1, (ctypes.c_int64 * len(r))(*r)
 
 
 def _weight_grads(dw, K: int, rows: int, cols: int, device, what: str):
@@ -394,42 +439,32 @@ def _weight_grads(dw, K: int, rows: int, cols: int, device, what: str):
     dw = list(dw)
     if len(dw) != K:
         raise ValueError("%s: one gradient per language, %d" % (what, K))
+    dt, shape = dw[0].dtype, (rows, cols)
     for g in dw:
-        if tuple(g.shape) != (rows, cols) or not g.is_contiguous() or g.device != device or \
-                g.dtype != dw[0].dtype:
+        if g.shape != shape or g.dtype is not dt or g.device != device or not g.is_contiguous():
             raise ValueError("%s must be contiguous %d x %d matrices of one dtype on %s"
                              % (what, rows, cols, device))
     return (ctypes.c_void_p * K)(*[g.data_ptr() for g in dw]), _dtype_code(dw[0])
-
-
-def _one_device(*tensors):
-    devs = {t.device for t in tensors if t is not None}
-    if len(devs) != 1:
-        raise ValueError("all tensors must be on one device, got %s" % sorted(map(str, devs)))
 
 
 def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T), and a = x w_gate^T, b = x w_up^T for the
     backward pass where given.  x [T, D], weights [F, D], outputs [T, F], all
     bfloat16, rows on 16 bytes."""
-    import torch
-    T, D, F = int(x.shape[0]), int(x.shape[1]), int(w_gate.shape[0])
+    dev = _cuda_device(x, "x")
+    T, D = x.shape
+    F = w_gate.shape[0]
     if isinstance(act, str):
         act = ACTS[act]
-    _one_device(x, w_gate, w_up, h, a, b)
-    px, ldx = _matrix(x, T, D, "x")
-    pg, ldw = _matrix(w_gate, F, D, "w_gate")
-    pu, ldu = _matrix(w_up, F, D, "w_up")
-    if ldu != ldw:
-        raise ValueError("w_gate and w_up must have one row stride")
-    ph, ldh = _matrix(h, T, F, "h") if h is not None else (None, 0)
-    pa, lda = _matrix(a, T, F, "a") if a is not None else (None, 0)
-    pb, ldb = _matrix(b, T, F, "b") if b is not None else (None, 0)
-    if lda != ldb:
-        raise ValueError("a and b must have one row stride")
-    with torch.cuda.device(x.device):
-        _check(load().bkmoo_gate_forward(px, ldx, pg, pu, ldw, T, D, F, act, ph, ldh, pa, pb, lda,
-                                         _stream_handle(stream, x.device)), "bkmoo_gate_forward")
+    px, ldx = _matrix(x, T, D, dev, "x")
+    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, "w_gate and w_up")
+    ph, ldh = _matrix(h, T, F, dev, "h") if h is not None else (None, 0)
+    if (a is None) != (b is None):
+        raise ValueError("a and b come together")
+    pa, pb, ld_ab = _pair(a, b, T, F, dev, "a and b") if a is not None else (None, None, 0)
+    with _Current(dev):
+        _check(load().bkmoo_gate_forward(px, ldx, pg, pu, ldw, T, D, F, act, ph, ldh, pa, pb,
+                                         ld_ab, _stream_handle(stream, dev)), "bkmoo_gate_forward")
 
 
 def bkmoo_gate_backward_workspace_size(T: int, F: int) -> int:
@@ -446,60 +481,48 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
     (contiguous [F, D], float32 or bfloat16; both lists may be None).  ws: a CUDA
     byte tensor of bkmoo_gate_backward_workspace_size; allocated (torch, on
     `stream`) where None."""
-    import torch
-    T, D, F = int(x.shape[0]), int(x.shape[1]), int(w_gate.shape[0])
+    dev = _cuda_device(x, "x")
+    T, D = x.shape
+    F = w_gate.shape[0]
     if isinstance(act, str):
         act = ACTS[act]
-    _one_device(dh, a, b, x, w_gate, w_up, dx)
-    r = _language_rows(rows, T)
-    K = len(r) - 1
-    pd, ldd = _matrix(dh, T, F, "dh")
-    pa, lda = _matrix(a, T, F, "a")
-    pb, ldb = _matrix(b, T, F, "b")
-    px, ldx = _matrix(x, T, D, "x")
-    pg, ldw = _matrix(w_gate, F, D, "w_gate")
-    pu, ldu = _matrix(w_up, F, D, "w_up")
-    if ldu != ldw or lda != ldb:
-        raise ValueError("w_gate and w_up, and a and b, must have one row stride")
-    pdx, lddx = _matrix(dx, T, D, "dx") if dx is not None else (None, 0)
+    K, r = _language_rows(rows, T)
+    px, ldx = _matrix(x, T, D, dev, "x")
+    pd, ldd = _matrix(dh, T, F, dev, "dh")
+    pa, pb, ld_ab = _pair(a, b, T, F, dev, "a and b")
+    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, "w_gate and w_up")
+    pdx, lddx = _matrix(dx, T, D, dev, "dx") if dx is not None else (None, 0)
     gg = gu = None
     dt = BKMOO_BF16
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("dw_gate and dw_up come together")
     if dw_gate is not None:
-        gg, dt = _weight_grads(dw_gate, K, F, D, x.device, "dw_gate")
-        gu, du = _weight_grads(dw_up, K, F, D, x.device, "dw_up")
+        gg, dt = _weight_grads(dw_gate, K, F, D, dev, "dw_gate")
+        gu, du = _weight_grads(dw_up, K, F, D, dev, "dw_up")
         if dt != du:
             raise ValueError("dw_gate and dw_up must have one dtype")
-    if stream is None:
-        stream = torch.cuda.current_stream(x.device)
-    with torch.cuda.device(x.device):
+    with _Current(dev):
         if ws is None:
-            with torch.cuda.stream(stream):
-                ws = torch.empty(bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8,
-                                 device=x.device)
-        _check(load().bkmoo_gate_backward(pd, ldd, pa, pb, lda, px, ldx, pg, pu, ldw, T, D, F, act,
-                                          K, r.ctypes.data, pdx, lddx, gg, gu, dt,
-                                          1 if accumulate else 0, ws.data_ptr(),
-                                          ws.numel() * ws.element_size(),
-                                          _stream_handle(stream, x.device)), "bkmoo_gate_backward")
+            ws = _scratch(bkmoo_gate_backward_workspace_size(T, F), dev, stream)
+        _check(load().bkmoo_gate_backward(pd, ldd, pa, pb, ld_ab, px, ldx, pg, pu, ldw, T, D, F,
+                                          act, K, r, pdx, lddx, gg, gu, dt, 1 if accumulate else 0,
+                                          ws.data_ptr(), ws.numel() * ws.element_size(),
+                                          _stream_handle(stream, dev)), "bkmoo_gate_backward")
 
 
 def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
     """dw[k] = dy[rows[k]:rows[k + 1]]^T x[rows[k]:rows[k + 1]] for every language:
     dy [T, M] and x [T, N] bfloat16, dw[k] contiguous [M, N], float32 or bfloat16."""
-    import torch
-    T, M, N = int(dy.shape[0]), int(dy.shape[1]), int(x.shape[1])
-    _one_device(dy, x)
-    r = _language_rows(rows, T)
-    K = len(r) - 1
-    pd, ldd = _matrix(dy, T, M, "dy")
-    px, ldx = _matrix(x, T, N, "x")
-    g, dt = _weight_grads(dw, K, M, N, x.device, "dw")
-    with torch.cuda.device(x.device):
-        _check(load().bkmoo_language_wgrad(pd, ldd, px, ldx, T, M, N, K, r.ctypes.data, g, dt,
-                                           1 if accumulate else 0,
-                                           _stream_handle(stream, x.device)),
+    dev = _cuda_device(dy, "dy")
+    T, M = dy.shape
+    N = x.shape[-1]
+    K, r = _language_rows(rows, T)
+    pd, ldd = _matrix(dy, T, M, dev, "dy")
+    px, ldx = _matrix(x, T, N, dev, "x")
+    g, dt = _weight_grads(dw, K, M, N, dev, "dw")
+    with _Current(dev):
+        _check(load().bkmoo_language_wgrad(pd, ldd, px, ldx, T, M, N, K, r, g, dt,
+                                           1 if accumulate else 0, _stream_handle(stream, dev)),
                "bkmoo_language_wgrad")
 
 
@@ -522,12 +545,9 @@ def bkmoo_grad_norm(grad, out_norm, ws=None, stream=None):
         raise ValueError("the gradient must be a contiguous CUDA tensor")
     if out_norm.dtype != torch.float32 or out_norm.numel() != 1 or out_norm.device != grad.device:
         raise ValueError("out_norm must be one float32 on the gradient's device")
-    if stream is None:
-        stream = torch.cuda.current_stream(grad.device)
-    with torch.cuda.device(grad.device):
+    with _Current(grad.device):
         if ws is None:
-            with torch.cuda.stream(stream):
-                ws = torch.empty(BKMOO_NORM_WS_BYTES, dtype=torch.uint8, device=grad.device)
+            ws = _scratch(BKMOO_NORM_WS_BYTES, grad.device, stream)
         _check(load().bkmoo_grad_norm(grad.data_ptr(), _dtype_code(grad), grad.numel(),
                                       out_norm.data_ptr(), ws.data_ptr(),
                                       ws.numel() * ws.element_size(),
@@ -552,11 +572,13 @@ def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None
     if not tensors:
         raise ValueError("need at least one tensor")
     dev, dt = grad.device, tensors[0].dtype
-    for t in tensors:
-        if t.device != dev or t.dtype != dt or not t.is_contiguous():
-            raise ValueError("the tensors must be contiguous, of one dtype and on the gradient's device")
-    sizes = np.fromiter((t.numel() for t in tensors), np.int64, len(tensors))
-    N = int(sizes.sum())
+    if any(t.dtype is not dt or t.device != dev or not t.is_contiguous() for t in tensors):
+        raise ValueError("the tensors must be contiguous, of one dtype and on the gradient's device")
+    n = len(tensors)
+    counts = [t.numel() for t in tensors]
+    sizes = (ctypes.c_int64 * n)(*counts)
+    ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+    N = sum(counts)
     eight = m.dtype == torch.float8_e4m3fn
     flat = [("grad", grad, None), ("m", m, torch.float8_e4m3fn if eight else torch.float32),
             ("v", v, m.dtype)]
@@ -578,18 +600,18 @@ def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None
                                   grad_norm.numel() != 1):
         raise ValueError("grad_norm must be one float32 on the gradient's device")
     if weight_decay is not None:
-        weight_decay = np.ascontiguousarray(np.broadcast_to(
-            np.asarray(weight_decay, dtype=np.float32), (len(tensors),)))
-    ptrs = (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+        each = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
+        if len(each) != n:
+            raise ValueError("weight_decay must be one number, or one per tensor")
+        weight_decay = (ctypes.c_float * n)(*each)
     p = params if params is not None else bkmoo_adamw_default_params()
 
     def ptr(t):
         return t.data_ptr() if t is not None else None
 
-    with torch.cuda.device(dev):
-        _check(load().bkmoo_adamw(ptrs, sizes.ctypes.data,
-                                  weight_decay.ctypes.data if weight_decay is not None else None,
-                                  len(tensors), _dtype_code(tensors[0]), grad.data_ptr(),
+    with _Current(dev):
+        _check(load().bkmoo_adamw(ptrs, sizes, weight_decay, n, _dtype_code(tensors[0]),
+                                  grad.data_ptr(),
                                   _dtype_code(grad), ptr(master), m.data_ptr(), v.data_ptr(),
                                   ptr(m_scale) if eight else None, ptr(v_scale) if eight else None,
                                   BKMOO_E4M3 if eight else BKMOO_F32, ctypes.byref(p),
