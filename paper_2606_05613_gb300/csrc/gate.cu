@@ -83,11 +83,10 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
 // dW_k = dy_k^T x_k for one or two dy (mats), every language.
 int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, int64_t ldx,
                  int64_t M, int64_t N, int32_t K, const int64_t* rows, void* const* const* dw,
-                 int32_t dw_dtype, int32_t accumulate, cudaStream_t s) {
+                 int32_t dw_dtype, int32_t accumulate, int sms, int32_t* status, cudaStream_t s) {
   TileArgs<kWeight> p = {};
-  int sms = 0, r = tile_sms(&sms);
-  if (r == BKMOO_OK) r = tile_status_word(s, &p.status);
-  if (r != BKMOO_OK) return r;
+  p.status = status;
+  int r = BKMOO_OK;
   const int elem = dw_dtype == BKMOO_F32 ? 4 : 2;
   bool any = false;
   for (int k = 0; k < K; ++k) {
@@ -118,10 +117,8 @@ int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, 
   p.n_lang = K;
   p.out_dtype = dw_dtype;
   p.accumulate = accumulate;
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * mats * K;
-  if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
-  p.tiles = (int32_t)tiles;
-  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, tiles, s);
+  p.tiles = p.tiles_m * p.tiles_n * mats * K;
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
 }
 
 bool grads_ok(void* const* dw, int32_t K, int32_t dtype) {
@@ -174,10 +171,8 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
   p.tiles_n = up(F, shape.bn / 2);
   p.nkt = nkt;
   p.act = act;
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-  if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
-  p.tiles = (int32_t)tiles;
-  return tile_launch(tile_gate_fn(shape.cg, shape.bn), shape, &p, tiles, s);
+  p.tiles = p.tiles_m * p.tiles_n;
+  return tile_launch(tile_gate_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
 }
 
 extern "C" int bkmoo_gate_backward_workspace_size(int64_t T, int64_t F, size_t* bytes) {
@@ -195,25 +190,26 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
                                    void* stream) {
   const bool weights = dw_gate || dw_up;
   if (!act_ok(act) || T < 0 || (dw_dtype != BKMOO_F32 && dw_dtype != BKMOO_BF16) ||
-      !operand_ok(w_gate, F, D, ldw) || !operand_ok(w_up, F, D, ldw) || !languages_ok(rows, K, T) ||
+      !operand_ok(w_gate, F, D, ldw) || !operand_ok(w_up, F, D, ldw) || !size_ok(F, D) ||
+      !languages_ok(rows, K, T) ||
       (!dx && !weights && T > 0) ||
       (weights && (!grads_ok(dw_gate, K, dw_dtype) || !grads_ok(dw_up, K, dw_dtype))))
     return BKMOO_ERR_INVALID;
+  size_t need = 0;
+  if (T > 0 && (!operand_ok(dh, T, F, ld_dh) || !operand_ok(a, T, F, ld_ab) ||
+                !operand_ok(b, T, F, ld_ab) || !operand_ok(x, T, D, ldx) ||
+                (dx && !operand_ok(dx, T, D, ld_dx)) || !ws || ((uintptr_t)ws & 255u) ||
+                bkmoo_gate_backward_workspace_size(T, F, &need) != BKMOO_OK))
+    return BKMOO_ERR_INVALID;
+  if (ws_bytes < need) return BKMOO_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const int64_t ld = (F + 7) / 8 * 8;
-  __nv_bfloat16* d[2] = {nullptr, nullptr};
+  int32_t* status = nullptr;
   int sms = 0, r = tile_sms(&sms);
+  if (r == BKMOO_OK) r = tile_status_word(s, &status);
   if (r != BKMOO_OK) return r;
+  const int64_t ld = (F + 7) / 8 * 8;
+  __nv_bfloat16* d[2] = {static_cast<__nv_bfloat16*>(ws), static_cast<__nv_bfloat16*>(ws) + need / 4};
   if (T > 0) {
-    if (!operand_ok(dh, T, F, ld_dh) || !operand_ok(a, T, F, ld_ab) || !operand_ok(b, T, F, ld_ab) ||
-        !operand_ok(x, T, D, ldx) || (dx && !operand_ok(dx, T, D, ld_dx)) || !ws ||
-        ((uintptr_t)ws & 255u))
-      return BKMOO_ERR_INVALID;
-    size_t need = 0;
-    (void)bkmoo_gate_backward_workspace_size(T, F, &need);
-    if (ws_bytes < need) return BKMOO_ERR_WORKSPACE;
-    d[0] = static_cast<__nv_bfloat16*>(ws);
-    d[1] = d[0] + need / 4;
     SlopeArgs q = {static_cast<const __nv_bfloat16*>(dh), static_cast<const __nv_bfloat16*>(a),
                    static_cast<const __nv_bfloat16*>(b), d[0], d[1], ld_dh, ld_ab, ld, T, (int32_t)F, act};
     const int64_t blocks = (T * (ld / 8) + 255) / 256, most = (int64_t)sms * 8;
@@ -226,7 +222,7 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     const int32_t nkt = 2 * up(F, kTileK);
     const TileShape shape = tile_shape(T, D, false, &nkt, 1, 1, sms);
     TileArgs<kInput> p = {};
-    r = tile_status_word(s, &p.status);
+    p.status = status;
     const void* w[2] = {w_gate, w_up};
     for (int i = 0; i < 2 && r == BKMOO_OK; ++i) {
       r = tile_map(&p.a[i], d[i], T, F, ld, kTileM);
@@ -239,27 +235,28 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     p.tiles_m = up(T, kTileM * shape.cg);
     p.tiles_n = up(D, shape.bn);
     p.nkt = nkt / 2;
-    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
-    if (tiles > 0x7fffffff) return BKMOO_ERR_INVALID;
-    p.tiles = (int32_t)tiles;
-    r = tile_launch(tile_input_fn(shape.cg, shape.bn), shape, &p, tiles, s);
+    p.tiles = p.tiles_m * p.tiles_n;
+    r = tile_launch(tile_input_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
     if (r != BKMOO_OK) return r;
   }
   if (!weights) return BKMOO_OK;
   const void* dy[2] = {d[0], d[1]};
   void* const* dw[2] = {dw_gate, dw_up};
-  return weight_grads(dy, ld, 2, x, ldx, F, D, K, rows, dw, dw_dtype, accumulate, s);
+  return weight_grads(dy, ld, 2, x, ldx, F, D, K, rows, dw, dw_dtype, accumulate, sms, status, s);
 }
 
 extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
                                     int64_t T, int64_t M, int64_t N, int32_t K, const int64_t* rows,
                                     void* const* dw, int32_t dw_dtype, int32_t accumulate,
                                     void* stream) {
-  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
-  if (T < 0 || M < 1 || N < 1 || M > kMost || N > kMost || !languages_ok(rows, K, T) ||
+  if (T < 0 || !size_ok(M, N) || !languages_ok(rows, K, T) ||
       (dw_dtype != BKMOO_F32 && dw_dtype != BKMOO_BF16) || !grads_ok(dw, K, dw_dtype) ||
       (T > 0 && (!operand_ok(dy, T, M, ld_dy) || !operand_ok(x, T, N, ldx))))
     return BKMOO_ERR_INVALID;
-  return weight_grads(&dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate,
-                      static_cast<cudaStream_t>(stream));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int32_t* status = nullptr;
+  int sms = 0, r = tile_sms(&sms);
+  if (r == BKMOO_OK) r = tile_status_word(s, &status);
+  if (r != BKMOO_OK) return r;
+  return weight_grads(&dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate, sms, status, s);
 }

@@ -8,9 +8,15 @@ namespace bkmoo {
 
 // A bf16 matrix that the tile kernels read: rows of `ld` elements.
 inline bool operand_ok(const void* p, int64_t rows, int64_t cols, int64_t ld) {
-  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;   // coordinates are 32 bits
+  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;   // coordinates and tiles are 32 bits
   return p && ((uintptr_t)p & 15u) == 0 && rows >= 0 && rows <= kMost && cols >= 1 &&
-         cols <= kMost && ld >= cols && ld % 8 == 0 && ld <= ((int64_t)1 << 38);
+         cols <= kMost && rows * cols <= ((int64_t)1 << 42) && ld >= cols && ld % 8 == 0 &&
+         ld <= ((int64_t)1 << 38);
+}
+// A language's weight gradient (32 of them at most).
+inline bool size_ok(int64_t M, int64_t N) {
+  constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
+  return M >= 1 && N >= 1 && M <= kMost && N <= kMost && M * N <= ((int64_t)1 << 37);
 }
 // Language bounds: 0 = rows[0] <= rows[1] <= ... <= rows[K] = T.
 inline bool languages_ok(const int64_t* rows, int32_t K, int64_t T) {

@@ -8,6 +8,7 @@ pointers and the current CUDA stream.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 import threading
@@ -368,12 +369,11 @@ def bkmoo_selftest_fp64(op: int, a, b, out, stream=None):
                                       _stream_handle(stream, out.device)), "bkmoo_selftest_fp64")
 
 
-def _matrix(t, rows: int, cols: int, device, what: str):
+def _matrix(t, rows: int, cols: int, dev: int, bf16, what: str):
     """(address, row stride) of a bf16 matrix the tile kernels take."""
-    import torch
-    if t.dtype is not torch.bfloat16 or t.shape != (rows, cols) or t.device != device:
-        raise ValueError("%s must be a bfloat16 matrix of %d x %d on %s, got %s %s on %s"
-                         % (what, rows, cols, device, t.dtype, tuple(t.shape), t.device))
+    if t.dtype is not bf16 or t.get_device() != dev or t.shape != (rows, cols):
+        raise ValueError("%s must be a bfloat16 matrix of %d x %d on cuda:%d, got %s %s on %s"
+                         % (what, rows, cols, dev, t.dtype, tuple(t.shape), t.device))
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("%s must have contiguous rows" % what)
@@ -386,85 +386,92 @@ def _matrix(t, rows: int, cols: int, device, what: str):
     return p, ld
 
 
-def _pair(t, u, rows: int, cols: int, device, what: str):
+def _pair(t, u, rows: int, cols: int, dev: int, bf16, what: str):
     """Addresses and the one row stride of two matrices of a kind."""
-    p, ld = _matrix(t, rows, cols, device, what)
-    q, lu = _matrix(u, rows, cols, device, what)
+    p, ld = _matrix(t, rows, cols, dev, bf16, what)
+    q, lu = _matrix(u, rows, cols, dev, bf16, what)
     if ld != lu:
         raise ValueError("%s: both must have one row stride" % what)
     return p, q, ld
 
 
-def _cuda_device(t, what: str):
-    if not t.is_cuda or t.dim() != 2:
+def _cuda_matrix(t, what: str):
+    """(rows, columns, device index) of a CUDA matrix."""
+    dev = t.get_device()
+    if dev < 0 or t.dim() != 2:
         raise ValueError("%s must be a CUDA matrix" % what)
-    return t.device
+    rows, cols = t.shape
+    return rows, cols, dev
 
 
-class _Current:
-    """Makes `device` current where it is not."""
-
-    def __init__(self, device):
-        import torch
-        self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-
-    def __exit__(self, *exc):
-        if self.ctx is not None:
-            self.ctx.__exit__(*exc)
+def _act_code(act) -> int:
+    return ACTS[act] if isinstance(act, str) else act
 
 
-def _scratch(nbytes: int, device, stream):
+def _raw_stream(torch, stream, dev: int) -> int:
+    return (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+
+
+def _call(torch, dev: int, where: str, fn, *args):
+    """fn(*args) with device `dev` current."""
+    if torch.cuda.current_device() == dev:
+        code = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            code = fn(*args)
+    if code != BKMOO_OK:
+        raise BkmooError(code, where)
+
+
+def _scratch(torch, nbytes: int, dev: int, stream):
     """A byte tensor for work on `stream` (None: the current one)."""
-    import torch
     if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
     with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
 
 
 def _language_rows(rows, T: int):
     """(K, array) of the language bounds."""
     r = [int(i) for i in rows]
-    if not 2 <= len(r) <= 17 or r[0] != 0 or r[-1] != T or any(j < i for i, j in zip(r, r[1:])):
+    last, ok = 0, 2 <= len(r) <= 17 and r[0] == 0 and r[-1] == T
+    for i in r:
+        ok = ok and i >= last
+        last = i
+    if not ok:
         raise ValueError("rows must be K + 1 bounds from 0 to the number of rows, 1 <= K <= 16")
     return len(r) - 1, (ctypes.c_int64 * len(r))(*r)
 
 
-def _weight_grads(dw, K: int, rows: int, cols: int, device, what: str):
+def _weight_grads(dw, K: int, rows: int, cols: int, dev: int, what: str):
     """(array of K addresses, dtype code) of a list of per-language gradients."""
-    dw = list(dw)
     if len(dw) != K:
         raise ValueError("%s: one gradient per language, %d" % (what, K))
-    dt, shape = dw[0].dtype, (rows, cols)
+    dt, shape, at = dw[0].dtype, (rows, cols), []
     for g in dw:
-        if g.shape != shape or g.dtype is not dt or g.device != device or not g.is_contiguous():
-            raise ValueError("%s must be contiguous %d x %d matrices of one dtype on %s"
-                             % (what, rows, cols, device))
-    return (ctypes.c_void_p * K)(*[g.data_ptr() for g in dw]), _dtype_code(dw[0])
+        if g.dtype is not dt or g.get_device() != dev or g.shape != shape or not g.is_contiguous():
+            raise ValueError("%s must be contiguous %d x %d matrices of one dtype on cuda:%d"
+                             % (what, rows, cols, dev))
+        at.append(g.data_ptr())
+    return (ctypes.c_void_p * K)(*at), _dtype_code(dw[0])
 
 
 def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T), and a = x w_gate^T, b = x w_up^T for the
     backward pass where given.  x [T, D], weights [F, D], outputs [T, F], all
     bfloat16, rows on 16 bytes."""
-    dev = _cuda_device(x, "x")
-    T, D = x.shape
+    import torch
+    bf16 = torch.bfloat16
+    T, D, dev = _cuda_matrix(x, "x")
     F = w_gate.shape[0]
-    if isinstance(act, str):
-        act = ACTS[act]
-    px, ldx = _matrix(x, T, D, dev, "x")
-    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, "w_gate and w_up")
-    ph, ldh = _matrix(h, T, F, dev, "h") if h is not None else (None, 0)
+    px, ldx = _matrix(x, T, D, dev, bf16, "x")
+    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, bf16, "w_gate and w_up")
+    ph, ldh = _matrix(h, T, F, dev, bf16, "h") if h is not None else (None, 0)
     if (a is None) != (b is None):
         raise ValueError("a and b come together")
-    pa, pb, ld_ab = _pair(a, b, T, F, dev, "a and b") if a is not None else (None, None, 0)
-    with _Current(dev):
-        _check(load().bkmoo_gate_forward(px, ldx, pg, pu, ldw, T, D, F, act, ph, ldh, pa, pb,
-                                         ld_ab, _stream_handle(stream, dev)), "bkmoo_gate_forward")
+    pa, pb, ld_ab = _pair(a, b, T, F, dev, bf16, "a and b") if a is not None else (None, None, 0)
+    _call(torch, dev, "bkmoo_gate_forward", load().bkmoo_gate_forward, px, ldx, pg, pu, ldw, T, D,
+          F, _act_code(act), ph, ldh, pa, pb, ld_ab, _raw_stream(torch, stream, dev))
 
 
 def bkmoo_gate_backward_workspace_size(T: int, F: int) -> int:
@@ -481,17 +488,16 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
     (contiguous [F, D], float32 or bfloat16; both lists may be None).  ws: a CUDA
     byte tensor of bkmoo_gate_backward_workspace_size; allocated (torch, on
     `stream`) where None."""
-    dev = _cuda_device(x, "x")
-    T, D = x.shape
+    import torch
+    bf16 = torch.bfloat16
+    T, D, dev = _cuda_matrix(x, "x")
     F = w_gate.shape[0]
-    if isinstance(act, str):
-        act = ACTS[act]
     K, r = _language_rows(rows, T)
-    px, ldx = _matrix(x, T, D, dev, "x")
-    pd, ldd = _matrix(dh, T, F, dev, "dh")
-    pa, pb, ld_ab = _pair(a, b, T, F, dev, "a and b")
-    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, "w_gate and w_up")
-    pdx, lddx = _matrix(dx, T, D, dev, "dx") if dx is not None else (None, 0)
+    px, ldx = _matrix(x, T, D, dev, bf16, "x")
+    pd, ldd = _matrix(dh, T, F, dev, bf16, "dh")
+    pa, pb, ld_ab = _pair(a, b, T, F, dev, bf16, "a and b")
+    pg, pu, ldw = _pair(w_gate, w_up, F, D, dev, bf16, "w_gate and w_up")
+    pdx, lddx = _matrix(dx, T, D, dev, bf16, "dx") if dx is not None else (None, 0)
     gg = gu = None
     dt = BKMOO_BF16
     if (dw_gate is None) != (dw_up is None):
@@ -501,29 +507,27 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
         gu, du = _weight_grads(dw_up, K, F, D, dev, "dw_up")
         if dt != du:
             raise ValueError("dw_gate and dw_up must have one dtype")
-    with _Current(dev):
-        if ws is None:
-            ws = _scratch(bkmoo_gate_backward_workspace_size(T, F), dev, stream)
-        _check(load().bkmoo_gate_backward(pd, ldd, pa, pb, ld_ab, px, ldx, pg, pu, ldw, T, D, F,
-                                          act, K, r, pdx, lddx, gg, gu, dt, 1 if accumulate else 0,
-                                          ws.data_ptr(), ws.numel() * ws.element_size(),
-                                          _stream_handle(stream, dev)), "bkmoo_gate_backward")
+    if ws is None:
+        ws = _scratch(torch, bkmoo_gate_backward_workspace_size(T, F), dev, stream)
+    _call(torch, dev, "bkmoo_gate_backward", load().bkmoo_gate_backward, pd, ldd, pa, pb, ld_ab,
+          px, ldx, pg, pu, ldw, T, D, F, _act_code(act), K, r, pdx, lddx, gg, gu, dt,
+          1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size(),
+          _raw_stream(torch, stream, dev))
 
 
 def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
     """dw[k] = dy[rows[k]:rows[k + 1]]^T x[rows[k]:rows[k + 1]] for every language:
     dy [T, M] and x [T, N] bfloat16, dw[k] contiguous [M, N], float32 or bfloat16."""
-    dev = _cuda_device(dy, "dy")
-    T, M = dy.shape
+    import torch
+    bf16 = torch.bfloat16
+    T, M, dev = _cuda_matrix(dy, "dy")
     N = x.shape[-1]
     K, r = _language_rows(rows, T)
-    pd, ldd = _matrix(dy, T, M, dev, "dy")
-    px, ldx = _matrix(x, T, N, dev, "x")
+    pd, ldd = _matrix(dy, T, M, dev, bf16, "dy")
+    px, ldx = _matrix(x, T, N, dev, bf16, "x")
     g, dt = _weight_grads(dw, K, M, N, dev, "dw")
-    with _Current(dev):
-        _check(load().bkmoo_language_wgrad(pd, ldd, px, ldx, T, M, N, K, r, g, dt,
-                                           1 if accumulate else 0, _stream_handle(stream, dev)),
-               "bkmoo_language_wgrad")
+    _call(torch, dev, "bkmoo_language_wgrad", load().bkmoo_language_wgrad, pd, ldd, px, ldx, T, M,
+          N, K, r, g, dt, 1 if accumulate else 0, _raw_stream(torch, stream, dev))
 
 
 def bkmoo_op_status(device=None, stream=None) -> int:
@@ -541,17 +545,16 @@ def bkmoo_grad_norm(grad, out_norm, ws=None, stream=None):
     element).  ws: a CUDA byte tensor of BKMOO_NORM_WS_BYTES; allocated (torch,
     on `stream`) where None."""
     import torch
-    if not grad.is_cuda or not grad.is_contiguous():
+    dev = grad.get_device()
+    if dev < 0 or not grad.is_contiguous():
         raise ValueError("the gradient must be a contiguous CUDA tensor")
-    if out_norm.dtype != torch.float32 or out_norm.numel() != 1 or out_norm.device != grad.device:
+    if out_norm.dtype is not torch.float32 or out_norm.numel() != 1 or out_norm.get_device() != dev:
         raise ValueError("out_norm must be one float32 on the gradient's device")
-    with _Current(grad.device):
-        if ws is None:
-            ws = _scratch(BKMOO_NORM_WS_BYTES, grad.device, stream)
-        _check(load().bkmoo_grad_norm(grad.data_ptr(), _dtype_code(grad), grad.numel(),
-                                      out_norm.data_ptr(), ws.data_ptr(),
-                                      ws.numel() * ws.element_size(),
-                                      _stream_handle(stream, grad.device)), "bkmoo_grad_norm")
+    if ws is None:
+        ws = _scratch(torch, BKMOO_NORM_WS_BYTES, dev, stream)
+    _call(torch, dev, "bkmoo_grad_norm", load().bkmoo_grad_norm, grad.data_ptr(), _dtype_code(grad),
+          grad.numel(), out_norm.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
+          _raw_stream(torch, stream, dev))
 
 
 def bkmoo_adamw_default_params() -> bkmoo_adamw_params:
@@ -560,62 +563,77 @@ def bkmoo_adamw_default_params() -> bkmoo_adamw_params:
     return p
 
 
+class TensorList:
+    """The tensors of bkmoo_adamw: contiguous CUDA tensors of one dtype, in the
+    order of the flat buffers, and their weight decay (one number, one per
+    tensor, or None).  Checked once; keeps the tensors and their addresses."""
+
+    def __init__(self, tensors, weight_decay=None):
+        import torch
+        tensors = list(tensors)
+        n = len(tensors)
+        if n == 0:
+            raise ValueError("need at least one tensor")
+        self.dtype, self.device = tensors[0].dtype, tensors[0].get_device()
+        T = torch.Tensor
+        if self.device < 0 or set(map(T.get_device, tensors)) != {self.device} or \
+                not all(map(T.is_contiguous, tensors)) or \
+                any(t.dtype is not self.dtype for t in tensors):
+            raise ValueError("the tensors must be contiguous CUDA tensors of one dtype on one device")
+        self.dtype_code = _dtype_code(tensors[0])
+        self.tensors = tensors
+        self._sizes = array.array("q", map(T.numel, tensors))
+        self._addresses = array.array("Q", map(T.data_ptr, tensors))
+        self.n_elems = sum(self._sizes)
+        self._decay = None
+        if weight_decay is not None:
+            self._decay = array.array("f", [weight_decay] * n if isinstance(weight_decay, (int, float))
+                                      else weight_decay)
+            if len(self._decay) != n:
+                raise ValueError("weight_decay must be one number, or one per tensor")
+        # addresses of the three arrays, as the C call takes them
+        self.args = (self._addresses.buffer_info()[0], self._sizes.buffer_info()[0],
+                     self._decay.buffer_info()[0] if self._decay is not None else None, n)
+
+
 def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None, m_scale=None,
                 v_scale=None, grad_norm=None, stream=None):
-    """One AdamW step of `tensors` (contiguous CUDA tensors of one dtype, in the
-    order of the flat buffers) with the flat gradient.  m, v: flat float32, or
-    flat float8_e4m3fn with one float32 scale per 256 elements (v then holds the
-    root of the second moment); master: flat float32 weights of bfloat16
-    tensors, or None.  weight_decay: one number per tensor, or one for all."""
+    """One AdamW step of `tensors` (a TensorList, or the tensors and weight_decay
+    one would make it of) with the flat gradient.  m, v: flat float32, or flat
+    float8_e4m3fn with one float32 scale per 256 elements (v then holds the root
+    of the second moment); master: flat float32 weights of bfloat16 tensors, or
+    None."""
     import torch
-    tensors = list(tensors)
-    if not tensors:
-        raise ValueError("need at least one tensor")
-    dev, dt = grad.device, tensors[0].dtype
-    if any(t.dtype is not dt or t.device != dev or not t.is_contiguous() for t in tensors):
-        raise ValueError("the tensors must be contiguous, of one dtype and on the gradient's device")
-    n = len(tensors)
-    counts = [t.numel() for t in tensors]
-    sizes = (ctypes.c_int64 * n)(*counts)
-    ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
-    N = sum(counts)
-    eight = m.dtype == torch.float8_e4m3fn
-    flat = [("grad", grad, None), ("m", m, torch.float8_e4m3fn if eight else torch.float32),
-            ("v", v, m.dtype)]
-    if master is not None:
-        if dt != torch.bfloat16:
-            raise ValueError("a master copy goes with bfloat16 tensors")
-        flat.append(("master", master, torch.float32))
-    for name, t, want in flat:
-        if not t.is_cuda or t.device != dev or not t.is_contiguous() or t.numel() != N or \
-                (want is not None and t.dtype != want):
-            raise ValueError("%s must be a flat CUDA tensor of the tensors' %d elements%s"
-                             % (name, N, "" if want is None else ", %s" % want))
+    if not isinstance(tensors, TensorList):
+        tensors = TensorList(tensors, weight_decay)
+    elif weight_decay is not None:
+        raise ValueError("the TensorList has its own weight decay")
+    dev, N = tensors.device, tensors.n_elems
+    f32, eight = torch.float32, m.dtype is torch.float8_e4m3fn
+    if master is not None and tensors.dtype is not torch.bfloat16:
+        raise ValueError("a master copy goes with bfloat16 tensors")
+    for name, t, want in (("grad", grad, grad.dtype), ("m", m, m.dtype if eight else f32),
+                          ("v", v, m.dtype), ("master", master, f32)):
+        if t is not None and (t.dtype is not want or t.get_device() != dev or t.numel() != N or
+                              not t.is_contiguous()):
+            raise ValueError("%s must be a flat tensor of the tensors' %d elements, %s, on cuda:%d"
+                             % (name, N, want, dev))
+    ms = vs = None
     if eight:
         for name, t in (("m_scale", m_scale), ("v_scale", v_scale)):
-            if t is None or t.dtype != torch.float32 or t.device != dev or \
-                    not t.is_contiguous() or t.numel() != (N + 255) // 256:
+            if t is None or t.dtype is not f32 or t.get_device() != dev or \
+                    t.numel() != (N + 255) // 256 or not t.is_contiguous():
                 raise ValueError("%s must hold one float32 per 256 elements" % name)
-    if grad_norm is not None and (grad_norm.dtype != torch.float32 or grad_norm.device != dev or
+        ms, vs = m_scale.data_ptr(), v_scale.data_ptr()
+    if grad_norm is not None and (grad_norm.dtype is not f32 or grad_norm.get_device() != dev or
                                   grad_norm.numel() != 1):
         raise ValueError("grad_norm must be one float32 on the gradient's device")
-    if weight_decay is not None:
-        each = [float(weight_decay)] * n if isinstance(weight_decay, (int, float)) else list(weight_decay)
-        if len(each) != n:
-            raise ValueError("weight_decay must be one number, or one per tensor")
-        weight_decay = (ctypes.c_float * n)(*each)
     p = params if params is not None else bkmoo_adamw_default_params()
-
-    def ptr(t):
-        return t.data_ptr() if t is not None else None
-
-    with _Current(dev):
-        _check(load().bkmoo_adamw(ptrs, sizes, weight_decay, n, _dtype_code(tensors[0]),
-                                  grad.data_ptr(),
-                                  _dtype_code(grad), ptr(master), m.data_ptr(), v.data_ptr(),
-                                  ptr(m_scale) if eight else None, ptr(v_scale) if eight else None,
-                                  BKMOO_E4M3 if eight else BKMOO_F32, ctypes.byref(p),
-                                  ptr(grad_norm), _stream_handle(stream, dev)), "bkmoo_adamw")
+    _call(torch, dev, "bkmoo_adamw", load().bkmoo_adamw, *tensors.args, tensors.dtype_code,
+          grad.data_ptr(), _dtype_code(grad), master.data_ptr() if master is not None else None,
+          m.data_ptr(), v.data_ptr(), ms, vs, BKMOO_E4M3 if eight else BKMOO_F32, ctypes.byref(p),
+          grad_norm.data_ptr() if grad_norm is not None else None,
+          _raw_stream(torch, stream, dev))
 
 
 class Resolver:
