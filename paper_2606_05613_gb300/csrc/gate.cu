@@ -80,15 +80,13 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
   }
 }
 
-// dW_k = dy_k^T x_k for one or two dy (mats), every language.
-int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, int64_t ldx,
-                 int64_t M, int64_t N, int32_t K, const int64_t* rows, void* const* const* dw,
-                 int32_t dw_dtype, int32_t accumulate, int sms, int32_t* status, cudaStream_t s) {
-  TileArgs<kWeight> p = {};
-  p.status = status;
-  int r = BKMOO_OK;
+// What does not depend on the tiles' shape of dW_k = dy_k^T x_k for one or two dy
+// (mats), every language.  *any: there is something to write.
+int weight_args(TileArgs<kWeight>& p, const void* const* dy, int64_t ld_dy, int mats, const void* x,
+                int64_t ldx, int64_t M, int64_t N, int32_t K, const int64_t* rows,
+                void* const* const* dw, int32_t dw_dtype, int32_t accumulate, bool* any) {
   const int elem = dw_dtype == BKMOO_F32 ? 4 : 2;
-  bool any = false;
+  *any = false;
   for (int k = 0; k < K; ++k) {
     const int64_t n = rows[k + 1] - rows[k], at = rows[k];
     p.nkt[k] = up(n, kTileK);
@@ -99,26 +97,26 @@ int weight_grads(const void* const* dy, int64_t ld_dy, int mats, const void* x, 
       p.out[i * kMaxK + k] = dw[i][k];
       p.vec[i * kMaxK + k] = store_width(dw[i][k], N, elem);
     }
-    any = any || n > 0 || !accumulate;
+    *any = *any || n > 0 || !accumulate;
     if (n == 0) continue;
-    r = tile_map(&p.b[k], static_cast<const __nv_bfloat16*>(x) + at * ldx, n, N, ldx, kTileK);
+    int r = tile_map(&p.b[k], static_cast<const __nv_bfloat16*>(x) + at * ldx, n, N, ldx, kTileK);
     for (int i = 0; i < mats && r == BKMOO_OK; ++i)
       r = tile_map(&p.a[i * kMaxK + k], static_cast<const __nv_bfloat16*>(dy[i]) + at * ld_dy, n, M,
                    ld_dy, kTileK);
     if (r != BKMOO_OK) return r;
   }
-  if (!any) return BKMOO_OK;
   p.rows = (int32_t)M;
   p.cols = (int32_t)N;
-  const TileShape shape = tile_shape(M, N, false, p.nkt, K, mats, sms);
-  p.tiles_m = up(M, kTileM * shape.cg);
-  p.tiles_n = up(N, shape.bn);
   p.mats = mats;
   p.n_lang = K;
   p.out_dtype = dw_dtype;
   p.accumulate = accumulate;
-  p.tiles = p.tiles_m * p.tiles_n * mats * K;
-  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
+  return BKMOO_OK;
+}
+void weight_tiles(TileArgs<kWeight>& p, TileShape shape) {
+  p.tiles_m = up(p.rows, kTileM * shape.cg);
+  p.tiles_n = up(p.cols, shape.bn);
+  p.tiles = p.tiles_m * p.tiles_n * p.mats * p.n_lang;
 }
 
 bool grads_ok(void* const* dw, int32_t K, int32_t dtype) {
@@ -155,7 +153,7 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
     return launch_gate_few(q, sms, s) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
   }
   const int32_t nkt = up(D, kTileK);
-  const TileShape shape = tile_shape(T, F, true, &nkt, 1, 1, sms);
+  const TileShape shape = tile_shape({T, F, true, &nkt, 1, 1}, nullptr, sms, nullptr);
   TileArgs<kGate> p = {};
   r = tile_status_word(s, &p.status);
   if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, kTileM);
@@ -218,31 +216,39 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
                       dim3(256), list, 0, s, true) != cudaSuccess)
       return BKMOO_ERR_CUDA;
   }
-  if (dx && T > 0) {
-    const int32_t nkt = 2 * up(F, kTileK);
-    const TileShape shape = tile_shape(T, D, false, &nkt, 1, 1, sms);
-    TileArgs<kInput> p = {};
-    p.status = status;
-    const void* w[2] = {w_gate, w_up};
-    for (int i = 0; i < 2 && r == BKMOO_OK; ++i) {
-      r = tile_map(&p.a[i], d[i], T, F, ld, kTileM);
-      if (r == BKMOO_OK) r = tile_map(&p.b[i], w[i], F, D, ldw, kTileK);
-    }
-    if (r != BKMOO_OK) return r;
-    p.out = {dx, ld_dx, store_width(dx, ld_dx, 2)};
-    p.rows = (int32_t)T;
-    p.cols = (int32_t)D;
-    p.tiles_m = up(T, kTileM * shape.cg);
-    p.tiles_n = up(D, shape.bn);
-    p.nkt = nkt / 2;
-    p.tiles = p.tiles_m * p.tiles_n;
-    r = tile_launch(tile_input_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
+  // both products in one launch, or the one that is wanted
+  TileArgs<kBoth> p = {};
+  p.status = status;
+  bool any = false;
+  if (weights) {
+    const void* dy[2] = {d[0], d[1]};
+    void* const* dw[2] = {dw_gate, dw_up};
+    r = weight_args(p.w, dy, ld, 2, x, ldx, F, D, K, rows, dw, dw_dtype, accumulate, &any);
     if (r != BKMOO_OK) return r;
   }
-  if (!weights) return BKMOO_OK;
-  const void* dy[2] = {d[0], d[1]};
-  void* const* dw[2] = {dw_gate, dw_up};
-  return weight_grads(dy, ld, 2, x, ldx, F, D, K, rows, dw, dw_dtype, accumulate, sms, status, s);
+  const bool input = dx && T > 0;
+  if (!input && !any) return BKMOO_OK;
+  const int32_t nkt = 2 * up(F, kTileK);
+  const TileSet in = {T, D, false, &nkt, 1, 1}, w = {F, D, false, p.w.nkt, K, 2};
+  const TileShape shape = input ? tile_shape(in, any ? &w : nullptr, sms, &p.head_start)
+                                : tile_shape(w, nullptr, sms, nullptr);
+  if (any) weight_tiles(p.w, shape);
+  if (input) {
+    const void* m[2] = {w_gate, w_up};
+    for (int i = 0; i < 2 && r == BKMOO_OK; ++i) {
+      r = tile_map(&p.in.a[i], d[i], T, F, ld, kTileM);
+      if (r == BKMOO_OK) r = tile_map(&p.in.b[i], m[i], F, D, ldw, kTileK);
+    }
+    if (r != BKMOO_OK) return r;
+    p.in.out = {dx, ld_dx, store_width(dx, ld_dx, 2)};
+    p.in.rows = (int32_t)T;
+    p.in.cols = (int32_t)D;
+    p.in.tiles_m = up(T, kTileM * shape.cg);
+    p.in.tiles_n = up(D, shape.bn);
+    p.in.nkt = nkt / 2;
+    p.in.tiles = p.in.tiles_m * p.in.tiles_n;
+  }
+  return tile_launch(tile_both_fn(shape.cg, shape.bn), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
 }
 
 extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
@@ -258,5 +264,12 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   int sms = 0, r = tile_sms(&sms);
   if (r == BKMOO_OK) r = tile_status_word(s, &status);
   if (r != BKMOO_OK) return r;
-  return weight_grads(&dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate, sms, status, s);
+  TileArgs<kWeight> p = {};
+  p.status = status;
+  bool any = false;
+  r = weight_args(p, &dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate, &any);
+  if (r != BKMOO_OK || !any) return r;
+  const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, sms, nullptr);
+  weight_tiles(p, shape);
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
 }

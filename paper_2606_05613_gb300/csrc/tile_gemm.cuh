@@ -4,6 +4,8 @@
 //   kGate    [a | b] = x [Wg; Wu]^T, h = act(a) b       sum over the input width
 //   kInput   dx = da Wg + db Wu                         sum over the hidden width
 //   kWeight  dW_k = dy_k^T x_k for every language k     sum over its rows
+//   kBoth    a launch of kInput's tiles and then kWeight's: the few long ones first,
+//            the many short ones where SMs come free
 //
 // A tile is 128 rows (256 with a CTA pair) by BN = 64, 128 or 256 columns of fp32
 // accumulators; for kGate half of them columns of a and half the same ones of b, so
@@ -18,11 +20,13 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "tensor_core.cuh"
 
 namespace bkmoo {
 
-enum TileKind { kGate = 0, kInput = 1, kWeight = 2 };
+enum TileKind { kGate = 0, kInput = 1, kWeight = 2, kBoth = 3 };
 
 constexpr int kTileM = 128;    // rows of a CTA's tile
 constexpr int kTileK = 64;     // of the sum per stage: 128 bytes, the swizzle's row
@@ -69,7 +73,6 @@ template <>
 struct TileArgs<kInput> {
   CUtensorMap a[2], b[2];       // da, db; Wg, Wu
   TileOut out;                  // dx
-  int32_t* status;
   int32_t rows, cols;           // T, D
   int32_t tiles_m, tiles_n, tiles;
   int32_t nkt;                  // of one of the two products
@@ -88,6 +91,40 @@ struct TileArgs<kWeight> {
   int32_t tiles_m, tiles_n, tiles;
   int32_t mats, n_lang;
   int32_t out_dtype, accumulate;
+};
+
+template <>
+struct TileArgs<kBoth> {
+  TileArgs<kInput> in;
+  TileArgs<kWeight> w;
+  int32_t* status;
+  int32_t head_start;           // see Walk
+};
+
+// The tiles of one CTA or pair: `unit` of `units`, every units-th of the first set
+// and then of the second.  Units that get one tile of the first set less than others
+// begin with head_start tiles of the second among themselves.
+struct Walk {
+  int unit, units, a, b, head, more;   // more: units with one tile of the first set more
+  int k = 0;
+  __device__ __forceinline__ Walk(int unit_, int units_, int a_, int b_, int head_)
+      : unit(unit_), units(units_), a(a_), b(b_), more(a_ % units_) {
+    head = more ? head_ : 0;
+  }
+  // The next tile: 0 none left, 1 of the first set, 2 of the second.
+  __device__ __forceinline__ int next(int& tile) {
+    tile = unit + k * units;
+    if (tile < a) {
+      ++k;
+      return 1;
+    }
+    const int j = k - a / units - (unit < more ? 1 : 0);   // of the second set
+    const bool early = more && unit >= more;
+    ++k;
+    if (early && j < head) tile = j * (units - more) + unit - more;
+    else tile = head * (units - more) + (j - (early ? head : 0)) * units + unit;
+    return tile < b ? 2 : 0;
+  }
 };
 
 struct Tile {
@@ -232,7 +269,7 @@ struct TileShared {
   uint64_t tfull[2], tempty[2];                                    // tempty: the first CTA's, for both
   uint64_t drain;
   uint32_t tmem;
-  int abort;
+  volatile int abort;
 };
 
 // Operand tiles of one step of the sum.
@@ -341,18 +378,96 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
   }
 }
 
+// The ring of stages and the two accumulators as a role goes through them.
+struct RingState {
+  int s = 0, laps = 0;   // stage, and how often the ring has been gone through
+  int n = 0;             // accumulators used
+};
+
+// Warp 8's lane: operand tiles into the ring.
+template <int KIND, int CG, int BN>
+__device__ __forceinline__ bool fill_tile(const TileArgs<KIND>& p, int i, RingState& r,
+                                          TileShared<CG, BN>& sh, unsigned char* ring, unsigned rank) {
+  const Tile t = tile_at<KIND, CG, BN>(p, i);
+  for (int kt = 0; kt < t.nkt; ++kt) {
+    if (!bar_wait<CG>(&sh.empty[r.s], (r.laps & 1) ^ 1, &sh.abort)) return false;
+    unsigned char* a = ring + r.s * tile_stage_bytes(CG, BN);
+    const uint32_t bar = CG == 1 ? st_smem(&sh.full[r.s]) : peer_smem(&sh.full[r.s], 0);
+    if (rank == 0) bar_arrive_tx(&sh.full[r.s], CG * tile_stage_bytes(CG, BN));
+    load_step<KIND, CG, BN>(p, t, kt, rank, a, a + kTileM * kTileK * 2, bar);
+    if (++r.s == tile_stages(CG, BN)) r.s = 0, ++r.laps;
+  }
+  return true;
+}
+
+// Warp 9's lane (of a pair's first CTA): the products of a tile.
+template <int KIND, int CG, int BN>
+__device__ __forceinline__ bool multiply_tile(const TileArgs<KIND>& p, int i, RingState& r,
+                                              TileShared<CG, BN>& sh, unsigned char* ring) {
+  constexpr bool A_ACROSS = KIND == kWeight, B_ACROSS = KIND != kGate;
+  constexpr uint32_t desc = product_desc(kTileM * CG, BN, A_ACROSS, B_ACROSS);
+  constexpr uint32_t chunk = 64 * kTileK * 2;
+  // 16 of the sum: 32 bytes along a swizzled row, or 16 rows of 128 bytes
+  constexpr uint32_t a_step = A_ACROSS ? 2048 : 32, b_step = B_ACROSS ? 2048 : 32;
+  const Tile t = tile_at<KIND, CG, BN>(p, i);
+  if (t.nkt == 0) return true;
+  const int acc = r.n & 1;
+  if (!bar_wait<CG>(&sh.tempty[acc], ((r.n >> 1) & 1) ^ 1, &sh.abort)) return false;
+  tc_fence_after();
+  const uint32_t d = sh.tmem + acc * BN;
+  for (int kt = 0; kt < t.nkt; ++kt) {
+    if (!bar_wait<CG>(&sh.full[r.s], r.laps & 1, &sh.abort)) return false;
+    tc_fence_after();
+    const uint32_t a = st_smem(ring + r.s * tile_stage_bytes(CG, BN)), b = a + kTileM * kTileK * 2;
+#pragma unroll
+    for (int k = 0; k < kTileK / 16; ++k)
+      tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
+                       desc, kt > 0 || k > 0);
+    products_arrive<CG>(&sh.empty[r.s]);
+    if (++r.s == tile_stages(CG, BN)) r.s = 0, ++r.laps;
+  }
+  products_arrive<CG>(&sh.tfull[acc]);
+  ++r.n;
+  return true;
+}
+
+// Warps 0 to 7: a finished tile to memory.
+template <int KIND, int CG, int BN>
+__device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingState& r,
+                                           TileShared<CG, BN>& sh, float* turn, unsigned rank) {
+  const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = wid & 3, half = wid >> 2;
+  const Tile t = tile_at<KIND, CG, BN>(p, i);
+  const int acc = r.n & 1;
+  if (t.nkt > 0) {
+    const bool ok = bar_wait<CG>(&sh.tfull[acc], (r.n >> 1) & 1, &sh.abort);
+    if (!__all_sync(0xffffffffu, ok)) return false;
+    tc_fence_after();
+  }
+  const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
+  take_tile<KIND, BN>(p, t, row, half, sh.tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN, t.nkt == 0,
+                      turn + wid * (kTurnBytes / 4));
+  if (t.nkt > 0) {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      if (rank == 0) bar_arrive(&sh.tempty[acc]);
+      else bar_arrive_at(peer_smem(&sh.tempty[acc], 0));
+    }
+    ++r.n;
+  }
+  return true;
+}
+
 template <int KIND, int CG, int BN>
 __global__ void __launch_bounds__(kTileThreads, 1)
     tile_gemm_kernel(const __grid_constant__ TileArgs<KIND> p) {
-  constexpr int S = tile_stages(CG, BN), A_BYTES = kTileM * kTileK * 2;
-  constexpr bool A_ACROSS = KIND == kWeight, B_ACROSS = KIND != kGate;
+  constexpr int S = tile_stages(CG, BN);
   extern __shared__ unsigned char raw[];
   __shared__ TileShared<CG, BN> sh;
   unsigned char* ring = raw + ((1024 - (st_smem(raw) & 1023)) & 1023);
   float* turn = reinterpret_cast<float*>(ring + S * tile_stage_bytes(CG, BN));
-  const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int wid = threadIdx.x >> 5;
   const unsigned rank = CG == 1 ? 0 : cluster_rank();
-  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
@@ -376,60 +491,43 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   tc_fence_after();
   grid_wait();
   const uint32_t tmem = sh.tmem;
-  volatile int* abort = &sh.abort;
 
+  // f over this CTA's tiles, until it gives up (a whole warp as one, or one lane)
+  auto each = [&](auto f) {
+    int i;
+    bool on = true;
+    if constexpr (KIND == kBoth) {
+      Walk walk(blockIdx.x / CG, gridDim.x / CG, p.in.tiles, p.w.tiles, p.head_start);
+      for (int set; on && (set = walk.next(i)) != 0;) {
+        if (set == 1) on = f(std::integral_constant<int, kInput>(), p.in, i);
+        else on = f(std::integral_constant<int, kWeight>(), p.w, i);
+      }
+    } else {
+      for (i = blockIdx.x / CG; on && i < p.tiles; i += gridDim.x / CG)
+        on = f(std::integral_constant<int, KIND>(), p, i);
+    }
+  };
+  RingState r;
   if (wid == kTileEpilogueWarps) {
     if (elect_one()) {
-      int s = 0, laps = 0;
-      for (int i = first; i < p.tiles && !*abort; i += stride) {
-        const Tile t = tile_at<KIND, CG, BN>(p, i);
-        for (int kt = 0; kt < t.nkt; ++kt) {
-          if (!bar_wait<CG>(&sh.empty[s], (laps & 1) ^ 1, abort)) break;
-          unsigned char* a = ring + s * tile_stage_bytes(CG, BN);
-          const uint32_t bar = CG == 1 ? st_smem(&sh.full[s]) : peer_smem(&sh.full[s], 0);
-          if (rank == 0) bar_arrive_tx(&sh.full[s], CG * tile_stage_bytes(CG, BN));
-          load_step<KIND, CG, BN>(p, t, kt, rank, a, a + A_BYTES, bar);
-          if (++s == S) s = 0, ++laps;
-        }
-      }
+      each([&](auto kind, const auto& q, int i) {
+        return fill_tile<decltype(kind)::value, CG, BN>(q, i, r, sh, ring, rank);
+      });
       // every copy has landed and been used before the CTA ends
       for (int i = 0; i < S; ++i) {
-        if (!bar_wait<CG>(&sh.empty[s], (laps & 1) ^ 1, abort) && rank == 0 && laps > 0) {
+        if (!bar_wait<CG>(&sh.empty[r.s], (r.laps & 1) ^ 1, &sh.abort) && rank == 0 && r.laps > 0) {
           int none = 0;
-          bar_wait<CG>(&sh.full[s], (laps & 1) ^ 1, &none);
+          bar_wait<CG>(&sh.full[r.s], (r.laps & 1) ^ 1, &none);
         }
-        if (++s == S) s = 0, ++laps;
+        if (++r.s == S) r.s = 0, ++r.laps;
       }
     }
   } else if (wid == kTileEpilogueWarps + 1) {
     if (rank == 0 && elect_one()) {
-      constexpr uint32_t desc = product_desc(kTileM * CG, BN, A_ACROSS, B_ACROSS);
-      constexpr uint32_t chunk = 64 * kTileK * 2;
-      // 16 of the sum: 32 bytes along a swizzled row, or 16 rows of 128 bytes
-      constexpr uint32_t a_step = A_ACROSS ? 2048 : 32, b_step = B_ACROSS ? 2048 : 32;
-      int s = 0, laps = 0, n = 0;
-      for (int i = first; i < p.tiles && !*abort; i += stride) {
-        const Tile t = tile_at<KIND, CG, BN>(p, i);
-        if (t.nkt == 0) continue;
-        const int acc = n & 1;
-        if (!bar_wait<CG>(&sh.tempty[acc], ((n >> 1) & 1) ^ 1, abort)) break;
-        tc_fence_after();
-        const uint32_t d = tmem + acc * BN;
-        for (int kt = 0; kt < t.nkt; ++kt) {
-          if (!bar_wait<CG>(&sh.full[s], laps & 1, abort)) break;
-          tc_fence_after();
-          const uint32_t a = st_smem(ring + s * tile_stage_bytes(CG, BN)), b = a + A_BYTES;
-#pragma unroll
-          for (int k = 0; k < kTileK / 16; ++k)
-            tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
-                             desc, kt > 0 || k > 0);
-          products_arrive<CG>(&sh.empty[s]);
-          if (++s == S) s = 0, ++laps;
-        }
-        products_arrive<CG>(&sh.tfull[acc]);
-        ++n;
-      }
-      if (*abort) {
+      each([&](auto kind, const auto& q, int i) {
+        return multiply_tile<decltype(kind)::value, CG, BN>(q, i, r, sh, ring);
+      });
+      if (sh.abort) {
         // no product is in flight when tensor memory is handed back
         int none = 0;
         products_arrive<CG>(&sh.drain);
@@ -437,31 +535,9 @@ __global__ void __launch_bounds__(kTileThreads, 1)
       }
     }
   } else {
-    const int quarter = wid & 3, half = wid >> 2;
-    int n = 0;
-    for (int i = first; i < p.tiles; i += stride) {
-      const Tile t = tile_at<KIND, CG, BN>(p, i);
-      const int acc = n & 1;
-      bool ok = true;
-      if (t.nkt > 0) {
-        ok = bar_wait<CG>(&sh.tfull[acc], (n >> 1) & 1, abort);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after();
-      }
-      const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
-      take_tile<KIND, BN>(p, t, row, half, tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN, t.nkt == 0,
-                          turn + wid * (kTurnBytes / 4));
-      if (t.nkt > 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (rank == 0) bar_arrive(&sh.tempty[acc]);
-          else bar_arrive_at(peer_smem(&sh.tempty[acc], 0));
-        }
-        ++n;
-      }
-    }
+    each([&](auto kind, const auto& q, int i) {
+      return drain_tile<decltype(kind)::value, CG, BN>(q, i, r, sh, turn, rank);
+    });
   }
   __syncwarp();
   tc_fence_before();
@@ -474,7 +550,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
 // The kernels, one translation unit each (nvcc runs them side by side).
 const void* tile_gate_fn(int cg, int bn);
-const void* tile_input_fn(int cg, int bn);
 const void* tile_weight_fn(int cg, int bn);
+const void* tile_both_fn(int cg, int bn);
 
 }  // namespace bkmoo

@@ -102,31 +102,56 @@ int tile_status_word(cudaStream_t s, int32_t** word) {
 // 768 <- 2048, 1000 rows 17.8 / 18.1 / 26.1 / 26.6, 4000 rows 48 / 38 / 36 / 35;
 // weight gradient 2048 x 768, 4 languages of 256 rows 11.3 / 8.6 / 9.1 / 10.9, of
 // 2048 36 / 22 / 25 / 25.
-TileShape tile_shape(int64_t rows, int64_t cols, bool gate, const int32_t* nkt, int groups, int mats,
-                     int sms) {
-  struct Cost {
-    TileShape s;
-    double step, out, launch;
-  };
-  static const Cost costs[4] = {{{1, 64}, 0.165, 0.8, 4.0},
+struct TileCost {
+  TileShape s;
+  double step, out, launch;
+};
+constexpr TileCost kCosts[4] = {{{1, 64}, 0.165, 0.8, 4.0},
                                 {{1, 128}, 0.217, 1.2, 4.7},
                                 {{1, 256}, 0.376, 2.2, 5.8},
                                 {{2, 256}, 0.320, 2.9, 7.0}};
-  TileShape best = costs[0].s;
+// Tiles of a set, and the mean and the longest time of one.
+struct SetCost {
+  int64_t tiles = 0;
+  double mean = 0.0, longest = 0.0;
+};
+SetCost set_cost(const TileSet& s, const TileCost& c) {
+  const int64_t m = kTileM * c.s.cg, n = s.gate ? c.s.bn / 2 : c.s.bn;
+  SetCost r;
+  r.tiles = (s.rows + m - 1) / m * ((s.cols + n - 1) / n) * s.mats * s.groups;
+  for (int g = 0; g < s.groups; ++g) {
+    const double t = s.nkt[g] * c.step > c.out ? s.nkt[g] * c.step : c.out;
+    r.longest = t > r.longest ? t : r.longest;
+    r.mean += t / s.groups;
+  }
+  return r;
+}
+TileShape tile_shape(const TileSet& a, const TileSet* b, int sms, int32_t* head_start) {
+  TileShape best = kCosts[0].s;
   double least = 0.0;
   for (int i = 0; i < 4; ++i) {
-    const Cost& c = costs[i];
-    const int64_t m = kTileM * c.s.cg, n = gate ? c.s.bn / 2 : c.s.bn, units = sms / c.s.cg;
-    const double each = (double)((rows + m - 1) / m) * ((cols + n - 1) / n) * mats;
-    double longest = 0.0, sum = 0.0;
-    for (int g = 0; g < groups; ++g) {
-      const double t = nkt[g] * c.step > c.out ? nkt[g] * c.step : c.out;
-      longest = t > longest ? t : longest;
-      sum += t;
+    const TileCost& c = kCosts[i];
+    const int64_t units = sms / c.s.cg;
+    const SetCost x = set_cost(a, c);
+    const SetCost y = b ? set_cost(*b, c) : SetCost();
+    double t = (double)((x.tiles + units - 1) / units) * x.mean;
+    int32_t head = 0;
+    if (b) {
+      // units with a tile of the first set less do the second's meanwhile
+      const int64_t more = x.tiles % units, spare = more ? units - more : 0;
+      const double fit = x.mean / y.mean;
+      head = (int32_t)fit;
+      const double left = (double)y.tiles - (double)spare * head;
+      if (left > 0.0) t += std::ceil(left / units) * y.mean;
     }
-    const double waves = std::ceil(each * groups / units) * (sum / groups);
-    const double t = c.launch + (waves > longest ? waves : longest);
-    if (i == 0 || t < least) least = t, best = c.s;
+    if (x.longest > t) t = x.longest;
+    if (y.longest > t) t = y.longest;
+    t += c.launch;
+    if (i == 0 || t < least) {
+      least = t;
+      best = c.s;
+      if (head_start) *head_start = head;
+    }
   }
   return best;
 }

@@ -42,10 +42,16 @@ int tile_status_word(cudaStream_t s, int32_t** word);
 struct TileShape {
   int cg, bn;
 };
-// The shape for rows x cols results (gate: cols of h, of which a tile has bn / 2)
-// of `mats` products each with `groups` sums of nkt steps.
-TileShape tile_shape(int64_t rows, int64_t cols, bool gate, const int32_t* nkt, int groups, int mats,
-                     int sms);
+// rows x cols results (gate: cols of h, of which a tile has bn / 2), `mats` products
+// each with `groups` sums of nkt steps.
+struct TileSet {
+  int64_t rows, cols;
+  bool gate;
+  const int32_t* nkt;
+  int groups, mats;
+};
+// The shape for one set, or two in turn, and the second's head start (Walk).
+TileShape tile_shape(const TileSet& a, const TileSet* b, int sms, int32_t* head_start);
 // Queues a tile kernel over `tiles` tiles.
 int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s);
 
