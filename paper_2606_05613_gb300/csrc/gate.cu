@@ -11,23 +11,6 @@ namespace {
 bool act_ok(int32_t act) { return act == BKMOO_SILU || act == BKMOO_GELU || act == BKMOO_GELU_TANH; }
 int32_t up(int64_t n, int64_t by) { return (int32_t)((n + by - 1) / by); }
 
-// act(a) and act'(a) (tile_gemm.cuh: activation).
-__device__ __forceinline__ void activation_slope(int act, float a, float* f, float* df) {
-  if (act == BKMOO_SILU) {
-    const float s = sigmoid(a);
-    *f = a * s;
-    *df = s * (1.0f + a * (1.0f - s));
-  } else if (act == BKMOO_GELU) {
-    const float c = 0.5f * erfcf(-0.70710678f * a);
-    *f = a * c;
-    *df = c + a * 0.39894228f * __expf(-0.5f * a * a);
-  } else {
-    const float q = a * a, s = sigmoid(1.59576912f * a * (1.0f + 0.044715f * q));
-    *f = a * s;
-    *df = s + a * s * (1.0f - s) * 1.59576912f * (1.0f + 0.134145f * q);
-  }
-}
-
 struct SlopeArgs {
   const __nv_bfloat16 *dh, *a, *b;
   __nv_bfloat16 *da, *db;
@@ -36,10 +19,30 @@ struct SlopeArgs {
   int32_t cols, act;
 };
 
+__device__ __forceinline__ void slope8(const uint4& xh, const uint4& xa, const uint4& xb, int act,
+                                       uint4* da, uint4* db) {
+  const uint32_t h[4] = {xh.x, xh.y, xh.z, xh.w}, u[4] = {xa.x, xa.y, xa.z, xa.w},
+                 v[4] = {xb.x, xb.y, xb.z, xb.w};
+  uint32_t oa[4], ob[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    auto wide = [](uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); };
+    float2 f, df;
+    activation_slope2(act, wide(u[j]), &f, &df);
+    const float2 g = wide(h[j]), x = __fmul2_rn(__fmul2_rn(g, wide(v[j])), df), y = __fmul2_rn(g, f);
+    oa[j] = pack_bf16(x.x, x.y);
+    ob[j] = pack_bf16(y.x, y.y);
+  }
+  *da = make_uint4(oa[0], oa[1], oa[2], oa[3]);
+  *db = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+}
 // da = dh b act'(a), db = dh act(a).  Bound by memory: 10 bytes an element, in
 // vectors of 8 (one thread one vector; the last of a row element by element).
 // The products behind it take bf16 operands, so da and db are rounded to bf16
-// here, once, from fp32.
+// here, once, from fp32.  8192 x 8192 105 us, 6.4 TB/s.  (Done inside the products'
+// kernel instead, by the warps that wait for its first tiles, row by row ahead of
+// them, it takes 140 us and slows the products beside it: 8192 rows 2048 -> 8192
+// backward 751 us so, 724 in turn.)
 __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
   grid_wait();
   const int64_t per = (p.cols + 7) / 8, n = p.rows * per;
@@ -51,23 +54,9 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
                         *b = p.b + row * p.ld_ab + col;
     __nv_bfloat16 *da = p.da + row * p.ld_d + col, *db = p.db + row * p.ld_d + col;
     if (col + 8 <= p.cols) {
-      const uint4 xh = __ldg(reinterpret_cast<const uint4*>(dh)), xa = __ldg(reinterpret_cast<const uint4*>(a)),
-                  xb = __ldg(reinterpret_cast<const uint4*>(b));
-      const uint32_t h[4] = {xh.x, xh.y, xh.z, xh.w}, u[4] = {xa.x, xa.y, xa.z, xa.w},
-                     v[4] = {xb.x, xb.y, xb.z, xb.w};
-      uint32_t oa[4], ob[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float f0, d0, f1, d1;
-        const float h0 = __uint_as_float(h[j] << 16), h1 = __uint_as_float(h[j] & 0xffff0000u);
-        activation_slope(p.act, __uint_as_float(u[j] << 16), &f0, &d0);
-        activation_slope(p.act, __uint_as_float(u[j] & 0xffff0000u), &f1, &d1);
-        oa[j] = pack_bf16(h0 * __uint_as_float(v[j] << 16) * d0,
-                          h1 * __uint_as_float(v[j] & 0xffff0000u) * d1);
-        ob[j] = pack_bf16(h0 * f0, h1 * f1);
-      }
-      *reinterpret_cast<uint4*>(da) = make_uint4(oa[0], oa[1], oa[2], oa[3]);
-      *reinterpret_cast<uint4*>(db) = make_uint4(ob[0], ob[1], ob[2], ob[3]);
+      slope8(__ldg(reinterpret_cast<const uint4*>(dh)), __ldg(reinterpret_cast<const uint4*>(a)),
+             __ldg(reinterpret_cast<const uint4*>(b)), p.act, reinterpret_cast<uint4*>(da),
+             reinterpret_cast<uint4*>(db));
     } else {
       for (int j = 0; col + j < p.cols; ++j) {
         float f, d;

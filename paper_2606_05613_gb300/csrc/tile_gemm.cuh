@@ -252,15 +252,91 @@ __device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int co
   if (o.p) store_row(static_cast<__nv_bfloat16*>(o.p) + row * o.ld + col, v, n, o.vec);
 }
 
-// act(a).  silu a / (1 + e^-a); gelu a Phi(a) with Phi(a) = erfc(-a / sqrt 2) / 2;
-// gelu_tanh a / (1 + e^(-2 z)), z = sqrt(2/pi) (a + 0.044715 a^3), which is
-// a (1 + tanh z) / 2 without its cancellation.  The fast exponential and
-// quotient are good to about 2^-20 of the result, a 2^11th of a bf16 rounding.
-__device__ __forceinline__ float sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }
-__device__ __forceinline__ float activation(int act, float a) {
-  if (act == BKMOO_SILU) return a * sigmoid(a);
-  if (act == BKMOO_GELU) return a * 0.5f * erfcf(-0.70710678f * a);
-  return a * sigmoid(1.59576912f * (a + 0.044715f * a * a * a));
+// ---- activations, two values at a time ---------------------------------------
+//
+// silu a s with s = 1 / (1 + e^-a); gelu_tanh a s with s = 1 / (1 + e^(-2 z)), z =
+// sqrt(2/pi) (a + 0.044715 a^3), which is a (1 + tanh z) / 2 without its
+// cancellation; gelu a Phi(a) with Phi(a) = erfc(-a / sqrt 2) / 2 and erfc by the
+// Chebyshev fit of Numerical Recipes (section 6.2: erfc(x) = t e^(-x^2 + P(t)) for
+// x >= 0, t = 1 / (1 + x / 2), fractional error below 1.2e-7), e^(-x^2) of which is
+// the derivative's too.  Powers of 2 and reciprocals are the hardware's, good to
+// about 2^-22 and rounded arguments' worth more: 2^-18 at most for results that
+// bf16 tells from 0.
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 power2(float2 x) {
+  float2 r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  return r;
+}
+__device__ __forceinline__ float2 inverse(float2 x) {
+  float2 r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  return r;
+}
+// 1 / (1 + 2^-x)
+__device__ __forceinline__ float2 sigmoid2(float2 x) {
+  return inverse(__fadd2_rn(power2(make_float2(-x.x, -x.y)), both(1.0f)));
+}
+// Phi(a), and e^(-a^2 / 2).
+__device__ __forceinline__ float2 normal2(float2 a, float2* bell) {
+  constexpr float kLog2e = 1.44269504f;
+  const float2 x = __fmul2_rn(make_float2(fabsf(a.x), fabsf(a.y)), both(0.70710678f));
+  const float2 t = inverse(__ffma2_rn(x, both(0.5f), both(1.0f)));
+  float2 q = both(0.17087277f);
+  q = __ffma2_rn(q, t, both(-0.82215223f));
+  q = __ffma2_rn(q, t, both(1.48851587f));
+  q = __ffma2_rn(q, t, both(-1.13520398f));
+  q = __ffma2_rn(q, t, both(0.27886807f));
+  q = __ffma2_rn(q, t, both(-0.18628806f));
+  q = __ffma2_rn(q, t, both(0.09678418f));
+  q = __ffma2_rn(q, t, both(0.37409196f));
+  q = __ffma2_rn(q, t, both(1.00002368f));
+  q = __ffma2_rn(q, t, both(-1.26551223f));
+  const float2 e = power2(__fmul2_rn(__fmul2_rn(a, a), both(-0.5f * kLog2e)));
+  *bell = e;
+  // half of erfc(|x|): Phi on the negative side
+  const float2 low = __fmul2_rn(__fmul2_rn(__fmul2_rn(t, both(0.5f)), e), power2(__fmul2_rn(q, both(kLog2e))));
+  return make_float2(a.x < 0.0f ? low.x : 1.0f - low.x, a.y < 0.0f ? low.y : 1.0f - low.y);
+}
+// 2 z of gelu_tanh times log2(e), and its derivative by a without the factor log2(e).
+__device__ __forceinline__ float2 tanh_arg(float2 a, float2 q) {
+  constexpr float k = 1.59576912f * 1.44269504f;
+  return __fmul2_rn(__fmul2_rn(a, both(k)), __ffma2_rn(q, both(0.044715f), both(1.0f)));
+}
+__device__ __forceinline__ float2 activation2(int act, float2 a) {
+  if (act == BKMOO_SILU) return __fmul2_rn(a, sigmoid2(__fmul2_rn(a, both(1.44269504f))));
+  if (act == BKMOO_GELU) {
+    float2 bell;
+    return __fmul2_rn(a, normal2(a, &bell));
+  }
+  return __fmul2_rn(a, sigmoid2(tanh_arg(a, __fmul2_rn(a, a))));
+}
+// act(a) and act'(a).
+__device__ __forceinline__ void activation_slope2(int act, float2 a, float2* f, float2* df) {
+  if (act == BKMOO_SILU) {
+    const float2 s = sigmoid2(__fmul2_rn(a, both(1.44269504f)));
+    *f = __fmul2_rn(a, s);
+    *df = __ffma2_rn(*f, __ffma2_rn(s, both(-1.0f), both(1.0f)), s);
+  } else if (act == BKMOO_GELU) {
+    float2 bell;
+    const float2 c = normal2(a, &bell);
+    *f = __fmul2_rn(a, c);
+    *df = __ffma2_rn(__fmul2_rn(a, both(0.39894228f)), bell, c);
+  } else {
+    const float2 q = __fmul2_rn(a, a), s = sigmoid2(tanh_arg(a, q));
+    *f = __fmul2_rn(a, s);
+    const float2 dz = __ffma2_rn(q, both(3.0f * 0.044715f * 1.59576912f), both(1.59576912f));
+    *df = __ffma2_rn(__fmul2_rn(*f, __ffma2_rn(s, both(-1.0f), both(1.0f))), dz, s);
+  }
+}
+__device__ __forceinline__ float activation(int act, float a) { return activation2(act, both(a)).x; }
+__device__ __forceinline__ void activation_slope(int act, float a, float* f, float* df) {
+  float2 f2, d2;
+  activation_slope2(act, both(a), &f2, &d2);
+  *f = f2.x;
+  *df = d2.x;
 }
 
 template <int CG, int BN>
@@ -347,7 +423,11 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
         store_bf16(p.out[2], row, t.n0 + at, b, n);
         if (p.out[0].p) {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) a[j] = activation(p.act, a[j]) * b[j];
+          for (int j = 0; j < 32; j += 2) {
+            const float2 f = activation2(p.act, make_float2(a[j], a[j + 1]));
+            a[j] = f.x * b[j];
+            a[j + 1] = f.y * b[j + 1];
+          }
           store_bf16(p.out[0], row, t.n0 + at, a, n);
         }
       }
