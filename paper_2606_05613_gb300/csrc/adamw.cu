@@ -465,7 +465,9 @@ const void* adamw_fn(int pd, int gd, bool e4m3, bool master) {
 // ---- norm ------------------------------------------------------------------
 
 constexpr int kNormThreads = 256;
-constexpr int kNormCtas = 1024;      // at most: partial sums in the workspace
+// At most, four an SM, so that one wave holds them: 4e8 bf16 134 us, 6.0 TB/s (1024,
+// of which 912 fit at a time, 162).
+constexpr int kNormCtas = 608;
 static_assert(kNormCtas * sizeof(double) <= BKMOO_NORM_WS_BYTES, "workspace");
 
 // Sum of squares: a thread's in fp32 over 8 vectors at a time, then fp64; a

@@ -409,7 +409,7 @@ def _act_code(act) -> int:
 
 
 def _raw_stream(torch, stream, dev: int) -> int:
-    return (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _call(torch, dev: int, where: str, fn, *args):
@@ -426,9 +426,9 @@ def _call(torch, dev: int, where: str, fn, *args):
 def _scratch(torch, nbytes: int, dev: int, stream):
     """A byte tensor for work on `stream` (None: the current one)."""
     if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev)
     with torch.cuda.stream(stream):
-        return torch.empty(nbytes, dtype=torch.uint8, device=torch.device("cuda", dev))
+        return torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
 
 def _language_rows(rows, T: int):
@@ -507,8 +507,8 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
         gu, du = _weight_grads(dw_up, K, F, D, dev, "dw_up")
         if dt != du:
             raise ValueError("dw_gate and dw_up must have one dtype")
-    if ws is None:
-        ws = _scratch(torch, bkmoo_gate_backward_workspace_size(T, F), dev, stream)
+    if ws is None:           # as bkmoo_gate_backward_workspace_size: da and db, rows on 16 bytes
+        ws = _scratch(torch, 2 * -(-T * ((F + 7) // 8 * 16) // 256) * 256, dev, stream)
     _call(torch, dev, "bkmoo_gate_backward", load().bkmoo_gate_backward, pd, ldd, pa, pb, ld_ab,
           px, ldx, pg, pu, ldw, T, D, F, _act_code(act), K, r, pdx, lddx, gg, gu, dt,
           1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size(),
