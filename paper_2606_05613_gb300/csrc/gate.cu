@@ -142,7 +142,7 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
     return launch_gate_few(q, sms, s) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
   }
   const int32_t nkt = up(D, kTileK);
-  const TileShape shape = tile_shape({T, F, true, &nkt, 1, 1}, nullptr, sms, nullptr);
+  const TileShape shape = tile_shape({T, F, true, &nkt, 1, 1}, nullptr, false, sms, nullptr);
   TileArgs<kGate> p = {};
   r = tile_status_word(s, &p.status);
   if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, kTileM);
@@ -219,8 +219,9 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
   if (!input && !any) return BKMOO_OK;
   const int32_t nkt = 2 * up(F, kTileK);
   const TileSet in = {T, D, false, &nkt, 1, 1}, w = {F, D, false, p.w.nkt, K, 2};
-  const TileShape shape = input ? tile_shape(in, any ? &w : nullptr, sms, &p.head_start)
-                                : tile_shape(w, nullptr, sms, nullptr);
+  const bool exact = any && dw_dtype == BKMOO_F32;
+  const TileShape shape = input ? tile_shape(in, any ? &w : nullptr, exact, sms, &p.head_start)
+                                : tile_shape(w, nullptr, exact, sms, nullptr);
   if (any) weight_tiles(p.w, shape);
   if (input) {
     const void* m[2] = {w_gate, w_up};
@@ -258,7 +259,7 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   bool any = false;
   r = weight_args(p, &dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate, &any);
   if (r != BKMOO_OK || !any) return r;
-  const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, sms, nullptr);
+  const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, dw_dtype == BKMOO_F32, sms, nullptr);
   weight_tiles(p, shape);
   return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
 }

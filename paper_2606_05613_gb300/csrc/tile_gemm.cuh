@@ -129,14 +129,23 @@ struct Walk {
 
 struct Tile {
   int g, m0, n0, nkt;   // g: kWeight's matrix * kMaxK + language
+  int span;             // steps of the sum that one accumulator takes (kExactSteps)
 };
+// The tensor cores drop what an addition shifts out of the accumulator: a sum of T
+// rows comes out about 1e-9 T of it low (1.9e-5 for 16384, more than all other
+// roundings of fp32 products together).  bf16 results do not show it.  For fp32 ones
+// an accumulator takes 512 of the sum, 5e-7, and the pieces are added in registers,
+// rounded to nearest; tiles are then at most 128 columns wide, for the registers.
+constexpr int kExactSteps = 8;
 
 template <int KIND, int CG, int BN>
 __device__ __forceinline__ Tile tile_at(const TileArgs<KIND>& p, int t) {
   Tile r;
   int i = t;
   r.g = 0;
+  r.span = 1 << 30;
   if constexpr (KIND == kWeight) {
+    if (p.out_dtype == BKMOO_F32) r.span = kExactSteps;
     const int per = p.tiles_m * p.tiles_n;
     const int unit = t / per;                 // language by language, its matrices in turn
     i = t - unit * per;
@@ -401,7 +410,8 @@ __device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile
 // the tile's sum is empty and the accumulator was not written.
 template <int KIND, int BN>
 __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t, int row, int half,
-                                          uint32_t acc, bool empty, float* turn) {
+                                          uint32_t acc, bool empty, float* turn,
+                                          const float (*before)[32]) {
   const bool live = row < p.rows;
   if constexpr (KIND == kGate) {
 #pragma unroll 1
@@ -434,9 +444,9 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
       __syncwarp();   // the loads are the whole warp's
     }
   } else {
-#pragma unroll 1
-    for (int at = 32 * half; at < BN; at += 64) {
-      const int n = p.cols - (t.n0 + at);
+#pragma unroll(KIND == kWeight && BN <= 128 ? 2 : 1)
+    for (int c = 0; c < BN / 64; ++c) {
+      const int at = 32 * half + 64 * c, n = p.cols - (t.n0 + at);
       uint32_t r[32];
       if (!empty) {
         tc_load32(r, acc + at);
@@ -446,6 +456,12 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
         float v[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[j]);
+        if constexpr (KIND == kWeight && BN <= 128) {
+          if (before) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += before[c][j];
+          }
+        }
         if constexpr (KIND == kInput) {
           if (live) store_bf16(p.out, row, t.n0 + at, v, n);
         } else if (!(empty && p.accumulate)) {
@@ -491,23 +507,25 @@ __device__ __forceinline__ bool multiply_tile(const TileArgs<KIND>& p, int i, Ri
   constexpr uint32_t a_step = A_ACROSS ? 2048 : 32, b_step = B_ACROSS ? 2048 : 32;
   const Tile t = tile_at<KIND, CG, BN>(p, i);
   if (t.nkt == 0) return true;
-  const int acc = r.n & 1;
-  if (!bar_wait<CG>(&sh.tempty[acc], ((r.n >> 1) & 1) ^ 1, &sh.abort)) return false;
-  tc_fence_after();
-  const uint32_t d = sh.tmem + acc * BN;
-  for (int kt = 0; kt < t.nkt; ++kt) {
-    if (!bar_wait<CG>(&sh.full[r.s], r.laps & 1, &sh.abort)) return false;
+  for (int k0 = 0; k0 < t.nkt; k0 += t.span) {
+    const int acc = r.n & 1, end = t.nkt - k0 < t.span ? t.nkt : k0 + t.span;
+    if (!bar_wait<CG>(&sh.tempty[acc], ((r.n >> 1) & 1) ^ 1, &sh.abort)) return false;
     tc_fence_after();
-    const uint32_t a = st_smem(ring + r.s * tile_stage_bytes(CG, BN)), b = a + kTileM * kTileK * 2;
+    const uint32_t d = sh.tmem + acc * BN;
+    for (int kt = k0; kt < end; ++kt) {
+      if (!bar_wait<CG>(&sh.full[r.s], r.laps & 1, &sh.abort)) return false;
+      tc_fence_after();
+      const uint32_t a = st_smem(ring + r.s * tile_stage_bytes(CG, BN)), b = a + kTileM * kTileK * 2;
 #pragma unroll
-    for (int k = 0; k < kTileK / 16; ++k)
-      tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
-                       desc, kt > 0 || k > 0);
-    products_arrive<CG>(&sh.empty[r.s]);
-    if (++r.s == tile_stages(CG, BN)) r.s = 0, ++r.laps;
+      for (int k = 0; k < kTileK / 16; ++k)
+        tile_product<CG>(d, operand_desc(a + k * a_step, chunk), operand_desc(b + k * b_step, chunk),
+                         desc, kt > k0 || k > 0);
+      products_arrive<CG>(&sh.empty[r.s]);
+      if (++r.s == tile_stages(CG, BN)) r.s = 0, ++r.laps;
+    }
+    products_arrive<CG>(&sh.tfull[acc]);
+    ++r.n;
   }
-  products_arrive<CG>(&sh.tfull[acc]);
-  ++r.n;
   return true;
 }
 
@@ -517,24 +535,53 @@ __device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingS
                                            TileShared<CG, BN>& sh, float* turn, unsigned rank) {
   const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = wid & 3, half = wid >> 2;
   const Tile t = tile_at<KIND, CG, BN>(p, i);
-  const int acc = r.n & 1;
-  if (t.nkt > 0) {
-    const bool ok = bar_wait<CG>(&sh.tfull[acc], (r.n >> 1) & 1, &sh.abort);
+  const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
+  const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+  auto wait = [&]() {
+    const bool ok = bar_wait<CG>(&sh.tfull[r.n & 1], (r.n >> 1) & 1, &sh.abort);
     if (!__all_sync(0xffffffffu, ok)) return false;
     tc_fence_after();
-  }
-  const int row = t.m0 + (int)rank * kTileM + quarter * 32 + lane;
-  take_tile<KIND, BN>(p, t, row, half, sh.tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN, t.nkt == 0,
-                      turn + wid * (kTurnBytes / 4));
-  if (t.nkt > 0) {
+    return true;
+  };
+  auto release = [&]() {
     tc_fence_before();
     __syncwarp();
     if (lane == 0) {
-      if (rank == 0) bar_arrive(&sh.tempty[acc]);
-      else bar_arrive_at(peer_smem(&sh.tempty[acc], 0));
+      if (rank == 0) bar_arrive(&sh.tempty[r.n & 1]);
+      else bar_arrive_at(peer_smem(&sh.tempty[r.n & 1], 0));
     }
     ++r.n;
+  };
+  if constexpr (KIND == kWeight && BN <= 128) {
+    if (t.nkt > t.span) {
+      float sum[BN / 64][32];
+#pragma unroll
+      for (int c = 0; c < BN / 64; ++c)
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
+      for (int k0 = 0; k0 + t.span < t.nkt; k0 += t.span) {
+        if (!wait()) return false;
+#pragma unroll
+        for (int c = 0; c < BN / 64; ++c) {
+          uint32_t v[32];
+          tc_load32(v, sh.tmem + lanes + (r.n & 1) * BN + 32 * half + 64 * c);
+          tc_landed(v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
+        }
+        release();
+      }
+      if (!wait()) return false;
+      take_tile<KIND, BN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, false,
+                          turn + wid * (kTurnBytes / 4), sum);
+      release();
+      return true;
+    }
   }
+  if (t.nkt > 0 && !wait()) return false;
+  take_tile<KIND, BN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
+                      turn + wid * (kTurnBytes / 4), nullptr);
+  if (t.nkt > 0) release();
   return true;
 }
 

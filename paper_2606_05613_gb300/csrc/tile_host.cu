@@ -110,6 +110,9 @@ constexpr TileCost kCosts[4] = {{{1, 64}, 0.165, 0.8, 4.0},
                                 {{1, 128}, 0.217, 1.2, 4.7},
                                 {{1, 256}, 0.376, 2.2, 5.8},
                                 {{2, 256}, 0.320, 2.9, 7.0}};
+// fp32 results, whose sums are taken in pieces (a pair of 128 columns was no faster
+// than one CTA's anywhere: 8192 x 2048, 16384 rows 444 us, 425).
+constexpr TileCost kExactCosts[2] = {{{1, 64}, 0.190, 1.55, 4.0}, {{1, 128}, 0.234, 3.5, 4.7}};
 // Tiles of a set, and the mean and the longest time of one.
 struct SetCost {
   int64_t tiles = 0;
@@ -126,11 +129,11 @@ SetCost set_cost(const TileSet& s, const TileCost& c) {
   }
   return r;
 }
-TileShape tile_shape(const TileSet& a, const TileSet* b, int sms, int32_t* head_start) {
+TileShape tile_shape(const TileSet& a, const TileSet* b, bool exact, int sms, int32_t* head_start) {
   TileShape best = kCosts[0].s;
   double least = 0.0;
-  for (int i = 0; i < 4; ++i) {
-    const TileCost& c = kCosts[i];
+  for (int i = 0; i < (exact ? 2 : 4); ++i) {
+    const TileCost& c = exact ? kExactCosts[i] : kCosts[i];
     const int64_t units = sms / c.s.cg;
     const SetCost x = set_cost(a, c);
     const SetCost y = b ? set_cost(*b, c) : SetCost();
