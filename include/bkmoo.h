@@ -484,9 +484,8 @@ int bkmoo_op_status(void* stream, int32_t* status);
  * bkmoo_grad_norm -- the 2-norm of a flat gradient (the direction), n elements
  * of fp32 or bf16, 16-byte aligned.  out_norm: device fp32, one value.  Squares
  * are summed in fp32 over at most 64 elements, then in fp64, in an order fixed
- * by n: deterministic.  Infinite where a square or the sum leaves fp32, NaN with
- * a NaN.  ws: device, 256-byte aligned, BKMOO_NORM_WS_BYTES, not shared by calls
- * that overlap.
+ * by n: deterministic; the sum and its root are rounded to fp32.  Infinite where a square or the sum leaves fp32, NaN with a NaN.  ws: device, 256-byte aligned,
+ * BKMOO_NORM_WS_BYTES, not shared by calls that overlap.
  */
 #define BKMOO_NORM_WS_BYTES 16384
 int bkmoo_grad_norm(const void* grad, int32_t dtype, int64_t n, float* out_norm, void* ws,

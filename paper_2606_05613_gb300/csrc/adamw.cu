@@ -40,6 +40,7 @@ struct AdamArgs {
   float rate;                        // lr / (1 - beta1^step)
   float root;                        // 1 / sqrt(1 - beta2^step)
   float eps;
+  float one;                         // 1
   uint64_t key;                      // of the rounding to 8 bits
   int64_t n;                         // flat elements
   int64_t first, blocks;             // this launch: blocks first .. first + blocks - 1
@@ -145,7 +146,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, int64_t i, int64_t n, ui
 }
 
 // Four values / their scale as e4m3 bytes, each rounded away from 0 with the
-// chance that its rest gives.  `inv` is 2^-120 / scale, and 2^-120 takes e4m3's
+// chance that its rest gives.  `inv` is 1 / scale, and 2^-120 takes e4m3's
 // smallest normal number, 2^-6, to fp32's, 2^-126: the product's bits from the
 // 20th on are the code, of subnormal values too, and what is below them is the
 // rest, of which the upper 16 bits meet the chance's (all 16 places up: the code
@@ -157,7 +158,7 @@ __device__ __forceinline__ uint32_t encode4(const float2 (&x)[2], float inv, con
   uint32_t s[4];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const float2 y = __fmul2_rn(x[j], make_float2(inv, inv));
+    const float2 y = __fmul2_rn(__fmul2_rn(x[j], make_float2(inv, inv)), make_float2(0x1p-120f, 0x1p-120f));
     const uint32_t bits[2] = {__float_as_uint(y.x), __float_as_uint(y.y)};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -174,8 +175,7 @@ __device__ __forceinline__ uint32_t encode4(const float2 (&x)[2], float inv, con
   }
   return c;
 }
-// The same where 2^-120 / scale is no normal number (a scale above 2^6) or the
-// block has a NaN or an infinity: `inv` is 1 / scale, and a NaN stays one.
+// The same for a block with a NaN or an infinity: a NaN stays one.
 template <bool SIGNED>
 __device__ __noinline__ uint32_t encode4_any(float2 x01, float2 x23, float inv, uint32_t w0, uint32_t w1,
                                              uint32_t w2, uint32_t w3) {
@@ -211,13 +211,27 @@ struct Loaded {
   int t;                 // the tensor of the block's first element
 };
 
-// Both to about 2^-23; below fp32's normal numbers (a gradient below 1e-19) 0 and
-// infinity.
-__device__ __forceinline__ float root_of(float x) {
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+// To 2^-23.
+__device__ __forceinline__ float2 near_root2(float2 x) {
+  float2 r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
   return r;
 }
+// Rounded root: the hardware's reciprocal root of x, good to 2^-22, and one step of
+// Heron's method on x y with the residual in one rounding (x - r r by FMA), which
+// leaves an error of 2^-45 before the last rounding: the rounded root but for one in a
+// million, in fewer instructions than __fsqrt_rn (4e8 elements 985 us with that).  0 for
+// 0, NaN for infinity; not for gradients below 1e-19, whose squares are no normal numbers.
+__device__ __forceinline__ float2 root2(float2 x) {
+  float2 y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 0x1p-126f)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 0x1p-126f)));
+  const float2 r = __fmul2_rn(x, y);
+  const float2 e = __ffma2_rn(make_float2(-r.x, -r.y), r, x);
+  return __ffma2_rn(e, __fmul2_rn(y, make_float2(0.5f, 0.5f)), r);
+}
+// To 2^-23.
 __device__ __forceinline__ float reciprocal(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -225,18 +239,22 @@ __device__ __forceinline__ float reciprocal(float x) {
 }
 
 // Two elements' step: moments in place (v as its root in 8 bits), the new weights
-// returned.  The moments round as written, product by product: in 8 bits a last
-// bit can move a code.
+// returned.  The moments round as written, product by product, and in 8 bits the root
+// is the rounded one: a last bit can move a code, and a code in this step the scale
+// of its block in the next.
 template <bool E4M3>
 struct Step {
-  float b1, one_b1, b2, one_b2, rate, root, eps, clip;
+  float b1, one_b1, b2, one_b2, rate, root, eps, one, clip;
   __device__ __forceinline__ float2 operator()(float2 g, float2 keep, float2 w, float2& m, float2& v) const {
     auto both = [](float x) { return make_float2(x, x); };
     const float2 gj = __fmul2_rn(g, both(clip));
     const float2 old = E4M3 ? __fmul2_rn(v, v) : v;
-    m = __fadd2_rn(__fmul2_rn(m, both(b1)), __fmul2_rn(gj, both(one_b1)));
-    const float2 vj = __fadd2_rn(__fmul2_rn(old, both(b2)), __fmul2_rn(__fmul2_rn(gj, gj), both(one_b2)));
-    const float2 r = make_float2(root_of(vj.x), root_of(vj.y));
+    // sums as x 1 + y with a 1 that the compiler does not know: it makes one rounding
+    // of a packed product and the sum it goes into
+    m = __ffma2_rn(__fmul2_rn(m, both(b1)), both(one), __fmul2_rn(gj, both(one_b1)));
+    const float2 vj = __ffma2_rn(__fmul2_rn(old, both(b2)), both(one),
+                                 __fmul2_rn(__fmul2_rn(gj, gj), both(one_b2)));
+    const float2 r = E4M3 ? root2(vj) : near_root2(vj);
     v = E4M3 ? r : vj;
     const float2 den = __ffma2_rn(r, both(root), both(eps));
     const float2 q = make_float2(reciprocal(den.x), reciprocal(den.y));
@@ -257,7 +275,7 @@ __global__ void __launch_bounds__(kAdamThreads, E4M3 ? 6 : 7)
   const int64_t end = a.first + a.blocks, stride = (int64_t)gridDim.x * kAdamWarps;
   int64_t blk = a.first + (int64_t)blockIdx.x * kAdamWarps + (threadIdx.x >> 5);
   if (blk >= end) return;
-  Step<E4M3> step = {a.b1, a.one_b1, a.b2, a.one_b2, a.rate, a.root, a.eps, 1.0f};
+  Step<E4M3> step = {a.b1, a.one_b1, a.b2, a.one_b2, a.rate, a.root, a.eps, a.one, a.one};
   if (a.norm) {
     const float norm = *a.norm;
     if (!(fabsf(norm) <= 3.4028235e38f)) return;      // not a step to take
@@ -402,19 +420,15 @@ __global__ void __launch_bounds__(kAdamThreads, E4M3 ? 6 : 7)
       rlow = __reduce_min_sync(0xffffffffu, rlow);
       if (mtop < 0x0d800000u) mtop = 0;               // below 2^-100
       if (rtop < 0x0d800000u) rtop = 0;
-      // one division for all four quotients: lanes 0 and 1 448 / top, 2 and 3 the
-      // scales top / 448
-      const float top = __uint_as_float((lane & 1) ? rtop : mtop);
-      const float q = __fdiv_rn((lane & 2) ? top : 448.0f, (lane & 2) ? 448.0f : top);
-      float mi = mtop != 0 ? __shfl_sync(0xffffffffu, q, 0) : 0.0f;
-      float ri = rtop != 0 ? __shfl_sync(0xffffffffu, q, 1) : 0.0f;
-      if (lane == 2) a.m_scale[blk] = q;
-      if (lane == 3) a.v_scale[blk] = q;
-      constexpr uint32_t kMost = 0x46e00000u;         // 28672 = 448 2^6
-      const bool plain = mtop <= kMost && rtop <= kMost;
-      if (plain) mi *= 0x1p-120f, ri *= 0x1p-120f;
+      const float mt = __uint_as_float(mtop), rt = __uint_as_float(rtop);
+      const float each = __frcp_rn((lane & 1) ? rt : mt);       // both reciprocals at once
+      const float mi = mtop != 0 ? __fmul_rn(448.0f, __shfl_sync(0xffffffffu, each, 0)) : 0.0f;
+      const float ri = rtop != 0 ? __fmul_rn(448.0f, __shfl_sync(0xffffffffu, each, 1)) : 0.0f;
+      if (lane == 0) a.m_scale[blk] = __fmul_rn(mt, 1.0f / 448.0f);
+      if (lane == 1) a.v_scale[blk] = __fmul_rn(rt, 1.0f / 448.0f);
+      const bool plain = mtop < 0x7f800000u && rtop < 0x7f800000u;
       // no root is as small as a code of 0
-      const bool above = __float_as_uint(__uint_as_float(rlow) * ri) >= 0x100000u;
+      const bool above = __float_as_uint(__uint_as_float(rlow) * ri * 0x1p-120f) >= 0x100000u;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t u[4], cm, cr;
@@ -465,13 +479,16 @@ const void* adamw_fn(int pd, int gd, bool e4m3, bool master) {
 // ---- norm ------------------------------------------------------------------
 
 constexpr int kNormThreads = 256;
-// At most, four an SM, so that one wave holds them: 4e8 bf16 134 us, 6.0 TB/s (1024,
+// At most, four an SM, so that one wave holds them: 4e8 bf16 137 us, 5.8 TB/s (1024,
 // of which 912 fit at a time, 162).
 constexpr int kNormCtas = 608;
 static_assert(kNormCtas * sizeof(double) <= BKMOO_NORM_WS_BYTES, "workspace");
 
 // Sum of squares: a thread's in fp32 over 8 vectors at a time, then fp64; a
-// CTA's by a fixed tree.  The order is fixed by n alone.
+// CTA's by a fixed tree.  The order is fixed by n alone.  (64 squares of bf16 values
+// come out 4e-8 of them low, for ties are frequent there: half a rounding of the fp32
+// result.  Four at a time with the roundings kept beside, 185 us for 4e8 elements
+// instead of 137.)
 template <class G>
 __global__ void __launch_bounds__(kNormThreads) norm_kernel(const G* g, int64_t n, double* part) {
   grid_wait();
@@ -503,7 +520,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(const G* g, int64_t 
   }
   if (blockIdx.x == 0 && threadIdx.x < n - vecs * V) {
     const float y = (float)g[vecs * V + threadIdx.x];
-    sum += (double)(y * y);
+    sum += (double)y * (double)y;
   }
   __shared__ double sh[kNormThreads];
   sh[threadIdx.x] = sum;
@@ -525,7 +542,7 @@ __global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(const double* pa
     if (threadIdx.x < w) sh[threadIdx.x] += sh[threadIdx.x + w];
     __syncthreads();
   }
-  if (threadIdx.x == 0) *out = (float)sqrt(sh[0]);
+  if (threadIdx.x == 0) *out = __fsqrt_rn((float)sh[0]);
 }
 
 bool at(const void* p, uintptr_t by) { return p && ((uintptr_t)p & (by - 1)) == 0; }
@@ -612,6 +629,7 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
   a.rate = (float)(p->lr / (1.0 - std::pow(p->beta1, (double)p->step)));
   a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(p->beta2, (double)p->step)));
   a.eps = (float)p->eps;
+  a.one = 1.0f;
   a.key = mix_word(p->seed + ((uint64_t)p->step + 1) * kGold);
   a.n = n;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
