@@ -86,6 +86,11 @@ class BucketMOO:
         d = moo.finish()        # every p.grad is now a view of d
         optimizer.step()
 
+    or, with the layers of language.py, one pass over a batch of all languages:
+        moo.begin_batch()
+        loss(model, batch, rows).backward()
+        d = moo.finish()
+
     All parameters that require gradients must share one device and one
     dtype, float32 or bfloat16.  The buffers (K gradients, the direction, the
     workspace) are allocated once, here.
@@ -137,14 +142,33 @@ class BucketMOO:
         self.grads[k].zero_()
         for i, p in enumerate(self.params):
             p.grad = self._view(self.grads[k], i)
+            p.language_grads = None
         self._lang = k
         if k == self.K - 1:
             self._left = list(self.layout.need)
             self._done = [False] * self.layout.n_buckets
 
+    def begin_batch(self) -> None:
+        """For one backward pass over a batch of all K languages, instead of K
+        passes: zero every language's buffer and give every parameter
+        `language_grads`, its K places in them.  The layers of language.py add
+        each language's gradient to its own place; a parameter that no such
+        layer uses keeps a gradient of 0 in every language.  finish() then
+        resolves the whole plan at once."""
+        import torch
+        torch.cuda.current_stream(self.device).wait_stream(self.side)
+        for g in self.grads:
+            g.zero_()
+        for i, p in enumerate(self.params):
+            p.grad = None
+            p.language_grads = [self._view(g, i) for g in self.grads]
+        self._lang = self.K - 1
+        self._left = list(self.layout.need)
+        self._done = [False] * self.layout.n_buckets
+
     def _make_hook(self, i):
         def hook(p):
-            if self._lang != self.K - 1:
+            if self._lang != self.K - 1 or getattr(p, "language_grads", None) is not None:
                 return
             for b in range(self.layout.first[i], self.layout.last[i] + 1):
                 self._left[b] -= 1
@@ -169,6 +193,10 @@ class BucketMOO:
         import torch
         if self._lang != self.K - 1:
             raise RuntimeError("finish() before the last language's backward pass")
+        if any(getattr(p, "language_grads", None) is not None and p.grad is not None
+               for p in self.params):
+            raise RuntimeError("a parameter got a gradient that is not apart by language: in a "
+                               "batch of all languages only language.py's layers may use them")
         b = 0
         B = self.layout.n_buckets
         while b < B:                        # runs of unresolved buckets
@@ -183,6 +211,7 @@ class BucketMOO:
         torch.cuda.current_stream(self.device).wait_stream(self.side)
         for i, p in enumerate(self.params):
             p.grad = self._view(self.direction, i)
+            p.language_grads = None
         self._lang = None
         return self.direction
 

@@ -1,0 +1,128 @@
+"""Layers whose weight gradients come apart by language in one backward pass.
+
+The resolve needs one gradient per language.  BucketMOO gets them from K
+backward passes; where a batch holds the rows of all K languages one after
+another, these layers give them in one: a linear layer's weight gradient is a
+sum over rows, so language k's is the sum over its own rows
+(bkmoo_gate_backward, bkmoo_language_wgrad).  `rows` are K + 1 bounds: language k
+has the batch's rows from rows[k] to rows[k + 1].
+
+Inside BucketMOO.begin_batch() ... finish() the gradients are added to the
+parameters' `language_grads`, their places in the K flat buffers; outside, the
+layers' weights receive the ordinary gradient of the whole batch.  Weights and
+activations are bfloat16 on a GPU; the products that no language splits
+(y = x W^T and its dx of LanguageLinear) are torch's.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import native
+
+
+def _languages(weight, rows, T):
+    """The language places of `weight` and its bounds, or one place for all of
+    the batch."""
+    places = getattr(weight, "language_grads", None)
+    if places is not None:
+        if rows is None or len(rows) != len(places) + 1:
+            raise ValueError("rows must be the bounds of the %d languages" % len(places))
+        return places, rows, None
+    whole = torch.zeros_like(weight, memory_format=torch.contiguous_format)
+    return [whole], [0, T], whole
+
+
+def _on_rows(t):
+    """t as a matrix whose rows start on 16 bytes."""
+    t = t.reshape(-1, t.shape[-1])
+    n = t.shape[1]
+    if t.stride(1) == 1 and t.stride(0) % 8 == 0 and t.stride(0) >= n and t.data_ptr() % 16 == 0:
+        return t
+    return t.new_empty(t.shape[0], (n + 7) // 8 * 8)[:, :n].copy_(t)
+
+
+def _room(t, rows, cols):
+    return t.new_empty(rows, (cols + 7) // 8 * 8)[:, :cols]
+
+
+class _Gate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act, rows):
+        lead, m = x.shape[:-1], _on_rows(x)
+        T, F = m.shape[0], w_gate.shape[0]
+        g, u = _on_rows(w_gate), _on_rows(w_up)
+        h = _room(m, T, F)
+        a = b = None
+        if any(ctx.needs_input_grad[:3]):
+            a, b = _room(m, T, F), _room(m, T, F)
+        native.bkmoo_gate_forward(m, g, u, act, h, a, b)
+        ctx.save_for_backward(m, w_gate, w_up, a, b)
+        ctx.act, ctx.rows, ctx.lead = act, rows, lead
+        return h.view(*lead, F) if len(lead) != 1 else h
+
+    @staticmethod
+    def backward(ctx, dh):
+        m, w_gate, w_up, a, b = ctx.saved_tensors
+        T, D = m.shape
+        dx = _room(m, T, D) if ctx.needs_input_grad[0] else None
+        weights = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+        dg = du = whole_g = whole_u = rows = None
+        if weights:
+            dg, rows, whole_g = _languages(w_gate, ctx.rows, T)
+            du, _, whole_u = _languages(w_up, ctx.rows, T)
+        native.bkmoo_gate_backward(_on_rows(dh), a, b, m, _on_rows(w_gate), _on_rows(w_up), ctx.act,
+                                   rows if weights else [0, T], dx, dg, du, accumulate=True)
+        if dx is not None:
+            dx = dx.reshape(*ctx.lead, D)
+        return dx, whole_g, whole_u, None, None
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, rows):
+        ctx.save_for_backward(x, weight)
+        ctx.rows = rows
+        return torch.matmul(x, weight.t())
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight = ctx.saved_tensors
+        dx = torch.matmul(dy, weight) if ctx.needs_input_grad[0] else None
+        whole = None
+        if ctx.needs_input_grad[1]:
+            m = _on_rows(x)
+            places, rows, whole = _languages(weight, ctx.rows, m.shape[0])
+            native.bkmoo_language_wgrad(_on_rows(dy), m, rows, places, accumulate=True)
+        return dx, whole, None
+
+
+class LanguageLinear(torch.nn.Module):
+    """y = x W^T, W [out, in], without a bias."""
+
+    def __init__(self, in_features: int, out_features: int, device="cuda"):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(out_features, in_features, device=device,
+                                                     dtype=torch.bfloat16))
+        torch.nn.init.normal_(self.weight, std=in_features ** -0.5)
+
+    def forward(self, x, rows=None):
+        return _Linear.apply(x, self.weight, rows)
+
+
+class GatedFeedForward(torch.nn.Module):
+    """y = (act(x Wg^T) * (x Wu^T)) Wd^T; act "silu", "gelu" or "gelu_tanh"."""
+
+    def __init__(self, width: int, hidden: int, act: str = "silu", device="cuda"):
+        super().__init__()
+        if act not in native.ACTS:
+            raise ValueError("act must be one of %s, got %r" % (sorted(native.ACTS), act))
+        self.act = act
+        self.w_gate, self.w_up = (
+            torch.nn.Parameter(torch.empty(hidden, width, device=device, dtype=torch.bfloat16))
+            for _ in range(2))
+        for w in (self.w_gate, self.w_up):
+            torch.nn.init.normal_(w, std=width ** -0.5)
+        self.down = LanguageLinear(hidden, width, device=device)
+
+    def forward(self, x, rows=None):
+        return self.down(_Gate.apply(x, self.w_gate, self.w_up, self.act, rows), rows)
