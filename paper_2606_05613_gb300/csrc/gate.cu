@@ -39,7 +39,8 @@ __device__ __forceinline__ void slope8(const uint4& xh, const uint4& xa, const u
 // da = dh b act'(a), db = dh act(a).  Bound by memory: 10 bytes an element, in
 // vectors of 8 (one thread one vector; the last of a row element by element).
 // The products behind it take bf16 operands, so da and db are rounded to bf16
-// here, once, from fp32.  8192 x 8192 105 us, 6.4 TB/s.  (Done inside the products'
+// here, once, from fp32.  8192 x 8192 99 us, 6.8 TB/s
+// (1216 CTAs that stay, of which 912 fit at a time, 109).  (Done inside the products'
 // kernel instead, by the warps that wait for its first tiles, row by row ahead of
 // them, it takes 140 us and slows the products beside it: 8192 rows 2048 -> 8192
 // backward 751 us so, 724 in turn.)
@@ -101,6 +102,13 @@ int weight_args(TileArgs<kWeight>& p, const void* const* dy, int64_t ld_dy, int 
   p.out_dtype = dw_dtype;
   p.accumulate = accumulate;
   return BKMOO_OK;
+}
+// Whether some gradient's pieces are not whole aligned vectors (TileOut).
+bool turned(const TileArgs<kWeight>& p) {
+  bool r = p.cols % 32 != 0;
+  for (int k = 0; k < p.n_lang; ++k)
+    for (int i = 0; i < p.mats; ++i) r = r || p.vec[i * kMaxK + k] < 16;
+  return r;
 }
 void weight_tiles(TileArgs<kWeight>& p, TileShape shape) {
   p.tiles_m = up(p.rows, kTileM * shape.cg);
@@ -199,7 +207,7 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
   if (T > 0) {
     SlopeArgs q = {static_cast<const __nv_bfloat16*>(dh), static_cast<const __nv_bfloat16*>(a),
                    static_cast<const __nv_bfloat16*>(b), d[0], d[1], ld_dh, ld_ab, ld, T, (int32_t)F, act};
-    const int64_t blocks = (T * (ld / 8) + 255) / 256, most = (int64_t)sms * 8;
+    const int64_t blocks = (T * (ld / 8) + 255) / 256, most = 1 << 30;
     void* list[] = {&q};
     if (launch_behind((const void*)gate_slope_kernel, dim3((unsigned)(blocks < most ? blocks : most)),
                       dim3(256), list, 0, s, true) != cudaSuccess)
@@ -238,7 +246,7 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     p.in.nkt = nkt / 2;
     p.in.tiles = p.in.tiles_m * p.in.tiles_n;
   }
-  return tile_launch(tile_both_fn(shape.cg, shape.bn), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
+  return tile_launch(tile_both_fn(shape.cg, shape.bn, any && turned(p.w)), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
 }
 
 extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
@@ -261,5 +269,5 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   if (r != BKMOO_OK || !any) return r;
   const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, dw_dtype == BKMOO_F32, sms, nullptr);
   weight_tiles(p, shape);
-  return tile_launch(tile_weight_fn(shape.cg, shape.bn), shape, &p, p.tiles, s);
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn, turned(p)), shape, &p, p.tiles, s);
 }

@@ -48,8 +48,9 @@ __host__ __device__ constexpr int tile_smem(int cg, int bn) {
          kTileEpilogueWarps * kTurnBytes;
 }
 
-// Where a result goes: rows of `ld` elements.  `vec` is the widest store that
-// every row's 32-column pieces allow: 32, 16 or 0 bytes (kWeight only).
+// Where a result goes: rows of `ld` elements.  `vec` is the widest store that every
+// row's 32-column pieces allow: 32 or 16 bytes, and for kWeight also 4 or 0 (no more
+// than an element).
 struct TileOut {
   void* p;
   int64_t ld;
@@ -233,27 +234,54 @@ __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162f
 __device__ __forceinline__ void as_type(float* p, float x) { *p = x; }
 __device__ __forceinline__ void as_type(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// The warp's 32 rows of 32 columns, of which the first `rows` and n exist, where
-// they are not aligned for vectors: turned in shared memory, so that the warp
-// writes a row at a time, 32 neighbours, instead of one element of 32 rows (771 x
-// 517 in fp32, 3 languages: 37 us so).
+// The warp's 32 rows of 32 columns, of which the first `rows` and n exist, where they
+// are not aligned for wide vectors: turned in shared memory (turn: rows of 33 floats,
+// of which 32 are the piece's), so that the warp writes a row at a time, 32
+// neighbours, instead of one element of 32 rows (771 x 517 fp32 in 3 languages 37 us
+// so).
 template <class T>
-__device__ __forceinline__ void put_turned(T* p, int64_t ld, const float (&v)[32], int rows, int n,
-                                           bool add, float* turn) {
+static __device__ __noinline__ void put_turned(T* p, int64_t ld, int rows, int n, const float* turn) {
   const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
-  __syncwarp();
   if (lane < n) {
 #pragma unroll 8
     for (int r = 0; r < 32; ++r) {
       if (r >= rows) break;
-      T* q = p + r * ld + lane;
-      const float x = turn[r * 33 + lane];
-      as_type(q, add ? x + as_float(*q) : x);
+      as_type(p + r * ld + lane, turn[r * 33 + lane]);
     }
   }
-  __syncwarp();
+}
+// The same, added to what is there, which is fetched 16 rows at a time (6716 x 6034
+// bf16 in 4 languages, 4243 rows, row by row 1641 us, 361 so).
+template <class T>
+static __device__ __noinline__ void add_turned(T* p, int64_t ld, int rows, int n, const float* turn) {
+  const int lane = threadIdx.x & 31;
+  T* q = p + lane;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32; r0 += 16) {
+    T old[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r0 + r < rows && lane < n) old[r] = q[(r0 + r) * ld];
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r0 + r < rows && lane < n)
+        as_type(q + (r0 + r) * ld, turn[(r0 + r) * 33 + lane] + as_float(old[r]));
+  }
+}
+// By pairs: two rows at a time, the upper lanes the second (ld is even).
+static __device__ __noinline__ void add_turned_pairs(__nv_bfloat16* p, int64_t ld, int rows, int n,
+                                                 const float* turn) {
+  const int lane = threadIdx.x & 31, up = lane >> 4, c = 2 * (lane & 15);
+  uint32_t* q = reinterpret_cast<uint32_t*>(p + up * ld + c);
+  uint32_t old[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (2 * r + up < rows && c < n) old[r] = q[r * ld];
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (2 * r + up < rows && c < n)
+      q[r * ld] = pack_bf16(turn[(2 * r + up) * 33 + c] + __uint_as_float(old[r] << 16),
+                            turn[(2 * r + up) * 33 + c + 1] + __uint_as_float(old[r] & 0xffff0000u));
 }
 
 __device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int col,
@@ -392,23 +420,39 @@ __device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t
   }
 }
 
-// A warp's 32 rows (this thread's: `row`) by 32 columns of a gradient.
-template <class T>
+// A warp's 32 rows (this thread's: `row`) by 32 columns of a gradient.  TURN: not all
+// gradients' pieces are whole and aligned (a kernel of its own: the code for it takes
+// registers that cost the others 3.5 %).
+template <class T, bool TURN>
 __device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile& t, int row, int at,
                                           float (&v)[32], int n, float* turn) {
   T* q = static_cast<T*>(p.out[t.g]) + (int64_t)row * p.cols + t.n0 + at;
-  if (p.vec[t.g] != 0 && n >= 32) {
+  if (!TURN || (p.vec[t.g] >= 16 && n >= 32)) {
     if (row < p.rows) put_row(q, v, p.vec[t.g], p.accumulate);
-  } else {
-    const int lane = threadIdx.x & 31;
-    put_turned(q - (int64_t)lane * p.cols, p.cols, v, p.rows - (row - lane), n, p.accumulate, turn);
+    return;
+  }
+  if constexpr (TURN) {
+    const int lane = threadIdx.x & 31, rows = p.rows - (row - lane);
+    T* first = q - (int64_t)lane * p.cols;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
+    __syncwarp();
+    if (!p.accumulate) {
+      put_turned(first, p.cols, rows, n, turn);
+    } else if constexpr (sizeof(T) == 2) {
+      if (p.vec[t.g] != 0) add_turned_pairs(first, p.cols, rows, n, turn);
+      else add_turned(first, p.cols, rows, n, turn);
+    } else {
+      add_turned(first, p.cols, rows, n, turn);
+    }
+    __syncwarp();
   }
 }
 
 // One warp's share of a finished tile: rows of its quarter, columns of its half.
 // `acc`: the accumulator's tensor-memory address for this warp's lanes; `empty`:
 // the tile's sum is empty and the accumulator was not written.
-template <int KIND, int BN>
+template <int KIND, int BN, bool TURN>
 __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t, int row, int half,
                                           uint32_t acc, bool empty, float* turn,
                                           const float (*before)[32]) {
@@ -465,8 +509,8 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
         if constexpr (KIND == kInput) {
           if (live) store_bf16(p.out, row, t.n0 + at, v, n);
         } else if (!(empty && p.accumulate)) {
-          if (p.out_dtype == BKMOO_BF16) put_piece<__nv_bfloat16>(p, t, row, at, v, n, turn);
-          else put_piece<float>(p, t, row, at, v, n, turn);
+          if (p.out_dtype == BKMOO_BF16) put_piece<__nv_bfloat16, TURN>(p, t, row, at, v, n, turn);
+          else put_piece<float, TURN>(p, t, row, at, v, n, turn);
         }
       }
       __syncwarp();   // the loads are the whole warp's
@@ -530,7 +574,7 @@ __device__ __forceinline__ bool multiply_tile(const TileArgs<KIND>& p, int i, Ri
 }
 
 // Warps 0 to 7: a finished tile to memory.
-template <int KIND, int CG, int BN>
+template <int KIND, int CG, int BN, bool TURN>
 __device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingState& r,
                                            TileShared<CG, BN>& sh, float* turn, unsigned rank) {
   const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = wid & 3, half = wid >> 2;
@@ -572,20 +616,20 @@ __device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingS
         release();
       }
       if (!wait()) return false;
-      take_tile<KIND, BN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, false,
+      take_tile<KIND, BN, TURN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, false,
                           turn + wid * (kTurnBytes / 4), sum);
       release();
       return true;
     }
   }
   if (t.nkt > 0 && !wait()) return false;
-  take_tile<KIND, BN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
+  take_tile<KIND, BN, TURN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
                       turn + wid * (kTurnBytes / 4), nullptr);
   if (t.nkt > 0) release();
   return true;
 }
 
-template <int KIND, int CG, int BN>
+template <int KIND, int CG, int BN, bool TURN>
 __global__ void __launch_bounds__(kTileThreads, 1)
     tile_gemm_kernel(const __grid_constant__ TileArgs<KIND> p) {
   constexpr int S = tile_stages(CG, BN);
@@ -663,7 +707,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
   } else {
     each([&](auto kind, const auto& q, int i) {
-      return drain_tile<decltype(kind)::value, CG, BN>(q, i, r, sh, turn, rank);
+      return drain_tile<decltype(kind)::value, CG, BN, TURN>(q, i, r, sh, turn, rank);
     });
   }
   __syncwarp();
@@ -677,7 +721,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
 // The kernels, one translation unit each (nvcc runs them side by side).
 const void* tile_gate_fn(int cg, int bn);
-const void* tile_weight_fn(int cg, int bn);
-const void* tile_both_fn(int cg, int bn);
+const void* tile_weight_fn(int cg, int bn, bool turn);
+const void* tile_both_fn(int cg, int bn, bool turn);
 
 }  // namespace bkmoo

@@ -16,7 +16,7 @@ __device__ int32_t g_status;
 struct PerDevice {
   void* status = nullptr;
   int sms = 0;
-  const void* sized[16] = {};    // kernels whose shared-memory limit is raised
+  const void* sized[24] = {};    // kernels whose shared-memory limit is raised
 };
 std::mutex g_mu;
 PerDevice g_dev[kMaxDevices];
@@ -143,7 +143,7 @@ TileShape tile_shape(const TileSet& a, const TileSet* b, bool exact, int sms, in
       // units with a tile of the first set less do the second's meanwhile
       const int64_t more = x.tiles % units, spare = more ? units - more : 0;
       const double fit = x.mean / y.mean;
-      head = (int32_t)fit;
+      head = (int32_t)(fit < 1e6 ? fit : 1e6);
       const double left = (double)y.tiles - (double)spare * head;
       if (left > 0.0) t += std::ceil(left / units) * y.mean;
     }
@@ -169,12 +169,12 @@ int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cuda
     std::lock_guard<std::mutex> lk(g_mu);
     const void** known = g_dev[dev].sized;
     int i = 0;
-    while (i < 16 && known[i] && known[i] != fn) ++i;
-    if (i == 16 || !known[i]) {
+    while (i < 24 && known[i] && known[i] != fn) ++i;
+    if (i == 24 || !known[i]) {
       if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
           cudaSuccess)
         return BKMOO_ERR_CUDA;
-      if (i < 16) known[i] = fn;
+      if (i < 24) known[i] = fn;
     }
   }
   const int64_t units = sms / cg;

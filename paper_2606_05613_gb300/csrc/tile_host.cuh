@@ -25,10 +25,10 @@ inline bool languages_ok(const int64_t* rows, int32_t K, int64_t T) {
     if (rows[k + 1] < rows[k]) return false;
   return true;
 }
-// Widest store that 32-column pieces of every row allow (tile_gemm.cuh).
+// Widest store that 32-column pieces of every row allow (TileOut).
 inline int store_width(const void* p, int64_t ld, int elem) {
   const uintptr_t at = (uintptr_t)p | (uintptr_t)(ld * elem);
-  return (at & 31u) == 0 ? 32 : (at & 15u) == 0 ? 16 : 0;
+  return (at & 31u) == 0 ? 32 : (at & 15u) == 0 ? 16 : (at & 3u) == 0 ? 4 : 0;
 }
 
 // Map of a matrix (rows x cols bf16, rows of ld elements) read in boxes of 64
