@@ -142,7 +142,7 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int sms = 0, r = tile_sms(&sms);
   if (r != BKMOO_OK) return r;
-  if (T <= kFewRows) {
+  if (few_rows(T, D, F)) {
     const FewArgs q = {static_cast<const __nv_bfloat16*>(x), static_cast<const __nv_bfloat16*>(w_gate),
                        static_cast<const __nv_bfloat16*>(w_up), static_cast<__nv_bfloat16*>(h),
                        static_cast<__nv_bfloat16*>(a), static_cast<__nv_bfloat16*>(b), ldx, ldw, ldh,

@@ -1,6 +1,6 @@
 // The gated projections for a few rows of x (serving): h = act(x Wg^T) (x Wu^T).
 //
-// Bound by the weights' bytes, each of which is used for at most 8 rows: they go
+// Bound by the weights' bytes, each of which is used for at most 32 rows: they go
 // from memory straight into registers, 16 bytes a lane, with no stop in shared
 // memory, and warp-wide products (mma m16n8k16, fp32 sums) do the arithmetic: 16
 // weight rows, 8 of Wg over the same 8 of Wu, by 8 rows of x, so that a lane ends
@@ -27,7 +27,8 @@ constexpr int kFewAhead = 2;        // windows of a warp in flight
 // Warps of an SM.  2 windows ahead of 24 warps: 2048 -> 8192 13.7 us, 4096 -> 12288
 // 33.7 (4.9 and 5.97 TB/s); 4 of 16 13.1, 37.5; 2 of 32, which spills, 14.2, 36.6;
 // windows of 32, 64 bytes of a row at a time, 4 of 24 14.7, 34.7.
-constexpr int kFewResident = 24;
+// (x takes the registers of 8 of them from 9 rows on.)
+constexpr int few_resident(int nt) { return nt == 1 ? 24 : 16; }
 
 // Elements k to k + 7 of a row of D, zeros beyond its end.
 template <bool STREAM>
@@ -60,49 +61,58 @@ __device__ __forceinline__ void product16(float (&c)[4], uint32_t a0, uint32_t a
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// WARPS share the sum.
-template <int WARPS>
-__global__ void __launch_bounds__(32 * WARPS, kFewResident / WARPS) gate_few_kernel(const FewArgs p) {
+// WARPS share the sum; NT groups of 8 rows of x.
+template <int WARPS, int NT>
+__global__ void __launch_bounds__(32 * WARPS, few_resident(NT) / WARPS) gate_few_kernel(const FewArgs p) {
   grid_wait();
   const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const int f0 = blockIdx.x * 8;
-  const bool wlive = f0 + g < p.F, xlive = g < p.T;
+  const bool wlive = f0 + g < p.F;
   const __nv_bfloat16 *wg = p.wg + (int64_t)(wlive ? f0 + g : 0) * p.ldw,
-                      *wu = p.wu + (int64_t)(wlive ? f0 + g : 0) * p.ldw,
-                      *x = p.x + (int64_t)(xlive ? g : 0) * p.ldx;
+                      *wu = p.wu + (int64_t)(wlive ? f0 + g : 0) * p.ldw;
   const uint4 zero = make_uint4(0, 0, 0, 0);
   const int windows = (p.D + kFewWindow - 1) / kFewWindow;
-  uint4 ag[kFewAhead][2], au[kFewAhead][2], b[kFewAhead][2];
+  uint4 ag[kFewAhead][2], au[kFewAhead][2], b[kFewAhead][2][NT];
   auto fetch = [&](int i, int w) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int k = kFewWindow * w + 16 * q + 8 * h;
       ag[i][h] = wlive && w < windows ? load8<true>(wg, k, p.D) : zero;
       au[i][h] = wlive && w < windows ? load8<true>(wu, k, p.D) : zero;
-      b[i][h] = xlive && w < windows ? load8<false>(x, k, p.D) : zero;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        const int t = 8 * n + g;
+        b[i][h][n] = t < p.T && w < windows ? load8<false>(p.x + t * p.ldx, k, p.D) : zero;
+      }
     }
   };
 #pragma unroll
   for (int i = 0; i < kFewAhead; ++i) fetch(i, wid + i * WARPS);
-  float c[4] = {};
+  float c[NT][4] = {};
   for (int w0 = wid; w0 < windows; w0 += WARPS * kFewAhead) {
 #pragma unroll
     for (int i = 0; i < kFewAhead; ++i) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        product16(c, ag[i][h].x, au[i][h].x, ag[i][h].y, au[i][h].y, b[i][h].x, b[i][h].y);
-        product16(c, ag[i][h].z, au[i][h].z, ag[i][h].w, au[i][h].w, b[i][h].z, b[i][h].w);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          product16(c[n], ag[i][h].x, au[i][h].x, ag[i][h].y, au[i][h].y, b[i][h][n].x, b[i][h][n].y);
+          product16(c[n], ag[i][h].z, au[i][h].z, ag[i][h].w, au[i][h].w, b[i][h][n].z, b[i][h][n].w);
+        }
       }
       fetch(i, w0 + (i + kFewAhead) * WARPS);
     }
   }
-  __shared__ float part[WARPS][2][8][8];     // [a or b][row of x][column]
-  part[wid][0][2 * q][g] = c[0];
-  part[wid][0][2 * q + 1][g] = c[1];
-  part[wid][1][2 * q][g] = c[2];
-  part[wid][1][2 * q + 1][g] = c[3];
+  __shared__ float part[WARPS][2][8 * NT][8];     // [a or b][row of x][column]
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    part[wid][0][8 * n + 2 * q][g] = c[n][0];
+    part[wid][0][8 * n + 2 * q + 1][g] = c[n][1];
+    part[wid][1][8 * n + 2 * q][g] = c[n][2];
+    part[wid][1][8 * n + 2 * q + 1][g] = c[n][3];
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 64; i += 32 * WARPS) {
+  for (int i = threadIdx.x; i < 64 * NT; i += 32 * WARPS) {
     const int t = i >> 3, f = i & 7, col = f0 + f;
     float a = 0.0f, b = 0.0f;
 #pragma unroll
@@ -119,21 +129,27 @@ __global__ void __launch_bounds__(32 * WARPS, kFewResident / WARPS) gate_few_ker
   }
 }
 
+template <int NT>
+const void* few_fn(int warps) {
+  return warps == 1   ? (const void*)gate_few_kernel<1, NT>
+         : warps == 2 ? (const void*)gate_few_kernel<2, NT>
+         : warps == 4 ? (const void*)gate_few_kernel<4, NT>
+                      : (const void*)gate_few_kernel<8, NT>;
+}
+
 }  // namespace
 
 cudaError_t launch_gate_few(const FewArgs& p, int sms, cudaStream_t s) {
   const int units = (p.F + 7) / 8, windows = (p.D + kFewWindow - 1) / kFewWindow;
-  const int64_t most = (int64_t)sms * kFewResident;
+  const int nt = p.T <= 8 ? 1 : p.T <= 16 ? 2 : 4;
+  const int64_t most = (int64_t)sms * few_resident(nt);
   // (a warp keeps two windows at least)
   int warps = 1;
   while (warps < 8 && (int64_t)units * warps * 2 <= most && windows >= 4 * warps) warps *= 2;
-  const void* fn = warps == 1   ? (const void*)gate_few_kernel<1>
-                   : warps == 2 ? (const void*)gate_few_kernel<2>
-                   : warps == 4 ? (const void*)gate_few_kernel<4>
-                                : (const void*)gate_few_kernel<8>;
   FewArgs q = p;
   void* list[] = {&q};
-  return launch_behind(fn, dim3(units), dim3(32 * warps), list, 0, s, true);
+  return launch_behind(nt == 1 ? few_fn<1>(warps) : nt == 2 ? few_fn<2>(warps) : few_fn<4>(warps),
+                       dim3(units), dim3(32 * warps), list, 0, s, true);
 }
 
 }  // namespace bkmoo

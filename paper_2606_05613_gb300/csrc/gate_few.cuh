@@ -7,7 +7,14 @@
 
 namespace bkmoo {
 
-constexpr int kFewRows = 8;
+// Whether T rows are few (against the tile kernel, steady, us: 16 rows 1024 -> 2816 4.4
+// / 7.4, 2909 -> 2782 11.2 / 12.1, 2048 -> 8192 14.3 / 14.5, 4096 -> 12288 44 / 37; 32
+// rows 1024 -> 2816 5.9 / 7.4, 384 -> 9728 6.7 / 8.6, 2909 -> 2782 15.2 / 12.1, 2048 ->
+// 8192 18.3 / 14.5): every 8 columns read x again, so the more rows, the less weights.
+inline bool few_rows(int64_t T, int64_t D, int64_t F) {
+  const double weights = 4.0 * (double)D * (double)F;      // bytes
+  return T <= 8 || (T <= 16 && weights <= 70e6) || (T <= 32 && weights <= 20e6);
+}
 
 struct FewArgs {
   const __nv_bfloat16 *x, *wg, *wu;

@@ -85,7 +85,9 @@ def _forward_ref(x, wg, wu, act):
 SHAPES = [(1, 64, 128), (1, 8, 1), (1, 2048, 8192), (2, 200, 24), (3, 72, 41), (5, 1003, 300),
           (8, 512, 640), (9, 512, 640), (16, 136, 3), (17, 2048, 1000), (37, 1003, 2731), (64, 256, 512), (65, 264, 520),
           (127, 65, 129), (128, 64, 128), (129, 130, 257), (256, 1024, 512), (257, 520, 384),
-          (511, 192, 1152), (1000, 768, 2048)]
+          (511, 192, 1152), (1000, 768, 2048),
+          # few rows by the tiles: much weight
+          (9, 2304, 8192), (16, 2310, 8000), (17, 1100, 4700), (30, 1024, 5003)]
 
 
 @pytest.mark.parametrize("act", ACTS)
