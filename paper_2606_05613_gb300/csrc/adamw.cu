@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kBlock = 256;          // elements per scale, and per warp and turn
 constexpr int kAdamTable = 1024;     // tensors a launch knows
-constexpr int kAdamThreads = 128;
+constexpr int kAdamThreads = 256;
 constexpr int64_t kAdamWarps = kAdamThreads / 32;
 
 struct AdamArgs {
@@ -266,7 +266,7 @@ __device__ __forceinline__ uint32_t top_of(uint32_t t, float a, float b) {
 }
 
 template <class P, class G, bool E4M3, bool MASTER>
-__global__ void __launch_bounds__(kAdamThreads, E4M3 ? 6 : 7)
+__global__ void __launch_bounds__(kAdamThreads, 3)
     adamw_kernel(const __grid_constant__ AdamArgs a) {
   grid_wait();
   using S = typename State<E4M3>::T;

@@ -103,12 +103,12 @@ int weight_args(TileArgs<kWeight>& p, const void* const* dy, int64_t ld_dy, int 
   p.accumulate = accumulate;
   return BKMOO_OK;
 }
-// Whether some gradient's pieces are not whole aligned vectors (TileOut).
-bool turned(const TileArgs<kWeight>& p) {
-  bool r = p.cols % 32 != 0;
+int weight_mode(const TileArgs<kWeight>& p) {
+  bool whole = p.cols % 32 == 0;
   for (int k = 0; k < p.n_lang; ++k)
-    for (int i = 0; i < p.mats; ++i) r = r || p.vec[i * kMaxK + k] < 16;
-  return r;
+    for (int i = 0; i < p.mats; ++i) whole = whole && p.vec[i * kMaxK + k] >= 16;
+  if (p.out_dtype == BKMOO_F32) return whole ? kSums : kSumsTurned;
+  return !whole ? kTurned : p.accumulate ? kAdded : kPlain;
 }
 void weight_tiles(TileArgs<kWeight>& p, TileShape shape) {
   p.tiles_m = up(p.rows, kTileM * shape.cg);
@@ -246,7 +246,7 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     p.in.nkt = nkt / 2;
     p.in.tiles = p.in.tiles_m * p.in.tiles_n;
   }
-  return tile_launch(tile_both_fn(shape.cg, shape.bn, any && turned(p.w)), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
+  return tile_launch(tile_both_fn(shape.cg, shape.bn, any ? weight_mode(p.w) : kPlain), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
 }
 
 extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
@@ -269,5 +269,5 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   if (r != BKMOO_OK || !any) return r;
   const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, dw_dtype == BKMOO_F32, sms, nullptr);
   weight_tiles(p, shape);
-  return tile_launch(tile_weight_fn(shape.cg, shape.bn, turned(p)), shape, &p, p.tiles, s);
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn, weight_mode(p)), shape, &p, p.tiles, s);
 }

@@ -26,6 +26,13 @@
 
 namespace bkmoo {
 
+// How kWeight's results are written, a kernel each (one for all spills registers, 3.5 %
+// of the plain one's time and more of the others'): bf16 in whole aligned pieces; bf16
+// added to what is there, the same; bf16 in pieces that are not whole or not aligned;
+// fp32, whole and aligned or not.
+enum TileMode { kPlain = 0, kAdded = 1, kTurned = 2, kSums = 3, kSumsTurned = 4 };
+constexpr bool mode_f32(int mode) { return mode == kSums || mode == kSumsTurned; }
+constexpr bool mode_turned(int mode) { return mode == kTurned || mode == kSumsTurned; }
 enum TileKind { kGate = 0, kInput = 1, kWeight = 2, kBoth = 3 };
 
 constexpr int kTileM = 128;    // rows of a CTA's tile
@@ -200,34 +207,78 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&v)[32]
     }
   }
 }
-// The same of whole pieces (n = 32), added to what is there where `add`.
-__device__ __forceinline__ void put_row(__nv_bfloat16* p, float (&v)[32], int vec, bool add) {
-  if (add) {
-    const uint4* q = reinterpret_cast<const uint4*>(p);
+// A warp's 32 rows of COLS bf16 columns (w: this lane's row) to memory, of which the
+// first `rows` exist, all 16-byte aligned: through shared memory, 16 bytes a lane, so
+// that a store covers whole lines (8 or 4 lanes a row) instead of 32 bytes of 32 rows.
+// Chunks of 16 bytes lie at their place xor the row's, free of bank conflicts.
+template <int COLS>
+__device__ __forceinline__ void put_block(__nv_bfloat16* first, int64_t ld, const uint32_t (&w)[COLS / 2],
+                                          int rows, float* turn) {
+  constexpr int CH = COLS / 8;
+  const int lane = threadIdx.x & 31;
+  auto place = [](int row, int j) { return row * CH + (j ^ (CH == 8 ? row & 7 : (row >> 1) & 3)); };
+  uint4* t = reinterpret_cast<uint4*>(turn);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint4 x = q[j];
-      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  for (int j = 0; j < CH; ++j)
+    t[place(lane, j)] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+  __syncwarp();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[8 * j + 2 * i] += __uint_as_float(w[i] << 16);
-        v[8 * j + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
+  for (int k = 0; k < CH; ++k) {
+    const int row = (k * 32 + lane) / CH, j = lane % CH;
+    if (row < rows) *reinterpret_cast<uint4*>(first + row * ld + 8 * j) = t[place(row, j)];
   }
-  store_row(p, v, 32, vec);
+  __syncwarp();
 }
-__device__ __forceinline__ void put_row(float* p, float (&v)[32], int, bool add) {
-  float4* q = reinterpret_cast<float4*>(p);
+// The first n columns of one row of them.
+template <int W>
+__device__ __forceinline__ void put_some(__nv_bfloat16* p, const uint32_t (&w)[W], int n) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    float4 x = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-    if (add) {
-      const float4 y = q[j];
-      x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+  for (int j = 0; j < W / 4; ++j) {
+    if (n >= 8 * j + 8) {
+      reinterpret_cast<uint4*>(p)[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (8 * j + i < n)
+          p[8 * j + i] = __ushort_as_bfloat16((unsigned short)(w[4 * j + i / 2] >> (16 * (i & 1))));
     }
-    q[j] = x;
   }
+}
+// The same of 32 fp32 columns, rounded to T and added to what is there where `add`.
+__device__ __forceinline__ void put4(float* q, float4 x, bool add, float4 old) {
+  if (add) x.x += old.x, x.y += old.y, x.z += old.z, x.w += old.w;
+  *reinterpret_cast<float4*>(q) = x;
+}
+__device__ __forceinline__ void put4(__nv_bfloat16* q, float4 x, bool add, uint2 old) {
+  if (add) {
+    x.x += __uint_as_float(old.x << 16), x.y += __uint_as_float(old.x & 0xffff0000u);
+    x.z += __uint_as_float(old.y << 16), x.w += __uint_as_float(old.y & 0xffff0000u);
+  }
+  *reinterpret_cast<uint2*>(q) = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+}
+template <class T>
+__device__ __forceinline__ void put_sums(T* first, int64_t ld, const float (&v)[32], int rows, bool add,
+                                         float* turn) {
+  using Four = typename std::conditional<sizeof(T) == 4, float4, uint2>::type;
+  const int lane = threadIdx.x & 31, j = lane & 7;
+  float4* t = reinterpret_cast<float4*>(turn);
+  T* q = first + (lane >> 3) * ld + 4 * j;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    t[lane * 8 + (i ^ (lane & 7))] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  __syncwarp();
+  Four old[8];
+  if (add) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (4 * k + (lane >> 3) < rows) old[k] = *reinterpret_cast<const Four*>(q + 4 * k * ld);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const int row = 4 * k + (lane >> 3);
+    if (row < rows) put4(q + 4 * k * ld, t[row * 8 + (j ^ (row & 7))], add, old[k]);
+  }
+  __syncwarp();
 }
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -420,20 +471,17 @@ __device__ __forceinline__ void load_step(const TileArgs<KIND>& p, const Tile& t
   }
 }
 
-// A warp's 32 rows (this thread's: `row`) by 32 columns of a gradient.  TURN: not all
-// gradients' pieces are whole and aligned (a kernel of its own: the code for it takes
-// registers that cost the others 3.5 %).
-template <class T, bool TURN>
+// A warp's 32 rows (this thread's: `row`) by 32 columns of a gradient.
+template <class T, int MODE>
 __device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile& t, int row, int at,
                                           float (&v)[32], int n, float* turn) {
-  T* q = static_cast<T*>(p.out[t.g]) + (int64_t)row * p.cols + t.n0 + at;
-  if (!TURN || (p.vec[t.g] >= 16 && n >= 32)) {
-    if (row < p.rows) put_row(q, v, p.vec[t.g], p.accumulate);
+  const int lane = threadIdx.x & 31, rows = p.rows - (row - lane);
+  T* first = static_cast<T*>(p.out[t.g]) + (int64_t)(row - lane) * p.cols + t.n0 + at;
+  if (!mode_turned(MODE) || (p.vec[t.g] >= 16 && n >= 32)) {
+    put_sums(first, p.cols, v, rows, p.accumulate, turn);
     return;
   }
-  if constexpr (TURN) {
-    const int lane = threadIdx.x & 31, rows = p.rows - (row - lane);
-    T* first = q - (int64_t)lane * p.cols;
+  if constexpr (mode_turned(MODE)) {
 #pragma unroll
     for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
     __syncwarp();
@@ -452,7 +500,7 @@ __device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile
 // One warp's share of a finished tile: rows of its quarter, columns of its half.
 // `acc`: the accumulator's tensor-memory address for this warp's lanes; `empty`:
 // the tile's sum is empty and the accumulator was not written.
-template <int KIND, int BN, bool TURN>
+template <int KIND, int BN, int MODE>
 __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t, int row, int half,
                                           uint32_t acc, bool empty, float* turn,
                                           const float (*before)[32]) {
@@ -488,32 +536,63 @@ __device__ __forceinline__ void take_tile(const TileArgs<KIND>& p, const Tile& t
       __syncwarp();   // the loads are the whole warp's
     }
   } else {
-#pragma unroll(KIND == kWeight && BN <= 128 ? 2 : 1)
-    for (int c = 0; c < BN / 64; ++c) {
-      const int at = 32 * half + 64 * c, n = p.cols - (t.n0 + at);
-      uint32_t r[32];
-      if (!empty) {
-        tc_load32(r, acc + at);
-        tc_landed(r);
-      }
-      if (n > 0) {
-        float v[32];
+    // the half's columns, in pieces of 32; two at a time where they go out as bf16
+    // whole lines
+    __nv_bfloat16* block = nullptr;
+    int64_t ld = 0;
+    if constexpr (KIND == kInput) {
+      block = static_cast<__nv_bfloat16*>(p.out.p), ld = p.out.ld;
+    } else if constexpr (MODE == kPlain) {
+      block = static_cast<__nv_bfloat16*>(p.out[t.g]), ld = p.cols;
+    }
+    const int row0 = row - (int)(threadIdx.x & 31);
+    constexpr int WIDE = BN >= 128 ? 64 : 32;
+    if constexpr (KIND == kInput || MODE == kPlain) {
+#pragma unroll 1
+      for (int c = 0; c < BN / 2; c += WIDE) {
+        const int at = half * (BN / 2) + c, n = p.cols - (t.n0 + at);
+        if (n <= 0) break;
+        uint32_t w[WIDE / 2];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[j]);
-        if constexpr (KIND == kWeight && BN <= 128) {
-          if (before) {
+        for (int i = 0; i < WIDE / 32; ++i) {
+          uint32_t r[32];
+          if (!empty) {
+            tc_load32(r, acc + at + 32 * i);
+            tc_landed(r);
+          }
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            w[16 * i + j] = empty ? 0u : pack_bf16(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1]));
+        }
+        if (n >= WIDE) {
+          put_block<WIDE>(block + (int64_t)row0 * ld + t.n0 + at, ld, w, p.rows - row0, turn);
+        } else if (live) {
+          put_some(block + row * ld + t.n0 + at, w, n);
+        }
+        __syncwarp();
+      }
+    } else {
+#pragma unroll(mode_f32(MODE) ? 2 : 1)
+      for (int c = 0; c < BN / 64; ++c) {
+        const int at = half * (BN / 2) + 32 * c, n = p.cols - (t.n0 + at);
+        uint32_t r[32];
+        if (!empty) {
+          tc_load32(r, acc + at);
+          tc_landed(r);
+        }
+        if (n > 0 && !(empty && p.accumulate)) {
+          float v[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = empty ? 0.0f : __uint_as_float(r[j]);
+          if constexpr (mode_f32(MODE)) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += before[c][j];
           }
+          put_piece<typename std::conditional<mode_f32(MODE), float, __nv_bfloat16>::type, MODE>(
+              p, t, row, at, v, n, turn);
         }
-        if constexpr (KIND == kInput) {
-          if (live) store_bf16(p.out, row, t.n0 + at, v, n);
-        } else if (!(empty && p.accumulate)) {
-          if (p.out_dtype == BKMOO_BF16) put_piece<__nv_bfloat16, TURN>(p, t, row, at, v, n, turn);
-          else put_piece<float, TURN>(p, t, row, at, v, n, turn);
-        }
+        __syncwarp();   // the loads are the whole warp's
       }
-      __syncwarp();   // the loads are the whole warp's
     }
   }
 }
@@ -574,7 +653,7 @@ __device__ __forceinline__ bool multiply_tile(const TileArgs<KIND>& p, int i, Ri
 }
 
 // Warps 0 to 7: a finished tile to memory.
-template <int KIND, int CG, int BN, bool TURN>
+template <int KIND, int CG, int BN, int MODE>
 __device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingState& r,
                                            TileShared<CG, BN>& sh, float* turn, unsigned rank) {
   const int wid = threadIdx.x >> 5, lane = threadIdx.x & 31, quarter = wid & 3, half = wid >> 2;
@@ -596,40 +675,38 @@ __device__ __forceinline__ bool drain_tile(const TileArgs<KIND>& p, int i, RingS
     }
     ++r.n;
   };
-  if constexpr (KIND == kWeight && BN <= 128) {
-    if (t.nkt > t.span) {
-      float sum[BN / 64][32];
+  if constexpr (KIND == kWeight && mode_f32(MODE)) {
+    float sum[BN / 64][32];          // of the pieces but the last
 #pragma unroll
-      for (int c = 0; c < BN / 64; ++c)
+    for (int c = 0; c < BN / 64; ++c)
 #pragma unroll
-        for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
-      for (int k0 = 0; k0 + t.span < t.nkt; k0 += t.span) {
-        if (!wait()) return false;
-#pragma unroll
-        for (int c = 0; c < BN / 64; ++c) {
-          uint32_t v[32];
-          tc_load32(v, sh.tmem + lanes + (r.n & 1) * BN + 32 * half + 64 * c);
-          tc_landed(v);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
-        }
-        release();
-      }
+      for (int j = 0; j < 32; ++j) sum[c][j] = 0.0f;
+#pragma unroll 1
+    for (int k0 = 0; k0 + t.span < t.nkt; k0 += t.span) {
       if (!wait()) return false;
-      take_tile<KIND, BN, TURN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, false,
-                          turn + wid * (kTurnBytes / 4), sum);
+#pragma unroll
+      for (int c = 0; c < BN / 64; ++c) {
+        uint32_t v[32];
+        tc_load32(v, sh.tmem + lanes + (r.n & 1) * BN + half * (BN / 2) + 32 * c);
+        tc_landed(v);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
+      }
       release();
-      return true;
     }
+    if (t.nkt > 0 && !wait()) return false;
+    take_tile<KIND, BN, MODE>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
+                              turn + wid * (kTurnBytes / 4), sum);
+  } else {
+    if (t.nkt > 0 && !wait()) return false;
+    take_tile<KIND, BN, MODE>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
+                              turn + wid * (kTurnBytes / 4), nullptr);
   }
-  if (t.nkt > 0 && !wait()) return false;
-  take_tile<KIND, BN, TURN>(p, t, row, half, sh.tmem + lanes + (r.n & 1) * BN, t.nkt == 0,
-                      turn + wid * (kTurnBytes / 4), nullptr);
   if (t.nkt > 0) release();
   return true;
 }
 
-template <int KIND, int CG, int BN, bool TURN>
+template <int KIND, int CG, int BN, int MODE>
 __global__ void __launch_bounds__(kTileThreads, 1)
     tile_gemm_kernel(const __grid_constant__ TileArgs<KIND> p) {
   constexpr int S = tile_stages(CG, BN);
@@ -707,7 +784,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     }
   } else {
     each([&](auto kind, const auto& q, int i) {
-      return drain_tile<decltype(kind)::value, CG, BN, TURN>(q, i, r, sh, turn, rank);
+      return drain_tile<decltype(kind)::value, CG, BN, MODE>(q, i, r, sh, turn, rank);
     });
   }
   __syncwarp();
@@ -721,7 +798,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
 
 // The kernels, one translation unit each (nvcc runs them side by side).
 const void* tile_gate_fn(int cg, int bn);
-const void* tile_weight_fn(int cg, int bn, bool turn);
-const void* tile_both_fn(int cg, int bn, bool turn);
+const void* tile_weight_fn(int cg, int bn, int mode);
+const void* tile_both_fn(int cg, int bn, int mode);
 
 }  // namespace bkmoo

@@ -16,7 +16,7 @@ __device__ int32_t g_status;
 struct PerDevice {
   void* status = nullptr;
   int sms = 0;
-  const void* sized[24] = {};    // kernels whose shared-memory limit is raised
+  const void* sized[32] = {};    // kernels whose shared-memory limit is raised
 };
 std::mutex g_mu;
 PerDevice g_dev[kMaxDevices];
@@ -169,12 +169,12 @@ int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cuda
     std::lock_guard<std::mutex> lk(g_mu);
     const void** known = g_dev[dev].sized;
     int i = 0;
-    while (i < 24 && known[i] && known[i] != fn) ++i;
-    if (i == 24 || !known[i]) {
+    while (i < 32 && known[i] && known[i] != fn) ++i;
+    if (i == 32 || !known[i]) {
       if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
           cudaSuccess)
         return BKMOO_ERR_CUDA;
-      if (i < 24) known[i] = fn;
+      if (i < 32) known[i] = fn;
     }
   }
   const int64_t units = sms / cg;
