@@ -288,51 +288,46 @@ __device__ __forceinline__ void as_type(__nv_bfloat16* p, float x) { *p = __floa
 // The warp's 32 rows of 32 columns, of which the first `rows` and n exist, where they
 // are not aligned for wide vectors: turned in shared memory (turn: rows of 33 floats,
 // of which 32 are the piece's), so that the warp writes a row at a time, 32
-// neighbours, instead of one element of 32 rows (771 x 517 fp32 in 3 languages 37 us
-// so).
+// neighbours, instead of one element of 32 rows.  What they are added to is fetched 16
+// rows at a time.
 template <class T>
-static __device__ __noinline__ void put_turned(T* p, int64_t ld, int rows, int n, const float* turn) {
-  const int lane = threadIdx.x & 31;
-  if (lane < n) {
-#pragma unroll 8
-    for (int r = 0; r < 32; ++r) {
-      if (r >= rows) break;
-      as_type(p + r * ld + lane, turn[r * 33 + lane]);
-    }
-  }
-}
-// The same, added to what is there, which is fetched 16 rows at a time (6716 x 6034
-// bf16 in 4 languages, 4243 rows, row by row 1641 us, 361 so).
-template <class T>
-static __device__ __noinline__ void add_turned(T* p, int64_t ld, int rows, int n, const float* turn) {
-  const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void put_turned(T* p, int64_t ld, int rows, int n, bool add, const float* turn) {
+  const int lane = threadIdx.x & 31, here = lane < n ? rows : 0;
   T* q = p + lane;
+  turn += lane;
 #pragma unroll 1
-  for (int r0 = 0; r0 < 32; r0 += 16) {
+  for (int r0 = 0; r0 < 32; r0 += 16, q += 16 * ld, turn += 16 * 33) {
     T old[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (r0 + r < rows && lane < n) old[r] = q[(r0 + r) * ld];
+      if (add && r0 + r < here) old[r] = q[r * ld];
 #pragma unroll
     for (int r = 0; r < 16; ++r)
-      if (r0 + r < rows && lane < n)
-        as_type(q + (r0 + r) * ld, turn[(r0 + r) * 33 + lane] + as_float(old[r]));
+      if (r0 + r < here) as_type(q + r * ld, add ? turn[r * 33] + as_float(old[r]) : turn[r * 33]);
   }
 }
-// By pairs: two rows at a time, the upper lanes the second (ld is even).
-static __device__ __noinline__ void add_turned_pairs(__nv_bfloat16* p, int64_t ld, int rows, int n,
+// bf16 by pairs (4-byte aligned, ld and so n even): two rows at a time, the upper
+// lanes the second.
+__device__ __forceinline__ void put_turned_pairs(__nv_bfloat16* p, int64_t ld, int rows, int n, bool add,
                                                  const float* turn) {
-  const int lane = threadIdx.x & 31, up = lane >> 4, c = 2 * (lane & 15);
+  const int lane = threadIdx.x & 31, up = lane >> 4, c = 2 * (lane & 15), here = c < n ? rows - up : 0;
   uint32_t* q = reinterpret_cast<uint32_t*>(p + up * ld + c);
-  uint32_t old[16];
+  turn += up * 33 + c;
+#pragma unroll 1
+  for (int r0 = 0; r0 < 32; r0 += 16, q += 8 * ld, turn += 16 * 33) {
+    uint32_t old[8];
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
-    if (2 * r + up < rows && c < n) old[r] = q[r * ld];
+    for (int r = 0; r < 8; ++r)
+      if (add && r0 + 2 * r < here) old[r] = q[r * ld];
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
-    if (2 * r + up < rows && c < n)
-      q[r * ld] = pack_bf16(turn[(2 * r + up) * 33 + c] + __uint_as_float(old[r] << 16),
-                            turn[(2 * r + up) * 33 + c + 1] + __uint_as_float(old[r] & 0xffff0000u));
+    for (int r = 0; r < 8; ++r) {
+      if (r0 + 2 * r < here) {
+        float lo = turn[r * 66], hi = turn[r * 66 + 1];
+        if (add) lo += __uint_as_float(old[r] << 16), hi += __uint_as_float(old[r] & 0xffff0000u);
+        q[r * ld] = pack_bf16(lo, hi);
+      }
+    }
+  }
 }
 
 __device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int col,
@@ -485,13 +480,11 @@ __device__ __forceinline__ void put_piece(const TileArgs<kWeight>& p, const Tile
 #pragma unroll
     for (int j = 0; j < 32; ++j) turn[lane * 33 + j] = v[j];
     __syncwarp();
-    if (!p.accumulate) {
-      put_turned(first, p.cols, rows, n, turn);
-    } else if constexpr (sizeof(T) == 2) {
-      if (p.vec[t.g] != 0) add_turned_pairs(first, p.cols, rows, n, turn);
-      else add_turned(first, p.cols, rows, n, turn);
+    if constexpr (sizeof(T) == 2) {
+      if (p.vec[t.g] != 0) put_turned_pairs(first, p.cols, rows, n, p.accumulate, turn);
+      else put_turned(first, p.cols, rows, n, p.accumulate, turn);
     } else {
-      add_turned(first, p.cols, rows, n, turn);
+      put_turned(first, p.cols, rows, n, p.accumulate, turn);
     }
     __syncwarp();
   }

@@ -370,3 +370,38 @@ def test_same_bits_again_on_streams_and_in_a_graph():
     torch.cuda.synchronize()
     for o in outs + [o]:
         assert all(torch.equal(o[k], first[k]) for k in first if k != "ws")
+
+
+# Sums of bf16 whose rows are on 4 bytes or less, at each width of tile; the first ones
+# ended in a fault of the GPU while results were written by functions that were called.
+@pytest.mark.parametrize("T,M,N,K", [(2174, 288, 2450, 8), (300, 288, 2450, 8), (700, 650, 534, 16), (2100, 900, 1030, 4),
+                                     (90, 100, 2451, 2), (4000, 1031, 1533, 2)])
+def test_added_weight_gradients_call_after_call(T, M, N, K):
+    """Bounds that change from call to call, an empty language among them, with nothing
+    between the calls: every sum is right, and the same calls give the same bits."""
+    gen = torch.Generator(device=DEV).manual_seed(T + M + N)
+    dy, x = _mat(gen, T, M, 0.1), _mat(gen, T, N)
+    rng = np.random.default_rng(T)
+    bounds = []
+    for k in range(3):
+        inner = np.sort(rng.integers(0, T + 1, K - 1))
+        inner[k % (K - 1)] = inner[k % (K - 1) - 1] if k % (K - 1) else 0
+        bounds.append([0] + [int(i) for i in inner] + [T])
+    for rows in bounds:
+        ref, err = _wgrad_ref(dy, x, rows)
+        _, dw, _ = _grads(K, M, N, torch.bfloat16, False, fill=0.75)
+        bk.bkmoo_language_wgrad(dy, x, rows, dw, accumulate=True)
+        for k in range(K):
+            total = ref[k] + 0.75
+            _check(dw[k], total, HALF * total.abs() + 1.02 * err[k] + 2.0 ** -23 * total.abs(), ("sum", k))
+    twice = []
+    for _ in range(2):
+        flat, dw, at = _grads(K, M, N, torch.bfloat16, False, fill=0.75)
+        for i in range(60):
+            bk.bkmoo_language_wgrad(dy, x, bounds[i % 3], dw, accumulate=True)
+        for f in flat:
+            assert bool((f[:at] == 5).all()) and bool((f[at + M * N:] == 5).all())
+        twice.append([w.clone() for w in dw])
+    for u, v in zip(*twice):
+        assert torch.equal(u, v)
+    assert bk.bkmoo_op_status(DEV) == 0
