@@ -92,27 +92,28 @@ int tile_status_word(cudaStream_t s, int32_t** word) {
   return BKMOO_OK;
 }
 
-// Time of a tile (us) from three sweeps on GB300 (forward 9 to 4000 rows, input
-// gradient 16 to 4000, weight gradients of 64 to 8192 rows in 1 and 4 languages,
-// widths 256 to 12288): a step of the sum where the SMs are full, a tile's way to
-// memory (under the next tile's sum if that is longer), and a launch with its first
-// and last tile.  Measured against the rule, us (64 / 128 / 256 columns / pair of
-// 256): forward 2048 -> 8192, 64 rows 18.7 / 17.0 / 18.5 / 18.5, 2000 rows 156 /
-// 109 / 94 / 79; 4096 -> 12288, 64 rows 42.5 / 42.8 / 37.4 / 48.9; input gradient
-// 768 <- 2048, 1000 rows 17.8 / 18.1 / 26.1 / 26.6, 4000 rows 48 / 38 / 36 / 35;
-// weight gradient 2048 x 768, 4 languages of 256 rows 11.3 / 8.6 / 9.1 / 10.9, of
-// 2048 36 / 22 / 25 / 25.
+// Time of a tile (us) from sweeps on GB300 (forward 9 to 4000 rows, input gradient 16
+// to 4000, weight gradients of 16 to 8192 rows in 1, 4 and 8 languages, widths 256 to
+// 12288): a step of the sum where the SMs are full, a tile's way to memory (under the
+// next tile's sum if that is longer), and a launch with its first and last tile.  What
+// the shapes take, us (64 / 128 / 256 columns / pair of 256): forward 2048 -> 8192, 64
+// rows 18.7 / 17.0 / 18.5 / 18.5, 2000 rows 156 / 109 / 94 / 79; 4096 -> 12288, 64 rows
+// 42.5 / 42.8 / 37.4 / 48.9; input gradient 768 <- 2048, 1000 rows 17.8 / 18.1 / 26.1 /
+// 26.6, 4000 rows 48 / 38 / 36 / 35; weight gradient 2048 x 768, 4 languages of 128 rows
+// 8.0 / 6.7 / 7.1 / 9.2, of 2048 37 / 23 / 25 / 25; 8192 x 2048, 8 languages of 64 rows 96
+// / 66 / 47 / 70, of 1024 341 / 203 / 179 / 157.
 struct TileCost {
   TileShape s;
   double step, out, launch;
 };
-constexpr TileCost kCosts[4] = {{{1, 64}, 0.165, 0.8, 4.0},
-                                {{1, 128}, 0.217, 1.2, 4.7},
-                                {{1, 256}, 0.376, 2.2, 5.8},
-                                {{2, 256}, 0.320, 2.9, 7.0}};
+constexpr TileCost kCosts[4] = {{{1, 64}, 0.165, 0.85, 3.5},
+                                {{1, 128}, 0.217, 1.15, 3.7},
+                                {{1, 256}, 0.360, 1.70, 4.6},
+                                {{2, 256}, 0.320, 2.40, 6.0}};
 // fp32 results, whose sums are taken in pieces (a pair of 128 columns was no faster
-// than one CTA's anywhere: 8192 x 2048, 16384 rows 444 us, 425).
-constexpr TileCost kExactCosts[2] = {{{1, 64}, 0.190, 1.55, 4.0}, {{1, 128}, 0.234, 3.5, 4.7}};
+// than one CTA's anywhere: 8192 x 2048, 16384 rows 444 us, 425).  8192 x 2048, 8 languages
+// of 64 rows 133 / 141, of 1024 372 / 269.
+constexpr TileCost kExactCosts[2] = {{{1, 64}, 0.190, 1.2, 3.6}, {{1, 128}, 0.237, 2.5, 5.1}};
 // Tiles of a set, and the mean and the longest time of one.
 struct SetCost {
   int64_t tiles = 0;
