@@ -150,7 +150,7 @@ extern "C" int bkmoo_gate_forward(const void* x, int64_t ldx, const void* w_gate
     return launch_gate_few(q, sms, s) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
   }
   const int32_t nkt = up(D, kTileK);
-  const TileShape shape = tile_shape({T, F, true, &nkt, 1, 1}, nullptr, false, sms, nullptr);
+  const TileShape shape = tile_shape({T, F, true, &nkt, 1, 1}, nullptr, kPlain, sms, nullptr);
   TileArgs<kGate> p = {};
   r = tile_status_word(s, &p.status);
   if (r == BKMOO_OK) r = tile_map(&p.a, x, T, D, ldx, kTileM);
@@ -227,9 +227,9 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
   if (!input && !any) return BKMOO_OK;
   const int32_t nkt = 2 * up(F, kTileK);
   const TileSet in = {T, D, false, &nkt, 1, 1}, w = {F, D, false, p.w.nkt, K, 2};
-  const bool exact = any && dw_dtype == BKMOO_F32;
-  const TileShape shape = input ? tile_shape(in, any ? &w : nullptr, exact, sms, &p.head_start)
-                                : tile_shape(w, nullptr, exact, sms, nullptr);
+  const int mode = any ? weight_mode(p.w) : kPlain;
+  const TileShape shape = input ? tile_shape(in, any ? &w : nullptr, mode, sms, &p.head_start)
+                                : tile_shape(w, nullptr, mode, sms, nullptr);
   if (any) weight_tiles(p.w, shape);
   if (input) {
     const void* m[2] = {w_gate, w_up};
@@ -246,7 +246,8 @@ extern "C" int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a,
     p.in.nkt = nkt / 2;
     p.in.tiles = p.in.tiles_m * p.in.tiles_n;
   }
-  return tile_launch(tile_both_fn(shape.cg, shape.bn, any ? weight_mode(p.w) : kPlain), shape, &p, (int64_t)p.in.tiles + p.w.tiles, s);
+  return tile_launch(tile_both_fn(shape.cg, shape.bn, mode), shape, &p,
+                     (int64_t)p.in.tiles + p.w.tiles, s);
 }
 
 extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t ldx,
@@ -267,7 +268,8 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   bool any = false;
   r = weight_args(p, &dy, ld_dy, 1, x, ldx, M, N, K, rows, &dw, dw_dtype, accumulate, &any);
   if (r != BKMOO_OK || !any) return r;
-  const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, dw_dtype == BKMOO_F32, sms, nullptr);
+  const int mode = weight_mode(p);
+  const TileShape shape = tile_shape({M, N, false, p.nkt, K, 1}, nullptr, mode, sms, nullptr);
   weight_tiles(p, shape);
-  return tile_launch(tile_weight_fn(shape.cg, shape.bn, weight_mode(p)), shape, &p, p.tiles, s);
+  return tile_launch(tile_weight_fn(shape.cg, shape.bn, mode), shape, &p, p.tiles, s);
 }

@@ -130,10 +130,15 @@ SetCost set_cost(const TileSet& s, const TileCost& c) {
   }
   return r;
 }
-TileShape tile_shape(const TileSet& a, const TileSet* b, bool exact, int sms, int32_t* head_start) {
+// Sums taken in pieces (kExactSteps) have shapes of their own.  bf16 gradients that are
+// turned take 128 columns at most: a kernel of 256 that wrote such gradients ended in a
+// fault of the GPU whose cause was not found, so there is none.
+TileShape tile_shape(const TileSet& a, const TileSet* b, int mode, int sms, int32_t* head_start) {
+  const bool exact = mode_f32(mode);
+  const int shapes = exact || mode == kTurned ? 2 : 4;
   TileShape best = kCosts[0].s;
   double least = 0.0;
-  for (int i = 0; i < (exact ? 2 : 4); ++i) {
+  for (int i = 0; i < shapes; ++i) {
     const TileCost& c = exact ? kExactCosts[i] : kCosts[i];
     const int64_t units = sms / c.s.cg;
     const SetCost x = set_cost(a, c);

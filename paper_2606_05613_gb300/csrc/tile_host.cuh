@@ -50,9 +50,9 @@ struct TileSet {
   const int32_t* nkt;
   int groups, mats;
 };
-// The shape for one set, or two in turn, and the second's head start (Walk).  exact:
-// sums are taken in pieces (kExactSteps).
-TileShape tile_shape(const TileSet& a, const TileSet* b, bool exact, int sms, int32_t* head_start);
+// The shape for one set, or two in turn, and the second's head start (Walk); mode: how
+// weight gradients are written (TileMode).
+TileShape tile_shape(const TileSet& a, const TileSet* b, int mode, int sms, int32_t* head_start);
 // Queues a tile kernel over `tiles` tiles.
 int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s);
 

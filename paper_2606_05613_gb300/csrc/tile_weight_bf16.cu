@@ -5,18 +5,22 @@
 namespace bkmoo {
 namespace {
 
-template <int MODE>
-const void* fn(int cg, int bn) {
-  if (cg == 2) return (const void*)tile_gemm_kernel<kWeight, 2, 256, MODE>;
-  if (bn == 256) return (const void*)tile_gemm_kernel<kWeight, 1, 256, MODE>;
-  if (bn == 128) return (const void*)tile_gemm_kernel<kWeight, 1, 128, MODE>;
-  return (const void*)tile_gemm_kernel<kWeight, 1, 64, MODE>;
+// (of 128 columns at most where results are turned: tile_shape)
+const void* added_fn(int cg, int bn) {
+  if (cg == 2) return (const void*)tile_gemm_kernel<kWeight, 2, 256, kAdded>;
+  if (bn == 256) return (const void*)tile_gemm_kernel<kWeight, 1, 256, kAdded>;
+  if (bn == 128) return (const void*)tile_gemm_kernel<kWeight, 1, 128, kAdded>;
+  return (const void*)tile_gemm_kernel<kWeight, 1, 64, kAdded>;
+}
+const void* turned_fn(int bn) {
+  return bn == 128 ? (const void*)tile_gemm_kernel<kWeight, 1, 128, kTurned>
+                   : (const void*)tile_gemm_kernel<kWeight, 1, 64, kTurned>;
 }
 
 }  // namespace
 
 const void* tile_weight_bf16_fn(int cg, int bn, bool turned) {
-  return turned ? fn<kTurned>(cg, bn) : fn<kAdded>(cg, bn);
+  return turned ? turned_fn(bn) : added_fn(cg, bn);
 }
 
 }  // namespace bkmoo

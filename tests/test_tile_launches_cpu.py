@@ -1,0 +1,84 @@
+"""CPU: which kernels a gate or weight-gradient call launches: csrc/gate.cu and
+csrc/tile_host.cu linked against a runtime that launches nothing and notes what it
+was asked for (fake_tiles_runtime.cpp, fake_tiles.cu).  152 SMs."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+from paper_2606_05613_gb300 import build as nb
+from paper_2606_05613_gb300 import native as bk
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+F32, BF16 = bk.BKMOO_F32, bk.BKMOO_BF16
+P = 1 << 40                       # an aligned address, never touched
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    d = tmp_path_factory.mktemp("fake_tiles")
+    objs = []
+    for src in (os.path.join(nb.CSRC, "gate.cu"), os.path.join(nb.CSRC, "tile_host.cu"),
+                os.path.join(HERE, "fake_tiles.cu"), os.path.join(HERE, "fake_tiles_runtime.cpp")):
+        objs.append(str(d / (os.path.basename(src) + ".o")))
+        subprocess.run([nb.nvcc()] + nb.ARCH + ["-I", nb.INCLUDE, "-I", nb.CSRC, "-std=c++17", "-Xcompiler", "-fPIC",
+                                                "--expt-relaxed-constexpr", "-c", src, "-o", objs[-1]], check=True)
+    so = str(d / "libfaketiles.so")
+    subprocess.run(["g++", "-shared", "-Wl,-Bsymbolic", "-o", so] + objs + ["-lpthread"], check=True)
+    lib = ctypes.CDLL(so)
+    lib.fake_notes.restype = ctypes.c_char_p
+    return lib
+
+
+def _launches(lib, call, *args):
+    """(return code, kernels launched) of a call."""
+    lib.fake_reset(0)
+    code = call(*args)
+    return code, [n for n in lib.fake_notes().decode().split() if not n.startswith("room:")]
+
+
+def _up(n):
+    return (n + 7) // 8 * 8
+
+
+def _even(T, K):
+    return (ctypes.c_int64 * (K + 1))(*[T * k // K for k in range(K + 1)])
+
+
+def _places(K, at):
+    return (ctypes.c_void_p * K)(*[P + (k << 36) + at for k in range(K)])
+
+
+I64 = ctypes.c_int64
+
+
+def _wgrad(lib, T, M, N, K, dtype, at=0, accumulate=0, rows=None):
+    return _launches(lib, lib.bkmoo_language_wgrad, ctypes.c_void_p(P), I64(_up(M)), ctypes.c_void_p(P), I64(_up(N)),
+                     I64(T), I64(M), I64(N), K, rows or _even(T, K), _places(K, at), dtype, accumulate, None)
+
+
+def _backward(lib, T, D, F, K, dtype, at=0, accumulate=0, dx=True, rows=None):
+    return _launches(lib, lib.bkmoo_gate_backward, ctypes.c_void_p(P), I64(_up(F)), ctypes.c_void_p(P), ctypes.c_void_p(P),
+                     I64(_up(F)), ctypes.c_void_p(P), I64(_up(D)), ctypes.c_void_p(P), ctypes.c_void_p(P), I64(_up(D)),
+                     I64(T), I64(D), I64(F), 0, K, rows or _even(T, K), ctypes.c_void_p(P if dx else 0), I64(_up(D)),
+                     _places(K, at), _places(K, at), dtype, accumulate, ctypes.c_void_p(P), ctypes.c_size_t(1 << 50), None)
+
+
+# bf16 gradients that are not whole or not aligned, from a few rows in many languages to
+# more than the card holds
+TURNED = [(2174, 288, 2450, 8), (300, 288, 2450, 8), (700, 650, 534, 16), (2100, 900, 1030, 4), (90, 100, 2451, 2),
+          (4000, 1031, 1533, 2), (649, 6178, 534, 16), (4243, 6716, 6034, 4), (16384, 8191, 8190, 1), (8192, 8192, 8192, 16)]
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("T,M,N,K", TURNED)
+def test_unaligned_bf16_gradients_take_at_most_128_columns(fake, T, M, N, K, accumulate):
+    """The kernels of 256 columns that write such gradients do not exist: one of them ended
+    in a fault of the GPU whose cause was not found."""
+    allowed = {"1x64-turned", "1x128-turned"}
+    code, names = _wgrad(fake, T, M, N, K, BF16, at=2 if N % 32 == 0 else 0, accumulate=accumulate)
+    assert code == 0 and len(names) == 1 and names[0][len("weight-"):] in allowed
+    for dx in (False, True):
+        code, names = _backward(fake, T, N, M, K, BF16, at=2 if N % 32 == 0 else 0, accumulate=accumulate, dx=dx)
+        assert code == 0 and names[0] == "pass" and len(names) == 2 and names[1][len("both-"):] in allowed
