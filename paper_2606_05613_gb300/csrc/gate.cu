@@ -107,7 +107,8 @@ int weight_mode(const TileArgs<kWeight>& p) {
   bool whole = p.cols % 32 == 0;
   for (int k = 0; k < p.n_lang; ++k)
     for (int i = 0; i < p.mats; ++i) whole = whole && p.vec[i * kMaxK + k] >= 16;
-  if (p.out_dtype == BKMOO_F32) return whole ? kSums : kSumsTurned;
+  if (p.out_dtype == BKMOO_F32)
+    return whole ? (p.accumulate ? kSumsAdded : kSums) : p.accumulate ? kSumsTurnedAdded : kSumsTurned;
   return !whole ? kTurned : p.accumulate ? kAdded : kPlain;
 }
 void weight_tiles(TileArgs<kWeight>& p, TileShape shape) {

@@ -12,6 +12,11 @@ const void* fn(int bn) {
 
 }  // namespace
 
-const void* tile_both_f32_fn(int bn, bool turned) { return turned ? fn<kSumsTurned>(bn) : fn<kSums>(bn); }
+const void* tile_both_f32_fn(int bn, int mode) {
+  return mode == kSums         ? fn<kSums>(bn)
+         : mode == kSumsAdded  ? fn<kSumsAdded>(bn)
+         : mode == kSumsTurned ? fn<kSumsTurned>(bn)
+                               : fn<kSumsTurnedAdded>(bn);
+}
 
 }  // namespace bkmoo

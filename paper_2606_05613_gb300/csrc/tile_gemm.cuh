@@ -28,11 +28,19 @@ namespace bkmoo {
 
 // How kWeight's results are written, a kernel each (one for all spills registers, 3.5 %
 // of the plain one's time and more of the others'): bf16 in whole aligned pieces; bf16
-// added to what is there, the same; bf16 in pieces that are not whole or not aligned;
-// fp32, whole and aligned or not.
-enum TileMode { kPlain = 0, kAdded = 1, kTurned = 2, kSums = 3, kSumsTurned = 4 };
-constexpr bool mode_f32(int mode) { return mode == kSums || mode == kSumsTurned; }
-constexpr bool mode_turned(int mode) { return mode == kTurned || mode == kSumsTurned; }
+// added to what is there, the same; bf16 in pieces that are not whole or not aligned,
+// added or not; fp32, whole and aligned or not, and each of them added or not.
+enum TileMode {
+  kPlain = 0, kAdded = 1, kTurned = 2, kSums = 3, kSumsTurned = 4, kSumsAdded = 5, kSumsTurnedAdded = 6
+};
+constexpr bool mode_f32(int mode) { return mode >= kSums; }
+constexpr bool mode_turned(int mode) {
+  return mode == kTurned || mode == kSumsTurned || mode == kSumsTurnedAdded;
+}
+// Kernels that fetch ahead what they add to (fetch_tile).
+constexpr bool mode_ahead(int mode) {
+  return mode == kAdded || mode == kSumsAdded || mode == kSumsTurnedAdded;
+}
 enum TileKind { kGate = 0, kInput = 1, kWeight = 2, kBoth = 3 };
 
 constexpr int kTileM = 128;    // rows of a CTA's tile
@@ -647,11 +655,14 @@ __device__ __forceinline__ bool multiply_tile(const TileArgs<KIND>& p, int i, Ri
 
 // What a tile's results are added to, towards the L2: this warp's rows, ahead of the
 // tile before it, whose writing covers the way from memory.  16 languages of 40 rows,
-// 6178 x 544: bf16 80 us without, 67 so, fp32 109 and 97 (28 and 62 with nothing to add
-// to); 6178 x 534, not aligned, 135 and 116, 161 and 143.
+// 6178 x 544: bf16 80 us without, 67 to 72 so, fp32 107 and 97; fp32 6178 x 534, not
+// aligned, 158 and 142.  Not in kernels that need not add, whose registers it costs: fp32
+// with nothing to add to 59 us without it, 62 with it; nor for turned bf16, where adding
+// gains little or nothing (6178 x 534 121 us without, 117 with it; 533 wide 111, 121;
+// 6716 x 6034 402, 407) and 533 wide with nothing to add to takes 81 us instead of 71.
 template <int BN, int CG>
 __device__ __forceinline__ void fetch_tile(const TileArgs<kWeight>& p, int i, unsigned rank) {
-  if (!p.accumulate || i >= p.tiles) return;
+  if (i >= p.tiles) return;
   const Tile t = tile_at<kWeight, CG, BN>(p, i);
   const int wid = threadIdx.x >> 5;
   const int row = t.m0 + (int)rank * kTileM + (wid & 3) * 32 + (threadIdx.x & 31);
@@ -810,7 +821,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
     each([&](auto kind, const auto& q, int i) {
       return drain_tile<decltype(kind)::value, CG, BN, MODE>(q, i, r, sh, turn, rank);
     }, [&](const auto& q, int i) {
-      if constexpr (MODE != kPlain) fetch_tile<BN, CG>(q, i, rank);
+      if constexpr (mode_ahead(MODE)) fetch_tile<BN, CG>(q, i, rank);
       __syncwarp();
     });
   }

@@ -8,7 +8,7 @@
 
 void note(const char* what);
 
-static char tables[4][3][257][5];      // [kind][CTAs][columns][mode]: the kernels' addresses
+static char tables[4][3][257][7];      // [kind][CTAs][columns][mode]: the kernels' addresses
 
 std::string name_of(const void* fn) {
   const char* p = static_cast<const char*>(fn);
@@ -16,9 +16,10 @@ std::string name_of(const void* fn) {
   if (p < first || p >= first + sizeof(tables)) return "pass";
   const int64_t i = p - first;
   static const char* kinds[] = {"gate", "input", "weight", "both"};
-  static const char* modes[] = {"plain", "added", "turned", "sums", "sums-turned"};
-  return std::string(kinds[i / (3 * 257 * 5)]) + "-" + std::to_string(i / (257 * 5) % 3) + "x" +
-         std::to_string(i / 5 % 257) + "-" + modes[i % 5];
+  static const char* modes[] = {"plain", "added", "turned", "sums", "sums-turned", "sums-added",
+                                "sums-turned-added"};
+  return std::string(kinds[i / (3 * 257 * 7)]) + "-" + std::to_string(i / (257 * 7) % 3) + "x" +
+         std::to_string(i / 7 % 257) + "-" + modes[i % 7];
 }
 
 namespace bkmoo {

@@ -82,3 +82,22 @@ def test_unaligned_bf16_gradients_take_at_most_128_columns(fake, T, M, N, K, acc
     for dx in (False, True):
         code, names = _backward(fake, T, N, M, K, BF16, at=2 if N % 32 == 0 else 0, accumulate=accumulate, dx=dx)
         assert code == 0 and names[0] == "pass" and len(names) == 2 and names[1][len("both-"):] in allowed
+
+
+@pytest.mark.parametrize("T,M,N,K,at,modes", [
+    (1024, 512, 544, 4, 0, ("sums", "sums-added", "plain", "added")),
+    (1024, 512, 545, 4, 0, ("sums-turned", "sums-turned-added", "turned", "turned")),
+    (1024, 512, 544, 4, 4, ("sums-turned", "sums-turned-added", "turned", "turned")),
+    (700, 1, 300, 2, 0, ("sums-turned", "sums-turned-added", "turned", "turned")),
+])
+def test_kernels_that_add_are_kernels_of_their_own(fake, T, M, N, K, at, modes):
+    """What fetches ahead the gradients that it adds to costs nothing where nothing is
+    added; bf16 gradients that are turned have one kernel for both, without it."""
+    want = iter(modes)
+    for dtype in (F32, BF16):
+        for accumulate in (0, 1):
+            mode = next(want)
+            code, names = _wgrad(fake, T, M, N, K, dtype, at=at, accumulate=accumulate)
+            assert code == 0 and [n.split("-", 2)[2] for n in names] == [mode]
+            code, names = _backward(fake, T, N, M, K, dtype, at=at, accumulate=accumulate)
+            assert code == 0 and [n.split("-", 2)[2] for n in names[1:]] == [mode]
