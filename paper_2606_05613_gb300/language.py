@@ -9,13 +9,15 @@ has the batch's rows from rows[k] to rows[k + 1].
 
 Inside BucketMOO.begin_batch() ... finish() the gradients are added to the
 parameters' `language_grads`, their places in the K flat buffers; outside, the
-layers' weights receive the ordinary gradient of the whole batch.  Weights and
+layers' weights receive the ordinary gradient of the whole batch.  The gradients
+have no graph: gradients of gradients are refused.  Weights and
 activations are bfloat16 on a GPU; the products that no language splits
 (y = x W^T and its dx of LanguageLinear) are torch's.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import native
 
@@ -61,6 +63,7 @@ class _Gate(torch.autograd.Function):
         return h.view(*lead, F) if len(lead) != 1 else h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dh):
         m, w_gate, w_up, a, b = ctx.saved_tensors
         T, D = m.shape
@@ -85,6 +88,7 @@ class _Linear(torch.autograd.Function):
         return torch.matmul(x, weight.t())
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight = ctx.saved_tensors
         dx = torch.matmul(dy, weight) if ctx.needs_input_grad[0] else None
