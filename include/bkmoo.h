@@ -455,7 +455,8 @@ int bkmoo_gate_backward_workspace_size(int64_t T, int64_t F, size_t* bytes);
  * da and db, the operands of bf16 products, are rounded to bf16 between; fp32
  * gradients are the unrounded fp32 sums of those.  ws: device, 256-byte
  * aligned, ws_bytes >= bkmoo_gate_backward_workspace_size, not shared by calls
- * that overlap.
+ * that overlap; the call leaves da there, and db from half of the workspace size
+ * on, as [T][F] with rows of F rounded up to 8.
  */
 int bkmoo_gate_backward(const void* dh, int64_t ld_dh, const void* a, const void* b, int64_t ld_ab,
                         const void* x, int64_t ldx, const void* w_gate, const void* w_up,

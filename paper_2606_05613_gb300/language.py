@@ -67,17 +67,31 @@ class _Gate(torch.autograd.Function):
     def backward(ctx, dh):
         m, w_gate, w_up, a, b = ctx.saved_tensors
         T, D = m.shape
+        F = w_gate.shape[0]
         dx = _room(m, T, D) if ctx.needs_input_grad[0] else None
-        weights = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
-        dg = du = whole_g = whole_u = rows = None
-        if weights:
-            dg, rows, whole_g = _languages(w_gate, ctx.rows, T)
-            du, _, whole_u = _languages(w_up, ctx.rows, T)
-        native.bkmoo_gate_backward(_on_rows(dh), a, b, m, _on_rows(w_gate), _on_rows(w_up), ctx.act,
-                                   rows if weights else [0, T], dx, dg, du, accumulate=True)
+        dh, g, u = _on_rows(dh), _on_rows(w_gate), _on_rows(w_up)
+        # [places, bounds, gradient of the whole batch or None] of the weights that are trained
+        to = [_languages(w, ctx.rows, T) if need else None
+              for w, need in zip((w_gate, w_up), ctx.needs_input_grad[1:3])]
+        if all(to) and (to[0][2] is None) == (to[1][2] is None):
+            native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, to[0][1], dx, to[0][0], to[1][0],
+                                       accumulate=True)
+        elif not any(to):
+            native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, [0, T], dx)
+        else:
+            # one of them is frozen, or they are apart by different bounds: da and db, which
+            # the call leaves in its workspace, and each weight's gradients from its own
+            ws = m.new_empty(native.bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8)
+            native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, [0, T],
+                                       dx if dx is not None else _room(m, T, D), ws=ws)
+            ld, half = (F + 7) // 8 * 8, ws.numel() // 2
+            for i, place in enumerate(to):
+                if place is not None:
+                    d = ws[i * half:i * half + T * ld * 2].view(torch.bfloat16).view(T, ld)[:, :F]
+                    native.bkmoo_language_wgrad(d, m, place[1], place[0], accumulate=True)
         if dx is not None:
             dx = dx.reshape(*ctx.lead, D)
-        return dx, whole_g, whole_u, None, None
+        return (dx, *(t[2] if t is not None else None for t in to), None, None)
 
 
 class _Linear(torch.autograd.Function):

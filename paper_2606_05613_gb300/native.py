@@ -487,7 +487,7 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
     language k (rows[k] to rows[k + 1] of the batch) its own dw_gate[k], dw_up[k]
     (contiguous [F, D], float32 or bfloat16; both lists may be None).  ws: a CUDA
     byte tensor of bkmoo_gate_backward_workspace_size; allocated (torch, on
-    `stream`) where None."""
+    `stream`) where None; the call leaves da and db in its halves (bkmoo.h)."""
     import torch
     bf16 = torch.bfloat16
     T, D, dev = _cuda_matrix(x, "x")

@@ -3,7 +3,8 @@ stand in for here."""
 import pytest
 import torch
 
-from paper_2606_05613_gb300 import language, native
+from paper_2606_05613_gb300 import build as nb
+from paper_2606_05613_gb300 import native
 from paper_2606_05613_gb300.language import GatedFeedForward, LanguageLinear
 
 
@@ -55,6 +56,11 @@ def _language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
     _store(dw, _by_language(dy.float(), x.float(), rows), accumulate)
 
 
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    nb.build()
+
+
 @pytest.fixture(autouse=True)
 def _plain(monkeypatch):
     monkeypatch.setattr(native, "bkmoo_gate_forward", _gate_forward)
@@ -91,3 +97,62 @@ def test_layers_give_the_gradients_of_the_formula():
     for g, r in zip(got, ref):
         # at most eight bf16 roundings behind one another, 2^-9 each in the 2-norm
         assert float((g.double() - r).norm() / r.norm()) <= 8 * 2.0 ** -9
+
+
+ROWS = [0, 4, 4, 10]
+
+
+def _places(weight, K=3):
+    weight.language_grads = [torch.zeros(weight.shape, dtype=torch.bfloat16) for _ in range(K)]
+    return weight.language_grads
+
+
+@pytest.mark.parametrize("input_grad", [True, False])
+@pytest.mark.parametrize("apart", [True, False])
+@pytest.mark.parametrize("frozen", ["w_gate", "w_up"])
+def test_one_of_the_gated_weights_is_frozen(frozen, apart, input_grad):
+    """The other one's gradients are what they are with both of them trained, apart by
+    language or not, and nothing is computed for the frozen one."""
+    def layer():
+        torch.manual_seed(2)
+        return GatedFeedForward(24, 40, device="cpu")
+
+    got = []
+    for freeze in (False, True):
+        f = layer()
+        if freeze:
+            getattr(f, frozen).requires_grad_(False)
+        trained = [p for p in f.parameters() if p.requires_grad]
+        places = [_places(p) for p in trained] if apart else None
+        x = _input().detach().requires_grad_(input_grad)
+        f(x, ROWS).float().square().sum().backward()
+        other = f.w_up if frozen == "w_gate" else f.w_gate
+        got.append(([x.grad] if input_grad else []) + (other.language_grads if apart else [other.grad]))
+        if freeze:
+            assert getattr(f, frozen).grad is None
+        if apart:
+            assert all(p.grad is None for p in trained) and places is not None
+    assert len(got[0]) == len(got[1]) and all(torch.equal(u, v) for u, v in zip(*got))
+
+
+def test_one_of_the_gated_weights_is_not_apart():
+    """A weight without places for its languages gets the ordinary gradient beside one that has."""
+    torch.manual_seed(3)
+    f = GatedFeedForward(24, 40, device="cpu")
+    both = GatedFeedForward(24, 40, device="cpu")
+    both.load_state_dict(f.state_dict())
+    _places(f.w_up)
+    f(_input(), ROWS).float().square().sum().backward()
+    both(_input()).float().square().sum().backward()
+    assert torch.equal(f.w_gate.grad, both.w_gate.grad) and f.w_up.grad is None
+    total = sum(g.float() for g in f.w_up.language_grads)
+    # the languages' sums rounded once each, against the whole batch's rounded once
+    assert float((total - both.w_up.grad.float()).norm()) <= 2 * 2.0 ** -9 * float(both.w_up.grad.float().norm())
+
+
+def test_bounds_must_fit_the_languages():
+    f = GatedFeedForward(24, 40, device="cpu")
+    _places(f.w_gate)
+    _places(f.w_up)
+    with pytest.raises(ValueError, match="bounds of the 3 languages"):
+        f(_input(), [0, 4, 10]).float().sum().backward()
