@@ -75,6 +75,34 @@ def bucket_layout(sizes: Sequence[int], elem_bytes: int, bucket_bytes: int) -> B
     return BucketLayout(offsets, starts, first, last, need)
 
 
+class LanguageGrads(list):
+    """A parameter's K places in the flat buffers, which are zeroed and resolved on
+    stream `home`.  A layer that writes them calls enter() before and leave() after: on
+    another stream than `home` it then runs behind what is queued there, and what is
+    queued there later behind it.  (Autograd does this for the gradients that it
+    accumulates itself.)"""
+
+    def __init__(self, places, home, device_index: int):
+        super().__init__(places)
+        self.home, self.device_index = home, device_index
+
+    def _other(self):
+        import torch
+        if torch._C._cuda_getCurrentRawStream(self.device_index) == self.home.cuda_stream:
+            return None
+        return torch.cuda.current_stream(self.device_index)
+
+    def enter(self) -> None:
+        here = self._other()
+        if here is not None:
+            here.wait_stream(self.home)
+
+    def leave(self) -> None:
+        here = self._other()
+        if here is not None:
+            self.home.wait_stream(here)
+
+
 class BucketMOO:
     """K per-language gradients of `params`, resolved bucket by bucket.
 
@@ -122,6 +150,7 @@ class BucketMOO:
         self.resolver = native.Resolver(K, dt, self.layout.offsets, dev)
         self.side = torch.cuda.Stream(device=dev)
         self._lang = None
+        self._home = None        # stream of begin_batch()
         self._left = list(self.layout.need)
         self._done = [False] * B
         self._hooks = [p.register_post_accumulate_grad_hook(self._make_hook(i))
@@ -143,6 +172,7 @@ class BucketMOO:
         for i, p in enumerate(self.params):
             p.grad = self._view(self.grads[k], i)
             p.language_grads = None
+        self._home = None
         self._lang = k
         if k == self.K - 1:
             self._left = list(self.layout.need)
@@ -156,12 +186,15 @@ class BucketMOO:
         layer uses keeps a gradient of 0 in every language.  finish() then
         resolves the whole plan at once."""
         import torch
-        torch.cuda.current_stream(self.device).wait_stream(self.side)
+        home = torch.cuda.current_stream(self.device)
+        home.wait_stream(self.side)
         for g in self.grads:
             g.zero_()
         for i, p in enumerate(self.params):
             p.grad = None
-            p.language_grads = [self._view(g, i) for g in self.grads]
+            p.language_grads = LanguageGrads([self._view(g, i) for g in self.grads], home,
+                                             p.get_device())
+        self._home = home
         self._lang = self.K - 1
         self._left = list(self.layout.need)
         self._done = [False] * self.layout.n_buckets
@@ -197,6 +230,11 @@ class BucketMOO:
                for p in self.params):
             raise RuntimeError("a parameter got a gradient that is not apart by language: in a "
                                "batch of all languages only language.py's layers may use them")
+        if self._home is not None:
+            here = torch.cuda.current_stream(self.device)
+            if here != self._home:
+                here.wait_stream(self._home)
+            self._home = None
         b = 0
         B = self.layout.n_buckets
         while b < B:                        # runs of unresolved buckets

@@ -34,6 +34,18 @@ def _languages(weight, rows, T):
     return [whole], [0, T], whole
 
 
+def _enter(to):
+    """Before a kernel writes what _languages gave: in the order of the streams
+    (hook.LanguageGrads)."""
+    if to is not None and hasattr(to[0], "enter"):
+        to[0].enter()
+
+
+def _leave(to):
+    if to is not None and hasattr(to[0], "leave"):
+        to[0].leave()
+
+
 def _on_rows(t):
     """t as a matrix whose rows start on 16 bytes."""
     t = t.reshape(-1, t.shape[-1])
@@ -73,6 +85,8 @@ class _Gate(torch.autograd.Function):
         # [places, bounds, gradient of the whole batch or None] of the weights that are trained
         to = [_languages(w, ctx.rows, T) if need else None
               for w, need in zip((w_gate, w_up), ctx.needs_input_grad[1:3])]
+        for t in to:
+            _enter(t)
         if all(to) and (to[0][2] is None) == (to[1][2] is None):
             native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, to[0][1], dx, to[0][0], to[1][0],
                                        accumulate=True)
@@ -89,6 +103,8 @@ class _Gate(torch.autograd.Function):
                 if place is not None:
                     d = ws[i * half:i * half + T * ld * 2].view(torch.bfloat16).view(T, ld)[:, :F]
                     native.bkmoo_language_wgrad(d, m, place[1], place[0], accumulate=True)
+        for t in to:
+            _leave(t)
         if dx is not None:
             dx = dx.reshape(*ctx.lead, D)
         return (dx, *(t[2] if t is not None else None for t in to), None, None)
@@ -109,8 +125,10 @@ class _Linear(torch.autograd.Function):
         whole = None
         if ctx.needs_input_grad[1]:
             m = _on_rows(x)
-            places, rows, whole = _languages(weight, ctx.rows, m.shape[0])
+            to = places, rows, whole = _languages(weight, ctx.rows, m.shape[0])
+            _enter(to)
             native.bkmoo_language_wgrad(_on_rows(dy), m, rows, places, accumulate=True)
+            _leave(to)
         return dx, whole, None
 
 

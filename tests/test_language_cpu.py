@@ -156,3 +156,46 @@ def test_bounds_must_fit_the_languages():
     _places(f.w_up)
     with pytest.raises(ValueError, match="bounds of the 3 languages"):
         f(_input(), [0, 4, 10]).float().sum().backward()
+
+
+class _Stream:
+    """A stream by name that notes what it waits for."""
+    notes = []
+
+    def __init__(self, name):
+        self.cuda_stream = name
+
+    def wait_stream(self, other):
+        self.notes.append((self.cuda_stream, "waits for", other.cuda_stream))
+
+
+@pytest.mark.parametrize("layer", ["gate", "linear"])
+@pytest.mark.parametrize("current", ["home", "other"])
+def test_gradients_written_on_another_stream(monkeypatch, layer, current):
+    """What zeroed and what resolves the places is on the stream of begin_batch(); where a
+    backward pass runs on another, each waits for the other around the write."""
+    from paper_2606_05613_gb300.hook import LanguageGrads
+    home, now = _Stream("home"), _Stream(current)
+    monkeypatch.setattr(_Stream, "notes", [])
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: now.cuda_stream, raising=False)
+
+    def noted(fn):
+        def call(*a, **k):
+            _Stream.notes.append("write")
+            return fn(*a, **k)
+        return call
+
+    monkeypatch.setattr(native, "bkmoo_gate_backward", noted(_gate_backward))
+    monkeypatch.setattr(native, "bkmoo_language_wgrad", noted(_language_wgrad))
+    torch.manual_seed(0)
+    f = GatedFeedForward(24, 40, device="cpu") if layer == "gate" else LanguageLinear(24, 40, device="cpu")
+    for p in f.parameters():
+        p.language_grads = LanguageGrads([torch.zeros(p.shape, dtype=torch.bfloat16) for _ in range(3)], home, 0)
+    f(_input(), ROWS).float().square().sum().backward()
+    one = ["write"] if current == "home" else [("other", "waits for", "home"), "write", ("home", "waits for", "other")]
+    # (the gated call writes two weights' places, each of which takes care of itself)
+    def once(notes):
+        return [n for i, n in enumerate(notes) if i == 0 or n != notes[i - 1]]
+
+    assert once(_Stream.notes) == once(one * (2 if layer == "gate" else 1))

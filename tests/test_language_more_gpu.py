@@ -1,4 +1,5 @@
-"""Layers of languages on the GPU where not all of their weights are trained."""
+"""Layers of languages on the GPU: weights that are not all trained, passes on another
+stream."""
 import pytest
 import torch
 
@@ -46,3 +47,44 @@ def test_one_of_the_gated_weights_is_frozen(frozen, input_grad):
             assert _relative(x.grad[i:j], ref[-1]) <= TOL
     moo.finish()
     assert getattr(layer, frozen).grad is None
+
+
+class _Late(torch.autograd.Function):
+    """Keeps the stream of its backward pass busy for some milliseconds first."""
+
+    @staticmethod
+    def forward(ctx, y):
+        return y.clone()
+
+    @staticmethod
+    def backward(ctx, dy):
+        torch.cuda._sleep(20_000_000)
+        return dy.clone()
+
+
+def test_a_pass_on_another_stream():
+    """begin_batch() and finish() on one stream, the model's passes on another that is late:
+    the direction is that of a run on one stream, bit for bit."""
+    torch.manual_seed(1)
+    layer = GatedFeedForward(72, 200).to(DEV)
+    moo = BucketMOO(layer.parameters(), K, 1 << 14, rule="mean")
+    x = torch.randn(ROWS[-1], 72, device=DEV).bfloat16()
+    c = torch.randn(ROWS[-1], 72, device=DEV).bfloat16()
+    other = torch.cuda.Stream()
+
+    def run(stream):
+        moo.begin_batch()
+        if stream is None:
+            layer(x, ROWS).backward(c)
+        else:
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                y = _Late.apply(layer(x, ROWS))
+            y.backward(c)
+        return moo.finish().clone(), [g.clone() for g in moo.grads]
+
+    d, grads = run(None)
+    for _ in range(2):
+        late, late_grads = run(other)
+        assert torch.equal(d, late) and all(torch.equal(u, v) for u, v in zip(grads, late_grads))
+    torch.cuda.synchronize()
