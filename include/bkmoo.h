@@ -482,6 +482,20 @@ int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t l
 int bkmoo_op_status(void* stream, int32_t* status);
 
 /*
+ * bkmoo_op_status_copy -- queue a copy of that word into *status (device memory, or
+ * pinned host memory for a copy that returns at once), neither waiting nor
+ * clearing it.
+ */
+int bkmoo_op_status_copy(void* stream, int32_t* status);
+
+/*
+ * bkmoo_selftest_give_up -- queue a wait of the kind those kernels make, for an
+ * arrival that nothing makes and 1 ms long, so that it gives up and the word says
+ * so (a self-test of what follows then).
+ */
+int bkmoo_selftest_give_up(void* stream);
+
+/*
  * bkmoo_grad_norm -- the 2-norm of a flat gradient (the direction), n elements
  * of fp32 or bf16, 16-byte aligned.  out_norm: device fp32, one value.  Squares
  * are summed in fp32 over at most 64 elements, then in fp64, in an order fixed
@@ -536,6 +550,8 @@ void bkmoo_adamw_default_params(bkmoo_adamw_params* p);
  * grad, m, v, master: 16-byte aligned; none may overlap another or a tensor.
  * grad_norm: device, as bkmoo_grad_norm gives it, needed where max_norm > 0.
  *   Where it is given and not finite, nothing is changed: the step is skipped.
+ *   So it is where bkmoo_op_status would report a call ahead of it that gave up,
+ *   until that is read: the gradient may be one of its undefined outputs.
  *   Without it a NaN or infinity in g reaches the state (an infinity in 8 bits
  *   its whole block).
  * Moments are computed in fp32.  Up to 1024 tensors take one launch.

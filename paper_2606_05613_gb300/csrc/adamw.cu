@@ -35,6 +35,7 @@ struct AdamArgs {
   float *m_scale, *v_scale;
   float* master;
   const float* norm;                 // NULL: neither clipped nor checked
+  const int32_t* ops;                // status of the kernels whose gradients these are, or NULL
   float max_norm;                    // 0: not clipped
   float b1, one_b1, b2, one_b2;
   float rate;                        // lr / (1 - beta1^step)
@@ -276,9 +277,11 @@ __global__ void __launch_bounds__(kAdamThreads, 3)
   int64_t blk = a.first + (int64_t)blockIdx.x * kAdamWarps + (threadIdx.x >> 5);
   if (blk >= end) return;
   Step<E4M3> step = {a.b1, a.one_b1, a.b2, a.one_b2, a.rate, a.root, a.eps, a.one, a.one};
+  const int32_t ops = a.ops ? *a.ops : BKMOO_OK;
+  const float norm = a.norm ? *a.norm : 0.0f;
+  if (ops != BKMOO_OK) return;                        // not a step to take
   if (a.norm) {
-    const float norm = *a.norm;
-    if (!(fabsf(norm) <= 3.4028235e38f)) return;      // not a step to take
+    if (!(fabsf(norm) <= 3.4028235e38f)) return;      // nor that
     if (a.max_norm > 0.0f) step.clip = fminf(1.0f, __fdiv_rn(a.max_norm, __fadd_rn(norm, 1e-6f)));
   }
   int t = 0;                        // the tensor of the block's first element
@@ -633,6 +636,9 @@ extern "C" int bkmoo_adamw(void* const* params, const int64_t* sizes, const floa
   a.key = mix_word(p->seed + ((uint64_t)p->step + 1) * kGold);
   a.n = n;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // (no word: first call on the device, during a capture; no such kernel has run then)
+  int32_t* ops = nullptr;
+  a.ops = tile_status_word(s, &ops) == BKMOO_OK ? ops : nullptr;
   const void* fn = adamw_fn(param_dtype, grad_dtype, e4m3, master != nullptr);
   int dev = 0, sms = 0, per_sm = 0;
   if (cudaGetDevice(&dev) != cudaSuccess ||

@@ -385,6 +385,9 @@ int stream_chunk_stages(int K);   // stages of a whole chunk
 // SMs of the current device (cached; host.cu).
 cudaError_t sm_count(int* n);
 
+// The current device's status word for tile kernels that may give up (tile_host.cu).
+int tile_status_word(cudaStream_t s, int32_t** word);
+
 // solve.cu
 // `behind`: launched behind the Gram pass (launch_behind).
 cudaError_t launch_solve(const PlanView& v, const SolveParams& p, float* out_weights,

@@ -10,7 +10,7 @@
 namespace bkmoo {
 
 // Waits of the tile kernels end on their own: each is for work of this CTA (or
-// pair) in flight, microseconds, and gives up after 2 s.
+// pair) in flight, microseconds, and gives up after 2 s (`limit`: of the self-test).
 constexpr uint64_t kTileWaitNs = 2000000000ull;
 
 template <int CG>
@@ -27,7 +27,8 @@ __device__ __forceinline__ bool bar_try_pair(uint64_t* b, unsigned parity) {
 }
 // True once the phase is over; false once the CTA has given up (*abort).
 template <int CG>
-__device__ __forceinline__ bool bar_wait(uint64_t* b, unsigned parity, volatile int* abort) {
+__device__ __forceinline__ bool bar_wait(uint64_t* b, unsigned parity, volatile int* abort,
+                                         uint64_t limit = kTileWaitNs) {
   for (int i = 0; i < 64; ++i)
     if (bar_try_pair<CG>(b, parity)) return true;
   const uint64_t t = stream_ns();
@@ -35,7 +36,7 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, unsigned parity, volatile 
     for (int i = 0; i < 64; ++i)
       if (bar_try_pair<CG>(b, parity)) return true;
     if (*abort) return false;
-    if (stream_ns() - t > kTileWaitNs) {
+    if (stream_ns() - t > limit) {
       *abort = 1;
       return false;
     }

@@ -30,6 +30,22 @@ using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, voi
                               const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// Two waits on an arrival that nothing makes, the second of which finds that the first has
+// given up, and its report as the tile kernels make it.
+__global__ void wait_runs_out_kernel(int32_t* status, uint64_t limit) {
+  __shared__ uint64_t bar;
+  __shared__ volatile int abort;
+  if (threadIdx.x == 0) {
+    bar_init(&bar, 1);
+    abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  const bool first = bar_wait<1>(&bar, 0, &abort, limit), second = bar_wait<1>(&bar, 0, &abort);
+  __syncthreads();
+  if (threadIdx.x == 0 && !first && !second && abort) atomicCAS(status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
+}
+
 EncodeFn encode_fn() {
   static const EncodeFn fn = [] {
     void* p = nullptr;
@@ -217,4 +233,24 @@ extern "C" int bkmoo_op_status(void* stream, int32_t* status) {
       cudaStreamSynchronize(s) != cudaSuccess)
     return BKMOO_ERR_CUDA;
   return BKMOO_OK;
+}
+
+extern "C" int bkmoo_op_status_copy(void* stream, int32_t* status) {
+  if (!status || ((uintptr_t)status & 3u)) return BKMOO_ERR_INVALID;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int32_t* word = nullptr;
+  const int r = tile_status_word(s, &word);
+  if (r != BKMOO_OK) return r;
+  return cudaMemcpyAsync(status, word, sizeof(int32_t), cudaMemcpyDefault, s) == cudaSuccess
+             ? BKMOO_OK
+             : BKMOO_ERR_CUDA;
+}
+
+extern "C" int bkmoo_selftest_give_up(void* stream) {
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int32_t* word = nullptr;
+  const int r = tile_status_word(s, &word);
+  if (r != BKMOO_OK) return r;
+  wait_runs_out_kernel<<<1, 32, 0, s>>>(word, 1000000);
+  return cudaGetLastError() == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
 }

@@ -36,8 +36,6 @@ inline int store_width(const void* p, int64_t ld, int elem) {
 int tile_map(CUtensorMap* m, const void* p, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 // SMs of the current device.
 int tile_sms(int* sms);
-// The device's status word for kernels that may give up.
-int tile_status_word(cudaStream_t s, int32_t** word);
 // A tile's shape: CTAs that share it and its columns.
 struct TileShape {
   int cg, bn;

@@ -151,6 +151,7 @@ class BucketMOO:
         self.side = torch.cuda.Stream(device=dev)
         self._lang = None
         self._home = None        # stream of begin_batch()
+        self._op_word = self._op_read = None
         self._left = list(self.layout.need)
         self._done = [False] * B
         self._hooks = [p.register_post_accumulate_grad_hook(self._make_hook(i))
@@ -166,6 +167,7 @@ class BucketMOO:
         if not 0 <= k < self.K:
             raise ValueError("language %d out of range" % k)
         import torch
+        self._check_ops()
         # language k's buffer may still be read by last step's resolves
         torch.cuda.current_stream(self.device).wait_stream(self.side)
         self.grads[k].zero_()
@@ -186,6 +188,7 @@ class BucketMOO:
         layer uses keeps a gradient of 0 in every language.  finish() then
         resolves the whole plan at once."""
         import torch
+        self._check_ops()
         home = torch.cuda.current_stream(self.device)
         home.wait_stream(self.side)
         for g in self.grads:
@@ -251,7 +254,36 @@ class BucketMOO:
             p.grad = self._view(self.direction, i)
             p.language_grads = None
         self._lang = None
+        self._check_ops()
+        self._read_ops()
         return self.direction
+
+    def _read_ops(self) -> None:
+        """Queue a read of the status word of language.py's kernels, where any ran and the
+        last read has been looked at."""
+        import torch
+        dev = self.params[0].get_device()
+        if self._op_read is not None or not native.ops_called(dev) or \
+                torch.cuda.is_current_stream_capturing():
+            return
+        if self._op_word is None:
+            self._op_word = torch.zeros(1, dtype=torch.int32, pin_memory=True)
+        with torch.cuda.device(dev):
+            native.bkmoo_op_status_copy(self._op_word)
+            self._op_read = torch.cuda.Event()
+            self._op_read.record()
+
+    def _check_ops(self) -> None:
+        """Raise if a kernel of language.py gave up in a step whose status has been read by now
+        (no wait: bkmoo_adamw does not take the steps in between)."""
+        import torch
+        if self._op_read is None or torch.cuda.is_current_stream_capturing() or \
+                not self._op_read.query():
+            return
+        self._op_read = None
+        if int(self._op_word) != native.BKMOO_OK:
+            code = native.bkmoo_op_status(self.device)
+            raise native.BkmooError(code or int(self._op_word), "a gate or weight-gradient kernel of an earlier step")
 
     def remove(self) -> None:
         for h in self._hooks:

@@ -144,6 +144,10 @@ def load():
                                              i32, vp]
         lib.bkmoo_op_status.restype = ctypes.c_int
         lib.bkmoo_op_status.argtypes = [vp, ctypes.POINTER(i32)]
+        lib.bkmoo_op_status_copy.restype = ctypes.c_int
+        lib.bkmoo_op_status_copy.argtypes = [vp, vp]
+        lib.bkmoo_selftest_give_up.restype = ctypes.c_int
+        lib.bkmoo_selftest_give_up.argtypes = [vp]
         lib.bkmoo_grad_norm.restype = ctypes.c_int
         lib.bkmoo_grad_norm.argtypes = [vp, i32, i64, vp, vp, sz, vp]
         lib.bkmoo_adamw_default_params.restype = None
@@ -412,6 +416,14 @@ def _raw_stream(torch, stream, dev: int) -> int:
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
+_op_devices = set()        # devices on which a gate or weight-gradient call has been made
+
+
+def ops_called(dev: int) -> bool:
+    """Whether the gate or weight-gradient calls have been used on device `dev`."""
+    return dev in _op_devices
+
+
 def _call(torch, dev: int, where: str, fn, *args):
     """fn(*args) with device `dev` current."""
     if torch.cuda.current_device() == dev:
@@ -470,6 +482,7 @@ def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None
     if (a is None) != (b is None):
         raise ValueError("a and b come together")
     pa, pb, ld_ab = _pair(a, b, T, F, dev, bf16, "a and b") if a is not None else (None, None, 0)
+    _op_devices.add(dev)
     _call(torch, dev, "bkmoo_gate_forward", load().bkmoo_gate_forward, px, ldx, pg, pu, ldw, T, D,
           F, _act_code(act), ph, ldh, pa, pb, ld_ab, _raw_stream(torch, stream, dev))
 
@@ -509,6 +522,7 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
             raise ValueError("dw_gate and dw_up must have one dtype")
     if ws is None:           # as bkmoo_gate_backward_workspace_size: da and db, rows on 16 bytes
         ws = _scratch(torch, 2 * -(-T * ((F + 7) // 8 * 16) // 256) * 256, dev, stream)
+    _op_devices.add(dev)
     _call(torch, dev, "bkmoo_gate_backward", load().bkmoo_gate_backward, pd, ldd, pa, pb, ld_ab,
           px, ldx, pg, pu, ldw, T, D, F, _act_code(act), K, r, pdx, lddx, gg, gu, dt,
           1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size(),
@@ -526,6 +540,7 @@ def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
     pd, ldd = _matrix(dy, T, M, dev, bf16, "dy")
     px, ldx = _matrix(x, T, N, dev, bf16, "x")
     g, dt = _weight_grads(dw, K, M, N, dev, "dw")
+    _op_devices.add(dev)
     _call(torch, dev, "bkmoo_language_wgrad", load().bkmoo_language_wgrad, pd, ldd, px, ldx, T, M,
           N, K, r, g, dt, 1 if accumulate else 0, _raw_stream(torch, stream, dev))
 
@@ -538,6 +553,25 @@ def bkmoo_op_status(device=None, stream=None) -> int:
         _check(load().bkmoo_op_status(_stream_handle(stream, device), ctypes.byref(st)),
                "bkmoo_op_status")
     return int(st.value)
+
+
+def bkmoo_op_status_copy(out, stream=None):
+    """Queue a copy of that word into `out`, one int32 on a GPU or in pinned memory;
+    neither waits nor clears it."""
+    import torch
+    dev = torch.cuda.current_device() if out.device.type == "cpu" else out.get_device()
+    if out.dtype is not torch.int32 or out.numel() != 1 or (out.device.type == "cpu" and not out.is_pinned()):
+        raise ValueError("out must be one int32 on a GPU or in pinned memory")
+    _call(torch, dev, "bkmoo_op_status_copy", load().bkmoo_op_status_copy,
+          _raw_stream(torch, stream, dev), out.data_ptr())
+
+
+def bkmoo_selftest_give_up(device=None, stream=None):
+    """Queue a wait of the gate and weight-gradient calls that gives up after 1 ms."""
+    import torch
+    dev = torch.cuda.current_device() if device is None else torch.device(device).index
+    _call(torch, dev, "bkmoo_selftest_give_up", load().bkmoo_selftest_give_up,
+          _raw_stream(torch, stream, dev))
 
 
 def bkmoo_grad_norm(grad, out_norm, ws=None, stream=None):

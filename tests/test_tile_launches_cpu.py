@@ -101,3 +101,10 @@ def test_kernels_that_add_are_kernels_of_their_own(fake, T, M, N, K, at, modes):
             assert code == 0 and [n.split("-", 2)[2] for n in names] == [mode]
             code, names = _backward(fake, T, N, M, K, dtype, at=at, accumulate=accumulate)
             assert code == 0 and [n.split("-", 2)[2] for n in names[1:]] == [mode]
+
+
+def test_status_copy_needs_a_place(fake):
+    """(the calls' refusals, and that a copy neither launches nor clears)"""
+    assert fake.bkmoo_op_status_copy(None, None) == bk.BKMOO_ERR_INVALID
+    assert fake.bkmoo_op_status_copy(None, ctypes.c_void_p(P + 2)) == bk.BKMOO_ERR_INVALID
+    assert _launches(fake, fake.bkmoo_op_status_copy, None, ctypes.c_void_p(P)) == (0, [])
