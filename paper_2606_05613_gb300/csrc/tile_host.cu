@@ -16,7 +16,6 @@ __device__ int32_t g_status;
 struct PerDevice {
   void* status = nullptr;
   int sms = 0;
-  const void* sized[32] = {};    // kernels whose shared-memory limit is raised
 };
 std::mutex g_mu;
 PerDevice g_dev[kMaxDevices];
@@ -183,22 +182,12 @@ TileShape tile_shape(const TileSet& a, const TileSet* b, int mode, int sms, int3
 
 int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s) {
   const int cg = shape.cg, smem = tile_smem(cg, shape.bn);
-  int dev = 0, sms = 0;
-  int r = current_device(&dev);
-  if (r == BKMOO_OK) r = tile_sms(&sms);
+  int sms = 0;
+  const int r = tile_sms(&sms);
   if (r != BKMOO_OK) return r;
-  {
-    std::lock_guard<std::mutex> lk(g_mu);
-    const void** known = g_dev[dev].sized;
-    int i = 0;
-    while (i < 32 && known[i] && known[i] != fn) ++i;
-    if (i == 32 || !known[i]) {
-      if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
-          cudaSuccess)
-        return BKMOO_ERR_CUDA;
-      if (i < 32) known[i] = fn;
-    }
-  }
+  // every time: the limit belongs to the context, which may be a new one
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    return BKMOO_ERR_CUDA;
   const int64_t units = sms / cg;
   cudaLaunchConfig_t cfg = {};
   // (the kernel waits at its top for the one ahead of it: launch_behind)

@@ -108,3 +108,15 @@ def test_status_copy_needs_a_place(fake):
     assert fake.bkmoo_op_status_copy(None, None) == bk.BKMOO_ERR_INVALID
     assert fake.bkmoo_op_status_copy(None, ctypes.c_void_p(P + 2)) == bk.BKMOO_ERR_INVALID
     assert _launches(fake, fake.bkmoo_op_status_copy, None, ctypes.c_void_p(P)) == (0, [])
+
+
+def test_every_launch_asks_for_its_shared_memory(fake):
+    """A kernel's limit on shared memory belongs to a context, which a cudaDeviceReset
+    between two calls replaces: it is raised for every launch, whatever ran before."""
+    for _ in range(2):
+        for T, M, N, K in TURNED + [(8192, 2048, 8192, 4), (64, 256, 256, 2)]:
+            for dtype in (F32, BF16):
+                for accumulate in (0, 1):
+                    code, names = _wgrad(fake, T, M, N, K, dtype, accumulate=accumulate)
+                    notes = fake.fake_notes().decode().split()
+                    assert code == 0 and notes == ["room:" + names[0], names[0]]
