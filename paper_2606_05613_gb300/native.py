@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
 import threading
 
@@ -597,27 +598,24 @@ def bkmoo_adamw_default_params() -> bkmoo_adamw_params:
     return p
 
 
+_DTYPE = operator.attrgetter("dtype")
+
+
 class TensorList:
     """The tensors of bkmoo_adamw: contiguous CUDA tensors of one dtype, in the
     order of the flat buffers, and their weight decay (one number, one per
-    tensor, or None).  Checked once; keeps the tensors and their addresses."""
+    tensor, or None).  Keeps the tensors, and their addresses for the call: a
+    tensor whose storage is replaced (p.data = ...) is followed, one that
+    changes its size, dtype or device is refused by the next call."""
 
     def __init__(self, tensors, weight_decay=None):
-        import torch
-        tensors = list(tensors)
-        n = len(tensors)
+        self.tensors = list(tensors)
+        n = len(self.tensors)
         if n == 0:
             raise ValueError("need at least one tensor")
-        self.dtype, self.device = tensors[0].dtype, tensors[0].get_device()
-        T = torch.Tensor
-        if self.device < 0 or set(map(T.get_device, tensors)) != {self.device} or \
-                not all(map(T.is_contiguous, tensors)) or \
-                any(t.dtype is not self.dtype for t in tensors):
-            raise ValueError("the tensors must be contiguous CUDA tensors of one dtype on one device")
-        self.dtype_code = _dtype_code(tensors[0])
-        self.tensors = tensors
-        self._sizes = array.array("q", map(T.numel, tensors))
-        self._addresses = array.array("Q", map(T.data_ptr, tensors))
+        self.dtype, self.device = self.tensors[0].dtype, self.tensors[0].get_device()
+        self._sizes, self._addresses = self._look()
+        self.dtype_code = _dtype_code(self.tensors[0])
         self.n_elems = sum(self._sizes)
         self._decay = None
         if weight_decay is not None:
@@ -625,9 +623,27 @@ class TensorList:
                                       else weight_decay)
             if len(self._decay) != n:
                 raise ValueError("weight_decay must be one number, or one per tensor")
-        # addresses of the three arrays, as the C call takes them
-        self.args = (self._addresses.buffer_info()[0], self._sizes.buffer_info()[0],
-                     self._decay.buffer_info()[0] if self._decay is not None else None, n)
+
+    def _look(self):
+        """(sizes, addresses) as they are now."""
+        import torch
+        T, tensors = torch.Tensor, self.tensors
+        if self.device < 0 or set(map(T.get_device, tensors)) != {self.device} or \
+                not all(map(T.is_contiguous, tensors)) or \
+                set(map(_DTYPE, tensors)) != {self.dtype}:
+            raise ValueError("the tensors must be contiguous CUDA tensors of one dtype on one device")
+        return array.array("q", map(T.numel, tensors)), array.array("Q", map(T.data_ptr, tensors))
+
+    def look_again(self) -> None:
+        sizes, self._addresses = self._look()
+        if sizes != self._sizes:
+            raise ValueError("the tensors' sizes have changed")
+
+    @property
+    def args(self):
+        """Addresses of the three arrays, as the C call takes them."""
+        return (self._addresses.buffer_info()[0], self._sizes.buffer_info()[0],
+                self._decay.buffer_info()[0] if self._decay is not None else None, len(self.tensors))
 
 
 def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None, m_scale=None,
@@ -642,6 +658,8 @@ def bkmoo_adamw(tensors, grad, m, v, params=None, weight_decay=None, master=None
         tensors = TensorList(tensors, weight_decay)
     elif weight_decay is not None:
         raise ValueError("the TensorList has its own weight decay")
+    else:
+        tensors.look_again()
     dev, N = tensors.device, tensors.n_elems
     f32, eight = torch.float32, m.dtype is torch.float8_e4m3fn
     if master is not None and tensors.dtype is not torch.bfloat16:

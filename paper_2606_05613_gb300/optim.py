@@ -17,7 +17,8 @@ class AdamW:
     them with the flat direction.
 
     state: "f32", or "e4m3" for 8-bit moments with a scale for every 256
-    elements.  master: keep the weights in float32 beside bfloat16 parameters.
+    elements.  master: keep the weights in float32 beside bfloat16 parameters; the
+    step goes from these, whatever the parameters have been set to since.
     weight_decay: one number, or one per parameter.  max_norm: clip the
     direction's norm to it; a step whose norm is not finite is skipped on the
     device (the step count moves on).  0 neither clips nor checks.
@@ -38,7 +39,7 @@ class AdamW:
         if not isinstance(decay, numbers.Real):
             decay = list(reversed(list(decay)))
         # the flat buffers hold the last registered parameter first
-        self.tensors = native.TensorList([p.detach() for p in reversed(params)], decay)
+        self.tensors = native.TensorList(reversed(params), decay)
         N, dev = self.tensors.n_elems, torch.device("cuda", self.tensors.device)
         if master and self.tensors.dtype != torch.bfloat16:
             raise ValueError("a master copy goes with bfloat16 parameters")
@@ -53,7 +54,7 @@ class AdamW:
                                       for _ in range(2))
         self.master = None
         if master:
-            self.master = torch.cat([t.reshape(-1) for t in self.tensors.tensors]).float()
+            self.master = torch.cat([t.detach().reshape(-1) for t in self.tensors.tensors]).float()
         self.norm = torch.zeros((), device=dev)
         self._ws = torch.empty(native.BKMOO_NORM_WS_BYTES, dtype=torch.uint8, device=dev)
 

@@ -1,0 +1,66 @@
+"""The optimizer object on the GPU: parameters whose storage is replaced, refused steps,
+its state."""
+import pytest
+import torch
+
+from paper_2606_05613_gb300 import native as bk
+from paper_2606_05613_gb300.optim import AdamW
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SIZES = (1000, 3, 4097)
+
+
+def _params(dtype=torch.float32, seed=0):
+    torch.manual_seed(seed)
+    return [torch.nn.Parameter(torch.randn(n, device=DEV).to(dtype)) for n in SIZES]
+
+
+def _direction(seed=1):
+    return torch.randn(sum(SIZES), device=DEV, generator=torch.Generator(device=DEV).manual_seed(seed))
+
+
+@pytest.mark.parametrize("dtype,master", [(torch.float32, False), (torch.bfloat16, True), (torch.bfloat16, False)])
+def test_parameters_that_move_are_followed(dtype, master):
+    """p.data = ... between two steps: the step goes to the new storage, as if nothing had moved."""
+    ends = []
+    for move in (False, True):
+        params = _params(dtype)
+        opt = AdamW(params, lr=1e-2, weight_decay=0.1, master=master)
+        for i in range(3):
+            if move:
+                old = [p.data for p in params]
+                for p in params:
+                    p.data = p.data.clone()
+                kept = [o.clone() for o in old]
+            opt.step(_direction(i))
+            if move:
+                assert all(torch.equal(o, k) for o, k in zip(old, kept))      # nothing is written there
+        ends.append([p.detach().clone() for p in params])
+    assert all(torch.equal(u, v) for u, v in zip(*ends))
+
+
+def test_parameters_that_change_are_refused():
+    params = _params()
+    opt = AdamW(params)
+    d = _direction()
+    opt.step(d)
+    kept = params[2].data
+    for other in (kept.bfloat16(), kept.cpu(), kept[:4000], kept.repeat(2)[::2]):
+        params[2].data = other
+        with pytest.raises(ValueError):
+            opt.step(d)
+    params[2].data = kept
+    opt.step(d)
+
+
+def test_a_tensor_list_follows_too():
+    p = _params()
+    tensors = bk.TensorList(p, 0.1)
+    m, v = torch.zeros(sum(SIZES), device=DEV), torch.zeros(sum(SIZES), device=DEV)
+    bk.bkmoo_adamw(tensors, _direction(), m, v)
+    for t in p:
+        t.data = torch.full_like(t.data, 2.0)
+    bk.bkmoo_adamw(tensors, torch.zeros(sum(SIZES), device=DEV), torch.zeros_like(m), torch.zeros_like(v))
+    for t in p:                            # only the decay is left of that step
+        assert bool(((t.detach() - 2.0 * (1.0 - 1e-4)).abs() <= 2.0 ** -22).all())
