@@ -72,7 +72,7 @@ class AdamW:
                            grad_norm=norm)
 
     def state_dict(self) -> dict:
-        return {"step": self.p.step, "m": self.m, "v": self.v, "m_scale": self.m_scale,
+        return {"step": self.p.step, "seed": self.p.seed, "m": self.m, "v": self.v, "m_scale": self.m_scale,
                 "v_scale": self.v_scale, "master": self.master}
 
     def load_state_dict(self, d: dict) -> None:
@@ -85,3 +85,4 @@ class AdamW:
             if d[name] is not None:
                 getattr(self, name).copy_(d[name])
         self.p.step = int(d["step"])
+        self.p.seed = int(d.get("seed", self.p.seed))

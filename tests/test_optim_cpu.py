@@ -1,0 +1,41 @@
+"""CPU: the bookkeeping of the optimizer object, without its kernels."""
+import pytest
+import torch
+
+from paper_2606_05613_gb300 import build as nb
+from paper_2606_05613_gb300 import native
+from paper_2606_05613_gb300.optim import AdamW
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    nb.build()
+
+
+class _Tensors:
+    def __init__(self, tensors):
+        self.tensors = tensors
+
+
+def _optimizer(params=()):
+    """An optimizer of CPU parameters, as its constructor leaves one of GPU parameters."""
+    opt = AdamW.__new__(AdamW)
+    opt.tensors = _Tensors(list(reversed(params)))
+    opt.p = native.bkmoo_adamw_default_params()
+    opt.p.step, opt.p.seed, opt.p.lr = 0, 77, 0.5
+    opt.m, opt.v = torch.zeros(8), torch.zeros(8)
+    opt.m_scale = opt.v_scale = opt.master = opt.norm = opt._ws = None
+    return opt
+
+
+def test_state_keeps_the_seed_of_the_rounding():
+    """Resumed steps draw what the run itself would have drawn."""
+    one, other = _optimizer(), _optimizer()
+    one.p.step, other.p.seed = 12, 5
+    other.load_state_dict(one.state_dict())
+    assert (other.p.step, other.p.seed) == (12, 77)
+    old = one.state_dict()
+    del old["seed"]                        # a state that was saved without one
+    other.p.seed = 5
+    other.load_state_dict(old)
+    assert (other.p.step, other.p.seed) == (12, 5)
