@@ -59,17 +59,23 @@ class AdamW:
         self._ws = torch.empty(native.BKMOO_NORM_WS_BYTES, dtype=torch.uint8, device=dev)
 
     def step(self, direction, lr: "float | None" = None) -> None:
-        """One step with the flat direction (float32 or bfloat16)."""
+        """One step with the flat direction (float32 or bfloat16).  lr: the rate from
+        this step on."""
+        before = self.p.step, self.p.lr
         if lr is not None:
             self.p.lr = lr
         self.p.step += 1
-        norm = None
-        if self.p.max_norm > 0:
-            native.bkmoo_grad_norm(direction, self.norm, ws=self._ws)
-            norm = self.norm
-        native.bkmoo_adamw(self.tensors, direction, self.m, self.v, params=self.p,
-                           master=self.master, m_scale=self.m_scale, v_scale=self.v_scale,
-                           grad_norm=norm)
+        try:
+            norm = None
+            if self.p.max_norm > 0:
+                native.bkmoo_grad_norm(direction, self.norm, ws=self._ws)
+                norm = self.norm
+            native.bkmoo_adamw(self.tensors, direction, self.m, self.v, params=self.p,
+                               master=self.master, m_scale=self.m_scale, v_scale=self.v_scale,
+                               grad_norm=norm)
+        except Exception:
+            self.p.step, self.p.lr = before      # a refused step does not count
+            raise
 
     def state_dict(self) -> dict:
         return {"step": self.p.step, "seed": self.p.seed, "m": self.m, "v": self.v, "m_scale": self.m_scale,

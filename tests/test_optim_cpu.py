@@ -39,3 +39,23 @@ def test_state_keeps_the_seed_of_the_rounding():
     other.p.seed = 5
     other.load_state_dict(old)
     assert (other.p.step, other.p.seed) == (12, 5)
+
+
+def test_a_refused_step_does_not_count(monkeypatch):
+    """The step's number goes into the bias corrections and the rounding: a call that is
+    refused leaves it, and the rate, as they were."""
+    opt = _optimizer()
+
+    def refuse(*a, **k):
+        raise ValueError("grad")
+
+    monkeypatch.setattr(native, "bkmoo_adamw", refuse)
+    with pytest.raises(ValueError):
+        opt.step(torch.zeros(9), lr=2.0)
+    assert (opt.p.step, opt.p.lr) == (0, 0.5)
+    taken = []
+    monkeypatch.setattr(native, "bkmoo_adamw", lambda *a, **k: taken.append((k["params"].step, k["params"].lr)))
+    opt.step(torch.zeros(8))
+    opt.step(torch.zeros(8), lr=2.0)
+    opt.step(torch.zeros(8))
+    assert taken == [(1, 0.5), (2, 2.0), (3, 2.0)] and opt.p.step == 3
