@@ -76,6 +76,8 @@ class AdamW:
         except Exception:
             self.p.step, self.p.lr = before      # a refused step does not count
             raise
+        # autograd does not see the kernel write: a backward pass over what these were fails
+        torch.autograd.graph.increment_version(self.tensors.tensors)
 
     def state_dict(self) -> dict:
         return {"step": self.p.step, "seed": self.p.seed, "m": self.m, "v": self.v, "m_scale": self.m_scale,

@@ -59,3 +59,18 @@ def test_a_refused_step_does_not_count(monkeypatch):
     opt.step(torch.zeros(8), lr=2.0)
     opt.step(torch.zeros(8))
     assert taken == [(1, 0.5), (2, 2.0), (3, 2.0)] and opt.p.step == 3
+
+
+def test_a_pass_that_spans_a_step_is_refused(monkeypatch):
+    """Weights that a step has changed since the forward pass are not the ones its backward
+    pass needs: autograd says so, as it does for torch's optimizers."""
+    monkeypatch.setattr(native, "bkmoo_adamw", lambda *a, **k: None)
+    w = torch.nn.Parameter(torch.randn(4, 4))
+    opt = _optimizer([w])
+    x = torch.randn(2, 4, requires_grad=True)
+    (x @ w).sum().backward()
+    opt.step(torch.zeros(16))
+    y = x @ w
+    opt.step(torch.zeros(16))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
