@@ -444,6 +444,13 @@ def _scratch(torch, nbytes: int, dev: int, stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=dev)
 
 
+def _workspace(ws, dev: int):
+    """(address, bytes) of a workspace that a caller gave."""
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor on cuda:%d" % dev)
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
 def _language_rows(rows, T: int):
     """(K, array) of the language bounds."""
     r = [int(i) for i in rows]
@@ -523,11 +530,11 @@ def bkmoo_gate_backward(dh, a, b, x, w_gate, w_up, act, rows, dx=None, dw_gate=N
             raise ValueError("dw_gate and dw_up must have one dtype")
     if ws is None:           # as bkmoo_gate_backward_workspace_size: da and db, rows on 16 bytes
         ws = _scratch(torch, 2 * -(-T * ((F + 7) // 8 * 16) // 256) * 256, dev, stream)
+    pws, nws = _workspace(ws, dev)
     _op_devices.add(dev)
     _call(torch, dev, "bkmoo_gate_backward", load().bkmoo_gate_backward, pd, ldd, pa, pb, ld_ab,
           px, ldx, pg, pu, ldw, T, D, F, _act_code(act), K, r, pdx, lddx, gg, gu, dt,
-          1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size(),
-          _raw_stream(torch, stream, dev))
+          1 if accumulate else 0, pws, nws, _raw_stream(torch, stream, dev))
 
 
 def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
@@ -588,8 +595,7 @@ def bkmoo_grad_norm(grad, out_norm, ws=None, stream=None):
     if ws is None:
         ws = _scratch(torch, BKMOO_NORM_WS_BYTES, dev, stream)
     _call(torch, dev, "bkmoo_grad_norm", load().bkmoo_grad_norm, grad.data_ptr(), _dtype_code(grad),
-          grad.numel(), out_norm.data_ptr(), ws.data_ptr(), ws.numel() * ws.element_size(),
-          _raw_stream(torch, stream, dev))
+          grad.numel(), out_norm.data_ptr(), *_workspace(ws, dev), _raw_stream(torch, stream, dev))
 
 
 def bkmoo_adamw_default_params() -> bkmoo_adamw_params:
