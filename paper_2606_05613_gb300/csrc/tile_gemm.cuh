@@ -418,7 +418,9 @@ __device__ __forceinline__ void activation_slope2(int act, float2 a, float2* f, 
   } else {
     const float2 q = __fmul2_rn(a, a), s = sigmoid2(tanh_arg(a, q));
     *f = __fmul2_rn(a, s);
-    const float2 dz = __ffma2_rn(q, both(3.0f * 0.044715f * 1.59576912f), both(1.59576912f));
+    // (a finite dz, for where a^2 is not its factor is 0)
+    const float2 dz = __ffma2_rn(make_float2(fminf(q.x, 1e30f), fminf(q.y, 1e30f)),
+                                 both(3.0f * 0.044715f * 1.59576912f), both(1.59576912f));
     *df = __ffma2_rn(__fmul2_rn(*f, __ffma2_rn(s, both(-1.0f), both(1.0f))), dz, s);
   }
 }
