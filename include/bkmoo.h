@@ -554,7 +554,9 @@ void bkmoo_adamw_default_params(bkmoo_adamw_params* p);
  *   until that is read: the gradient may be one of its undefined outputs.
  *   Without it a NaN or infinity in g reaches the state (an infinity in 8 bits
  *   its whole block).
- * Moments are computed in fp32.  Up to 1024 tensors take one launch.
+ * Moments are computed in fp32.  In 8 bits the root of a v below 2^-126 (gradients
+ * below about 1e-19) comes out up to 100 times too small, which an eps of 1e-15 or
+ * more hides from the weights.  Up to 1024 tensors take one launch.
  */
 int bkmoo_adamw(void* const* params, const int64_t* sizes, const float* weight_decay,
                 int32_t n_params, int32_t param_dtype, const void* grad, int32_t grad_dtype,

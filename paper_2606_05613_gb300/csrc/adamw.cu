@@ -212,11 +212,11 @@ struct Loaded {
   int t;                 // the tensor of the block's first element
 };
 
-// To 2^-23.
+// To 2^-23, of subnormal numbers too.
 __device__ __forceinline__ float2 near_root2(float2 x) {
   float2 r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r.x) : "f"(x.x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r.y) : "f"(x.y));
   return r;
 }
 // Rounded root: the hardware's reciprocal root of x, good to 2^-22, and one step of

@@ -64,3 +64,17 @@ def test_a_tensor_list_follows_too():
     bk.bkmoo_adamw(tensors, torch.zeros(sum(SIZES), device=DEV), torch.zeros_like(m), torch.zeros_like(v))
     for t in p:                            # only the decay is left of that step
         assert bool(((t.detach() - 2.0 * (1.0 - 1e-4)).abs() <= 2.0 ** -22).all())
+
+
+@pytest.mark.parametrize("size", [1e-18, 1e-19, 3e-20])
+def test_second_moments_below_the_normal_numbers(size):
+    """Gradients whose squares fp32 holds as subnormal numbers only, and no eps: the first
+    step is the rate, as the formula has it.  (1 - beta2) g^2 is a multiple of 2^-149, so its
+    root is off by at most 2^-150 of it; the rest are fp32 roundings."""
+    p = [torch.nn.Parameter(torch.zeros(n, device=DEV)) for n in SIZES]
+    opt = AdamW(p, lr=1e-2, betas=(0.9, 0.95), eps=0.0)
+    g = torch.where(_direction() > 0, size, -size)
+    opt.step(g)
+    off = 2.0 ** -150 / (0.05 * size * size) + 2.0 ** -150 / (size * size) + 2.0 ** -18
+    flat = torch.cat([t.detach() for t in reversed(p)])
+    assert bool(((flat + 1e-2 * torch.sign(g)).abs() <= 1e-2 * off).all())
