@@ -9,6 +9,7 @@ import pytest
 
 from paper_2606_05613_gb300 import build as nb
 from paper_2606_05613_gb300 import native as bk
+from tile_shapes import BACKWARD, FORWARD, WGRAD, rows
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 F32, BF16 = bk.BKMOO_F32, bk.BKMOO_BF16
@@ -120,3 +121,27 @@ def test_every_launch_asks_for_its_shared_memory(fake):
                     code, names = _wgrad(fake, T, M, N, K, dtype, accumulate=accumulate)
                     notes = fake.fake_notes().decode().split()
                     assert code == 0 and notes == ["room:" + names[0], names[0]]
+
+
+def _bounds(T, K):
+    return (ctypes.c_int64 * (K + 1))(*rows(T, K))
+
+
+@pytest.mark.parametrize("T,D,F,shape", FORWARD)
+def test_sizes_of_the_forward_tests(fake, T, D, F, shape):
+    v = ctypes.c_void_p(P)
+    code, names = _launches(fake, fake.bkmoo_gate_forward, v, I64(_up(D)), v, v, I64(_up(D)), I64(T), I64(D), I64(F), 0,
+                            v, I64(_up(F)), v, v, I64(_up(F)), None)
+    assert (code, names) == (0, ["gate-%s-plain" % shape])
+
+
+@pytest.mark.parametrize("call,T,A,B,K,aligned,odd,sums",
+                         [("both",) + c for c in BACKWARD] + [("weight",) + c for c in WGRAD])
+def test_sizes_of_the_gradient_tests(fake, call, T, A, B, K, aligned, odd, sums):
+    run = _backward if call == "both" else _wgrad
+    for accumulate in (0, 1):
+        for dtype, at, shape, mode in ((BF16, 0, aligned, ("plain", "added")[accumulate]), (BF16, 6, odd, "turned"),
+                                       (F32, 0, sums, ("sums", "sums-added")[accumulate]),
+                                       (F32, 12, sums, ("sums-turned", "sums-turned-added")[accumulate])):
+            code, names = run(fake, T, A, B, K, dtype, at=at, accumulate=accumulate, rows=_bounds(T, K))
+            assert code == 0 and names[-1] == "%s-%s-%s" % (call, shape, mode)
