@@ -78,3 +78,29 @@ def test_second_moments_below_the_normal_numbers(size):
     off = 2.0 ** -150 / (0.05 * size * size) + 2.0 ** -150 / (size * size) + 2.0 ** -18
     flat = torch.cat([t.detach() for t in reversed(p)])
     assert bool(((flat + 1e-2 * torch.sign(g)).abs() <= 1e-2 * off).all())
+
+
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_bf16_parameters_without_a_master_copy(state):
+    """Every step against the formula in 64 bits from the weights and moments before it: the
+    weights widened, stepped and rounded to nearest, 2^-8 of them at most, beside the fp32
+    step's own roundings (the rate is 1e-2, a first moment over the root at most 10)."""
+    p = _params(torch.bfloat16)
+    lr, b1, b2, eps, decay = 1e-2, 0.9, 0.95, 1e-8, 0.1
+    opt = AdamW(p, lr=lr, betas=(b1, b2), eps=eps, weight_decay=decay, max_norm=0.5, state=state)
+
+    def flat():
+        return torch.cat([t.detach() for t in reversed(p)]).double()
+
+    def moment(code, scale):
+        return code.double() if scale is None else code.double() * scale.double().repeat_interleave(256)[:code.numel()]
+
+    for t in range(1, 11):
+        g = _direction(t)
+        w, m, v = flat(), moment(opt.m, opt.m_scale), moment(opt.v, opt.v_scale)
+        opt.step(g)
+        g = g.double() * min(1.0, 0.5 / (float(g.double().norm()) + 1e-6))
+        m = b1 * m + (1 - b1) * g
+        v = b2 * (v if state == "f32" else v * v) + (1 - b2) * g * g
+        want = w * (1 - lr * decay) - lr * (m / (1 - b1 ** t)) / (torch.sqrt(v / (1 - b2 ** t)) + eps)
+        assert bool(((flat() - want).abs() <= 2.0 ** -8 * want.abs() + 10 * lr * 2.0 ** -18).all())
