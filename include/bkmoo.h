@@ -499,8 +499,11 @@ int bkmoo_selftest_give_up(void* stream);
  * bkmoo_grad_norm -- the 2-norm of a flat gradient (the direction), n elements
  * of fp32 or bf16, 16-byte aligned.  out_norm: device fp32, one value.  Squares
  * are summed in fp32 over at most 64 elements, then in fp64, in an order fixed
- * by n: deterministic; the sum and its root are rounded to fp32.  Infinite where a square or the sum leaves fp32, NaN with a NaN.  ws: device, 256-byte aligned,
- * BKMOO_NORM_WS_BYTES, not shared by calls that overlap.
+ * by n: deterministic; the sum and its root are rounded to fp32.  Infinite where a
+ * square or the sum leaves fp32, NaN with a NaN, and where bkmoo_op_status would
+ * report a call ahead of it that gave up, until that is read: the gradient may be one
+ * of its undefined outputs.  ws: device, 256-byte aligned, BKMOO_NORM_WS_BYTES, not
+ * shared by calls that overlap.
  */
 #define BKMOO_NORM_WS_BYTES 16384
 int bkmoo_grad_norm(const void* grad, int32_t dtype, int64_t n, float* out_norm, void* ws,
@@ -550,8 +553,8 @@ void bkmoo_adamw_default_params(bkmoo_adamw_params* p);
  * grad, m, v, master: 16-byte aligned; none may overlap another or a tensor.
  * grad_norm: device, as bkmoo_grad_norm gives it, needed where max_norm > 0.
  *   Where it is given and not finite, nothing is changed: the step is skipped.
- *   So it is where bkmoo_op_status would report a call ahead of it that gave up,
- *   until that is read: the gradient may be one of its undefined outputs.
+ *   So it is, without one, where bkmoo_op_status would report a call ahead of it
+ *   that gave up, until that is read (with one, the norm of such a gradient is NaN).
  *   Without it a NaN or infinity in g reaches the state (an infinity in 8 bits
  *   its whole block).
  * Moments are computed in fp32.  In 8 bits the root of a v below 2^-126 (gradients

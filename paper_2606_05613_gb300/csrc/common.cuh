@@ -385,7 +385,8 @@ int stream_chunk_stages(int K);   // stages of a whole chunk
 // SMs of the current device (cached; host.cu).
 cudaError_t sm_count(int* n);
 
-// The current device's status word for tile kernels that may give up (tile_host.cu).
+// The current device's status word for tile kernels that may give up, and behind it a float
+// that is 0, or NaN once one has (tile_host.cu).
 int tile_status_word(cudaStream_t s, int32_t** word);
 
 // solve.cu

@@ -43,6 +43,12 @@ __device__ __forceinline__ bool bar_wait(uint64_t* b, unsigned parity, volatile 
   }
 }
 
+// The device's status word and the float behind it (tile_status_word).
+__device__ __forceinline__ void report_give_up(int32_t* status) {
+  atomicCAS(status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
+  status[1] = 0x7fc00000;
+}
+
 // Address of `p`'s counterpart in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t peer_smem(const void* p, unsigned rank) {
   uint32_t r;

@@ -833,7 +833,7 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   if (CG == 2) cluster_sync();
   tc_fence_after();
   if (wid == kTileEpilogueWarps + 1) tmem_free<CG>(tmem, 2 * BN);
-  if (threadIdx.x == 0 && sh.abort) atomicCAS(p.status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
+  if (threadIdx.x == 0 && sh.abort) report_give_up(p.status);
 }
 
 // The kernels, one translation unit each (nvcc runs them side by side).

@@ -10,8 +10,8 @@ namespace {
 
 constexpr int kMaxDevices = 64;
 
-// BKMOO_OK, or the first error of a tile kernel since it was last read.
-__device__ int32_t g_status;
+// BKMOO_OK, or the first error of a tile kernel since it was last read (report_give_up).
+__device__ int32_t g_status[2];
 
 struct PerDevice {
   void* status = nullptr;
@@ -42,7 +42,7 @@ __global__ void wait_runs_out_kernel(int32_t* status, uint64_t limit) {
   __syncthreads();
   const bool first = bar_wait<1>(&bar, 0, &abort, limit), second = bar_wait<1>(&bar, 0, &abort);
   __syncthreads();
-  if (threadIdx.x == 0 && !first && !second && abort) atomicCAS(status, BKMOO_OK, BKMOO_ERR_TIMEOUT);
+  if (threadIdx.x == 0 && !first && !second && abort) report_give_up(status);
 }
 
 EncodeFn encode_fn() {
@@ -218,7 +218,7 @@ extern "C" int bkmoo_op_status(void* stream, int32_t* status) {
   const int r = tile_status_word(s, &word);
   if (r != BKMOO_OK) return r;
   if (cudaMemcpyAsync(status, word, sizeof(int32_t), cudaMemcpyDeviceToHost, s) != cudaSuccess ||
-      cudaMemsetAsync(word, 0, sizeof(int32_t), s) != cudaSuccess ||
+      cudaMemsetAsync(word, 0, 2 * sizeof(int32_t), s) != cudaSuccess ||
       cudaStreamSynchronize(s) != cudaSuccess)
     return BKMOO_ERR_CUDA;
   return BKMOO_OK;

@@ -87,3 +87,14 @@ def test_the_training_loop_hears_of_it():
     torch.cuda.synchronize()
     assert not any(torch.equal(u, v) for u, v in zip(before, moo.params))
     moo.begin_batch()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_norm_of_an_undefined_gradient(dtype):
+    g, norm = torch.ones(1 << 16, dtype=dtype, device=DEV), torch.zeros((), device=DEV)
+    bk.bkmoo_selftest_give_up(DEV)
+    bk.bkmoo_grad_norm(g, norm)
+    assert bool(torch.isnan(norm))
+    assert bk.bkmoo_op_status(DEV) == bk.BKMOO_ERR_TIMEOUT
+    bk.bkmoo_grad_norm(g, norm)
+    assert float(norm) == 256.0
