@@ -489,11 +489,12 @@ int bkmoo_op_status(void* stream, int32_t* status);
 int bkmoo_op_status_copy(void* stream, int32_t* status);
 
 /*
- * bkmoo_selftest_give_up -- queue a wait of the kind those kernels make, for an
- * arrival that nothing makes and 1 ms long, so that it gives up and the word says
- * so (a self-test of what follows then).
+ * bkmoo_selftest_give_up -- queue a kernel that gives up, so that the word says so (a
+ * self-test of that and of what follows).  what 0: a single wait of the kind those
+ * kernels make, for an arrival that nothing makes, 1 ms long; 1 and 2: the forward
+ * pass's kernel of one CTA and of a pair, whose operands are never copied (2 s).
  */
-int bkmoo_selftest_give_up(void* stream);
+int bkmoo_selftest_give_up(int32_t what, void* stream);
 
 /*
  * bkmoo_grad_norm -- the 2-norm of a flat gradient (the direction), n elements

@@ -274,3 +274,19 @@ extern "C" int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x
   weight_tiles(p, shape);
   return tile_launch(tile_weight_fn(shape.cg, shape.bn, mode), shape, &p, p.tiles, s);
 }
+
+// (Nothing is read or written but the status word: no operand is copied, and the warps that
+// write results wait for a sum that never comes.)
+extern "C" int bkmoo_selftest_give_up(int32_t what, void* stream) {
+  if (what < 0 || what > 2) return BKMOO_ERR_INVALID;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  TileArgs<kGate> p = {};
+  const int r = tile_status_word(s, &p.status);
+  if (r != BKMOO_OK) return r;
+  if (what == 0) return launch_wait_runs_out(p.status, s);
+  const TileShape shape = {what, 256};
+  p.rows = kTileM * what;
+  p.cols = 128;
+  p.tiles = p.tiles_m = p.tiles_n = p.nkt = p.withhold = 1;
+  return tile_launch(tile_gate_fn(shape.cg, shape.bn), shape, &p, 1, s);
+}

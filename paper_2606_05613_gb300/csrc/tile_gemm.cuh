@@ -84,6 +84,7 @@ struct TileArgs<kGate> {
   int32_t tiles_m, tiles_n, tiles;
   int32_t nkt;
   int32_t act;
+  int32_t withhold;             // self-test: no operand is ever copied, every wait runs out
 };
 template <>
 struct TileArgs<kInput> {
@@ -793,8 +794,10 @@ __global__ void __launch_bounds__(kTileThreads, 1)
   };
   auto none = [](const auto&, int) {};
   RingState r;
+  bool feed = true;
+  if constexpr (KIND == kGate) feed = !p.withhold;
   if (wid == kTileEpilogueWarps) {
-    if (elect_one()) {
+    if (feed && elect_one()) {
       each([&](auto kind, const auto& q, int i) {
         return fill_tile<decltype(kind)::value, CG, BN>(q, i, r, sh, ring, rank);
       }, none);

@@ -207,6 +207,14 @@ int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cuda
   return cudaLaunchKernelExC(&cfg, fn, list) == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
 }
 
+int launch_wait_runs_out(int32_t* status, cudaStream_t s) {
+  uint64_t limit = 1000000;
+  void* list[] = {&status, &limit};
+  return launch_behind((const void*)wait_runs_out_kernel, dim3(1), dim3(32), list, 0, s, false) == cudaSuccess
+             ? BKMOO_OK
+             : BKMOO_ERR_CUDA;
+}
+
 }  // namespace bkmoo
 
 using namespace bkmoo;
@@ -233,13 +241,4 @@ extern "C" int bkmoo_op_status_copy(void* stream, int32_t* status) {
   return cudaMemcpyAsync(status, word, sizeof(int32_t), cudaMemcpyDefault, s) == cudaSuccess
              ? BKMOO_OK
              : BKMOO_ERR_CUDA;
-}
-
-extern "C" int bkmoo_selftest_give_up(void* stream) {
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int32_t* word = nullptr;
-  const int r = tile_status_word(s, &word);
-  if (r != BKMOO_OK) return r;
-  wait_runs_out_kernel<<<1, 32, 0, s>>>(word, 1000000);
-  return cudaGetLastError() == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
 }

@@ -51,6 +51,8 @@ struct TileSet {
 // The shape for one set, or two in turn, and the second's head start (Walk); mode: how
 // weight gradients are written (TileMode).
 TileShape tile_shape(const TileSet& a, const TileSet* b, int mode, int sms, int32_t* head_start);
+// Queues the self-test of a single wait.
+int launch_wait_runs_out(int32_t* status, cudaStream_t s);
 // Queues a tile kernel over `tiles` tiles.
 int tile_launch(const void* fn, TileShape shape, void* args, int64_t tiles, cudaStream_t s);
 

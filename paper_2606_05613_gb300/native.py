@@ -148,7 +148,7 @@ def load():
         lib.bkmoo_op_status_copy.restype = ctypes.c_int
         lib.bkmoo_op_status_copy.argtypes = [vp, vp]
         lib.bkmoo_selftest_give_up.restype = ctypes.c_int
-        lib.bkmoo_selftest_give_up.argtypes = [vp]
+        lib.bkmoo_selftest_give_up.argtypes = [i32, vp]
         lib.bkmoo_grad_norm.restype = ctypes.c_int
         lib.bkmoo_grad_norm.argtypes = [vp, i32, i64, vp, vp, sz, vp]
         lib.bkmoo_adamw_default_params.restype = None
@@ -574,11 +574,12 @@ def bkmoo_op_status_copy(out, stream=None):
           _raw_stream(torch, stream, dev), out.data_ptr())
 
 
-def bkmoo_selftest_give_up(device=None, stream=None):
-    """Queue a wait of the gate and weight-gradient calls that gives up after 1 ms."""
+def bkmoo_selftest_give_up(device=None, what: int = 0, stream=None):
+    """Queue a kernel that gives up: a wait alone of 1 ms (0), or the forward pass's
+    kernel of one CTA or of a pair without its operands, 2 s (1, 2)."""
     import torch
     dev = torch.cuda.current_device() if device is None else torch.device(device).index
-    _call(torch, dev, "bkmoo_selftest_give_up", load().bkmoo_selftest_give_up,
+    _call(torch, dev, "bkmoo_selftest_give_up", load().bkmoo_selftest_give_up, what,
           _raw_stream(torch, stream, dev))
 
 

@@ -98,3 +98,20 @@ def test_the_norm_of_an_undefined_gradient(dtype):
     assert bk.bkmoo_op_status(DEV) == bk.BKMOO_ERR_TIMEOUT
     bk.bkmoo_grad_norm(g, norm)
     assert float(norm) == 256.0
+
+
+@pytest.mark.parametrize("ctas", [1, 2])
+def test_a_kernel_without_its_operands_ends(ctas):
+    """Each of its waits ends, it hands back its tensor memory and says so; what runs behind
+    it, on every SM, is right."""
+    torch.manual_seed(0)
+    x, w = torch.randn(2051, 520, device=DEV).bfloat16(), (torch.randn(2 * 4104, 520, device=DEV) * 0.05).bfloat16()
+    first, after = (torch.empty(2051, 4104, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    bk.bkmoo_gate_forward(x, w[:4104], w[4104:], "silu", first)
+    for _ in range(2):
+        bk.bkmoo_selftest_give_up(DEV, ctas)
+    bk.bkmoo_gate_forward(x, w[:4104], w[4104:], "silu", after)
+    assert bk.bkmoo_op_status(DEV) == bk.BKMOO_ERR_TIMEOUT
+    assert torch.equal(first, after)
+    bk.bkmoo_gate_forward(x, w[:4104], w[4104:], "silu", after)
+    assert bk.bkmoo_op_status(DEV) == bk.BKMOO_OK

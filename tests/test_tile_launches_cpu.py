@@ -145,3 +145,10 @@ def test_sizes_of_the_gradient_tests(fake, call, T, A, B, K, aligned, odd, sums)
                                        (F32, 12, sums, ("sums-turned", "sums-turned-added")[accumulate])):
             code, names = run(fake, T, A, B, K, dtype, at=at, accumulate=accumulate, rows=_bounds(T, K))
             assert code == 0 and names[-1] == "%s-%s-%s" % (call, shape, mode)
+
+
+def test_kernels_of_the_self_test(fake):
+    for what, names in ((0, ["pass"]), (1, ["gate-1x256-plain"]), (2, ["gate-2x256-plain"])):
+        assert _launches(fake, fake.bkmoo_selftest_give_up, what, None) == (0, names)
+    for bad in (-1, 3):
+        assert _launches(fake, fake.bkmoo_selftest_give_up, bad, None) == (bk.BKMOO_ERR_INVALID, [])
