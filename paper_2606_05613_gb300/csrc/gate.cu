@@ -55,8 +55,9 @@ __global__ void __launch_bounds__(256) gate_slope_kernel(const SlopeArgs p) {
                         *b = p.b + row * p.ld_ab + col;
     __nv_bfloat16 *da = p.da + row * p.ld_d + col, *db = p.db + row * p.ld_d + col;
     if (col + 8 <= p.cols) {
-      slope8(__ldg(reinterpret_cast<const uint4*>(dh)), __ldg(reinterpret_cast<const uint4*>(a)),
-             __ldg(reinterpret_cast<const uint4*>(b)), p.act, reinterpret_cast<uint4*>(da),
+      // (not by the read-only path: the kernel may begin before the one that writes dh has ended)
+      slope8(*reinterpret_cast<const uint4*>(dh), *reinterpret_cast<const uint4*>(a),
+             *reinterpret_cast<const uint4*>(b), p.act, reinterpret_cast<uint4*>(da),
              reinterpret_cast<uint4*>(db));
     } else {
       for (int j = 0; col + j < p.cols; ++j) {

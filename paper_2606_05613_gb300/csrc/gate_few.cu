@@ -30,20 +30,23 @@ constexpr int kFewAhead = 2;        // windows of a warp in flight
 // (x takes the registers of 8 of them from 9 rows on.)
 constexpr int few_resident(int nt) { return nt == 1 ? 24 : 16; }
 
-// Elements k to k + 7 of a row of D, zeros beyond its end.
+// Elements k to k + 7 of a row of D, zeros beyond its end.  (Not by the read-only path:
+// the kernel may begin before the one that writes x or the weights has ended.)
 template <bool STREAM>
 __device__ __forceinline__ uint4 load8(const __nv_bfloat16* row, int k, int D) {
   if (k + 8 <= D) {
     const uint4* p = reinterpret_cast<const uint4*>(row + k);
     uint4 v;
     if (STREAM)
-      asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                   : "l"(p));
+                   : "l"(p)
+                   : "memory");
     else
-      asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+      asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];"
                    : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                   : "l"(p));
+                   : "l"(p)
+                   : "memory");
     return v;
   }
   uint32_t w[4] = {0, 0, 0, 0};
