@@ -352,8 +352,9 @@ __device__ __forceinline__ void store_bf16(const TileOut& o, int64_t row, int co
 // Chebyshev fit of Numerical Recipes (section 6.2: erfc(x) = t e^(-x^2 + P(t)) for
 // x >= 0, t = 1 / (1 + x / 2), fractional error below 1.2e-7), e^(-x^2) of which is
 // the derivative's too.  Powers of 2 and reciprocals are the hardware's, good to
-// about 2^-22 and rounded arguments' worth more: 2^-18 at most for results that
-// bf16 tells from 0.
+// about 2^-22 and rounded arguments' worth more: 2^-18 at most.  Where e^-a, or the bell
+// of gelu, leaves fp32's normal numbers (a < -87 and -13) the result, below 1e-35 there,
+// is 0.
 __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 power2(float2 x) {
   float2 r;
