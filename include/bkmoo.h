@@ -475,6 +475,117 @@ int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t l
                          int32_t dw_dtype, int32_t accumulate, void* stream);
 
 /*
+ * The operators of a language model around its layers, for the same batches: the
+ * embedding at its front, the norms of queries and keys, and the log probabilities at its
+ * end.  Common to the calls below: `ids`, `positions` and `targets` are device arrays
+ * [T] of int32 (id_bytes 4) or int64 (8).  rows, dw pointers, dw_dtype and accumulate
+ * are those of bkmoo_gate_backward.  Sums are fp32 in an order fixed by the sizes and
+ * bounds: the same call gives the same bits.  Results are rounded once.  T = 0 queues
+ * nothing (gradients that are not added to are set to 0).
+ *
+ * bkmoo_embedding_forward -- y_t = scale W[id_t].  table: [V][D] of dtype (fp32 or bf16)
+ * with rows of ld_table elements, y: [T][D] of the same with rows of ldy, both at any
+ * element's address (16-byte vectors where all rows start on 16 bytes).  An id outside
+ * 0 .. V - 1 is padding: its y is 0.  V < 2^28, D <= 2^23; scale is finite as fp32.
+ */
+int bkmoo_embedding_forward(const void* table, int64_t ld_table, int32_t dtype, int64_t V,
+                            int64_t D, const void* ids, int32_t id_bytes, int64_t T, double scale,
+                            void* y, int64_t ldy, void* stream);
+
+/* Bytes of device workspace bkmoo_embedding_backward needs.  Host only. */
+int bkmoo_embedding_backward_workspace_size(int64_t T, int64_t D, size_t* bytes);
+
+/*
+ * bkmoo_embedding_backward -- dW_k[v] = scale sum of dy_t over language k's rows t with
+ * id_t = v, in the order of t.  dy: [T][D] of dtype, rows of ld_dy, at any element's
+ * address; padding has no gradient, and its rows are not read.  dw: host array of K device
+ * pointers, each to a contiguous [V][D] of dw_dtype at any element's address.  accumulate:
+ * 0 writes every row, 1 adds to the rows that have a token and leaves the others alone.
+ * ws: device, 256-byte aligned, ws_bytes >= the size above, not shared by calls that
+ * overlap.
+ */
+int bkmoo_embedding_backward(const void* dy, int64_t ld_dy, int32_t dtype, const void* ids,
+                             int32_t id_bytes, int64_t T, int64_t V, int64_t D, double scale,
+                             int32_t K, const int64_t* rows, void* const* dw, int32_t dw_dtype,
+                             int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * bkmoo_qk_norm_forward -- every head x of the queries and keys normed, weighed and
+ * rotated by its token's position: y = w x / sqrt(mean(x^2) + eps), then pair i of the
+ * first `rot` elements, (a, b), becomes (a cos - b sin, b cos + a sin) of the angle
+ * position inv_freq[i]; pairs are (i, i + rot / 2), or with `interleaved` (2i, 2i + 1).
+ *
+ * q: bf16, head h of token t at q + t ldq + h head_dim; k, q_out and k_out likewise (columns
+ * of one wider matrix may hold several).  16-byte aligned, row strides multiples of 8.
+ * head_dim: a multiple of 16 up to 256; rot: a multiple of 16 up to head_dim, 0 for none.
+ * q_out may be q, with the same stride, and k_out k; otherwise nothing overlaps.  w_q, w_k:
+ * [head_dim] of w_dtype (fp32 or bf16).  inv_freq: host, rot / 2 radians a position (read
+ * before the call returns); positions may be negative or as far as 2^40: the angle's
+ * fraction of a turn is exact to 2^-32 (and to the rounding of inv_freq).  Squares are summed
+ * in fp32, so elements beyond 1.8e19 leave nothing of their head.
+ */
+int bkmoo_qk_norm_forward(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* w_q,
+                          const void* w_k, int32_t w_dtype, int64_t T, int64_t q_heads,
+                          int64_t k_heads, int64_t head_dim, const void* positions,
+                          int32_t id_bytes, const double* inv_freq, int64_t rot,
+                          int32_t interleaved, double eps, void* q_out, int64_t ldq_out,
+                          void* k_out, int64_t ldk_out, void* stream);
+
+/* Bytes of device workspace bkmoo_qk_norm_backward needs for weight gradients.  Host only. */
+int bkmoo_qk_norm_backward_workspace_size(int64_t head_dim, size_t* bytes);
+
+/*
+ * bkmoo_qk_norm_backward -- from dq_out and dk_out, the gradients of the forward call's
+ * results, and its inputs: dq and dk (dq may be dq_out, with the same stride, and dk dk_out),
+ * and every language's own gradients of the two weights, dw_q[k] and dw_k[k]: contiguous
+ * [head_dim] of dw_dtype at any element's address; both arrays NULL: not wanted (then ws is
+ * not used).  ws: device, 256-byte aligned, ws_bytes >= the size above, not shared by calls
+ * that overlap.
+ */
+int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, const void* dk_out,
+                           int64_t ld_dk_out, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                           const void* w_q, const void* w_k, int32_t w_dtype, int64_t T,
+                           int64_t q_heads, int64_t k_heads, int64_t head_dim, const void* positions,
+                           int32_t id_bytes, const double* inv_freq, int64_t rot,
+                           int32_t interleaved, double eps, int32_t K, const int64_t* rows, void* dq,
+                           int64_t ld_dq, void* dk, int64_t ld_dk, void* const* dw_q,
+                           void* const* dw_k, int32_t dw_dtype, int32_t accumulate, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/*
+ * bkmoo_token_logp_forward -- for each row z of logits, with m = max z and
+ * L = log sum e^(z - m): logp = z[target] - m - L; stats (m, L), what the backward call
+ * needs; entropy -sum p log p; and the n_top most likely tokens with their log
+ * probabilities, the likeliest first, the lower index first among equal logits.
+ *
+ * logits: [T][V] of dtype (fp32 or bf16), rows of ld, at any element's address.  A target
+ * outside 0 .. V - 1 is padding: its logp is 0.  stats: [T][2], 8-byte aligned, or NULL;
+ * entropy: [T] or NULL; n_top: 0 to min(32, V), top_ids and top_logp [T][n_top], unused
+ * where 0.  Minus infinity is a token that is ruled out; a row of nothing else has logp
+ * and top_logp minus infinity (padding 0) and entropy 0; so has a log probability below
+ * fp32's range minus infinity.  A NaN, or plus infinity, makes
+ * its row's results NaN (NaN ranks below minus infinity in top_ids, which are distinct
+ * and in range all the same).  V <= 2^30.
+ */
+int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t dtype, int64_t T, int64_t V,
+                             const void* targets, int32_t id_bytes, float* logp, float* stats,
+                             float* entropy, int32_t n_top, int64_t* top_ids, float* top_logp,
+                             void* stream);
+
+/*
+ * bkmoo_token_logp_backward -- d_logits from d_logp [T] and d_entropy [T] (or NULL), the
+ * gradients of logp and entropy, with the forward call's stats and, for d_entropy, entropy:
+ *   d_logits_v = d_logp ([v = target] - p_v) - d_entropy p_v (log p_v + entropy).
+ * The d_logp of padding counts as 0.  A row whose d_logp and d_entropy are 0 gets zeros and
+ * is not read, nor is a row of nothing but minus infinity.  d_logits: [T][V] of dtype, rows
+ * of ld_d; it may be logits, with the same stride.
+ */
+int bkmoo_token_logp_backward(const void* logits, int64_t ld, int32_t dtype, int64_t T, int64_t V,
+                              const void* targets, int32_t id_bytes, const float* stats,
+                              const float* entropy, const float* d_logp, const float* d_entropy,
+                              void* d_logits, int64_t ld_d, void* stream);
+
+/*
  * bkmoo_op_status -- synchronise `stream` and read the current device's status
  * word of the gate and weight-gradient calls: BKMOO_OK, or BKMOO_ERR_TIMEOUT if
  * one of them gave up since it was last read.  Clears it.  Writes *status.

@@ -1,0 +1,496 @@
+// Queries and keys normed head by head, times a weight, and rotated by their position, and
+// the backward pass with the weights' gradients apart by language (include/bkmoo.h).
+//
+// r = 1 / sqrt(mean(x^2) + eps), n = x r, y = w n, and pairs (a, b) of y turned by
+// pos f_i: a cos - b sin, b cos + a sin.  Back: dy is do turned the other way,
+// dw = sum dy n, dx = r (w dy - n mean(w dy n)).  Everything of a head is in the registers
+// of 1 to 16 lanes, 16 elements each, the two halves of 8 pairs: one pass, bound by memory.
+//
+// A position's angle in turns is pos f / 2 pi, of which only the fraction counts.  The
+// frequency is kept as a 64-bit fraction of a turn, so that the product modulo 2^64 is that
+// fraction, exact however far the position is, without a number of 64 bits' precision.
+#include <math.h>
+
+#include "tile_host.cuh"
+#include "row_ops.cuh"
+
+namespace bkmoo {
+namespace {
+
+constexpr int kQkThreads = 256;
+constexpr int kQkWarps = kQkThreads / 32;
+constexpr int kMaxHead = 256;
+
+struct QkSide {
+  const __nv_bfloat16 *x, *dout;
+  __nv_bfloat16* out;                   // forward: the result; backward: dx
+  const void* w;
+  int64_t ld, ld_dout, ld_out;          // from token to token
+  int32_t heads, steps;                 // steps: groups of heads that a warp takes at once
+};
+struct QkArgs {
+  QkSide side[2];
+  const void* pos;
+  int32_t id_bytes, w_f32;
+  int32_t hd, rot;
+  float eps, inv_hd;
+  int64_t T;
+  uint64_t turn[kMaxHead / 2];          // 2^64 f / 2 pi
+};
+
+// The angles of a token's pairs, [2][rot / 2], by a warp.
+__device__ __forceinline__ void angles(const QkArgs& a, int64_t t, int lane, float (*room)[kMaxHead / 2]) {
+  __syncwarp();
+  const uint64_t pos = (uint64_t)load_id(a.pos, a.id_bytes, t);
+  for (int i = lane; i < a.rot / 2; i += 32) {
+    // half turns in [-1, 1)
+    const float half = __int2float_rn((int32_t)((pos * a.turn[i] + 0x80000000ull) >> 32)) * 0x1p-31f;
+    float s, c;
+    sincospif(half, &s, &c);
+    room[0][i] = c;
+    room[1][i] = s;
+  }
+  __syncwarp();
+}
+
+// Where a lane's 16 elements of a head lie: two vectors of 8.
+struct Place {
+  int lo, hi, pair;                     // columns; its first pair
+  bool live, turns;
+};
+template <bool NEIGHBOURS>
+__device__ __forceinline__ Place place_of_lane(const QkArgs& a, int l) {
+  Place p;
+  p.live = 16 * l < a.hd;
+  p.turns = 16 * l < a.rot;
+  p.pair = 8 * l;
+  p.lo = 16 * l;
+  p.hi = p.lo + 8;
+  if (!NEIGHBOURS && p.turns) {
+    p.lo = 8 * l;
+    p.hi = p.lo + a.rot / 2;
+  }
+  return p;
+}
+struct Angles {
+  float c[8], s[8];
+};
+__device__ __forceinline__ Angles angles_of(const Place& p, float (*room)[kMaxHead / 2]) {
+  Angles g;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    g.c[j] = p.turns ? room[0][p.pair + j] : 1.0f;
+    g.s[j] = p.turns ? room[1][p.pair + j] : 0.0f;
+  }
+  return g;
+}
+// y: the lane's elements, the vector at lo and then the one at hi.  BACK: the other way.
+template <bool NEIGHBOURS, bool BACK>
+__device__ __forceinline__ void rotate(float (&y)[16], const Angles& g) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float& a = y[NEIGHBOURS ? 2 * j : j];
+    float& b = y[NEIGHBOURS ? 2 * j + 1 : j + 8];
+    const float s = BACK ? -g.s[j] : g.s[j], x = a;
+    a = fmaf(-b, s, x * g.c[j]);
+    b = fmaf(x, s, b * g.c[j]);
+  }
+}
+__device__ __forceinline__ void weights_of(const QkArgs& a, const void* w, const Place& p, float (&v)[16]) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const int c = (j < 8 ? p.lo : p.hi) + (j & 7);
+    v[j] = !p.live ? 0.0f
+           : a.w_f32 ? static_cast<const float*>(w)[c]
+                     : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c]);
+  }
+}
+struct Pair {
+  uint4 lo, hi;
+};
+__device__ __forceinline__ Pair load_pair(const __nv_bfloat16* head, const Place& p, bool live) {
+  Pair v;
+  v.lo = v.hi = make_uint4(0, 0, 0, 0);
+  if (live) {
+    v.lo = *reinterpret_cast<const uint4*>(head + p.lo);
+    v.hi = *reinterpret_cast<const uint4*>(head + p.hi);
+  }
+  return v;
+}
+__device__ __forceinline__ void unpack16(const Pair& v, float (&x)[16]) {
+  float a[8], b[8];
+  unpack(v.lo, a);
+  unpack(v.hi, b);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) x[j] = a[j], x[j + 8] = b[j];
+}
+__device__ __forceinline__ void store_pair(__nv_bfloat16* head, const Place& p, const float (&x)[16]) {
+  const float a[8] = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]},
+              b[8] = {x[8], x[9], x[10], x[11], x[12], x[13], x[14], x[15]};
+  *reinterpret_cast<uint4*>(head + p.lo) = repack(a);
+  *reinterpret_cast<uint4*>(head + p.hi) = repack(b);
+}
+template <int G>
+__device__ __forceinline__ float over_head(float v) {
+#pragma unroll
+  for (int w = G / 2; w > 0; w >>= 1) v += __shfl_xor_sync(0xffffffffu, v, w);
+  return v;
+}
+
+// G lanes a head.  A warp takes a run of steps, each 32 / G heads of a token's queries or keys.
+template <int G, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kQkThreads) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
+  grid_wait();
+  __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int per = a.side[0].steps + a.side[1].steps;
+  const int64_t total = a.T * per, from = ((int64_t)blockIdx.x * kQkWarps + wid) * each;
+  const int64_t to = from + each < total ? from + each : total;
+  if (from >= to) return;
+  const Place p = place_of_lane<NEIGHBOURS>(a, lane % G);
+  int64_t t = from / per;
+  int step = (int)(from - t * per);
+  bool new_token = true;
+  int which = -1;
+  Angles g;
+  float w[16];
+  for (int64_t i = from; i < to; ++i) {
+    const int k = step >= a.side[0].steps;
+    const QkSide& s = a.side[k];
+    const int head = (step - (k ? a.side[0].steps : 0)) * (32 / G) + lane / G;
+    const bool live = p.live && head < s.heads;
+    const Pair v = load_pair(s.x + t * s.ld + (int64_t)head * a.hd, p, live);
+    if (new_token) {
+      angles(a, t, lane, room[wid]);
+      g = angles_of(p, room[wid]);
+    }
+    if (which != k) weights_of(a, s.w, p, w);
+    which = k;
+    float x[16], sum = 0.0f;
+    unpack16(v, x);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum = fmaf(x[j], x[j], sum);
+    const float r = rsqrtf(fmaf(over_head<G>(sum), a.inv_hd, a.eps));
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = x[j] * r * w[j];
+    rotate<NEIGHBOURS, false>(x, g);
+    if (live) store_pair(s.out + t * s.ld_out + (int64_t)head * a.hd, p, x);
+    new_token = ++step == per;
+    if (new_token) step = 0, ++t;
+  }
+}
+
+// The backward pass by CTAs that each take a run of one side's and one language's steps.
+struct QkRuns {
+  int32_t K, weights;
+  int32_t first[2 * kMaxK + 1];         // CTAs of (side, language), side by side
+  int64_t rows[kMaxK + 1];
+  float* part;                          // [CTA][hd]
+};
+template <int G, bool NEIGHBOURS>
+__global__ void __launch_bounds__(kQkThreads) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
+                                                                  const __grid_constant__ QkRuns q) {
+  grid_wait();
+  __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % G;
+  int run = 0;
+  while ((int)blockIdx.x >= q.first[run + 1]) ++run;
+  const int k = run / q.K, lang = run % q.K, ctas = q.first[run + 1] - q.first[run];
+  const QkSide& s = a.side[k];
+  const int64_t all = (q.rows[lang + 1] - q.rows[lang]) * s.steps, warps = (int64_t)ctas * kQkWarps;
+  const int64_t me = (int64_t)(blockIdx.x - q.first[run]) * kQkWarps + wid;
+  const int64_t each = (all + warps - 1) / warps;
+  const int64_t from = me * each < all ? me * each : all, to = from + each < all ? from + each : all;
+  const Place p = place_of_lane<NEIGHBOURS>(a, l);
+  float w[16], dw[16] = {};
+  weights_of(a, s.w, p, w);
+  int64_t t = q.rows[lang] + from / s.steps;
+  int step = (int)(from % s.steps);
+  bool new_token = true;
+  Angles g;
+  for (int64_t i = from; i < to; ++i) {
+    const int head = step * (32 / G) + lane / G;
+    const bool live = p.live && head < s.heads;
+    const Pair vx = load_pair(s.x + t * s.ld + (int64_t)head * a.hd, p, live);
+    const Pair vd = load_pair(s.dout + t * s.ld_dout + (int64_t)head * a.hd, p, live);
+    if (new_token) {
+      angles(a, t, lane, room[wid]);
+      g = angles_of(p, room[wid]);
+    }
+    float x[16], d[16], sum = 0.0f, dot = 0.0f;
+    unpack16(vx, x);
+    unpack16(vd, d);
+    rotate<NEIGHBOURS, true>(d, g);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      sum = fmaf(x[j], x[j], sum);
+      dot = fmaf(d[j] * w[j], x[j], dot);
+    }
+    // (0 beyond the last head: without eps, 1 / sqrt(0) would leave NaN in dw)
+    const float squares = over_head<G>(sum), r = live ? rsqrtf(fmaf(squares, a.inv_hd, a.eps)) : 0.0f;
+    const float c = over_head<G>(dot) * r * r * a.inv_hd;     // mean(w dy n) / n's x
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      dw[j] = fmaf(d[j], x[j] * r, dw[j]);
+      d[j] = r * fmaf(-x[j], c, d[j] * w[j]);
+    }
+    if (live) store_pair(s.out + t * s.ld_out + (int64_t)head * a.hd, p, d);
+    new_token = ++step == s.steps;
+    if (new_token) step = 0, ++t;
+  }
+  if (!q.weights) return;
+  __shared__ float sums[kQkWarps][kMaxHead];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+#pragma unroll
+    for (int h = G; h < 32; h *= 2) dw[j] += __shfl_xor_sync(0xffffffffu, dw[j], h);
+    if (lane < G && p.live) sums[wid][(j < 8 ? p.lo : p.hi) + (j & 7)] = dw[j];
+  }
+  __syncthreads();
+  for (int c = threadIdx.x; c < a.hd; c += kQkThreads) {
+    float v = 0.0f;
+    for (int i = 0; i < kQkWarps; ++i) v += sums[i][c];
+    q.part[(int64_t)blockIdx.x * a.hd + c] = v;
+  }
+}
+
+// The CTAs' sums of one side's and one language's columns joined in the order of the CTAs,
+// 32 columns a CTA.
+struct QkWeightGrads {
+  void* dw[2 * kMaxK];
+  int32_t first[2 * kMaxK + 1];
+  const float* part;
+  int32_t hd, f32, accumulate;
+};
+__global__ void __launch_bounds__(1024) qk_weight_kernel(const __grid_constant__ QkWeightGrads a) {
+  grid_wait();
+  const int run = blockIdx.x, c = blockIdx.y * 32 + (threadIdx.x & 31), at = threadIdx.x >> 5;
+  __shared__ float sums[32][32];
+  float v = 0.0f;
+  if (c < a.hd)
+    for (int i = a.first[run] + at; i < a.first[run + 1]; i += 32) v += a.part[(int64_t)i * a.hd + c];
+  sums[at][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (at != 0 || c >= a.hd) return;
+  for (int i = 1; i < 32; ++i) v += sums[i][threadIdx.x];
+  if (a.f32) {
+    float* p = static_cast<float*>(a.dw[run]) + c;
+    *p = a.accumulate ? *p + v : v;
+  } else {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.dw[run]) + c;
+    *p = __float2bfloat16_rn(a.accumulate ? __bfloat162float(*p) + v : v);
+  }
+}
+
+template <int G>
+const void* forward_fn(bool n) {
+  return n ? (const void*)qk_norm_kernel<G, true> : (const void*)qk_norm_kernel<G, false>;
+}
+template <int G>
+const void* backward_fn(bool n) {
+  return n ? (const void*)qk_norm_grad_kernel<G, true> : (const void*)qk_norm_grad_kernel<G, false>;
+}
+
+int lanes_of(int64_t hd) {
+  int g = 1;
+  while (16 * g < hd) g *= 2;
+  return g;
+}
+
+bool heads_ok(const void* p, int64_t T, int64_t heads, int64_t hd, int64_t ld) {
+  return T == 0 || (aligned_at(p, 16) && ld >= heads * hd && ld % 8 == 0 && ld <= ((int64_t)1 << 38));
+}
+bool qk_sizes_ok(int64_t T, int64_t hq, int64_t hk, int64_t hd, const double* freq, int64_t rot, double eps) {
+  if (T < 0 || T > ((int64_t)1 << 31) - 1024 || hq < 1 || hk < 1 || hq > 65536 || hk > 65536 || hd < 16 ||
+      hd > kMaxHead || hd % 16 || rot < 0 || rot > hd || rot % 16 || !(eps >= 0.0) || !std::isfinite(eps) ||
+      (rot > 0 && !freq))
+    return false;
+  for (int64_t i = 0; i < rot / 2; ++i)
+    if (!std::isfinite(freq[i])) return false;
+  return true;
+}
+void fill(QkArgs& a, int64_t T, int64_t hq, int64_t hk, int64_t hd, const double* freq, int64_t rot, double eps) {
+  const int at_once = 32 / lanes_of(hd);
+  a.side[0].heads = (int32_t)hq;
+  a.side[1].heads = (int32_t)hk;
+  for (int i = 0; i < 2; ++i) a.side[i].steps = (a.side[i].heads + at_once - 1) / at_once;
+  a.hd = (int32_t)hd;
+  a.rot = (int32_t)rot;
+  a.eps = (float)eps;
+  a.inv_hd = 1.0f / (float)hd;
+  a.T = T;
+  for (int64_t i = 0; i < rot / 2; ++i) {
+    const double turns = freq[i] * 0.15915494309189533577;        // 1 / 2 pi
+    const double part = std::ldexp(turns - std::floor(turns), 64);
+    a.turn[i] = part < 18446744073709551616.0 ? (uint64_t)part : 0;
+  }
+}
+// CTAs that are resident at once.
+int resident(const void* fn, int* ctas) {
+  int dev = 0, sms = 0, per = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, fn, kQkThreads, 0) != cudaSuccess)
+    return BKMOO_ERR_CUDA;
+  *ctas = sms * (per < 1 ? 1 : per);
+  return BKMOO_OK;
+}
+constexpr int kMostCtas = 2048;         // of the backward pass, whose sums the workspace holds
+
+bool places_ok(void* const* dw, int32_t K, int32_t dtype) {
+  for (int k = 0; k < K; ++k)
+    if (!aligned_at(dw[k], float_bytes(dtype))) return false;
+  return true;
+}
+
+}  // namespace
+}  // namespace bkmoo
+
+using namespace bkmoo;
+
+extern "C" int bkmoo_qk_norm_forward(const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                     const void* w_q, const void* w_k, int32_t w_dtype, int64_t T,
+                                     int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                     const void* positions, int32_t id_bytes, const double* inv_freq,
+                                     int64_t rot, int32_t interleaved, double eps, void* q_out,
+                                     int64_t ldq_out, void* k_out, int64_t ldk_out, void* stream) {
+  if (!is_float(w_dtype) || !is_id(id_bytes) || !qk_sizes_ok(T, q_heads, k_heads, head_dim, inv_freq, rot, eps) ||
+      !aligned_at(w_q, float_bytes(w_dtype)) || !aligned_at(w_k, float_bytes(w_dtype)))
+    return BKMOO_ERR_INVALID;
+  if (T == 0) return BKMOO_OK;
+  if (!heads_ok(q, T, q_heads, head_dim, ldq) || !heads_ok(k, T, k_heads, head_dim, ldk) ||
+      !heads_ok(q_out, T, q_heads, head_dim, ldq_out) || !heads_ok(k_out, T, k_heads, head_dim, ldk_out) ||
+      (q == q_out && ldq != ldq_out) || (k == k_out && ldk != ldk_out) || !aligned_at(positions, id_bytes))
+    return BKMOO_ERR_INVALID;
+  QkArgs a = {};
+  fill(a, T, q_heads, k_heads, head_dim, inv_freq, rot, eps);
+  a.side[0].x = static_cast<const __nv_bfloat16*>(q);
+  a.side[1].x = static_cast<const __nv_bfloat16*>(k);
+  a.side[0].out = static_cast<__nv_bfloat16*>(q_out);
+  a.side[1].out = static_cast<__nv_bfloat16*>(k_out);
+  a.side[0].w = w_q;
+  a.side[1].w = w_k;
+  a.side[0].ld = ldq;
+  a.side[1].ld = ldk;
+  a.side[0].ld_out = ldq_out;
+  a.side[1].ld_out = ldk_out;
+  a.pos = positions;
+  a.id_bytes = id_bytes;
+  a.w_f32 = w_dtype == BKMOO_F32;
+  const int g = lanes_of(head_dim);
+  const void* fn = g == 1   ? forward_fn<1>(interleaved)
+                   : g == 2 ? forward_fn<2>(interleaved)
+                   : g == 4 ? forward_fn<4>(interleaved)
+                   : g == 8 ? forward_fn<8>(interleaved)
+                            : forward_fn<16>(interleaved);
+  int ctas = 0;
+  if (resident(fn, &ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  const int64_t total = T * (a.side[0].steps + a.side[1].steps);
+  int64_t each = (total + (int64_t)ctas * kQkWarps - 1) / ((int64_t)ctas * kQkWarps);
+  const int64_t grid = (total + each * kQkWarps - 1) / (each * kQkWarps);
+  void* list[] = {&a, &each};
+  return launch_behind(fn, dim3((unsigned)grid), dim3(kQkThreads), list, 0, static_cast<cudaStream_t>(stream),
+                       true) == cudaSuccess
+             ? BKMOO_OK
+             : BKMOO_ERR_CUDA;
+}
+
+extern "C" int bkmoo_qk_norm_backward_workspace_size(int64_t head_dim, size_t* bytes) {
+  if (!bytes || head_dim < 16 || head_dim > kMaxHead || head_dim % 16) return BKMOO_ERR_INVALID;
+  *bytes = (size_t)kMostCtas * (size_t)head_dim * sizeof(float);
+  return BKMOO_OK;
+}
+
+extern "C" int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, const void* dk_out,
+                                      int64_t ld_dk_out, const void* q, int64_t ldq, const void* k,
+                                      int64_t ldk, const void* w_q, const void* w_k, int32_t w_dtype,
+                                      int64_t T, int64_t q_heads, int64_t k_heads, int64_t head_dim,
+                                      const void* positions, int32_t id_bytes, const double* inv_freq,
+                                      int64_t rot, int32_t interleaved, double eps, int32_t K,
+                                      const int64_t* rows, void* dq, int64_t ld_dq, void* dk,
+                                      int64_t ld_dk, void* const* dw_q, void* const* dw_k,
+                                      int32_t dw_dtype, int32_t accumulate, void* ws, size_t ws_bytes,
+                                      void* stream) {
+  const bool weights = dw_q || dw_k;
+  if (!is_float(w_dtype) || !is_id(id_bytes) || !is_float(dw_dtype) ||
+      !qk_sizes_ok(T, q_heads, k_heads, head_dim, inv_freq, rot, eps) || !languages_ok(rows, K, T) ||
+      !aligned_at(w_q, float_bytes(w_dtype)) || !aligned_at(w_k, float_bytes(w_dtype)) ||
+      (weights && (!dw_q || !dw_k || !places_ok(dw_q, K, dw_dtype) || !places_ok(dw_k, K, dw_dtype))) ||
+      (weights && !aligned_at(ws, 256)) || !heads_ok(q, T, q_heads, head_dim, ldq) ||
+      !heads_ok(k, T, k_heads, head_dim, ldk) || !heads_ok(dq_out, T, q_heads, head_dim, ld_dq_out) ||
+      !heads_ok(dk_out, T, k_heads, head_dim, ld_dk_out) || !heads_ok(dq, T, q_heads, head_dim, ld_dq) ||
+      !heads_ok(dk, T, k_heads, head_dim, ld_dk) ||
+      (T > 0 && ((dq == dq_out && ld_dq != ld_dq_out) || (dk == dk_out && ld_dk != ld_dk_out) ||
+                 !aligned_at(positions, id_bytes))))
+    return BKMOO_ERR_INVALID;
+  size_t need = 0;
+  if (bkmoo_qk_norm_backward_workspace_size(head_dim, &need) != BKMOO_OK) return BKMOO_ERR_INVALID;
+  if (weights && ws_bytes < need) return BKMOO_ERR_WORKSPACE;
+  if (T == 0 && (!weights || accumulate)) return BKMOO_OK;
+  QkArgs a = {};
+  fill(a, T, q_heads, k_heads, head_dim, inv_freq, rot, eps);
+  const void* x[2] = {q, k};
+  const void* d[2] = {dq_out, dk_out};
+  void* out[2] = {dq, dk};
+  const void* w[2] = {w_q, w_k};
+  const int64_t ld[2] = {ldq, ldk}, ld_dout[2] = {ld_dq_out, ld_dk_out}, ld_out[2] = {ld_dq, ld_dk};
+  for (int i = 0; i < 2; ++i) {
+    QkSide& s = a.side[i];
+    s.x = static_cast<const __nv_bfloat16*>(x[i]);
+    s.dout = static_cast<const __nv_bfloat16*>(d[i]);
+    s.out = static_cast<__nv_bfloat16*>(out[i]);
+    s.w = w[i];
+    s.ld = ld[i];
+    s.ld_dout = ld_dout[i];
+    s.ld_out = ld_out[i];
+  }
+  a.pos = positions;
+  a.id_bytes = id_bytes;
+  a.w_f32 = w_dtype == BKMOO_F32;
+  const int g = lanes_of(head_dim);
+  const void* fn = g == 1   ? backward_fn<1>(interleaved)
+                   : g == 2 ? backward_fn<2>(interleaved)
+                   : g == 4 ? backward_fn<4>(interleaved)
+                   : g == 8 ? backward_fn<8>(interleaved)
+                            : backward_fn<16>(interleaved);
+  int ctas = 0;
+  if (resident(fn, &ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  // one CTA more for each part that is not whole
+  const int most = kMostCtas - 2 * kMaxK;
+  if (ctas > most) ctas = most;
+  QkRuns r = {};
+  r.K = K;
+  r.weights = weights;
+  r.part = static_cast<float*>(ws);
+  const int64_t total = T * (a.side[0].steps + a.side[1].steps);
+  int64_t budget = (total + ctas - 1) / ctas;            // steps of a CTA
+  if (budget < kQkWarps) budget = kQkWarps;
+  for (int i = 0; i < 2; ++i)
+    for (int l = 0; l < K; ++l) {
+      const int64_t steps = (rows[l + 1] - rows[l]) * a.side[i].steps;
+      r.first[i * K + l + 1] = r.first[i * K + l] + (int32_t)((steps + budget - 1) / budget);
+    }
+  for (int l = 0; l <= K; ++l) r.rows[l] = rows[l];
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const int grid = r.first[2 * K];
+  if (grid > 0) {
+    void* list[] = {&a, &r};
+    if (launch_behind(fn, dim3(grid), dim3(kQkThreads), list, 0, s, true) != cudaSuccess) return BKMOO_ERR_CUDA;
+  }
+  if (!weights) return BKMOO_OK;
+  QkWeightGrads v = {};
+  for (int l = 0; l < K; ++l) {
+    v.dw[l] = dw_q[l];
+    v.dw[K + l] = dw_k[l];
+  }
+  for (int i = 0; i <= 2 * K; ++i) v.first[i] = r.first[i];
+  v.part = r.part;
+  v.hd = a.hd;
+  v.f32 = dw_dtype == BKMOO_F32;
+  v.accumulate = accumulate;
+  void* list[] = {&v};
+  return launch_behind((const void*)qk_weight_kernel, dim3(2 * K, (a.hd + 31) / 32), dim3(1024), list, 0, s, true) ==
+                 cudaSuccess
+             ? BKMOO_OK
+             : BKMOO_ERR_CUDA;
+}

@@ -156,6 +156,27 @@ def load():
         lib.bkmoo_adamw.restype = ctypes.c_int
         lib.bkmoo_adamw.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp, vp, vp, vp, i32,
                                     ctypes.POINTER(bkmoo_adamw_params), vp, vp]
+        f64 = ctypes.c_double
+        lib.bkmoo_embedding_forward.restype = ctypes.c_int
+        lib.bkmoo_embedding_forward.argtypes = [vp, i64, i32, i64, i64, vp, i32, i64, f64, vp, i64, vp]
+        lib.bkmoo_embedding_backward_workspace_size.restype = ctypes.c_int
+        lib.bkmoo_embedding_backward_workspace_size.argtypes = [i64, i64, ctypes.POINTER(sz)]
+        lib.bkmoo_embedding_backward.restype = ctypes.c_int
+        lib.bkmoo_embedding_backward.argtypes = [vp, i64, i32, vp, i32, i64, i64, i64, f64, i32, vp, vp,
+                                                 i32, i32, vp, sz, vp]
+        lib.bkmoo_qk_norm_forward.restype = ctypes.c_int
+        lib.bkmoo_qk_norm_forward.argtypes = [vp, i64, vp, i64, vp, vp, i32, i64, i64, i64, i64, vp, i32,
+                                              vp, i64, i32, f64, vp, i64, vp, i64, vp]
+        lib.bkmoo_qk_norm_backward_workspace_size.restype = ctypes.c_int
+        lib.bkmoo_qk_norm_backward_workspace_size.argtypes = [i64, ctypes.POINTER(sz)]
+        lib.bkmoo_qk_norm_backward.restype = ctypes.c_int
+        lib.bkmoo_qk_norm_backward.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i32, i64, i64,
+                                               i64, i64, vp, i32, vp, i64, i32, f64, i32, vp, vp, i64,
+                                               vp, i64, vp, vp, i32, i32, vp, sz, vp]
+        lib.bkmoo_token_logp_forward.restype = ctypes.c_int
+        lib.bkmoo_token_logp_forward.argtypes = [vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, i32, vp, vp, vp]
+        lib.bkmoo_token_logp_backward.restype = ctypes.c_int
+        lib.bkmoo_token_logp_backward.argtypes = [vp, i64, i32, i64, i64, vp, i32, vp, vp, vp, vp, vp, i64, vp]
         _lib = lib
         return lib
 
@@ -476,6 +497,14 @@ def _weight_grads(dw, K: int, rows: int, cols: int, dev: int, what: str):
     return (ctypes.c_void_p * K)(*at), _dtype_code(dw[0])
 
 
+def _vector_grads(dw, K: int, n: int, dev: int, what: str):
+    """The same of per-language gradients of a vector of n."""
+    if len(dw) != K:
+        raise ValueError("%s: one gradient per language, %d" % (what, K))
+    dt = dw[0].dtype
+    return (ctypes.c_void_p * K)(*[_plain(g, dt, n, dev, what) for g in dw]), _dtype_code(dw[0])
+
+
 def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None):
     """h = act(x w_gate^T) * (x w_up^T), and a = x w_gate^T, b = x w_up^T for the
     backward pass where given.  x [T, D], weights [F, D], outputs [T, F], all
@@ -551,6 +580,226 @@ def bkmoo_language_wgrad(dy, x, rows, dw, accumulate=False, stream=None):
     _op_devices.add(dev)
     _call(torch, dev, "bkmoo_language_wgrad", load().bkmoo_language_wgrad, pd, ldd, px, ldx, T, M,
           N, K, r, g, dt, 1 if accumulate else 0, _raw_stream(torch, stream, dev))
+
+
+def _float_rows(t, rows: int, cols: int, dev: int, dtype, what: str):
+    """(address, row stride) of a matrix of any alignment."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != (rows, cols):
+        raise ValueError("%s must be a matrix of %d x %d, %s, on cuda:%d, got %s %s on %s"
+                         % (what, rows, cols, dtype, dev, t.dtype, tuple(t.shape), t.device))
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError("%s must have contiguous rows" % what)
+    if rows < 2:
+        ld = cols
+    if ld < cols:
+        raise ValueError("%s: rows must not overlap" % what)
+    return t.data_ptr(), ld
+
+
+def _whole_numbers(torch, t, T: int, dev: int, what: str):
+    """(address, bytes of one) of T ids or positions."""
+    if t.get_device() != dev or t.numel() != T or not t.is_contiguous() or \
+            (t.dtype is not torch.int64 and t.dtype is not torch.int32):
+        raise ValueError("%s must be %d contiguous int64 or int32 on cuda:%d" % (what, T, dev))
+    return t.data_ptr(), 8 if t.dtype is torch.int64 else 4
+
+
+def _plain(t, dtype, numel: int, dev: int, what: str):
+    """Address of a contiguous tensor, or None of None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != dev or t.numel() != numel or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous %s on cuda:%d" % (what, numel, dtype, dev))
+    return t.data_ptr()
+
+
+def bkmoo_embedding_forward(table, ids, out, scale=1.0, stream=None):
+    """out[t] = scale table[ids[t]], 0 where ids[t] is outside the table.  table [V, D]
+    and out [T, D] float32 or bfloat16 (one dtype), ids [T] int64 or int32."""
+    import torch
+    V, D, dev = _cuda_matrix(table, "table")
+    T = ids.numel()
+    pt, ldt = _float_rows(table, V, D, dev, table.dtype, "table")
+    po, ldo = _float_rows(out, T, D, dev, table.dtype, "out")
+    pi, nb = _whole_numbers(torch, ids, T, dev, "ids")
+    _call(torch, dev, "bkmoo_embedding_forward", load().bkmoo_embedding_forward, pt, ldt,
+          _dtype_code(table), V, D, pi, nb, T, scale, po, ldo, _raw_stream(torch, stream, dev))
+
+
+def bkmoo_embedding_backward_workspace_size(T: int, D: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().bkmoo_embedding_backward_workspace_size(T, D, ctypes.byref(n)),
+           "bkmoo_embedding_backward_workspace_size")
+    return int(n.value)
+
+
+def bkmoo_embedding_backward(dy, ids, rows, dw, scale=1.0, accumulate=False, ws=None, stream=None):
+    """dw[k][v] = scale sum of dy[t] over language k's rows (rows[k] to rows[k + 1]) with
+    ids[t] = v, or added to it.  dy [T, D] float32 or bfloat16; dw[k] contiguous [V, D],
+    float32 or bfloat16.  ws: a CUDA byte tensor of bkmoo_embedding_backward_workspace_size;
+    allocated (torch, on `stream`) where None."""
+    import torch
+    T, D, dev = _cuda_matrix(dy, "dy")
+    K, r = _language_rows(rows, T)
+    pd, ldd = _float_rows(dy, T, D, dev, dy.dtype, "dy")
+    pi, nb = _whole_numbers(torch, ids, T, dev, "ids")
+    V = dw[0].shape[0] if len(dw) else 0
+    g, dt = _weight_grads(dw, K, V, D, dev, "dw")
+    if ws is None:
+        ws = _scratch(torch, bkmoo_embedding_backward_workspace_size(T, D), dev, stream)
+    pws, nws = _workspace(ws, dev)
+    _call(torch, dev, "bkmoo_embedding_backward", load().bkmoo_embedding_backward, pd, ldd,
+          _dtype_code(dy), pi, nb, T, V, D, scale, K, r, g, dt, 1 if accumulate else 0, pws, nws,
+          _raw_stream(torch, stream, dev))
+
+
+def rope_frequencies(rot: int, base: float):
+    """The rotation's frequencies base^(-2i / rot), radians a position, for the calls below
+    (which take any sequence of them)."""
+    n = rot // 2
+    return (ctypes.c_double * n)(*[base ** (-2.0 * i / rot) for i in range(n)])
+
+
+def _frequencies(inv_freq):
+    """(array, rot)."""
+    if not isinstance(inv_freq, ctypes.Array) or inv_freq._type_ is not ctypes.c_double:
+        inv_freq = (ctypes.c_double * len(inv_freq))(*[float(f) for f in inv_freq])
+    return inv_freq, 2 * len(inv_freq)
+
+
+def _heads(t, T: int, heads: int, width: int, dev: int, bf16, what: str):
+    """(address, stride from token to token) of [T, heads, width]."""
+    if t.dtype is not bf16 or t.get_device() != dev or t.shape != (T, heads, width):
+        raise ValueError("%s must be bfloat16 of %d x %d x %d on cuda:%d, got %s %s on %s"
+                         % (what, T, heads, width, dev, t.dtype, tuple(t.shape), t.device))
+    ld, between, step = t.stride()
+    if (step != 1 and width > 1) or (between != width and heads > 1):
+        raise ValueError("%s: a token's heads must be contiguous" % what)
+    if T < 2:
+        ld = (heads * width + 7) // 8 * 8
+    p = t.data_ptr()
+    if ld < heads * width or ld % 8 or p % 16:
+        raise ValueError("%s: tokens must start on 16 bytes" % what)
+    return p, ld
+
+
+def _cuda_heads(t, what: str):
+    dev = t.get_device()
+    if dev < 0 or t.dim() != 3:
+        raise ValueError("%s must be a CUDA tensor [tokens, heads, width]" % what)
+    return (*t.shape, dev)
+
+
+def bkmoo_qk_norm_forward(q, k, w_q, w_k, positions, inv_freq, q_out, k_out, eps=1e-6,
+                          interleaved=False, stream=None):
+    """Queries [T, heads, width] and keys [T, key heads, width] normed per head, times w_q and
+    w_k [width], the first 2 len(inv_freq) elements rotated by positions [T]; pairs half the
+    rotated width apart, or neighbours where `interleaved`.  q and k bfloat16, the heads of a
+    token contiguous; q_out may be q and k_out k."""
+    import torch
+    bf16 = torch.bfloat16
+    T, hq, width, dev = _cuda_heads(q, "q")
+    hk = k.shape[1]
+    pq, ldq = _heads(q, T, hq, width, dev, bf16, "q")
+    pk, ldk = _heads(k, T, hk, width, dev, bf16, "k")
+    po, ldo = _heads(q_out, T, hq, width, dev, bf16, "q_out")
+    pp, ldp = _heads(k_out, T, hk, width, dev, bf16, "k_out")
+    wq, wk = _plain(w_q, w_q.dtype, width, dev, "w_q"), _plain(w_k, w_q.dtype, width, dev, "w_k")
+    pos, nb = _whole_numbers(torch, positions, T, dev, "positions")
+    f, rot = _frequencies(inv_freq)
+    _call(torch, dev, "bkmoo_qk_norm_forward", load().bkmoo_qk_norm_forward, pq, ldq, pk, ldk, wq, wk,
+          _dtype_code(w_q), T, hq, hk, width, pos, nb, f, rot, 1 if interleaved else 0, eps, po, ldo,
+          pp, ldp, _raw_stream(torch, stream, dev))
+
+
+def bkmoo_qk_norm_backward_workspace_size(width: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load().bkmoo_qk_norm_backward_workspace_size(width, ctypes.byref(n)),
+           "bkmoo_qk_norm_backward_workspace_size")
+    return int(n.value)
+
+
+def bkmoo_qk_norm_backward(dq_out, dk_out, q, k, w_q, w_k, positions, inv_freq, rows, dq, dk, dw_q=None,
+                           dw_k=None, eps=1e-6, interleaved=False, accumulate=False, ws=None, stream=None):
+    """From dq_out and dk_out, with the forward pass's inputs: dq and dk (which may be dq_out
+    and dk_out), and for every language its own dw_q[k], dw_k[k] (contiguous [width], float32 or
+    bfloat16; both lists may be None).  ws: a CUDA byte tensor of
+    bkmoo_qk_norm_backward_workspace_size; allocated (torch, on `stream`) where None."""
+    import torch
+    bf16 = torch.bfloat16
+    T, hq, width, dev = _cuda_heads(q, "q")
+    hk = k.shape[1]
+    K, r = _language_rows(rows, T)
+    pq, ldq = _heads(q, T, hq, width, dev, bf16, "q")
+    pk, ldk = _heads(k, T, hk, width, dev, bf16, "k")
+    pa, lda = _heads(dq_out, T, hq, width, dev, bf16, "dq_out")
+    pb, ldb = _heads(dk_out, T, hk, width, dev, bf16, "dk_out")
+    po, ldo = _heads(dq, T, hq, width, dev, bf16, "dq")
+    pp, ldp = _heads(dk, T, hk, width, dev, bf16, "dk")
+    wq, wk = _plain(w_q, w_q.dtype, width, dev, "w_q"), _plain(w_k, w_q.dtype, width, dev, "w_k")
+    pos, nb = _whole_numbers(torch, positions, T, dev, "positions")
+    f, rot = _frequencies(inv_freq)
+    gq = gk = pws = None
+    dt, nws = BKMOO_F32, 0
+    if (dw_q is None) != (dw_k is None):
+        raise ValueError("dw_q and dw_k come together")
+    if dw_q is not None:
+        gq, dt = _vector_grads(dw_q, K, width, dev, "dw_q")
+        gk, du = _vector_grads(dw_k, K, width, dev, "dw_k")
+        if dt != du:
+            raise ValueError("dw_q and dw_k must have one dtype")
+        if ws is None:
+            ws = _scratch(torch, bkmoo_qk_norm_backward_workspace_size(width), dev, stream)
+    if ws is not None:
+        pws, nws = _workspace(ws, dev)
+    _call(torch, dev, "bkmoo_qk_norm_backward", load().bkmoo_qk_norm_backward, pa, lda, pb, ldb, pq, ldq,
+          pk, ldk, wq, wk, _dtype_code(w_q), T, hq, hk, width, pos, nb, f, rot, 1 if interleaved else 0,
+          eps, K, r, po, ldo, pp, ldp, gq, gk, dt, 1 if accumulate else 0, pws, nws,
+          _raw_stream(torch, stream, dev))
+
+
+def bkmoo_token_logp_forward(logits, targets, logp, stats=None, entropy=None, top_ids=None, top_logp=None,
+                             stream=None):
+    """logp[t] = log probability of targets[t] under logits[t] (0 where the target is outside
+    the vocabulary), with stats [T, 2] for the backward pass, the rows' entropy [T], and their
+    n most likely tokens, top_ids [T, n] int64 and top_logp [T, n], where given.  logits [T, V]
+    float32 or bfloat16; the others float32."""
+    import torch
+    f32 = torch.float32
+    T, V, dev = _cuda_matrix(logits, "logits")
+    pl, ld = _float_rows(logits, T, V, dev, logits.dtype, "logits")
+    pt, nb = _whole_numbers(torch, targets, T, dev, "targets")
+    if (top_ids is None) != (top_logp is None):
+        raise ValueError("top_ids and top_logp come together")
+    n = 0
+    if top_ids is not None:
+        n = top_ids.shape[-1]
+        if top_ids.shape != (T, n) or top_logp.shape != (T, n):
+            raise ValueError("top_ids and top_logp must be [tokens, n]")
+    _call(torch, dev, "bkmoo_token_logp_forward", load().bkmoo_token_logp_forward, pl, ld,
+          _dtype_code(logits), T, V, pt, nb, _plain(logp, f32, T, dev, "logp"),
+          _plain(stats, f32, 2 * T, dev, "stats"), _plain(entropy, f32, T, dev, "entropy"), n,
+          _plain(top_ids, torch.int64, n * T, dev, "top_ids"),
+          _plain(top_logp, f32, n * T, dev, "top_logp"), _raw_stream(torch, stream, dev))
+
+
+def bkmoo_token_logp_backward(logits, targets, stats, d_logp, d_logits, entropy=None, d_entropy=None,
+                              stream=None):
+    """d_logits [T, V] (which may be logits) from d_logp [T], with the forward pass's stats,
+    and from d_entropy [T] with its entropy where given."""
+    import torch
+    f32 = torch.float32
+    T, V, dev = _cuda_matrix(logits, "logits")
+    pl, ld = _float_rows(logits, T, V, dev, logits.dtype, "logits")
+    po, ldo = _float_rows(d_logits, T, V, dev, logits.dtype, "d_logits")
+    pt, nb = _whole_numbers(torch, targets, T, dev, "targets")
+    if d_entropy is not None and entropy is None:
+        raise ValueError("d_entropy goes with entropy")
+    _call(torch, dev, "bkmoo_token_logp_backward", load().bkmoo_token_logp_backward, pl, ld,
+          _dtype_code(logits), T, V, pt, nb, _plain(stats, f32, 2 * T, dev, "stats"),
+          _plain(entropy, f32, T, dev, "entropy"), _plain(d_logp, f32, T, dev, "d_logp"),
+          _plain(d_entropy, f32, T, dev, "d_entropy"), po, ldo, _raw_stream(torch, stream, dev))
 
 
 def bkmoo_op_status(device=None, stream=None) -> int:
