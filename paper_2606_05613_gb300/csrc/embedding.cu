@@ -21,9 +21,8 @@ namespace bkmoo {
 namespace {
 
 constexpr int kEmbedThreads = 256;
-constexpr int kSortRun = 1024;          // rows that a CTA sorts
+constexpr int kSortRun = 256;           // rows that a CTA sorts
 constexpr int kMerge = 32;              // runs merged at once
-constexpr int kPiece = 32;              // places of a warp
 constexpr int kColumns = 256;           // columns of a warp: 8 a lane
 constexpr uint32_t kNoToken = 0xffffffffu;
 
@@ -37,32 +36,83 @@ struct LookupArgs {
   uint32_t D, per;                      // columns; threads' pieces of a row
   float scale;
 };
-// VEC: 16 bytes a thread at a time, else an element.
-template <class E, bool VEC>
-__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const LookupArgs a) {
+// VEC: 16 bytes a thread at a time, else an element.  A thread has AHEAD of them on their way
+// at once: 4 where there are more than the card holds threads.
+template <class E, bool VEC, int AHEAD>
+__global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_constant__ LookupArgs a) {
   grid_wait();
   constexpr int N = VEC ? kVec<E> : 1;
   const int64_t n = a.T * a.per;
-  for (int64_t i = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kEmbedThreads) {
-    const int64_t t = n < (1ll << 32) ? (uint32_t)i / a.per : i / a.per;
-    const int64_t c = (i - t * a.per) * N;
-    const int64_t id = load_id(a.ids, a.id_bytes, t);
-    const bool none = id < 0 || id >= a.V;
-    const E* from = static_cast<const E*>(a.table) + (none ? 0 : id) * a.ld + c;
-    E* to = static_cast<E*>(a.y) + t * a.ld_y + c;
-    if (VEC) {
-      float x[kVec<E>] = {};
-      if (!none) unpack(*reinterpret_cast<const uint4*>(from), x);
+  for (int64_t i0 = (int64_t)blockIdx.x * (kEmbedThreads * AHEAD) + threadIdx.x; i0 < n;
+       i0 += (int64_t)gridDim.x * (kEmbedThreads * AHEAD)) {
+    int64_t t[AHEAD], c[AHEAD], id[AHEAD];
+    uint4 v[AHEAD];
+    float x[AHEAD];
 #pragma unroll
-      for (int j = 0; j < kVec<E>; ++j) x[j] *= a.scale;
-      *reinterpret_cast<uint4*>(to) = repack(x);
-    } else {
-      *to = narrow<E>(none ? 0.0f : widen(*from) * a.scale);
+    for (int j = 0; j < AHEAD; ++j) {
+      const int64_t i = i0 + j * kEmbedThreads;
+      id[j] = -1;
+      if (i >= n) continue;
+      t[j] = n < (1ll << 32) ? (uint32_t)i / a.per : i / a.per;
+      c[j] = (i - t[j] * a.per) * N;
+      id[j] = load_id(a.ids, a.id_bytes, t[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const bool none = id[j] < 0 || id[j] >= a.V;
+      const E* from = static_cast<const E*>(a.table) + (none ? 0 : id[j] * a.ld + c[j]);
+      v[j] = make_uint4(0, 0, 0, 0);
+      x[j] = 0.0f;
+      if (VEC && !none) v[j] = *reinterpret_cast<const uint4*>(from);
+      if (!VEC && !none) x[j] = widen(*from);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (i0 + j * kEmbedThreads >= n) break;
+      E* to = static_cast<E*>(a.y) + t[j] * a.ld_y + c[j];
+      if (VEC) {
+        float y[kVec<E>];
+        unpack(v[j], y);
+#pragma unroll
+        for (int e = 0; e < kVec<E>; ++e) y[e] *= a.scale;
+        *reinterpret_cast<uint4*>(to) = repack(y);
+      } else {
+        *to = narrow<E>(x[j] * a.scale);
+      }
     }
   }
 }
+template <class E>
+const void* embed_fn(bool vec, bool ahead) {
+  return vec ? ahead ? (const void*)embed_kernel<E, true, 4> : (const void*)embed_kernel<E, true, 1>
+             : ahead ? (const void*)embed_kernel<E, false, 4> : (const void*)embed_kernel<E, false, 1>;
+}
 
 // ---- order -----------------------------------------------------------------
+
+// Gradients that are written instead of added to begin as 0.  The kernels of the order, which
+// leave most of the card idle, have CTAs for that beside their own.
+constexpr int kFillBytes = 32768;
+struct FillArgs {
+  void* dw[kMaxK];
+  int64_t bytes;                        // of a language's gradient
+  int64_t units, from, own;             // kFillBytes in a gradient; the first here; CTAs ahead of them
+};
+__device__ __forceinline__ void fill(const FillArgs& a) {
+  const int64_t i = a.from + blockIdx.x - a.own, k = i / a.units, u = i - k * a.units;
+  char* p = static_cast<char*>(a.dw[k]);
+  const int64_t ahead = (int64_t)(-(uintptr_t)p & 15), whole = a.bytes > ahead ? (a.bytes - ahead) & ~(int64_t)15 : 0;
+  if (u == 0) {                         // what lies outside the whole vectors, by 2 bytes
+    const int64_t c = threadIdx.x < 8 ? 2 * threadIdx.x : ahead + whole + 2 * (threadIdx.x - 8);
+    if (threadIdx.x < 16 && c < (threadIdx.x < 8 ? (ahead < a.bytes ? ahead : a.bytes) : a.bytes))
+      *reinterpret_cast<uint16_t*>(p + c) = 0;
+  }
+#pragma unroll
+  for (int j = 0; j < kFillBytes / 16 / kEmbedThreads; ++j) {
+    const int64_t c = u * kFillBytes + 16 * (j * kEmbedThreads + threadIdx.x);
+    if (c < whole) *reinterpret_cast<uint4*>(p + ahead + c) = make_uint4(0, 0, 0, 0);
+  }
+}
 
 // A row's (language, token, t): language and token in the upper half, kNoToken where the
 // row has none.
@@ -73,8 +123,9 @@ struct OrderArgs {
   int32_t id_bytes, K;
   int64_t rows[kMaxK + 1];
 };
-__global__ void __launch_bounds__(kSortRun) sort_runs_kernel(const OrderArgs a) {
+__global__ void __launch_bounds__(kSortRun) sort_runs_kernel(const __grid_constant__ OrderArgs a, const __grid_constant__ FillArgs f) {
   grid_wait();
+  if (blockIdx.x >= f.own) return fill(f);
   const int tid = threadIdx.x;
   const int64_t t = (int64_t)blockIdx.x * kSortRun + tid;
   uint64_t mine = ~0ull;
@@ -106,28 +157,79 @@ __global__ void __launch_bounds__(kSortRun) sort_runs_kernel(const OrderArgs a) 
   if (t < a.T) a.out[t] = mine;
 }
 
-// Runs of `run` sorted places merged in groups of kMerge.
-__global__ void __launch_bounds__(kEmbedThreads)
-    merge_runs_kernel(const uint64_t* in, uint64_t* out, const int64_t T, const int64_t run) {
+// The first merge: a CTA for 64 rows of a run of kSortRun, 4 threads a row with 8 runs each.
+// The keys alone lie in shared memory: equal ones are in the order of their runs.
+struct MergeArgs {
+  const uint64_t* in;
+  uint64_t* out;
+  int64_t T, run;
+};
+constexpr int kMergeRows = kEmbedThreads / 4;
+__global__ void __launch_bounds__(kEmbedThreads) merge_keys_kernel(const __grid_constant__ MergeArgs a, const __grid_constant__ FillArgs f) {
   grid_wait();
-  const int64_t i = (int64_t)blockIdx.x * kEmbedThreads + threadIdx.x;
-  if (i >= T) return;
-  const uint64_t mine = in[i];
-  const int64_t own = i / run, group = own / kMerge * kMerge;
-  int64_t place = group * run + (i - own * run);
-#pragma unroll 4
+  if (blockIdx.x >= f.own) return fill(f);
+  __shared__ uint32_t keys[kMerge][kSortRun];
+  const int tid = threadIdx.x;
+  const int64_t own = (int64_t)blockIdx.x * kMergeRows / kSortRun, first = own / kMerge * kMerge * kSortRun;
+#pragma unroll 8
   for (int j = 0; j < kMerge; ++j) {
-    const int64_t from = (group + j) * run;
-    if (group + j == own || from >= T) continue;
-    int64_t lo = 0, hi = T - from < run ? T - from : run;      // how many are less than mine
+    const int64_t i = first + j * kSortRun + tid;
+    keys[j][tid] = i < a.T ? (uint32_t)(a.in[i] >> 32) : kNoToken;
+  }
+  const int64_t i = (int64_t)blockIdx.x * kMergeRows + tid / 4;
+  const uint64_t mine = i < a.T ? a.in[i] : ~0ull;
+  const uint32_t key = (uint32_t)(mine >> 32);
+  const int me = (int)(own % kMerge);
+  __syncthreads();
+  // places of each run that come before this row
+  int before[kMerge / 4] = {};
+#pragma unroll
+  for (int step = kSortRun / 2; step > 0; step /= 2) {
+#pragma unroll
+    for (int j = 0; j < kMerge / 4; ++j) {
+      const int r = 4 * j + (tid & 3);
+      const uint32_t there = keys[r][before[j] + step - 1];
+      if (there < key || (there == key && r < me)) before[j] += step;
+    }
+  }
+  int place = 0;
+#pragma unroll
+  for (int j = 0; j < kMerge / 4; ++j) {
+    const int r = 4 * j + (tid & 3);
+    if (r == me) continue;
+    const uint32_t there = keys[r][before[j]];          // (all but one have been looked at)
+    place += before[j] + (there < key || (there == key && r < me) ? 1 : 0);
+  }
+  place += __shfl_xor_sync(0xffffffffu, place, 1);
+  place += __shfl_xor_sync(0xffffffffu, place, 2);
+  if (i < a.T && (tid & 3) == 0) a.out[first + (i - own * kSortRun) + place] = mine;
+}
+
+// A later merge: runs of `run` places in groups of kMerge, 8 threads a row with a run each in
+// turn.
+constexpr int kMergeLanes = 8;
+__global__ void __launch_bounds__(kEmbedThreads) merge_runs_kernel(const __grid_constant__ MergeArgs a, const __grid_constant__ FillArgs f) {
+  grid_wait();
+  if (blockIdx.x >= f.own) return fill(f);
+  const int64_t i = ((int64_t)blockIdx.x * kEmbedThreads + threadIdx.x) / kMergeLanes;
+  const bool live = i < a.T;
+  const uint64_t mine = live ? a.in[i] : 0;
+  const int64_t own = i / a.run, group = own / kMerge * kMerge;
+  int64_t place = 0;
+  for (int j = threadIdx.x % kMergeLanes; j < kMerge; j += kMergeLanes) {
+    const int64_t from = (group + j) * a.run;
+    if (!live || group + j == own || from >= a.T) continue;
+    int64_t lo = 0, hi = a.T - from < a.run ? a.T - from : a.run;      // how many are less than mine
     while (lo < hi) {
       const int64_t mid = (lo + hi) / 2;
-      if (in[from + mid] < mine) lo = mid + 1;
+      if (a.in[from + mid] < mine) lo = mid + 1;
       else hi = mid;
     }
     place += lo;
   }
-  out[place] = mine;
+#pragma unroll
+  for (int w = kMergeLanes / 2; w > 0; w /= 2) place += __shfl_xor_sync(0xffffffffu, place, w);
+  if (live && threadIdx.x % kMergeLanes == 0) a.out[group * a.run + (i - own * a.run) + place] = mine;
 }
 
 // ---- sums ------------------------------------------------------------------
@@ -137,159 +239,230 @@ struct SumArgs {
   const void* dy;
   float* part;                          // [piece][2][columns]
   void* dw[kMaxK];
-  int64_t ld, T, V, D, ld_part;
+  int64_t ld, T, V, D, ld_part, pieces;
   float scale;
-  int32_t accumulate;
+  int32_t accumulate, piece;            // places of a warp, 8 to 32
+  uint32_t blocks;                      // of kColumns columns
 };
 
 __device__ __forceinline__ uint32_t key_at(const SumArgs& a, int64_t i) {
   return i < 0 || i >= a.T ? kNoToken : (uint32_t)(a.order[i] >> 32);
 }
 
-// A lane's 8 columns: side by side where rows start on 16 bytes, else 32 apart.
-template <bool VEC>
-__device__ __forceinline__ int64_t column(int64_t c0, int lane, int j) {
-  return VEC ? c0 + 8 * lane + j : c0 + lane + 32 * j;
-}
+// A lane's 8 columns of a row from c0 on: side by side where rows start on 16 bytes, else 32
+// apart; 0 beyond the last column.
 template <class E, bool VEC>
-__device__ __forceinline__ void load8(const E* row, int64_t c0, int lane, int64_t D, float (&x)[8]) {
-  if (VEC) {
+struct Eight {
+  uint4 v[sizeof(E) / 2];
+  __device__ __forceinline__ void load(const E* row, int64_t c0, int lane, int64_t D) {
     const int64_t c = c0 + 8 * lane;
-    const uint4* p = reinterpret_cast<const uint4*>(row + c);
-    if (sizeof(E) == 2) {
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (c < D) v = p[0];
-      unpack(v, x);
-    } else {
-      uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-      if (c < D) v[0] = p[0];
-      if (c + 4 < D) v[1] = p[1];
-      float y[4], z[4];
-      unpack(v[0], y);
-      unpack(v[1], z);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = y[j], x[j + 4] = z[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t c = column<false>(c0, lane, j);
-      x[j] = c < D ? widen(row[c]) : 0.0f;
+    for (int j = 0; j < (int)sizeof(E) / 2; ++j) {
+      v[j] = make_uint4(0, 0, 0, 0);
+      if (c + j * kVec<E> < D) v[j] = reinterpret_cast<const uint4*>(row + c)[j];
     }
   }
-}
-template <class E, bool VEC>
-__device__ __forceinline__ void store8(E* row, int64_t c0, int lane, int64_t D, const float (&x)[8]) {
-  if (VEC) {
-    const int64_t c = c0 + 8 * lane;
-    uint4* p = reinterpret_cast<uint4*>(row + c);
-    if (sizeof(E) == 2) {
-      if (c < D) p[0] = repack(x);
-    } else {
-      const float y[4] = {x[0], x[1], x[2], x[3]}, z[4] = {x[4], x[5], x[6], x[7]};
-      if (c < D) p[0] = repack(y);
-      if (c + 4 < D) p[1] = repack(z);
-    }
-  } else {
+  __device__ __forceinline__ void get(float (&x)[8]) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int64_t c = column<false>(c0, lane, j);
-      if (c < D) row[c] = narrow<E>(x[j]);
+    for (int j = 0; j < (int)sizeof(E) / 2; ++j) {
+      float y[kVec<E>];
+      unpack(v[j], y);
+#pragma unroll
+      for (int e = 0; e < kVec<E>; ++e) x[j * kVec<E> + e] = y[e];
     }
   }
-}
-// A finished sum to its place.
-template <class W, bool VEC>
-__device__ __forceinline__ void finish(const SumArgs& a, uint32_t key, int64_t c0, int lane, const float (&sum)[8]) {
+  static __device__ __forceinline__ void store(E* row, int64_t c0, int lane, int64_t D, const float (&x)[8]) {
+    const int64_t c = c0 + 8 * lane;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(E) / 2; ++j) {
+      float y[kVec<E>];
+#pragma unroll
+      for (int e = 0; e < kVec<E>; ++e) y[e] = x[j * kVec<E> + e];
+      if (c + j * kVec<E> < D) reinterpret_cast<uint4*>(row + c)[j] = repack(y);
+    }
+  }
+};
+template <class E>
+struct Eight<E, false> {
+  E v[8];
+  __device__ __forceinline__ void load(const E* row, int64_t c0, int lane, int64_t D) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c0 + lane + 32 * j < D ? row[c0 + lane + 32 * j] : narrow<E>(0.0f);
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = widen(v[j]);
+  }
+  static __device__ __forceinline__ void store(E* row, int64_t c0, int lane, int64_t D, const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c0 + lane + 32 * j < D) row[c0 + lane + 32 * j] = narrow<E>(x[j]);
+  }
+};
+using Part8 = Eight<float, true>;       // (a lane's 8 columns side by side, whichever they are)
+
+template <class W>
+__device__ __forceinline__ W* place_of(const SumArgs& a, uint32_t key) {
   const uint32_t k = key / (uint32_t)a.V, v = key % (uint32_t)a.V;
-  W* row = static_cast<W*>(a.dw[k]) + (int64_t)v * a.D;
+  return static_cast<W*>(a.dw[k]) + (int64_t)v * a.D;
+}
+// A finished sum to its place, which held `old`.
+template <class W, bool VEC>
+__device__ __forceinline__ void finish(const SumArgs& a, W* row, int64_t c0, int lane, const float (&sum)[8], const Eight<W, VEC>& old) {
   float x[8];
   if (a.accumulate) {
-    load8<W, VEC>(row, c0, lane, a.D, x);
+    old.get(x);
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = fmaf(sum[j], a.scale, x[j]);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) x[j] = sum[j] * a.scale;
   }
-  store8<W, VEC>(row, c0, lane, a.D, x);
+  Eight<W, VEC>::store(row, c0, lane, a.D, x);
 }
 __device__ __forceinline__ float* part_row(const SumArgs& a, int64_t piece, int which, int64_t c0) {
   return a.part + (piece * 2 + which) * a.ld_part + c0;
 }
 
-// A warp's piece: places kPiece * piece and on, 256 columns from c0.  What begins before the
-// piece goes to its first part, what goes on behind it to its second.
+// A warp's piece: places a.piece * piece and on, 256 columns from c0.  What begins before the
+// piece goes to its first part, what goes on behind it to its second.  kRowsAhead rows, and
+// the places that they are added to, are on their way at once.
+constexpr int kSumThreads = 128;
+constexpr int kRowsAhead = 4;
 template <class E, class W, bool VEC>
-__global__ void __launch_bounds__(kEmbedThreads) sum_pieces_kernel(const SumArgs a, const uint32_t blocks, const int64_t pieces) {
+__global__ void __launch_bounds__(kSumThreads) sum_pieces_kernel(const __grid_constant__ SumArgs a) {
   grid_wait();
   const int lane = threadIdx.x & 31;
-  const int64_t unit = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5);
-  const int64_t piece = unit / blocks, c0 = (unit - piece * blocks) * kColumns;
-  if (piece >= pieces) return;
-  const int64_t at = piece * kPiece;
-  const uint64_t mine = at + lane < a.T ? a.order[at + lane] : ~0ull;
+  const int64_t unit = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
+  const int64_t piece = unit / a.blocks, c0 = (unit - piece * a.blocks) * kColumns;
+  if (piece >= a.pieces) return;
+  const int64_t at = piece * a.piece;
+  const bool in = lane < a.piece;
+  const uint64_t mine = in && at + lane < a.T ? a.order[at + lane] : ~0ull;
+  const uint32_t before = key_at(a, at - 1), behind = key_at(a, at + a.piece);
   const uint32_t key = (uint32_t)(mine >> 32), row = (uint32_t)mine;
-  const uint32_t next = key_at(a, at + lane + 1), before = key_at(a, at - 1);
+  const uint32_t beside = __shfl_down_sync(0xffffffffu, key, 1), next = lane == a.piece - 1 ? behind : beside;
   const int n = __popc(__ballot_sync(0xffffffffu, key != kNoToken));
-  const uint32_t ends = __ballot_sync(0xffffffffu, key != next);
-  bool first = __shfl_sync(0xffffffffu, key, 0) == before;      // the sum began before the piece
+  const uint32_t ends = __ballot_sync(0xffffffffu, key != kNoToken && key != next);
+  const bool first = n > 0 && __shfl_sync(0xffffffffu, key, 0) == before;      // the sum began before the piece
+  const uint32_t whole = first ? ends & (ends - 1) : ends;      // ends of the sums that began here
   float sum[8] = {};
-  for (int i = 0; i < n; ++i) {
-    float x[8];
-    load8<E, VEC>(static_cast<const E*>(a.dy) + (int64_t)__shfl_sync(0xffffffffu, row, i) * a.ld, c0, lane, a.D, x);
+  for (int i0 = 0; i0 < n; i0 += kRowsAhead) {
+    Eight<E, VEC> dy[kRowsAhead];
+    Eight<W, VEC> old[kRowsAhead];
+    W* to[kRowsAhead];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += x[j];
-    const bool end = ends >> i & 1;
-    if (!end && i + 1 < n) continue;
-    if (first || !end)
-      store8<float, true>(part_row(a, piece, first ? 0 : 1, c0), 0, lane, kColumns, sum);
-    else
-      finish<W, VEC>(a, __shfl_sync(0xffffffffu, key, i), c0, lane, sum);
-    first = false;
+    for (int j = 0; j < kRowsAhead; ++j)
+      if (i0 + j < n)
+        dy[j].load(static_cast<const E*>(a.dy) + (int64_t)__shfl_sync(0xffffffffu, row, i0 + j) * a.ld, c0, lane, a.D);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+    for (int j = 0; j < kRowsAhead; ++j)
+      if (whole >> (i0 + j) & 1) {
+        to[j] = place_of<W>(a, __shfl_sync(0xffffffffu, key, i0 + j));
+        if (a.accumulate) old[j].load(to[j], c0, lane, a.D);
+      }
+#pragma unroll
+    for (int j = 0; j < kRowsAhead; ++j) {
+      if (i0 + j >= n) break;
+      float x[8];
+      dy[j].get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+      if (whole >> (i0 + j) & 1) {
+        finish<W, VEC>(a, to[j], c0, lane, sum, old[j]);
+      } else if (ends >> (i0 + j) & 1) {
+        Part8::store(part_row(a, piece, 0, c0), 0, lane, kColumns, sum);
+      } else if (i0 + j == n - 1) {     // goes on
+        Part8::store(part_row(a, piece, first && ends == 0 ? 0 : 1, c0), 0, lane, kColumns, sum);
+      } else {
+        continue;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+    }
   }
 }
 
-// The sums of more than one piece: a CTA for each piece in which one begins that goes on,
-// its warps each a part of the pieces.
-template <class W, bool VEC>
-__global__ void __launch_bounds__(kEmbedThreads) join_pieces_kernel(const SumArgs a) {
-  grid_wait();
-  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const int64_t piece = blockIdx.x, c0 = (int64_t)blockIdx.y * kColumns, last = piece * kPiece + kPiece - 1;
-  const uint32_t key = key_at(a, last);
-  if (key == kNoToken || key_at(a, last + 1) != key) return;
-  if (key_at(a, piece * kPiece) == key && key_at(a, piece * kPiece - 1) == key) return;   // began before
-  // the last place that holds the token
-  int64_t lo = last + 1, hi = a.T;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if ((uint32_t)(a.order[mid] >> 32) <= key) lo = mid + 1;
-    else hi = mid;
-  }
-  const int64_t end = (lo - 1) / kPiece, n = end - piece;       // pieces behind this one
-  const int64_t each = (n + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
-  const int64_t from = piece + 1 + wid * each, to = from + each <= end ? from + each : end + 1;
-  float sum[8] = {};
-  if (wid == 0) load8<float, true>(part_row(a, piece, 1, c0), 0, lane, kColumns, sum);
-  for (int64_t p = from; p < to; ++p) {
-    float x[8];
-    load8<float, true>(part_row(a, p, 0, c0), 0, lane, kColumns, x);
+// Parts from .. to - 1 of pieces in which a sum goes on, added to `sum`.
+__device__ __forceinline__ void add_parts(const SumArgs& a, int64_t from, int64_t to, int64_t c0, int lane, float (&sum)[8]) {
+  constexpr int kAhead = 4;
+  for (int64_t p = from; p < to; p += kAhead) {
+    Part8 v[kAhead];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum[j] += x[j];
+    for (int j = 0; j < kAhead; ++j)
+      if (p + j < to) v[j].load(part_row(a, p + j, 0, c0), 0, lane, kColumns);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (p + j >= to) break;
+      float x[8];
+      v[j].get(x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+    }
   }
-  // (a lane's 8 columns as load8<., VEC> has them, whatever their places in a part)
-  __shared__ float room[kEmbedThreads / 32][kColumns];
+}
+
+// The sums of more than one piece, by the warp of the piece in which they begin; by all warps
+// of its CTA where they go on for more than 31 pieces.
+template <class W, bool VEC>
+__global__ void __launch_bounds__(kEmbedThreads) join_pieces_kernel(const __grid_constant__ SumArgs a) {
+  grid_wait();
+  constexpr int kWarpsHere = kEmbedThreads / 32;
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int64_t piece = (int64_t)blockIdx.x * kWarpsHere + wid, c0 = (int64_t)blockIdx.y * kColumns;
+  __shared__ int64_t long_piece;
+  __shared__ float room[kWarpsHere][kColumns];
+  if (threadIdx.x == 0) long_piece = -1;
+  __syncthreads();
+  // the keys of this piece's last place and of the first ones of those behind it
+  const int64_t start = (piece + lane) * a.piece;
+  const uint32_t ahead = key_at(a, start), tail = key_at(a, (piece + 1) * a.piece - 1), prior = key_at(a, piece * a.piece - 1);
+  const uint32_t head = __shfl_sync(0xffffffffu, ahead, 0);
+  const bool begins = piece < a.pieces && tail != kNoToken && !(head == tail && prior == tail);
+  const uint32_t same = __ballot_sync(0xffffffffu, lane > 0 && ahead == tail) >> 1;
+  const int on = __ffs(~same) - 1;      // pieces behind this one that hold the token, at most 31
+  W* to = begins && on > 0 ? place_of<W>(a, tail) : nullptr;
+  if (to && on < 31) {
+    Eight<W, VEC> old;
+    if (a.accumulate) old.load(to, c0, lane, a.D);
+    float sum[8];
+    Part8 v;
+    v.load(part_row(a, piece, 1, c0), 0, lane, kColumns);
+    v.get(sum);
+    add_parts(a, piece + 1, piece + 1 + on, c0, lane, sum);
+    finish<W, VEC>(a, to, c0, lane, sum, old);
+  }
+  if (to && on >= 31 && lane == 0) long_piece = piece;   // at most one of 8 neighbours
+  __syncthreads();
+  const int64_t from = long_piece;
+  if (from < 0) return;
+  const uint32_t key = key_at(a, (from + 1) * a.piece - 1);
+  int64_t n = 0;
+  for (;;) {
+    const int64_t p = from + 1 + n + threadIdx.x;
+    const int c = __syncthreads_count(p < a.pieces && key_at(a, p * a.piece) == key);
+    n += c;
+    if (c < kEmbedThreads) break;
+  }
+  const int64_t each = (n + kWarpsHere - 1) / kWarpsHere, lo = from + 1 + wid * each, end = from + 1 + n;
+  float sum[8] = {};
+  if (wid == 0) {
+    Part8 v;
+    v.load(part_row(a, from, 1, c0), 0, lane, kColumns);
+    v.get(sum);
+  }
+  add_parts(a, lo, lo + each < end ? lo + each : end, c0, lane, sum);
 #pragma unroll
   for (int j = 0; j < 8; ++j) room[wid][lane + 32 * j] = sum[j];
   __syncthreads();
   if (wid != 0) return;
-  for (int w = 1; w < kEmbedThreads / 32; ++w)
+  for (int w = 1; w < kWarpsHere; ++w)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum[j] += room[w][lane + 32 * j];
-  finish<W, VEC>(a, key, c0, lane, sum);
+  W* row = place_of<W>(a, key);
+  Eight<W, VEC> old;
+  if (a.accumulate) old.load(row, c0, lane, a.D);
+  finish<W, VEC>(a, row, c0, lane, sum, old);
 }
 
 int64_t up_by(int64_t n, int64_t by) { return (n + by - 1) / by; }
@@ -305,14 +478,22 @@ bool embed_sizes_ok(int64_t T, int64_t V, int64_t D, double scale) {
          D <= ((int64_t)1 << 23) && std::isfinite((float)scale);
 }
 
+// Places of a warp's piece: as many as leave 2432 warps (16 for each of 152 SMs), 8 to 32.
+int piece_of(int64_t T, int64_t blocks) {
+  int piece = 32;
+  while (piece > 8 && up_by(T, piece) * blocks < 2432) piece /= 2;
+  return piece;
+}
 struct EmbedRoom {
   size_t order[2], part, total;
   int64_t pieces, blocks;
+  int piece;
 };
 EmbedRoom embed_room(int64_t T, int64_t D) {
   EmbedRoom r;
-  r.pieces = up_by(T, kPiece);
   r.blocks = up_by(D, kColumns);
+  r.piece = piece_of(T, r.blocks);
+  r.pieces = up_by(T, r.piece);
   r.order[0] = 0;
   r.order[1] = align256((size_t)T * 8);
   r.part = r.order[1] + (T > kSortRun ? align256((size_t)T * 8) : 0);
@@ -341,10 +522,9 @@ extern "C" int bkmoo_embedding_forward(const void* table, int64_t ld_table, int3
   const bool vec = on_vectors(table, dtype, D, ld_table) && on_vectors(y, dtype, D, ldy);
   const int n = vec ? (int)(16 / float_bytes(dtype)) : 1;
   LookupArgs a = {table, ids, y, ld_table, ldy, T, V, id_bytes, (uint32_t)D, (uint32_t)(D / n), (float)scale};
-  const void* fn = dtype == BKMOO_F32 ? vec ? (const void*)embed_kernel<float, true> : (const void*)embed_kernel<float, false>
-                   : vec ? (const void*)embed_kernel<__nv_bfloat16, true>
-                         : (const void*)embed_kernel<__nv_bfloat16, false>;
-  const int64_t ctas = up_by(T * a.per, kEmbedThreads), most = 1 << 20;
+  const bool ahead = T * a.per > 152 * 2048;
+  const void* fn = dtype == BKMOO_F32 ? embed_fn<float>(vec, ahead) : embed_fn<__nv_bfloat16>(vec, ahead);
+  const int64_t ctas = up_by(T * a.per, kEmbedThreads * (ahead ? 4 : 1)), most = 1 << 20;
   void* list[] = {&a};
   return launch_behind(fn, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kEmbedThreads), list, 0,
                        static_cast<cudaStream_t>(stream), true) == cudaSuccess
@@ -373,44 +553,64 @@ extern "C" int bkmoo_embedding_backward(const void* dy, int64_t ld_dy, int32_t d
     vec = vec && on_vectors(dw[k], dw_dtype, D, D);
   }
   const EmbedRoom room = embed_room(T, D);
-  const int64_t ctas = up_by(room.pieces * room.blocks, kEmbedThreads / 32);
-  if (ctas > 0x7fffffffll) return BKMOO_ERR_INVALID;
+  const int64_t ctas = up_by(room.pieces * room.blocks, kSumThreads / 32);
+  const size_t grad_bytes = (size_t)(V * D) * float_bytes(dw_dtype);
+  int64_t levels = 1;                   // kernels of the order
+  for (int64_t run = kSortRun; run < T; run *= kMerge) ++levels;
+  FillArgs f = {};
+  f.bytes = (int64_t)grad_bytes;
+  f.units = up_by(f.bytes, kFillBytes);
+  for (int k = 0; k < K; ++k) f.dw[k] = dw[k];
+  const int64_t fills = accumulate ? 0 : K * f.units;
+  if (ctas > 0x7fffffffll || fills + up_by(T, kMergeRows) + up_by(T * kMergeLanes, kEmbedThreads) > 0x7fffffffll)
+    return BKMOO_ERR_INVALID;
   if (T > 0 && ws_bytes < room.total) return BKMOO_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (!accumulate)
-    for (int k = 0; k < K; ++k)
-      if (cudaMemsetAsync(dw[k], 0, (size_t)(V * D) * float_bytes(dw_dtype), s) != cudaSuccess) return BKMOO_ERR_CUDA;
-  if (T == 0) return BKMOO_OK;
+  if (T == 0) {
+    for (int k = 0; k < K && !accumulate; ++k)
+      if (cudaMemsetAsync(dw[k], 0, grad_bytes, s) != cudaSuccess) return BKMOO_ERR_CUDA;
+    return BKMOO_OK;
+  }
   char* base = static_cast<char*>(ws);
   uint64_t *order = reinterpret_cast<uint64_t*>(base + room.order[0]), *other = reinterpret_cast<uint64_t*>(base + room.order[1]);
-  OrderArgs o = {ids, order, T, V, id_bytes, K, {}};
-  for (int k = 0; k <= K; ++k) o.rows[k] = rows[k];
-  void* sort_list[] = {&o};
-  cudaError_t e = launch_behind((const void*)sort_runs_kernel, dim3((unsigned)up_by(T, kSortRun)), dim3(kSortRun), sort_list, 0, s, true);
-  for (int64_t run = kSortRun; run < T && e == cudaSuccess; run *= kMerge) {
-    void* list[] = {&order, &other, &T, &run};
-    e = launch_behind((const void*)merge_runs_kernel, dim3((unsigned)up_by(T, kEmbedThreads)), dim3(kEmbedThreads), list, 0, s, true);
+  // the order, and a part of the zeros with each of its kernels
+  cudaError_t e = cudaSuccess;
+  int64_t run = kSortRun;
+  for (int64_t level = 0; level < levels && e == cudaSuccess; ++level) {
+    f.from = fills * level / levels;
+    f.own = level == 0 ? up_by(T, kSortRun) : level == 1 ? up_by(T, kMergeRows) : up_by(T * kMergeLanes, kEmbedThreads);
+    const dim3 grid((unsigned)(f.own + fills * (level + 1) / levels - f.from));
+    if (level == 0) {
+      OrderArgs o = {ids, order, T, V, id_bytes, K, {}};
+      for (int k = 0; k <= K; ++k) o.rows[k] = rows[k];
+      void* list[] = {&o, &f};
+      e = launch_behind((const void*)sort_runs_kernel, grid, dim3(kSortRun), list, 0, s, true);
+      continue;
+    }
+    MergeArgs m = {order, other, T, run};
+    void* list[] = {&m, &f};
+    e = launch_behind(level == 1 ? (const void*)merge_keys_kernel : (const void*)merge_runs_kernel, grid, dim3(kEmbedThreads), list, 0, s,
+                      true);
+    run *= kMerge;
     uint64_t* t = order;
     order = other;
     other = t;
   }
   if (e != cudaSuccess) return BKMOO_ERR_CUDA;
-  SumArgs a = {order, dy, reinterpret_cast<float*>(base + room.part), {}, ld_dy, T, V, D, room.blocks * kColumns, (float)scale, accumulate};
+  SumArgs a = {order, dy, reinterpret_cast<float*>(base + room.part), {}, ld_dy, T, V, D, room.blocks * kColumns, room.pieces,
+               (float)scale, accumulate, room.piece, (uint32_t)room.blocks};
   for (int k = 0; k < K; ++k) a.dw[k] = dw[k];
-  uint32_t blocks = (uint32_t)room.blocks;
-  int64_t pieces = room.pieces;
-  void* sum_list[] = {&a, &blocks, &pieces};
-  const bool f = dw_dtype == BKMOO_F32;
-  const void* fn = dtype == BKMOO_F32 ? f ? sum_fn<float, float>(vec) : sum_fn<float, __nv_bfloat16>(vec)
-                   : f ? sum_fn<__nv_bfloat16, float>(vec)
-                       : sum_fn<__nv_bfloat16, __nv_bfloat16>(vec);
-  e = launch_behind(fn, dim3((unsigned)ctas), dim3(kEmbedThreads), sum_list, 0, s, true);
-  if (e == cudaSuccess && pieces > 1) {
-    void* list[] = {&a};
-    fn = f ? vec ? (const void*)join_pieces_kernel<float, true> : (const void*)join_pieces_kernel<float, false>
+  void* list[] = {&a};
+  const bool wide = dw_dtype == BKMOO_F32;
+  const void* fn = dtype == BKMOO_F32 ? wide ? sum_fn<float, float>(vec) : sum_fn<float, __nv_bfloat16>(vec)
+                   : wide ? sum_fn<__nv_bfloat16, float>(vec)
+                          : sum_fn<__nv_bfloat16, __nv_bfloat16>(vec);
+  e = launch_behind(fn, dim3((unsigned)ctas), dim3(kSumThreads), list, 0, s, true);
+  if (e == cudaSuccess && room.pieces > 1) {
+    fn = wide ? vec ? (const void*)join_pieces_kernel<float, true> : (const void*)join_pieces_kernel<float, false>
          : vec ? (const void*)join_pieces_kernel<__nv_bfloat16, true>
                : (const void*)join_pieces_kernel<__nv_bfloat16, false>;
-    e = launch_behind(fn, dim3((unsigned)(pieces - 1), blocks), dim3(kEmbedThreads), list, 0, s, true);
+    e = launch_behind(fn, dim3((unsigned)up_by(room.pieces - 1, kEmbedThreads / 32), a.blocks), dim3(kEmbedThreads), list, 0, s, true);
   }
   return e == cudaSuccess ? BKMOO_OK : BKMOO_ERR_CUDA;
 }
