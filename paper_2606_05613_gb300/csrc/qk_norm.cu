@@ -17,9 +17,10 @@
 namespace bkmoo {
 namespace {
 
-constexpr int kQkThreads = 256;
+constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
 constexpr int kMaxHead = 256;
+constexpr int kAhead = 4;               // steps of a warp whose loads are on their way
 
 struct QkSide {
   const __nv_bfloat16 *x, *dout;
@@ -39,9 +40,8 @@ struct QkArgs {
 };
 
 // The angles of a token's pairs, [2][rot / 2], by a warp.
-__device__ __forceinline__ void angles(const QkArgs& a, int64_t t, int lane, float (*room)[kMaxHead / 2]) {
+__device__ __forceinline__ void angles(const QkArgs& a, uint64_t pos, int lane, float (*room)[kMaxHead / 2]) {
   __syncwarp();
-  const uint64_t pos = (uint64_t)load_id(a.pos, a.id_bytes, t);
   for (int i = lane; i < a.rot / 2; i += 32) {
     // half turns in [-1, 1)
     const float half = __int2float_rn((int32_t)((pos * a.turn[i] + 0x80000000ull) >> 32)) * 0x1p-31f;
@@ -96,31 +96,30 @@ __device__ __forceinline__ void rotate(float (&y)[16], const Angles& g) {
     b = fmaf(x, s, b * g.c[j]);
   }
 }
-__device__ __forceinline__ void weights_of(const QkArgs& a, const void* w, const Place& p, float (&v)[16]) {
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    const int c = (j < 8 ? p.lo : p.hi) + (j & 7);
-    v[j] = !p.live ? 0.0f
-           : a.w_f32 ? static_cast<const float*>(w)[c]
-                     : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c]);
-  }
+__device__ __forceinline__ float weight_at(const QkArgs& a, const void* w, int c) {
+  return a.w_f32 ? static_cast<const float*>(w)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c]);
 }
+// Loads go to shared memory, each lane's to a place of its own that only it reads: a copy
+// that is on its way holds no register.
 struct Pair {
-  uint4 lo, hi;
+  uint4 lo[32], hi[32];
 };
-__device__ __forceinline__ Pair load_pair(const __nv_bfloat16* head, const Place& p, bool live) {
-  Pair v;
-  v.lo = v.hi = make_uint4(0, 0, 0, 0);
-  if (live) {
-    v.lo = *reinterpret_cast<const uint4*>(head + p.lo);
-    v.hi = *reinterpret_cast<const uint4*>(head + p.hi);
-  }
-  return v;
+__device__ __forceinline__ void copy16(uint4* to, const __nv_bfloat16* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
 }
-__device__ __forceinline__ void unpack16(const Pair& v, float (&x)[16]) {
-  float a[8], b[8];
-  unpack(v.lo, a);
-  unpack(v.hi, b);
+__device__ __forceinline__ void copy_pair(Pair& to, const __nv_bfloat16* head, const Place& p, int lane) {
+  copy16(&to.lo[lane], head + p.lo);
+  copy16(&to.hi[lane], head + p.hi);
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the newest kAhead - 1 steps' copies have come.
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory"); }
+__device__ __forceinline__ void get_pair(const Pair& v, int lane, bool live, float (&x)[16]) {
+  float a[8] = {}, b[8] = {};
+  if (live) {
+    unpack(v.lo[lane], a);
+    unpack(v.hi[lane], b);
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = a[j], x[j + 8] = b[j];
 }
@@ -137,46 +136,85 @@ __device__ __forceinline__ float over_head(float v) {
   return v;
 }
 
+// A walk over steps: groups of heads, token after token.
+struct Walk {
+  int64_t t;
+  int step;
+  __device__ __forceinline__ bool next(int per) {        // whether a token begins
+    if (++step < per) return false;
+    step = 0;
+    ++t;
+    return true;
+  }
+};
+
 // G lanes a head.  A warp takes a run of steps, each 32 / G heads of a token's queries or keys.
 template <int G, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kQkThreads) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
   grid_wait();
   __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ Pair ring[kQkWarps][kAhead];
+  __shared__ __align__(16) float weights[2][kMaxHead];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int per = a.side[0].steps + a.side[1].steps;
   const int64_t total = a.T * per, from = ((int64_t)blockIdx.x * kQkWarps + wid) * each;
   const int64_t to = from + each < total ? from + each : total;
-  if (from >= to) return;
   const Place p = place_of_lane<NEIGHBOURS>(a, lane % G);
-  int64_t t = from / per;
-  int step = (int)(from - t * per);
-  bool new_token = true;
-  int which = -1;
-  Angles g;
-  float w[16];
-  for (int64_t i = from; i < to; ++i) {
-    const int k = step >= a.side[0].steps;
-    const QkSide& s = a.side[k];
-    const int head = (step - (k ? a.side[0].steps : 0)) * (32 / G) + lane / G;
-    const bool live = p.live && head < s.heads;
-    const Pair v = load_pair(s.x + t * s.ld + (int64_t)head * a.hd, p, live);
-    if (new_token) {
-      angles(a, t, lane, room[wid]);
-      g = angles_of(p, room[wid]);
+  Walk here = {from / per, 0}, there;
+  here.step = (int)(from - here.t * per);
+  there = here;
+  struct Head {
+    int k, head;
+    bool live;
+  };
+  auto head_of = [&](const Walk& w) {
+    Head h;
+    h.k = w.step >= a.side[0].steps;
+    h.head = (w.step - (h.k ? a.side[0].steps : 0)) * (32 / G) + lane / G;
+    h.live = p.live && h.head < a.side[h.k].heads;
+    return h;
+  };
+  int64_t ahead = from;
+  auto fetch = [&]() {
+    if (ahead < to) {
+      const Head h = head_of(there);
+      const QkSide& s = a.side[h.k];
+      if (h.live) copy_pair(ring[wid][(ahead - from) % kAhead], s.x + there.t * s.ld + (int64_t)h.head * a.hd, p, lane);
+      there.next(per);
     }
-    if (which != k) weights_of(a, s.w, p, w);
-    which = k;
+    ++ahead;
+    copies_end();
+  };
+#pragma unroll
+  for (int j = 0; j < kAhead - 1; ++j) fetch();
+  for (int i = threadIdx.x; i < 2 * a.hd; i += kQkThreads) {
+    const int k = i >= a.hd, c = i - (k ? a.hd : 0);
+    weights[k][c] = weight_at(a, a.side[k].w, c);
+  }
+  __syncthreads();
+  if (from >= to) return;
+  int64_t pos = load_id(a.pos, a.id_bytes, here.t);
+  bool new_token = true;
+  Angles g;
+  for (int64_t i = from; i < to; ++i) {
+    fetch();
+    if (new_token) {
+      angles(a, (uint64_t)pos, lane, room[wid]);
+      g = angles_of(p, room[wid]);
+      if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
+    }
+    const Head h = head_of(here);
+    copies_wait();
     float x[16], sum = 0.0f;
-    unpack16(v, x);
+    get_pair(ring[wid][(i - from) % kAhead], lane, h.live, x);
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum = fmaf(x[j], x[j], sum);
     const float r = rsqrtf(fmaf(over_head<G>(sum), a.inv_hd, a.eps));
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = x[j] * r * w[j];
+    for (int j = 0; j < 16; ++j) x[j] = x[j] * r * (p.live ? weights[h.k][(j < 8 ? p.lo : p.hi) + (j & 7)] : 0.0f);
     rotate<NEIGHBOURS, false>(x, g);
-    if (live) store_pair(s.out + t * s.ld_out + (int64_t)head * a.hd, p, x);
-    new_token = ++step == per;
-    if (new_token) step = 0, ++t;
+    if (h.live) store_pair(a.side[h.k].out + here.t * a.side[h.k].ld_out + (int64_t)h.head * a.hd, p, x);
+    new_token = here.next(per);
   }
 }
 
@@ -188,10 +226,11 @@ struct QkRuns {
   float* part;                          // [CTA][hd]
 };
 template <int G, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kQkThreads) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
+__global__ void __launch_bounds__(kQkThreads, 4) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
                                                                   const __grid_constant__ QkRuns q) {
   grid_wait();
   __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ Pair ring[kQkWarps][kAhead][2];             // x, dout
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % G;
   int run = 0;
   while ((int)blockIdx.x >= q.first[run + 1]) ++run;
@@ -202,24 +241,43 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_grad_kernel(const __grid_c
   const int64_t each = (all + warps - 1) / warps;
   const int64_t from = me * each < all ? me * each : all, to = from + each < all ? from + each : all;
   const Place p = place_of_lane<NEIGHBOURS>(a, l);
+  Walk here = {q.rows[lang] + from / s.steps, (int)(from % s.steps)}, there = here;
+  int64_t ahead = from;
+  auto fetch = [&]() {
+    if (ahead < to) {
+      const int head = there.step * (32 / G) + lane / G;
+      Pair* r = ring[wid][(ahead - from) % kAhead];
+      if (p.live && head < s.heads) {
+        copy_pair(r[0], s.x + there.t * s.ld + (int64_t)head * a.hd, p, lane);
+        copy_pair(r[1], s.dout + there.t * s.ld_dout + (int64_t)head * a.hd, p, lane);
+      }
+      there.next(s.steps);
+    }
+    ++ahead;
+    copies_end();
+  };
+#pragma unroll
+  for (int j = 0; j < kAhead - 1; ++j) fetch();
   float w[16], dw[16] = {};
-  weights_of(a, s.w, p, w);
-  int64_t t = q.rows[lang] + from / s.steps;
-  int step = (int)(from % s.steps);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) w[j] = p.live ? weight_at(a, s.w, (j < 8 ? p.lo : p.hi) + (j & 7)) : 0.0f;
+  int64_t pos = from < to ? load_id(a.pos, a.id_bytes, here.t) : 0;
   bool new_token = true;
   Angles g;
   for (int64_t i = from; i < to; ++i) {
-    const int head = step * (32 / G) + lane / G;
-    const bool live = p.live && head < s.heads;
-    const Pair vx = load_pair(s.x + t * s.ld + (int64_t)head * a.hd, p, live);
-    const Pair vd = load_pair(s.dout + t * s.ld_dout + (int64_t)head * a.hd, p, live);
+    fetch();
     if (new_token) {
-      angles(a, t, lane, room[wid]);
+      angles(a, (uint64_t)pos, lane, room[wid]);
       g = angles_of(p, room[wid]);
+      if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
     }
+    const int head = here.step * (32 / G) + lane / G;
+    const bool live = p.live && head < s.heads;
+    copies_wait();
+    const Pair* v = ring[wid][(i - from) % kAhead];
     float x[16], d[16], sum = 0.0f, dot = 0.0f;
-    unpack16(vx, x);
-    unpack16(vd, d);
+    get_pair(v[0], lane, live, x);
+    get_pair(v[1], lane, live, d);
     rotate<NEIGHBOURS, true>(d, g);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
@@ -234,9 +292,8 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_grad_kernel(const __grid_c
       dw[j] = fmaf(d[j], x[j] * r, dw[j]);
       d[j] = r * fmaf(-x[j], c, d[j] * w[j]);
     }
-    if (live) store_pair(s.out + t * s.ld_out + (int64_t)head * a.hd, p, d);
-    new_token = ++step == s.steps;
-    if (new_token) step = 0, ++t;
+    if (live) store_pair(s.out + here.t * s.ld_out + (int64_t)head * a.hd, p, d);
+    new_token = here.next(s.steps);
   }
   if (!q.weights) return;
   __shared__ float sums[kQkWarps][kMaxHead];
