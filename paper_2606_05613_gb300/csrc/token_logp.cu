@@ -6,9 +6,10 @@
 // e^-d (u - d s).  Then log p_v = z_v - m - log s, and H = log s - u / s, a sum of two
 // terms that are not negative.  Bound by memory: a row is read once.
 //
-// The n most likely tokens need no second pass over the row: the n-th largest of the
-// threads' maxima is a bound that at least n elements reach, and the elements that reach
-// it lie with the threads whose maximum does, n of them unless there are ties.
+// The n most likely tokens need no second pass over the row: each warp gives the q-th largest
+// of its threads' maxima, q its share of n, so n elements at least reach the least of these.
+// The elements that do lie in a few threads' best batches of vectors, which are read again
+// (a thread whose second batch reaches it too has all of its own read again).
 #include <math.h>
 
 #include "row_ops.cuh"
@@ -17,10 +18,10 @@
 namespace bkmoo {
 namespace {
 
-constexpr int kLogpThreads = 256;
-constexpr int kLogpWarps = kLogpThreads / 32;
+constexpr int kGradThreads = 256;
 constexpr int kMaxTop = 32;
 constexpr int kMaxCluster = 8;
+constexpr int kAhead = 4;               // vectors of a thread that are on their way at once
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // (z - m) log2(e) below this counts as this where it is multiplied by 2^itself: 2^-1000 is 0
 // and 0 times minus infinity would not be.
@@ -41,45 +42,6 @@ struct LogpArgs {
   float* top_logp;
 };
 
-// m, s and u of a set of logits, u in units of log2.
-struct Sums {
-  float m, s, u;
-};
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
-// a and b of two disjoint sets.
-template <bool ENTROPY>
-__device__ __forceinline__ Sums join(const Sums& a, const Sums& b) {
-  Sums r;
-  r.m = fmaxf(a.m, b.m);
-  const float at = base_of(r.m);
-  // a set without a finite logit has s = 0; minus infinity less a finite number would do for
-  // 2^x but not for u
-  const float da = fmaxf((a.m - at) * kLog2e, kLowest), db = fmaxf((b.m - at) * kLog2e, kLowest);
-  const float ea = exp2f(da), eb = exp2f(db);
-  r.s = a.s * ea + b.s * eb;
-  r.u = ENTROPY ? ea * fmaf(da, a.s, a.u) + eb * fmaf(db, b.s, b.u) : 0.0f;
-  return r;
-}
-template <bool ENTROPY, int N>
-__device__ __forceinline__ void take(Sums& r, const float (&z)[N]) {
-  float top = z[0];
-#pragma unroll
-  for (int j = 1; j < N; ++j) top = fmaxf(top, z[j]);
-  if (top > r.m) {
-    const float d = fmaxf((r.m - top) * kLog2e, kLowest), e = exp2f(d);
-    if (ENTROPY) r.u = e * fmaf(d, r.s, r.u);
-    r.s *= e;
-    r.m = top;
-  }
-  const float at = base_of(r.m);
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const float x = (z[j] - at) * kLog2e, e = exp2f(x);
-    r.s += e;
-    if (ENTROPY) r.u = fmaf(e, fmaxf(x, kLowest), r.u);
-  }
-}
-
 // A value as a whole number of the same order, NaN below all; equal values (0 and -0 among
 // them) give equal numbers.
 __device__ __forceinline__ uint32_t ordered(float z) {
@@ -92,6 +54,65 @@ __device__ __forceinline__ float value_of(uint32_t o) {
 // The order of (value, index): the larger value first, then the lower index.  Never 0.
 __device__ __forceinline__ uint64_t place_of(float z, int v) { return (uint64_t)ordered(z) << 32 | (uint32_t)~v; }
 
+// m, s and u of a set of logits, u in units of log2.
+struct Sums {
+  float m, s, u;
+};
+// 2^x by one instruction, off by 2^-22 of itself; 0 below 2^-126.
+__device__ __forceinline__ float pow2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+// The sets of a warp's first W lanes (the others hold none), their sums in the lanes' order: all
+// to the largest maximum first, then plain sums.
+template <bool ENTROPY, int W>
+__device__ __forceinline__ Sums join_lanes(Sums r) {
+  const float m = value_of(__reduce_max_sync(0xffffffffu, ordered(r.m)));
+  // a set without a finite logit has s = 0; minus infinity less a finite number would do for
+  // 2^x but not for u
+  const float d = fmaxf((r.m - base_of(m)) * kLog2e, kLowest), e = pow2(d);
+  if (ENTROPY) r.u = e * fmaf(d, r.s, r.u);
+  r.s *= e;
+  r.m = m;
+#pragma unroll
+  for (int w = 1; w < W; w *= 2) {
+    r.s += __shfl_xor_sync(0xffffffffu, r.s, w);
+    if (ENTROPY) r.u += __shfl_xor_sync(0xffffffffu, r.u, w);
+  }
+  return r;
+}
+// A new maximum, if `top` is one.
+template <bool ENTROPY>
+__device__ __forceinline__ bool raise(Sums& r, float top) {
+  if (!(top > r.m)) return false;
+  const float d = fmaxf((r.m - top) * kLog2e, kLowest), e = pow2(d);
+  if (ENTROPY) r.u = e * fmaf(d, r.s, r.u);
+  r.s *= e;
+  r.m = top;
+  return true;
+}
+// z, none of them above the maximum.
+template <bool ENTROPY, int N>
+__device__ __forceinline__ void take(Sums& r, const float (&z)[N]) {
+  const float at = base_of(r.m);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const float x = (z[j] - at) * kLog2e, e = pow2(x);
+    r.s += e;
+    if (ENTROPY) r.u = fmaf(e, fmaxf(x, kLowest), r.u);
+  }
+}
+// The largest of a vector, NaN aside.
+__device__ __forceinline__ float largest(const uint4& v, float) {
+  return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+__device__ __forceinline__ float largest(const uint4& v, __nv_bfloat16) {
+  const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+  const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(__low2float(m), __high2float(m));
+}
 // Columns of a row's part: elements ahead of the first whole 16-byte vector and behind the
 // last by thread, vectors in between.
 template <class E>
@@ -121,6 +142,14 @@ template <class E>
 __device__ __forceinline__ uint4 vector_at(const Part<E>& p, int i) {
   return __ldcg(reinterpret_cast<const uint4*>(p.row + p.body) + i);
 }
+__device__ __forceinline__ uint32_t word(const uint4& v, int i) {
+  return i < 2 ? i == 0 ? v.x : v.y : i == 2 ? v.z : v.w;
+}
+__device__ __forceinline__ float element(const uint4& v, int e, float) { return __uint_as_float(word(v, e)); }
+__device__ __forceinline__ float element(const uint4& v, int e, __nv_bfloat16) {
+  const uint32_t w = word(v, e / 2);
+  return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+}
 // The single element of thread t, if it has one: (value, column).
 template <class E>
 __device__ __forceinline__ int single_at(const Part<E>& p, int t) {
@@ -129,78 +158,133 @@ __device__ __forceinline__ int single_at(const Part<E>& p, int t) {
   return -1;
 }
 
-template <class E>
-constexpr int kBuffer = kMaxTop + kLogpThreads * kVec<E>;
+template <class E, int N>
+constexpr int kBuffer = kMaxTop + N * kVec<E>;
+constexpr int kScan = 64;               // elements that first_of looks at in a step
 
-// The n first of buffer[0..count) in order into list, zeros behind them; count may be less.
+// The n first of buffer[0..count) in order into list, zeros behind them; 4 threads an element.
+// The buffer's memory goes on to the next multiple of kScan.
+template <int N>
 __device__ void first_of(const uint64_t* buffer, int count, int n, uint64_t* list) {
-  for (int i = threadIdx.x; i < n; i += kLogpThreads)
-    if (i >= count) list[i] = 0;
-  for (int i = threadIdx.x; i < count; i += kLogpThreads) {
-    const uint64_t mine = buffer[i];
+  const int sub = threadIdx.x % 4;
+  for (int i = count + threadIdx.x; i < n; i += N) list[i] = 0;
+  for (int i0 = 0; i0 < count; i0 += N / 4) {
+    const int i = i0 + threadIdx.x / 4;
+    const uint64_t mine = i < count ? buffer[i] : ~0ull;
     int before = 0;
-    for (int j = 0; j < count; ++j) before += buffer[j] > mine;
-    if (before < n) list[before] = mine;
+    for (int j0 = 0; j0 < count; j0 += kScan) {
+#pragma unroll
+      for (int k = 0; k < kScan / 8; ++k) {
+        const int j = j0 + 8 * k + 2 * sub;
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(buffer + j);
+        before += (j < count && v.x > mine) + (j + 1 < count && v.y > mine);
+      }
+    }
+#pragma unroll
+    for (int w = 1; w < 4; w *= 2) before += __shfl_xor_sync(0xffffffffu, before, w);
+    if (sub == 0 && i < count && before < n) list[before] = mine;
   }
 }
 
-template <class E>
+template <class E, int N>
 struct TopRoom {
-  uint64_t buffer[kBuffer<E>];
+  alignas(16) uint64_t buffer[(kBuffer<E, N> + kScan - 1) / kScan * kScan];
   uint64_t list[kMaxTop];
-  uint64_t merged[kMaxTop * kMaxCluster];
-  uint32_t best[kLogpThreads];
-  int16_t who[kLogpThreads];
-  int candidates, count;
-  uint32_t bound;
+  uint64_t merged[kMaxTop * kMaxCluster];       // the cluster's lists
+  int near[N], who[N];                  // threads of which one batch is looked at again, all of them
+  int n_near, n_who, count;
+  uint32_t bounds[N / 32];
 };
 
-// list: the n first places of this CTA's part, given every thread's maximum.
-template <class E>
-__device__ void top_of_part(const Part<E>& p, float m, int n, TopRoom<E>& t) {
+// The largest of a thread's vectors, its batch of kAhead (by its first vector), and the largest
+// of the other batches.
+struct Best {
+  float first, second;
+  int at;
+};
+// list: the n first places of this CTA's part.
+template <class E, int N>
+__device__ void top_of_part(const Part<E>& p, const Best& mine, int n, TopRoom<E, N>& t) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  constexpr int kWarpsHere = N / 32;
   // (a thread without a finite maximum may have nothing but NaN, which is below all)
-  t.best[tid] = m > -INFINITY ? ordered(m) : 0u;
-  if (tid == 0) t.candidates = t.count = 0;
-  __syncthreads();
-  if (wid == 0) {
-    // the n-th largest of the maxima, its low half dropped: 16 halvings
-    uint32_t mine[kLogpThreads / 32];
-#pragma unroll
-    for (int j = 0; j < kLogpThreads / 32; ++j) mine[j] = t.best[lane + 32 * j] >> 16;
-    uint32_t bound = 0;
-    for (uint32_t bit = 0x8000u; bit != 0; bit >>= 1) {
-      int reach = 0;
-#pragma unroll
-      for (int j = 0; j < kLogpThreads / 32; ++j) reach += mine[j] >= (bound | bit);
-      if (__reduce_add_sync(0xffffffffu, reach) >= n) bound |= bit;
-    }
-    if (lane == 0) t.bound = bound << 16;
+  const uint32_t best = mine.first > -INFINITY ? ordered(mine.first) : 0u;
+  const uint32_t other = mine.second > -INFINITY ? ordered(mine.second) : 0u;
+  if (tid == 0) t.n_near = t.n_who = t.count = 0;
+  // Each warp's q-th largest maximum, q its share of n among the warps that have a vector for
+  // every lane: n maxima at least reach the least of these.
+  const int full = min(kWarpsHere, (p.last - p.first) / 32);
+  uint32_t left = best, share = 0;
+  for (int q = full > 0 ? (n + full - 1) / full : 0; q > 0;) {
+    share = __reduce_max_sync(0xffffffffu, left);
+    if (share == 0) break;
+    const bool it = left == share;
+    q -= __popc(__ballot_sync(0xffffffffu, it));
+    if (it) left = 0;
   }
+  if (lane == 0) t.bounds[wid] = share;
   __syncthreads();
-  const uint32_t bound = t.bound;
-  if (t.best[tid] >= bound) t.who[atomicAdd(&t.candidates, 1)] = (int16_t)tid;
-  auto keep = [&](float z, int v) {
-    if (ordered(z) >= bound) {
-      const int at = atomicAdd(&t.count, 1);
-      if (at < kBuffer<E>) t.buffer[at] = place_of(z, v);
-    }
+  uint32_t bound = t.bounds[0];
+#pragma unroll
+  for (int w = 1; w < kWarpsHere; ++w)
+    if (w < full) bound = min(bound, t.bounds[w]);
+  auto note = [&](bool it, int* list, int* n, int what) {
+    const uint32_t those = __ballot_sync(0xffffffffu, it);
+    int at = 0;
+    if (those == 0) return;
+    if (lane == 0) at = atomicAdd(n, __popc(those));
+    at = __shfl_sync(0xffffffffu, at, 0) + __popc(those & ((1u << lane) - 1));
+    if (it) list[at] = what;
+  };
+  note(best >= bound && other < bound, t.near, &t.n_near, mine.at);
+  note(best >= bound && other >= bound, t.who, &t.n_who, p.first + tid);
+  const float low = value_of(bound);
+  auto reaches = [&](float z) { return bound == 0 || z >= low; };
+  auto keep = [&](uint32_t those, const auto& z, int v) {
+    int at = atomicAdd(&t.count, __popc(those));
+    for (; those; those &= those - 1, ++at)
+      if (at < kBuffer<E, N>) t.buffer[at] = place_of(z(__ffs(those) - 1), v + __ffs(those) - 1);
   };
   const int single = single_at(p, tid);
-  if (single >= 0) keep(widen(p.row[single]), single);
+  if (single >= 0) {
+    const float z = widen(p.row[single]);
+    if (reaches(z)) keep(1u, [&](int) { return z; }, single);
+  }
   __syncthreads();
-  const int candidates = t.candidates;
-  for (int c = wid; c < candidates; c += kLogpWarps) {
-    for (int i = p.first + t.who[c] + lane * kLogpThreads; i < p.last; i += 32 * kLogpThreads) {
-      float z[kVec<E>];
-      unpack(vector_at(p, i), z);
+  // those vectors, by all threads
+  const int near = kAhead * t.n_near, whole = t.n_who;
+  const int items = near + whole * ((p.last - p.first + N - 1) / N);
+  for (int i0 = tid; i0 < items; i0 += kAhead * N) {
+    uint4 x[kAhead];
+    int at[kAhead];
 #pragma unroll
-      for (int j = 0; j < kVec<E>; ++j) keep(z[j], p.body + i * kVec<E> + j);
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * N;
+      at[k] = p.last;
+      if (i >= items) continue;
+      if (i < near) {
+        at[k] = t.near[i / kAhead] + i % kAhead * N;
+      } else {
+        const int j = (i - near) / whole;
+        at[k] = t.who[i - near - j * whole] + j * N;
+      }
+      if (at[k] < p.last) x[k] = vector_at(p, at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (at[k] >= p.last) continue;
+      float z[kVec<E>];
+      unpack(x[k], z);
+      uint32_t those = 0;
+#pragma unroll
+      for (int e = 0; e < kVec<E>; ++e) those |= reaches(z[e]) ? 1u << e : 0u;
+      // (the elements by their number from the words: an index into registers is none)
+      if (those) keep(those, [&](int e) { return element(x[k], e, E()); }, p.body + at[k] * kVec<E>);
     }
   }
   __syncthreads();
-  if (t.count <= kBuffer<E>) {
-    first_of(t.buffer, t.count, n, t.list);
+  if (t.count <= kBuffer<E, N>) {
+    first_of<N>(t.buffer, t.count, n, t.list);
     return;
   }
   // More elements reach the bound than there is room for (equal logits, or the best ones
@@ -213,7 +297,7 @@ __device__ void top_of_part(const Part<E>& p, float m, int n, TopRoom<E>& t) {
     const uint64_t at = place_of(z, v);
     if (at > least) t.buffer[atomicAdd(&t.count, 1)] = at;
   };
-  for (int from = p.first - kLogpThreads; from < p.last; from += kLogpThreads) {
+  for (int from = p.first - N; from < p.last; from += N) {
     if (from < p.first) {
       if (single >= 0) better(widen(p.row[single]), single);
     } else if (from + tid < p.last) {
@@ -225,108 +309,127 @@ __device__ void top_of_part(const Part<E>& p, float m, int n, TopRoom<E>& t) {
     __syncthreads();
     const int count = t.count;
     if (count > n) {
-      first_of(t.buffer, count, n, t.list);
+      first_of<N>(t.buffer, count, n, t.list);
       __syncthreads();
       least = t.list[n - 1];
-      for (int i = tid; i < n; i += kLogpThreads) t.buffer[i] = t.list[i];
+      for (int i = tid; i < n; i += N) t.buffer[i] = t.list[i];
       if (tid == 0) t.count = n;
     }
     __syncthreads();
   }
-  first_of(t.buffer, t.count, n, t.list);
+  first_of<N>(t.buffer, t.count, n, t.list);
 }
 
-__device__ __forceinline__ Sums sums_at(const Sums* p, unsigned rank) {
+// Writes to shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ void put_sums(const Sums* p, unsigned rank, const Sums& v) {
   const uint32_t at = peer_smem(p, rank);
-  Sums r;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(r.m) : "r"(at) : "memory");
-  asm volatile("ld.shared::cluster.f32 %0, [%1 + 4];" : "=f"(r.s) : "r"(at) : "memory");
-  asm volatile("ld.shared::cluster.f32 %0, [%1 + 8];" : "=f"(r.u) : "r"(at) : "memory");
-  return r;
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(v.m) : "memory");
+  asm volatile("st.shared::cluster.f32 [%0 + 4], %1;" ::"r"(at), "f"(v.s) : "memory");
+  asm volatile("st.shared::cluster.f32 [%0 + 8], %1;" ::"r"(at), "f"(v.u) : "memory");
 }
-__device__ __forceinline__ uint64_t word_at(const uint64_t* p, unsigned rank) {
-  uint64_t r;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(r) : "r"(peer_smem(p, rank)) : "memory");
-  return r;
+__device__ __forceinline__ void put_word(const uint64_t* p, unsigned rank, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(peer_smem(p, rank)), "l"(v) : "memory");
 }
+// The halves of a barrier over the cluster.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// A row by a cluster of CTAs (one, two, four or eight), each a part of it.
-template <class E, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(kLogpThreads) token_logp_kernel(const LogpArgs a, const int parts) {
+// A row by a cluster of CTAs (one, two, four or eight), each a part of it.  Memory-bound: 8192 x
+// 128256 bf16 294 us (7.1 TB/s), with the entropy 296, with the 20 likeliest too 350; 1531 x
+// 50257 fp32 52, 50 and 59 us.  One row of 151936 takes 4.0 us and 6.8, a chain of latencies.
+// 6 CTAs of 256 to an SM leave 40 registers: at 5, 1531 rows are two rounds and a little.
+template <class E, bool ENTROPY, bool TOP, int N>
+__global__ void __launch_bounds__(N, N == 32 ? 32 : 1536 / N) token_logp_kernel(const LogpArgs a, const int parts) {
   grid_wait();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const unsigned rank = parts > 1 ? cluster_rank() : 0;
+  if (parts > 1) cluster_arrive();
   const int64_t t = blockIdx.x / (unsigned)parts;
   const Part<E> p = part_of(static_cast<const E*>(a.logits) + t * a.ld, a.V, rank, parts);
+  const int64_t target = load_id(a.targets, a.id_bytes, t);
   Sums r = {-INFINITY, 0.0f, 0.0f};
-  constexpr int kAhead = 4;
-  int i = p.first + tid;
-  for (; i + (kAhead - 1) * kLogpThreads < p.last; i += kAhead * kLogpThreads) {
+  Best best = {-INFINITY, -INFINITY, p.first + tid};
+  for (int i = p.first + tid; i < p.last; i += kAhead * N) {
     uint4 v[kAhead];
+    float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) v[j] = vector_at(p, i + j * kLogpThreads);
+    for (int j = 0; j < kAhead; ++j)
+      if (i + j * N < p.last) v[j] = vector_at(p, i + j * N);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i + j * N < p.last) top = fmaxf(top, largest(v[j], E()));
+    const float old = r.m;
+    if (raise<ENTROPY>(r, top)) {
+      if (TOP) best.second = old, best.at = i;
+    } else if (TOP) {
+      best.second = fmaxf(best.second, top);
+    }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
+      if (i + j * N >= p.last) break;
       float z[kVec<E>];
       unpack(v[j], z);
       take<ENTROPY>(r, z);
     }
   }
-  for (; i < p.last; i += kLogpThreads) {
-    float z[kVec<E>];
-    unpack(vector_at(p, i), z);
-    take<ENTROPY>(r, z);
-  }
+  best.first = r.m;
   const int single = single_at(p, tid);
   if (single >= 0) {
     const float z[1] = {widen(p.row[single])};
+    raise<ENTROPY>(r, z[0]);
     take<ENTROPY>(r, z);
   }
-  const float best = r.m;
-#pragma unroll
-  for (int w = 16; w > 0; w >>= 1) {
-    const Sums o = {__shfl_xor_sync(0xffffffffu, r.m, w), __shfl_xor_sync(0xffffffffu, r.s, w),
-                    ENTROPY ? __shfl_xor_sync(0xffffffffu, r.u, w) : 0.0f};
-    // the lower lane first, so that both come to the same sum
-    r = (lane & w) ? join<ENTROPY>(o, r) : join<ENTROPY>(r, o);
-  }
-  __shared__ Sums warps[kLogpWarps];
+  const bool has = target >= 0 && target < a.V;
+  const E z_target = tid == 0 && has ? p.row[target] : narrow<E>(0.0f);
+  r = join_lanes<ENTROPY, 32>(r);
+  constexpr int kWarpsHere = N / 32;
+  const Sums nothing = {-INFINITY, 0.0f, 0.0f};
+  __shared__ Sums warps[kWarpsHere];
   __shared__ Sums whole;
   if (lane == 0) warps[wid] = r;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kLogpWarps; ++w) r = join<ENTROPY>(r, warps[w]);
-    whole = r;
+  if (wid == 0) {
+    r = join_lanes<ENTROPY, kWarpsHere>(lane < kWarpsHere ? warps[lane] : nothing);
+    if (lane == 0) whole = r;
   }
   extern __shared__ __align__(16) unsigned char room[];
-  TopRoom<E>& top = *reinterpret_cast<TopRoom<E>*>(room);
+  TopRoom<E, N>& top = *reinterpret_cast<TopRoom<E, N>*>(room);
   if (TOP) top_of_part(p, best, a.n_top, top);
   if (parts > 1) {
-    cluster_sync();                       // the others' sums and lists are there
-    if (rank == 0) {
-      if (tid == 0) {
-        Sums all = whole;
-        for (int k = 1; k < parts; ++k) all = join<ENTROPY>(all, sums_at(&whole, k));
-        r = all;
-      }
-      if (TOP)
-        for (int j = tid; j < parts * a.n_top; j += kLogpThreads)
-          top.merged[j] = word_at(&top.list[j % a.n_top], j / a.n_top);
-    }
-    cluster_sync();                       // they have been read
+    // to the first CTA, all of which have begun by now
+    __shared__ Sums peers[kMaxCluster];
+    __syncthreads();
+    cluster_wait();
+    if (TOP && tid == 0) top.count = 0;     // (after the last use of it, ahead of the barrier below)
+    if (TOP && tid < a.n_top) put_word(&top.merged[rank * a.n_top + tid], 0, top.list[tid]);
+    if (tid == 0) put_sums(&peers[rank], 0, whole);
+    cluster_sync();
     if (rank != 0) return;
-    if (tid == 0) whole = r;
-    if (TOP) first_of(top.merged, parts * a.n_top, a.n_top, top.list);
+    if (wid == 0) {
+      r = join_lanes<ENTROPY, kMaxCluster>(lane < parts ? peers[lane] : nothing);
+      if (lane == 0) whole = r;
+    }
+    if (TOP) {
+      // at least n_top of the lists' elements are no lower than the lowest of their q-th ones
+      const int n = a.n_top, q = (n + parts - 1) / parts;
+      uint64_t least = ~0ull;
+#pragma unroll
+      for (int k = 0; k < kMaxCluster; ++k)
+        if (k < parts) least = min(least, top.merged[k * n + q - 1]);
+      for (int i = tid; i < parts * n; i += N) {
+        const uint64_t v = top.merged[i];
+        if (v >= least) top.buffer[atomicAdd(&top.count, 1)] = v;
+      }
+      __syncthreads();
+      first_of<N>(top.buffer, top.count, n, top.list);
+    }
   }
   __syncthreads();
   const float m = whole.m, L = logf(whole.s);
   const bool empty = whole.s == 0.0f;   // nothing but minus infinity (a finite maximum adds 1, NaN NaN)
   if (tid == 0) {
     if (a.stats) a.stats[t] = make_float2(m, L);
-    const int64_t v = load_id(a.targets, a.id_bytes, t);
-    float out = 0.0f;
-    if (v >= 0 && v < a.V) out = empty ? -INFINITY : widen(p.row[v]) - m - L;
-    a.logp[t] = out;
+    a.logp[t] = !has ? 0.0f : empty ? -INFINITY : widen(z_target) - m - L;
     if (ENTROPY) a.entropy[t] = empty ? 0.0f : L - whole.u / whole.s * kLn2;
   }
   if (TOP && tid < a.n_top) {
@@ -350,12 +453,12 @@ struct LogpGradArgs {
 };
 constexpr int kGradVecs = 4;             // of a thread
 template <class E>
-constexpr int kGradPiece = kLogpThreads * kGradVecs * kVec<E>;
+constexpr int kGradPiece = kGradThreads * kGradVecs * kVec<E>;
 
 // dz_v = g ([v = target] - p_v) - h p_v (log p_v + H).  Bound by memory: a row is read and
 // written once.  A row whose g and h are 0 is not read.
 template <class E, bool ENTROPY>
-__global__ void __launch_bounds__(kLogpThreads) token_logp_grad_kernel(const LogpGradArgs a) {
+__global__ void __launch_bounds__(kGradThreads) token_logp_grad_kernel(const LogpGradArgs a) {
   grid_wait();
   const int64_t t = blockIdx.x / a.pieces;
   const int piece = (int)(blockIdx.x % a.pieces);
@@ -381,17 +484,17 @@ __global__ void __launch_bounds__(kLogpThreads) token_logp_grad_kernel(const Log
       const int s = single_at(p, tid);
       if (s >= 0) out[s] = narrow<E>(none ? 0.0f : grad(widen(row[s]), s));
     }
-    const int i0 = piece * kLogpThreads * kGradVecs + tid;
+    const int i0 = piece * kGradThreads * kGradVecs + tid;
     uint4* to = reinterpret_cast<uint4*>(out + p.body);
     uint4 x[kGradVecs];
     if (!none) {
 #pragma unroll
       for (int j = 0; j < kGradVecs; ++j)
-        if (i0 + j * kLogpThreads < p.vecs) x[j] = vector_at(p, i0 + j * kLogpThreads);
+        if (i0 + j * kGradThreads < p.vecs) x[j] = vector_at(p, i0 + j * kGradThreads);
     }
 #pragma unroll
     for (int j = 0; j < kGradVecs; ++j) {
-      const int i = i0 + j * kLogpThreads;
+      const int i = i0 + j * kGradThreads;
       if (i >= p.vecs) break;
       if (none) {
         to[i] = make_uint4(0, 0, 0, 0);
@@ -404,16 +507,23 @@ __global__ void __launch_bounds__(kLogpThreads) token_logp_grad_kernel(const Log
       to[i] = repack(z);
     }
   } else {
-    for (int v = piece * kGradPiece<E> + tid, k = 0; k < kGradVecs * kVec<E> && v < a.V; ++k, v += kLogpThreads)
+    for (int v = piece * kGradPiece<E> + tid, k = 0; k < kGradVecs * kVec<E> && v < a.V; ++k, v += kGradThreads)
       out[v] = narrow<E>(none ? 0.0f : grad(widen(row[v]), v));
   }
 }
 
-template <class E>
+template <class E, int N>
 const void* logp_fn(bool entropy, bool top) {
-  return entropy ? top ? (const void*)token_logp_kernel<E, true, true> : (const void*)token_logp_kernel<E, true, false>
-         : top   ? (const void*)token_logp_kernel<E, false, true>
-                 : (const void*)token_logp_kernel<E, false, false>;
+  return entropy ? top ? (const void*)token_logp_kernel<E, true, true, N> : (const void*)token_logp_kernel<E, true, false, N>
+         : top   ? (const void*)token_logp_kernel<E, false, true, N>
+                 : (const void*)token_logp_kernel<E, false, false, N>;
+}
+template <class E>
+const void* logp_fn(int threads, bool entropy, bool top, size_t* room) {
+  *room = !top ? 0 : threads == 32 ? sizeof(TopRoom<E, 32>) : threads == 128 ? sizeof(TopRoom<E, 128>) : sizeof(TopRoom<E, 256>);
+  return threads == 32    ? logp_fn<E, 32>(entropy, top)
+         : threads == 128 ? logp_fn<E, 128>(entropy, top)
+                          : logp_fn<E, 256>(entropy, top);
 }
 
 bool logits_ok(const void* p, int32_t dtype, int64_t T, int64_t V, int64_t ld) {
@@ -441,13 +551,25 @@ extern "C" int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t 
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return BKMOO_ERR_CUDA;
+  // Few rows: by more CTAs, while all are on the card at once and have 4096 logits each (300 x
+  // 32000 bf16: 7.3 us by one, 5.9 by two, 7.2 by four; 1 x 151936: 5.0 by four, 4.0 by eight).
   int parts = 1;
   while (parts < kMaxCluster && T * parts * 2 <= 8 * sms && V / (2 * parts) >= 4096) parts *= 2;
   if (T * parts > 0x7fffffffll) return BKMOO_ERR_INVALID;
   LogpArgs a = {logits, ld, T, (int32_t)V, targets, id_bytes, n_top, logp,
                 reinterpret_cast<float2*>(stats), entropy, top_ids, top_logp};
   const bool f32 = dtype == BKMOO_F32;
-  const void* fn = f32 ? logp_fn<float>(entropy, n_top > 0) : logp_fn<__nv_bfloat16>(entropy, n_top > 0);
+  const int64_t vecs = V / parts * (int64_t)float_bytes(dtype) / 16;
+  // Threads a row (a warp alone, 128 or 256): the fewer, the less of a row's time goes into what
+  // its threads do together, but a long row by few is slow.  20000 bf16 rows of 2000: 15, 27 and
+  // 45 us, the 20 likeliest 48, 83 and 143; 4096 of 10007: 14, 14.5 and 18 (31, 29, 40); 1500
+  // fp32 of 262144: 359, 219 and 240 (750, 273, 256).  Where rows are few, latency counts:
+  // 20 rows of 4000 3.2, 2.2 and 2.3 (8.4, 4.5, 4.2).
+  const bool many = T * parts >= 8 * sms;
+  const int threads = vecs < (many ? 768 : 256) ? 32 : vecs < (many ? 6000 : 1024) ? 128 : 256;
+  size_t room = 0;
+  const void* fn = f32 ? logp_fn<float>(threads, entropy, n_top > 0, &room)
+                       : logp_fn<__nv_bfloat16>(threads, entropy, n_top > 0, &room);
   void* list[] = {&a, &parts};
   cudaLaunchConfig_t cfg = {};
   // (the kernel waits at its top for the one ahead of it: launch_behind)
@@ -458,8 +580,8 @@ extern "C" int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t 
   attr[1].val.clusterDim.x = parts;
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3((unsigned)(T * parts));
-  cfg.blockDim = dim3(kLogpThreads);
-  cfg.dynamicSmemBytes = n_top == 0 ? 0 : f32 ? sizeof(TopRoom<float>) : sizeof(TopRoom<__nv_bfloat16>);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = room;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cfg.attrs = attr;
   cfg.numAttrs = parts > 1 ? 2 : 1;
@@ -489,7 +611,7 @@ extern "C" int bkmoo_token_logp_backward(const void* logits, int64_t ld, int32_t
                    : d_entropy ? (const void*)token_logp_grad_kernel<__nv_bfloat16, true>
                                : (const void*)token_logp_grad_kernel<__nv_bfloat16, false>;
   void* list[] = {&a};
-  return launch_behind(fn, dim3((unsigned)(T * pieces)), dim3(kLogpThreads), list, 0,
+  return launch_behind(fn, dim3((unsigned)(T * pieces)), dim3(kGradThreads), list, 0,
                        static_cast<cudaStream_t>(stream), true) == cudaSuccess
              ? BKMOO_OK
              : BKMOO_ERR_CUDA;
