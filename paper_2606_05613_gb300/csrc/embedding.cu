@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kEmbedThreads) merge_keys_kernel(const __grid_
   __shared__ uint32_t keys[kMerge][kSortRun];
   const int tid = threadIdx.x;
   const int64_t own = (int64_t)blockIdx.x * kMergeRows / kSortRun, first = own / kMerge * kMerge * kSortRun;
-#pragma unroll 8
+#pragma unroll
   for (int j = 0; j < kMerge; ++j) {
     const int64_t i = first + j * kSortRun + tid;
     keys[j][tid] = i < a.T ? (uint32_t)(a.in[i] >> 32) : kNoToken;
@@ -330,7 +330,7 @@ __device__ __forceinline__ float* part_row(const SumArgs& a, int64_t piece, int 
 constexpr int kSumThreads = 128;
 constexpr int kRowsAhead = 4;
 template <class E, class W, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) sum_pieces_kernel(const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(kSumThreads, sizeof(E) + sizeof(W) == 4 && VEC ? 8 : 5) sum_pieces_kernel(const __grid_constant__ SumArgs a) {
   grid_wait();
   const int lane = threadIdx.x & 31;
   const int64_t unit = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
@@ -346,21 +346,22 @@ __global__ void __launch_bounds__(kSumThreads) sum_pieces_kernel(const __grid_co
   const uint32_t ends = __ballot_sync(0xffffffffu, key != kNoToken && key != next);
   const bool first = n > 0 && __shfl_sync(0xffffffffu, key, 0) == before;      // the sum began before the piece
   const uint32_t whole = first ? ends & (ends - 1) : ends;      // ends of the sums that began here
+  // each lane's own row and the place that it is added to
+  const uint64_t from = (uint64_t)(static_cast<const E*>(a.dy) + (int64_t)row * a.ld);
+  const uint64_t place = key == kNoToken ? 0 : (uint64_t)place_of<W>(a, key);
   float sum[8] = {};
   for (int i0 = 0; i0 < n; i0 += kRowsAhead) {
     Eight<E, VEC> dy[kRowsAhead];
     Eight<W, VEC> old[kRowsAhead];
-    W* to[kRowsAhead];
 #pragma unroll
     for (int j = 0; j < kRowsAhead; ++j)
-      if (i0 + j < n)
-        dy[j].load(static_cast<const E*>(a.dy) + (int64_t)__shfl_sync(0xffffffffu, row, i0 + j) * a.ld, c0, lane, a.D);
+      if (i0 + j < n) dy[j].load(reinterpret_cast<const E*>(__shfl_sync(0xffffffffu, from, i0 + j)), c0, lane, a.D);
+    if (a.accumulate) {
 #pragma unroll
-    for (int j = 0; j < kRowsAhead; ++j)
-      if (whole >> (i0 + j) & 1) {
-        to[j] = place_of<W>(a, __shfl_sync(0xffffffffu, key, i0 + j));
-        if (a.accumulate) old[j].load(to[j], c0, lane, a.D);
-      }
+      for (int j = 0; j < kRowsAhead; ++j)
+        if (whole >> (i0 + j) & 1)
+          old[j].load(reinterpret_cast<const W*>(__shfl_sync(0xffffffffu, place, i0 + j)), c0, lane, a.D);
+    }
 #pragma unroll
     for (int j = 0; j < kRowsAhead; ++j) {
       if (i0 + j >= n) break;
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kSumThreads) sum_pieces_kernel(const __grid_co
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += x[e];
       if (whole >> (i0 + j) & 1) {
-        finish<W, VEC>(a, to[j], c0, lane, sum, old[j]);
+        finish<W, VEC>(a, reinterpret_cast<W*>(__shfl_sync(0xffffffffu, place, i0 + j)), c0, lane, sum, old[j]);
       } else if (ends >> (i0 + j) & 1) {
         Part8::store(part_row(a, piece, 0, c0), 0, lane, kColumns, sum);
       } else if (i0 + j == n - 1) {     // goes on
