@@ -20,6 +20,7 @@ namespace {
 constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
 constexpr int kMaxHead = 256;
+constexpr int kForwardCtas = 6, kBackwardCtas = 4;     // on an SM
 constexpr int kAhead = 4;               // steps of a warp whose loads are on their way
 
 struct QkSide {
@@ -75,12 +76,18 @@ __device__ __forceinline__ Place place_of_lane(const QkArgs& a, int l) {
 struct Angles {
   float c[8], s[8];
 };
+__device__ __forceinline__ void eight(const float* p, float* x) {      // p: on 16 bytes
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
 __device__ __forceinline__ Angles angles_of(const Place& p, float (*room)[kMaxHead / 2]) {
   Angles g;
+  if (p.turns) {
+    eight(&room[0][p.pair], g.c);
+    eight(&room[1][p.pair], g.s);
+  } else {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    g.c[j] = p.turns ? room[0][p.pair + j] : 1.0f;
-    g.s[j] = p.turns ? room[1][p.pair + j] : 0.0f;
+    for (int j = 0; j < 8; ++j) g.c[j] = 1.0f, g.s[j] = 0.0f;
   }
   return g;
 }
@@ -104,22 +111,25 @@ __device__ __forceinline__ float weight_at(const QkArgs& a, const void* w, int c
 struct Pair {
   uint4 lo[32], hi[32];
 };
-__device__ __forceinline__ void copy16(uint4* to, const __nv_bfloat16* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+// (Where !live nothing is read and the place becomes 0.)
+__device__ __forceinline__ void copy16(uint4* to, const __nv_bfloat16* from, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from),
+               "r"(live ? 16 : 0)
+               : "memory");
 }
-__device__ __forceinline__ void copy_pair(Pair& to, const __nv_bfloat16* head, const Place& p, int lane) {
-  copy16(&to.lo[lane], head + p.lo);
-  copy16(&to.hi[lane], head + p.hi);
+__device__ __forceinline__ void copy_pair(Pair& to, const __nv_bfloat16* head, const __nv_bfloat16* any, const Place& p, int lane,
+                                          bool live) {
+  copy16(&to.lo[lane], live ? head + p.lo : any, live);
+  copy16(&to.hi[lane], live ? head + p.hi : any, live);
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // All but the newest kAhead - 1 steps' copies have come.
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory"); }
-__device__ __forceinline__ void get_pair(const Pair& v, int lane, bool live, float (&x)[16]) {
-  float a[8] = {}, b[8] = {};
-  if (live) {
-    unpack(v.lo[lane], a);
-    unpack(v.hi[lane], b);
-  }
+__device__ __forceinline__ void get_pair(const Pair& v, int lane, float (&x)[16]) {
+  float a[8], b[8];
+  unpack(v.lo[lane], a);
+  unpack(v.hi[lane], b);
 #pragma unroll
   for (int j = 0; j < 8; ++j) x[j] = a[j], x[j + 8] = b[j];
 }
@@ -136,54 +146,60 @@ __device__ __forceinline__ float over_head(float v) {
   return v;
 }
 
-// A walk over steps: groups of heads, token after token.
-struct Walk {
+// A warp's way through steps: groups of 32 / G heads, the queries' of a token and then its
+// keys', token after token.  at: the lane's head in one array, behind the last of them no matter where.
+template <class E>
+struct Way {
   int64_t t;
-  int step;
-  __device__ __forceinline__ bool next(int per) {        // whether a token begins
-    if (++step < per) return false;
-    step = 0;
-    ++t;
-    return true;
-  }
+  int k, left, over;                    // the side, its steps from here, its heads from the lane's
+  E* at;
 };
 
-// G lanes a head.  A warp takes a run of steps, each 32 / G heads of a token's queries or keys.
+// G lanes a head.  A warp takes a run of steps.
 template <int G, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kQkThreads) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
+__global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
   grid_wait();
-  __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
   __shared__ Pair ring[kQkWarps][kAhead];
   __shared__ __align__(16) float weights[2][kMaxHead];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const int per = a.side[0].steps + a.side[1].steps;
+  const int per = a.side[0].steps + a.side[1].steps, step_elems = 32 / G * a.hd;
   const int64_t total = a.T * per, from = ((int64_t)blockIdx.x * kQkWarps + wid) * each;
   const int64_t to = from + each < total ? from + each : total;
+  const int steps = from < to ? (int)(to - from) : 0;
   const Place p = place_of_lane<NEIGHBOURS>(a, lane % G);
-  Walk here = {from / per, 0}, there;
-  here.step = (int)(from - here.t * per);
-  there = here;
-  struct Head {
-    int k, head;
-    bool live;
+  // to step i of a side of a token
+  auto set = [&](auto& w, auto* const x, int64_t ld, int i) {
+    const int head = i * (32 / G) + lane / G;
+    w.left = a.side[w.k].steps - i;
+    w.over = p.live ? a.side[w.k].heads - head : 0;
+    w.at = x + w.t * ld + (int64_t)head * a.hd;
   };
-  auto head_of = [&](const Walk& w) {
-    Head h;
-    h.k = w.step >= a.side[0].steps;
-    h.head = (w.step - (h.k ? a.side[0].steps : 0)) * (32 / G) + lane / G;
-    h.live = p.live && h.head < a.side[h.k].heads;
-    return h;
+  Way<const __nv_bfloat16> there;
+  Way<__nv_bfloat16> here;
+  {
+    const int step = (int)(from % per), k = step >= a.side[0].steps, i = step - (k ? a.side[0].steps : 0);
+    here.t = there.t = from / per;
+    here.k = there.k = k;
+    set(there, a.side[k].x, a.side[k].ld, i);
+    set(here, a.side[k].out, a.side[k].ld_out, i);
+  }
+  // whether the side ends
+  auto next = [&](auto& w) {
+    w.over -= 32 / G;
+    w.at += step_elems;
+    if (--w.left > 0) return false;
+    w.k ^= 1;
+    if (w.k == 0) ++w.t;
+    return true;
   };
-  int64_t ahead = from;
+  int ahead = 0;
   auto fetch = [&]() {
-    if (ahead < to) {
-      const Head h = head_of(there);
-      const QkSide& s = a.side[h.k];
-      if (h.live) copy_pair(ring[wid][(ahead - from) % kAhead], s.x + there.t * s.ld + (int64_t)h.head * a.hd, p, lane);
-      there.next(per);
-    }
-    ++ahead;
+    const bool live = there.over > 0 && ahead < steps;
+    copy_pair(ring[wid][ahead % kAhead], there.at, a.side[0].x, p, lane, live);
     copies_end();
+    if (next(there)) set(there, a.side[there.k].x, a.side[there.k].ld, 0);
+    ++ahead;
   };
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
@@ -192,30 +208,51 @@ __global__ void __launch_bounds__(kQkThreads) qk_norm_kernel(const __grid_consta
     weights[k][c] = weight_at(a, a.side[k].w, c);
   }
   __syncthreads();
-  if (from >= to) return;
-  int64_t pos = load_id(a.pos, a.id_bytes, here.t);
-  bool new_token = true;
-  Angles g;
-  for (int64_t i = from; i < to; ++i) {
+  int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, here.t) : 0;
+  bool begins = true, new_token = true;
+  // r times these of the pair's two elements: the rotation of the weighed ones
+  float ca[8], sa[8], cb[8], sb[8];
+  for (int i = 0; i < steps; ++i) {
     fetch();
-    if (new_token) {
-      angles(a, (uint64_t)pos, lane, room[wid]);
-      g = angles_of(p, room[wid]);
-      if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
+    if (begins) {
+      if (new_token) {
+        angles(a, (uint64_t)pos, lane, room[wid]);
+        if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
+      }
+      const Angles g = angles_of(p, room[wid]);
+      float w[16];
+      eight(&weights[here.k][p.live ? p.lo : 0], w);
+      eight(&weights[here.k][p.live ? p.hi : 0], w + 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float wa = w[NEIGHBOURS ? 2 * j : j], wb = w[NEIGHBOURS ? 2 * j + 1 : j + 8];
+        ca[j] = wa * g.c[j];
+        sa[j] = wa * g.s[j];
+        cb[j] = wb * g.c[j];
+        sb[j] = wb * g.s[j];
+      }
     }
-    const Head h = head_of(here);
     copies_wait();
     float x[16], sum = 0.0f;
-    get_pair(ring[wid][(i - from) % kAhead], lane, h.live, x);
+    get_pair(ring[wid][i % kAhead], lane, x);
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum = fmaf(x[j], x[j], sum);
     const float r = rsqrtf(fmaf(over_head<G>(sum), a.inv_hd, a.eps));
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = x[j] * r * (p.live ? weights[h.k][(j < 8 ? p.lo : p.hi) + (j & 7)] : 0.0f);
-    rotate<NEIGHBOURS, false>(x, g);
-    if (h.live) store_pair(a.side[h.k].out + here.t * a.side[h.k].ld_out + (int64_t)h.head * a.hd, p, x);
-    new_token = here.next(per);
+    for (int j = 0; j < 8; ++j) {
+      float& u = x[NEIGHBOURS ? 2 * j : j];
+      float& v = x[NEIGHBOURS ? 2 * j + 1 : j + 8];
+      const float y = fmaf(-v, sb[j], u * ca[j]);
+      v = r * fmaf(u, sa[j], v * cb[j]);
+      u = r * y;
+    }
+    if (here.over > 0) store_pair(here.at, p, x);
+    const int64_t t = here.t;
+    begins = next(here);
+    if (begins) set(here, a.side[here.k].out, a.side[here.k].ld_out, 0);
+    new_token = here.t != t;
   }
+  copies_wait_all();
 }
 
 // The backward pass by CTAs that each take a run of one side's and one language's steps.
@@ -226,11 +263,12 @@ struct QkRuns {
   float* part;                          // [CTA][hd]
 };
 template <int G, bool NEIGHBOURS>
-__global__ void __launch_bounds__(kQkThreads, 4) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
+__global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
                                                                   const __grid_constant__ QkRuns q) {
   grid_wait();
-  __shared__ float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
   __shared__ Pair ring[kQkWarps][kAhead][2];             // x, dout
+  __shared__ __align__(16) float weights[kMaxHead];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % G;
   int run = 0;
   while ((int)blockIdx.x >= q.first[run + 1]) ++run;
@@ -241,60 +279,73 @@ __global__ void __launch_bounds__(kQkThreads, 4) qk_norm_grad_kernel(const __gri
   const int64_t each = (all + warps - 1) / warps;
   const int64_t from = me * each < all ? me * each : all, to = from + each < all ? from + each : all;
   const Place p = place_of_lane<NEIGHBOURS>(a, l);
-  Walk here = {q.rows[lang] + from / s.steps, (int)(from % s.steps)}, there = here;
-  int64_t ahead = from;
+  const int steps = (int)(to - from), step_elems = 32 / G * a.hd;
+  // the lane's head in each array, and what leads from a token's last to the next one's first
+  const int64_t t0 = q.rows[lang] + from / s.steps;
+  const int step0 = (int)(from % s.steps), head0 = lane / G;
+  const int64_t back = (int64_t)(s.steps - 1) * step_elems, in = (int64_t)(step0 * (32 / G) + head0) * a.hd;
+  const __nv_bfloat16 *at_x = s.x + t0 * s.ld + in, *at_d = s.dout + t0 * s.ld_dout + in;
+  __nv_bfloat16* at_out = s.out + t0 * s.ld_out + in;
+  int step = step0, step_there = step0, ahead = 0;
+  int64_t t = t0;
+  auto live_at = [&](int step) { return p.live && step * (32 / G) + head0 < s.heads; };
   auto fetch = [&]() {
-    if (ahead < to) {
-      const int head = there.step * (32 / G) + lane / G;
-      Pair* r = ring[wid][(ahead - from) % kAhead];
-      if (p.live && head < s.heads) {
-        copy_pair(r[0], s.x + there.t * s.ld + (int64_t)head * a.hd, p, lane);
-        copy_pair(r[1], s.dout + there.t * s.ld_dout + (int64_t)head * a.hd, p, lane);
-      }
-      there.next(s.steps);
-    }
-    ++ahead;
+    Pair* r = ring[wid][ahead % kAhead];
+    const bool live = ahead < steps && live_at(step_there);
+    copy_pair(r[0], at_x, s.x, p, lane, live);
+    copy_pair(r[1], at_d, s.x, p, lane, live);
     copies_end();
+    const bool end = ++step_there == s.steps;
+    if (end) step_there = 0;
+    at_x += end ? s.ld - back : step_elems;
+    at_d += end ? s.ld_dout - back : step_elems;
+    ++ahead;
   };
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
-  float w[16], dw[16] = {};
-#pragma unroll
-  for (int j = 0; j < 16; ++j) w[j] = p.live ? weight_at(a, s.w, (j < 8 ? p.lo : p.hi) + (j & 7)) : 0.0f;
-  int64_t pos = from < to ? load_id(a.pos, a.id_bytes, here.t) : 0;
+  for (int c = threadIdx.x; c < a.hd; c += kQkThreads) weights[c] = weight_at(a, s.w, c);
+  __syncthreads();
+  float dw[16] = {};
+  int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, t) : 0;
   bool new_token = true;
   Angles g;
-  for (int64_t i = from; i < to; ++i) {
+  for (int i = 0; i < steps; ++i) {
     fetch();
     if (new_token) {
       angles(a, (uint64_t)pos, lane, room[wid]);
       g = angles_of(p, room[wid]);
-      if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
+      if (t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, t + 1);
     }
-    const int head = here.step * (32 / G) + lane / G;
-    const bool live = p.live && head < s.heads;
+    const bool live = live_at(step);
     copies_wait();
-    const Pair* v = ring[wid][(i - from) % kAhead];
-    float x[16], d[16], sum = 0.0f, dot = 0.0f;
-    get_pair(v[0], lane, live, x);
-    get_pair(v[1], lane, live, d);
+    const Pair* v = ring[wid][i % kAhead];
+    float x[16], d[16], w[16], sum = 0.0f, dot = 0.0f;
+    eight(&weights[p.live ? p.lo : 0], w);
+    eight(&weights[p.live ? p.hi : 0], w + 8);
+    get_pair(v[0], lane, x);
+    get_pair(v[1], lane, d);
     rotate<NEIGHBOURS, true>(d, g);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       sum = fmaf(x[j], x[j], sum);
-      dot = fmaf(d[j] * w[j], x[j], dot);
+      w[j] *= d[j];
+      dot = fmaf(w[j], x[j], dot);
     }
     // (0 beyond the last head: without eps, 1 / sqrt(0) would leave NaN in dw)
     const float squares = over_head<G>(sum), r = live ? rsqrtf(fmaf(squares, a.inv_hd, a.eps)) : 0.0f;
     const float c = over_head<G>(dot) * r * r * a.inv_hd;     // mean(w dy n) / n's x
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
-      dw[j] = fmaf(d[j], x[j] * r, dw[j]);
-      d[j] = r * fmaf(-x[j], c, d[j] * w[j]);
+      const float n = x[j] * r;
+      dw[j] = fmaf(d[j], n, dw[j]);
+      d[j] = r * fmaf(-x[j], c, w[j]);
     }
-    if (live) store_pair(s.out + here.t * s.ld_out + (int64_t)head * a.hd, p, d);
-    new_token = here.next(s.steps);
+    if (live) store_pair(at_out, p, d);
+    new_token = ++step == s.steps;
+    at_out += new_token ? s.ld_out - back : step_elems;
+    if (new_token) step = 0, ++t;
   }
+  copies_wait_all();
   if (!q.weights) return;
   __shared__ float sums[kQkWarps][kMaxHead];
 #pragma unroll
@@ -378,19 +429,9 @@ void fill(QkArgs& a, int64_t T, int64_t hq, int64_t hk, int64_t hd, const double
   a.T = T;
   for (int64_t i = 0; i < rot / 2; ++i) {
     const double turns = freq[i] * 0.15915494309189533577;        // 1 / 2 pi
-    const double part = std::ldexp(turns - std::floor(turns), 64);
+    const double part = (turns - std::floor(turns)) * 18446744073709551616.0;     // exact
     a.turn[i] = part < 18446744073709551616.0 ? (uint64_t)part : 0;
   }
-}
-// CTAs that are resident at once.
-int resident(const void* fn, int* ctas) {
-  int dev = 0, sms = 0, per = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per, fn, kQkThreads, 0) != cudaSuccess)
-    return BKMOO_ERR_CUDA;
-  *ctas = sms * (per < 1 ? 1 : per);
-  return BKMOO_OK;
 }
 constexpr int kMostCtas = 2048;         // of the backward pass, whose sums the workspace holds
 
@@ -441,7 +482,8 @@ extern "C" int bkmoo_qk_norm_forward(const void* q, int64_t ldq, const void* k, 
                    : g == 8 ? forward_fn<8>(interleaved)
                             : forward_fn<16>(interleaved);
   int ctas = 0;
-  if (resident(fn, &ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  if (tile_sms(&ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  ctas *= kForwardCtas;
   const int64_t total = T * (a.side[0].steps + a.side[1].steps);
   int64_t each = (total + (int64_t)ctas * kQkWarps - 1) / ((int64_t)ctas * kQkWarps);
   const int64_t grid = (total + each * kQkWarps - 1) / (each * kQkWarps);
@@ -511,7 +553,8 @@ extern "C" int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, con
                    : g == 8 ? backward_fn<8>(interleaved)
                             : backward_fn<16>(interleaved);
   int ctas = 0;
-  if (resident(fn, &ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  if (tile_sms(&ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
+  ctas *= kBackwardCtas;
   // one CTA more for each part that is not whole
   const int most = kMostCtas - 2 * kMaxK;
   if (ctas > most) ctas = most;
