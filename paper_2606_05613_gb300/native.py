@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import array
 import ctypes
+import functools
 import operator
 import os
 import threading
@@ -472,6 +473,10 @@ def _workspace(ws, dev: int):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
+_Pointers = [ctypes.c_void_p * n for n in range(17)]      # arrays of one for each language
+_Bounds = [ctypes.c_int64 * n for n in range(18)]
+
+
 def _language_rows(rows, T: int):
     """(K, array) of the language bounds."""
     r = [int(i) for i in rows]
@@ -481,7 +486,7 @@ def _language_rows(rows, T: int):
         last = i
     if not ok:
         raise ValueError("rows must be K + 1 bounds from 0 to the number of rows, 1 <= K <= 16")
-    return len(r) - 1, (ctypes.c_int64 * len(r))(*r)
+    return len(r) - 1, _Bounds[len(r)](*r)
 
 
 def _weight_grads(dw, K: int, rows: int, cols: int, dev: int, what: str):
@@ -494,15 +499,19 @@ def _weight_grads(dw, K: int, rows: int, cols: int, dev: int, what: str):
             raise ValueError("%s must be contiguous %d x %d matrices of one dtype on cuda:%d"
                              % (what, rows, cols, dev))
         at.append(g.data_ptr())
-    return (ctypes.c_void_p * K)(*at), _dtype_code(dw[0])
+    return _Pointers[K](*at), _dtype_code(dw[0])
 
 
 def _vector_grads(dw, K: int, n: int, dev: int, what: str):
     """The same of per-language gradients of a vector of n."""
     if len(dw) != K:
         raise ValueError("%s: one gradient per language, %d" % (what, K))
-    dt = dw[0].dtype
-    return (ctypes.c_void_p * K)(*[_plain(g, dt, n, dev, what) for g in dw]), _dtype_code(dw[0])
+    dt, at = dw[0].dtype, []
+    for g in dw:
+        if g.dtype is not dt or g.get_device() != dev or g.numel() != n or not g.is_contiguous():
+            raise ValueError("%s must be %d contiguous elements of one dtype on cuda:%d" % (what, n, dev))
+        at.append(g.data_ptr())
+    return _Pointers[K](*at), _dtype_code(dw[0])
 
 
 def bkmoo_gate_forward(x, w_gate, w_up, act, h=None, a=None, b=None, stream=None):
@@ -627,6 +636,7 @@ def bkmoo_embedding_forward(table, ids, out, scale=1.0, stream=None):
           _dtype_code(table), V, D, pi, nb, T, scale, po, ldo, _raw_stream(torch, stream, dev))
 
 
+@functools.lru_cache(maxsize=1024)
 def bkmoo_embedding_backward_workspace_size(T: int, D: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load().bkmoo_embedding_backward_workspace_size(T, D, ctypes.byref(n)),
@@ -647,8 +657,11 @@ def bkmoo_embedding_backward(dy, ids, rows, dw, scale=1.0, accumulate=False, ws=
     V = dw[0].shape[0] if len(dw) else 0
     g, dt = _weight_grads(dw, K, V, D, dev, "dw")
     if ws is None:
-        ws = _scratch(torch, bkmoo_embedding_backward_workspace_size(T, D), dev, stream)
-    pws, nws = _workspace(ws, dev)
+        nws = bkmoo_embedding_backward_workspace_size(T, D)
+        ws = _scratch(torch, nws, dev, stream)
+        pws = ws.data_ptr()
+    else:
+        pws, nws = _workspace(ws, dev)
     _call(torch, dev, "bkmoo_embedding_backward", load().bkmoo_embedding_backward, pd, ldd,
           _dtype_code(dy), pi, nb, T, V, D, scale, K, r, g, dt, 1 if accumulate else 0, pws, nws,
           _raw_stream(torch, stream, dev))
@@ -713,6 +726,7 @@ def bkmoo_qk_norm_forward(q, k, w_q, w_k, positions, inv_freq, q_out, k_out, eps
           pp, ldp, _raw_stream(torch, stream, dev))
 
 
+@functools.lru_cache(maxsize=None)
 def bkmoo_qk_norm_backward_workspace_size(width: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load().bkmoo_qk_norm_backward_workspace_size(width, ctypes.byref(n)),
@@ -750,9 +764,11 @@ def bkmoo_qk_norm_backward(dq_out, dk_out, q, k, w_q, w_k, positions, inv_freq, 
         if dt != du:
             raise ValueError("dw_q and dw_k must have one dtype")
         if ws is None:
-            ws = _scratch(torch, bkmoo_qk_norm_backward_workspace_size(width), dev, stream)
-    if ws is not None:
-        pws, nws = _workspace(ws, dev)
+            nws = bkmoo_qk_norm_backward_workspace_size(width)
+            ws = _scratch(torch, nws, dev, stream)
+            pws = ws.data_ptr()
+        else:
+            pws, nws = _workspace(ws, dev)
     _call(torch, dev, "bkmoo_qk_norm_backward", load().bkmoo_qk_norm_backward, pa, lda, pb, ldb, pq, ldq,
           pk, ldk, wq, wk, _dtype_code(w_q), T, hq, hk, width, pos, nb, f, rot, 1 if interleaved else 0,
           eps, K, r, po, ldo, pp, ldp, gq, gk, dt, 1 if accumulate else 0, pws, nws,
