@@ -4,17 +4,27 @@ The resolve needs one gradient per language.  BucketMOO gets them from K
 backward passes; where a batch holds the rows of all K languages one after
 another, these layers give them in one: a linear layer's weight gradient is a
 sum over rows, so language k's is the sum over its own rows
-(bkmoo_gate_backward, bkmoo_language_wgrad).  `rows` are K + 1 bounds: language k
-has the batch's rows from rows[k] to rows[k + 1].
+(bkmoo_gate_backward, bkmoo_language_wgrad); so are an embedding's, over the rows
+that hold a token, and that of the weights that scale normed queries and keys
+(bkmoo_embedding_backward, bkmoo_qk_norm_backward).  `rows` are K + 1 bounds:
+language k has the batch's rows from rows[k] to rows[k + 1].
 
 Inside BucketMOO.begin_batch() ... finish() the gradients are added to the
 parameters' `language_grads`, their places in the K flat buffers; outside, the
 layers' weights receive the ordinary gradient of the whole batch.  The gradients
 have no graph: gradients of gradients are refused.  Weights and
-activations are bfloat16 on a GPU; the products that no language splits
+activations are bfloat16 on a GPU (an embedding's and the logits of
+token_log_probs may be float32); the products that no language splits
 (y = x W^T and its dx of LanguageLinear) are torch's.
+
+A captured step (torch.cuda.graph) has begin_batch(), the forward and the
+backward pass all in the capture, and no graph of an eager pass over the same
+weights may be alive then: autograd would tie the capture to that pass's stream.
 """
 from __future__ import annotations
+
+import collections
+import functools
 
 import torch
 from torch.autograd.function import once_differentiable
@@ -130,6 +140,178 @@ class _Linear(torch.autograd.Function):
             native.bkmoo_language_wgrad(_on_rows(dy), m, rows, places, accumulate=True)
             _leave(to)
         return dx, whole, None
+
+
+def _matrix(t):
+    """t as a matrix with contiguous rows that do not overlap."""
+    t = t.reshape(-1, t.shape[-1])
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
+def _on_heads(t):
+    """t as [tokens, heads, width], a token's heads side by side and on 16 bytes."""
+    heads, width = t.shape[-2:]
+    t = t.reshape(-1, heads, width)
+    ld, between, step = t.stride()
+    if step == 1 and (between == width or heads == 1) and ld % 8 == 0 and ld >= heads * width and t.data_ptr() % 16 == 0:
+        return t
+    return torch.empty(t.shape, dtype=t.dtype, device=t.device).copy_(t)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, weight, scale, rows):
+        flat = ids.reshape(-1).contiguous()
+        y = weight.new_empty(flat.numel(), weight.shape[1])
+        native.bkmoo_embedding_forward(_matrix(weight), flat, y, scale)
+        ctx.save_for_backward(flat, weight)
+        ctx.scale, ctx.rows = scale, rows
+        return y.view(*ids.shape, weight.shape[1])
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        flat, weight = ctx.saved_tensors
+        if not ctx.needs_input_grad[1]:
+            return None, None, None, None
+        to = places, rows, whole = _languages(weight, ctx.rows, flat.numel())
+        _enter(to)
+        native.bkmoo_embedding_backward(_matrix(dy), flat, rows, places, ctx.scale, accumulate=True)
+        _leave(to)
+        return None, whole, None, None
+
+
+class _QueryKeyNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, w_q, w_k, positions, inv_freq, eps, interleaved, rows):
+        a, b = _on_heads(q), _on_heads(k)
+        u, v = w_q.contiguous(), w_k.contiguous()
+        pos = positions.reshape(-1).contiguous()
+        qo, ko = torch.empty(a.shape, dtype=a.dtype, device=a.device), torch.empty(b.shape, dtype=b.dtype, device=b.device)
+        native.bkmoo_qk_norm_forward(a, b, u, v, pos, inv_freq, qo, ko, eps, interleaved)
+        ctx.save_for_backward(a, b, w_q, w_k, pos)
+        ctx.fixed = inv_freq, eps, interleaved
+        ctx.rows, ctx.shapes = rows, (q.shape, k.shape)
+        return qo.view(q.shape), ko.view(k.shape)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dqo, dko):
+        q, k, w_q, w_k, pos = ctx.saved_tensors
+        inv_freq, eps, interleaved = ctx.fixed
+        T = q.shape[0]
+        dqo, dko, u, v = _on_heads(dqo), _on_heads(dko), w_q.contiguous(), w_k.contiguous()
+        dq, dk = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        # [places, bounds, gradient of the whole batch or None] of the weights that are trained
+        to = [_languages(w, ctx.rows, T) if need else None for w, need in zip((w_q, w_k), ctx.needs_input_grad[2:4])]
+
+        def call(rows, dw_q=None, dw_k=None):
+            native.bkmoo_qk_norm_backward(dqo, dko, q, k, u, v, pos, inv_freq, rows, dq, dk, dw_q, dw_k, eps, interleaved,
+                                          accumulate=True)
+
+        for t in to:
+            _enter(t)
+        if all(to) and (to[0][2] is None) == (to[1][2] is None):
+            call(to[0][1], to[0][0], to[1][0])
+        elif not any(to):
+            call([0, T])
+        else:
+            # one of them is frozen, or they are apart by different bounds: each with a place
+            # beside it for what the other one would get
+            for i, t in enumerate(to):
+                if t is not None:
+                    other = [torch.zeros_like(g) for g in t[0]]
+                    call(t[1], *((t[0], other) if i == 0 else (other, t[0])))
+        for t in to:
+            _leave(t)
+        return (dq.view(ctx.shapes[0]), dk.view(ctx.shapes[1]), *(t[2] if t is not None else None for t in to),
+                None, None, None, None, None)
+
+
+class _TokenLogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, targets, entropy, top):
+        z, lead = _matrix(logits), logits.shape[:-1]
+        t = targets.reshape(-1).contiguous()
+        T = z.shape[0]
+        logp, stats = torch.empty(T, device=z.device), torch.empty(T, 2, device=z.device)
+        H = torch.empty(T, device=z.device) if entropy else None
+        ids = torch.empty(T, top, dtype=torch.int64, device=z.device) if top else None
+        best = torch.empty(T, top, device=z.device) if top else None
+        native.bkmoo_token_logp_forward(z, t, logp, stats, H, ids, best)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(z, t, stats, H)
+        ctx.shape = logits.shape
+        out = [logp.view(lead)]
+        if entropy:
+            out.append(H.view(lead))
+        if top:
+            out += [ids.view(*lead, top), best.view(*lead, top)]
+            ctx.mark_non_differentiable(*out[-2:])
+        return tuple(out)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, g, *more):
+        z, t, stats, H = ctx.saved_tensors
+        h = more[0] if H is not None else None
+        g = torch.zeros(z.shape[0], device=z.device) if g is None else g.reshape(-1).contiguous()
+        dz = _room(z, *z.shape)
+        native.bkmoo_token_logp_backward(z, t, stats, g, dz, H, None if h is None else h.reshape(-1).contiguous())
+        return dz.reshape(ctx.shape), None, None, None
+
+
+TokenLogProbs = collections.namedtuple("TokenLogProbs", "logp entropy top_ids top_logp")
+
+
+def token_log_probs(logits, targets, entropy=False, top=0):
+    """Log probability of each row's target (0 where it is outside the vocabulary: padding), and
+    where asked for the rows' entropy and their `top` (32 at most) most likely tokens with their
+    log probabilities.  logits [..., vocabulary], float32 or bfloat16; targets [...], int64
+    or int32.  logp and entropy have gradients."""
+    if targets.shape != logits.shape[:-1]:
+        raise ValueError("one target for each row of logits, got %s and %s" % (tuple(targets.shape), tuple(logits.shape)))
+    out = list(_TokenLogProbs.apply(logits, targets, entropy, top))
+    logp = out.pop(0)
+    H = out.pop(0) if entropy else None
+    return TokenLogProbs(logp, H, *(out if top else (None, None)))
+
+
+class Embedding(torch.nn.Module):
+    """y = scale W[token], W [tokens, width]; 0 for a token outside the table (padding)."""
+
+    def __init__(self, tokens: int, width: int, scale: float = 1.0, device="cuda", dtype=torch.bfloat16):
+        super().__init__()
+        self.scale = scale
+        self.weight = torch.nn.Parameter(torch.empty(tokens, width, device=device, dtype=dtype))
+        torch.nn.init.normal_(self.weight, std=1.0 / max(abs(scale), 1.0))
+
+    def forward(self, ids, rows=None):
+        return _Embedding.apply(ids, self.weight, self.scale, rows)
+
+
+_frequencies = functools.lru_cache(maxsize=None)(native.rope_frequencies)
+
+
+class QueryKeyNorm(torch.nn.Module):
+    """Queries [..., heads, width] and keys [..., key heads, width] normed head by head, scaled by
+    a weight each and their first `rotated` elements turned by the token's position."""
+
+    def __init__(self, width: int, rotated=None, base: float = 10000.0, interleaved=False, eps: float = 1e-6, device="cuda"):
+        super().__init__()
+        self.eps, self.interleaved = eps, interleaved
+        self.rotated, self.base = width if rotated is None else rotated, base
+        self.w_q, self.w_k = (torch.nn.Parameter(torch.ones(width, device=device, dtype=torch.bfloat16)) for _ in range(2))
+
+    @property
+    def inv_freq(self):
+        return _frequencies(self.rotated, self.base)
+
+    def forward(self, q, k, positions, rows=None):
+        if q.shape[:-2] != k.shape[:-2] or positions.shape != q.shape[:-2]:
+            raise ValueError("queries, keys and positions must have the same tokens, got %s, %s and %s"
+                             % (tuple(q.shape[:-2]), tuple(k.shape[:-2]), tuple(positions.shape)))
+        return _QueryKeyNorm.apply(q, k, self.w_q, self.w_k, positions, self.inv_freq, self.eps, self.interleaved, rows)
 
 
 class LanguageLinear(torch.nn.Module):
