@@ -159,6 +159,7 @@ struct Way {
 template <int G, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
   grid_wait();
+  grid_release();
   __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
   __shared__ Pair ring[kQkWarps][kAhead];
   __shared__ __align__(16) float weights[2][kMaxHead];
@@ -266,6 +267,7 @@ template <int G, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel(const __grid_constant__ QkArgs a,
                                                                   const __grid_constant__ QkRuns q) {
   grid_wait();
+  grid_release();
   __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
   __shared__ Pair ring[kQkWarps][kAhead][2];             // x, dout
   __shared__ __align__(16) float weights[kMaxHead];
@@ -372,6 +374,7 @@ struct QkWeightGrads {
 };
 __global__ void __launch_bounds__(1024) qk_weight_kernel(const __grid_constant__ QkWeightGrads a) {
   grid_wait();
+  grid_release();
   const int run = blockIdx.x, c = blockIdx.y * 32 + (threadIdx.x & 31), at = threadIdx.x >> 5;
   __shared__ float sums[32][32];
   float v = 0.0f;

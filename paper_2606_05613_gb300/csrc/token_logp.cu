@@ -341,6 +341,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 template <class E, bool ENTROPY, bool TOP, int N>
 __global__ void __launch_bounds__(N, N == 32 ? 32 : 1536 / N) token_logp_kernel(const LogpArgs a, const int parts) {
   grid_wait();
+  grid_release();
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const unsigned rank = parts > 1 ? cluster_rank() : 0;
   if (parts > 1) cluster_arrive();
@@ -460,6 +461,7 @@ constexpr int kGradPiece = kGradThreads * kGradVecs * kVec<E>;
 template <class E, bool ENTROPY>
 __global__ void __launch_bounds__(kGradThreads) token_logp_grad_kernel(const LogpGradArgs a) {
   grid_wait();
+  grid_release();
   const int64_t t = blockIdx.x / a.pieces;
   const int piece = (int)(blockIdx.x % a.pieces);
   const E* row = static_cast<const E*>(a.logits) + t * a.ld;

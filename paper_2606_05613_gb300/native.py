@@ -480,11 +480,7 @@ _Bounds = [ctypes.c_int64 * n for n in range(18)]
 def _language_rows(rows, T: int):
     """(K, array) of the language bounds."""
     r = [int(i) for i in rows]
-    last, ok = 0, 2 <= len(r) <= 17 and r[0] == 0 and r[-1] == T
-    for i in r:
-        ok = ok and i >= last
-        last = i
-    if not ok:
+    if not 2 <= len(r) <= 17 or r[0] != 0 or r[-1] != T or r != sorted(r):
         raise ValueError("rows must be K + 1 bounds from 0 to the number of rows, 1 <= K <= 16")
     return len(r) - 1, _Bounds[len(r)](*r)
 
