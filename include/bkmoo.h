@@ -486,7 +486,8 @@ int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t l
  * bkmoo_embedding_forward -- y_t = scale W[id_t].  table: [V][D] of dtype (fp32 or bf16)
  * with rows of ld_table elements, y: [T][D] of the same with rows of ldy, both at any
  * element's address (16-byte vectors where all rows start on 16 bytes).  An id outside
- * 0 .. V - 1 is padding: its y is 0.  V < 2^28, D <= 2^23; scale is finite as fp32.
+ * 0 .. V - 1 is padding: its y is 0.  V < 2^28, D <= 2^23; scale is finite as fp32; y does
+ * not overlap the table.
  */
 int bkmoo_embedding_forward(const void* table, int64_t ld_table, int32_t dtype, int64_t V,
                             int64_t D, const void* ids, int32_t id_bytes, int64_t T, double scale,
@@ -499,7 +500,8 @@ int bkmoo_embedding_backward_workspace_size(int64_t T, int64_t D, size_t* bytes)
  * bkmoo_embedding_backward -- dW_k[v] = scale sum of dy_t over language k's rows t with
  * id_t = v, in the order of t.  dy: [T][D] of dtype, rows of ld_dy, at any element's
  * address; padding has no gradient, and its rows are not read.  dw: host array of K device
- * pointers, each to a contiguous [V][D] of dw_dtype at any element's address.  accumulate:
+ * pointers, each to a contiguous [V][D] of dw_dtype at any element's address, none of which
+ * overlap.  accumulate:
  * 0 writes every row, 1 adds to the rows that have a token and leaves the others alone.
  * ws: device, 256-byte aligned, ws_bytes >= the size above, not shared by calls that
  * overlap.
@@ -538,8 +540,8 @@ int bkmoo_qk_norm_backward_workspace_size(int64_t head_dim, size_t* bytes);
  * bkmoo_qk_norm_backward -- from dq_out and dk_out, the gradients of the forward call's
  * results, and its inputs: dq and dk (dq may be dq_out, with the same stride, and dk dk_out),
  * and every language's own gradients of the two weights, dw_q[k] and dw_k[k]: contiguous
- * [head_dim] of dw_dtype at any element's address; both arrays NULL: not wanted (then ws is
- * not used).  ws: device, 256-byte aligned, ws_bytes >= the size above, not shared by calls
+ * [head_dim] of dw_dtype at any element's address, none of which overlap; both arrays NULL:
+ * not wanted (then ws is not used).  ws: device, 256-byte aligned, ws_bytes >= the size above, not shared by calls
  * that overlap.
  */
 int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, const void* dk_out,

@@ -553,6 +553,7 @@ extern "C" int bkmoo_embedding_backward(const void* dy, int64_t ld_dy, int32_t d
     if (!aligned_at(dw[k], float_bytes(dw_dtype))) return BKMOO_ERR_INVALID;
     vec = vec && on_vectors(dw[k], dw_dtype, D, D);
   }
+  if (!apart(dw, K, (size_t)(V * D) * float_bytes(dw_dtype))) return BKMOO_ERR_INVALID;
   const EmbedRoom room = embed_room(T, D);
   const int64_t ctas = up_by(room.pieces * room.blocks, kSumThreads / 32);
   const size_t grad_bytes = (size_t)(V * D) * float_bytes(dw_dtype);

@@ -525,6 +525,11 @@ extern "C" int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, con
       (T > 0 && ((dq == dq_out && ld_dq != ld_dq_out) || (dk == dk_out && ld_dk != ld_dk_out) ||
                  !aligned_at(positions, id_bytes))))
     return BKMOO_ERR_INVALID;
+  if (weights) {
+    const void* all[2 * kMaxK];
+    for (int l = 0; l < K; ++l) all[l] = dw_q[l], all[K + l] = dw_k[l];
+    if (!apart(all, 2 * K, (size_t)head_dim * float_bytes(dw_dtype))) return BKMOO_ERR_INVALID;
+  }
   size_t need = 0;
   if (bkmoo_qk_norm_backward_workspace_size(head_dim, &need) != BKMOO_OK) return BKMOO_ERR_INVALID;
   if (weights && ws_bytes < need) return BKMOO_ERR_WORKSPACE;

@@ -11,6 +11,15 @@ namespace bkmoo {
 inline bool aligned_at(const void* p, uintptr_t by) { return p && ((uintptr_t)p & (by - 1)) == 0; }
 inline bool is_float(int32_t dt) { return dt == BKMOO_F32 || dt == BKMOO_BF16; }
 inline uintptr_t float_bytes(int32_t dt) { return dt == BKMOO_F32 ? 4 : 2; }
+// Whether no two of n arrays of `bytes` overlap.
+inline bool apart(const void* const* p, int n, size_t bytes) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < i; ++j) {
+      const uintptr_t a = (uintptr_t)p[i], b = (uintptr_t)p[j];
+      if ((a < b ? b - a : a - b) < bytes) return false;
+    }
+  return true;
+}
 inline bool is_id(int32_t bytes) { return bytes == 4 || bytes == 8; }
 
 // (Loads below are plain ones, not by the read-only path: a kernel may begin before the one

@@ -58,7 +58,7 @@ def test_embedding_forward_without_rows_does_nothing():
     assert _call(bk.load().bkmoo_embedding_forward, LOOKUP, dict(T=0, ids=None, y=None)) == OK
 
 
-SUMS = dict(dy=P, ld=64, dt=1, ids=P, nb=8, T=5, V=100, D=64, scale=1.0, K=2, rows=_rows(0, 2, 5), dw=_ptrs(P, P), wt=1, acc=0,
+SUMS = dict(dy=P, ld=64, dt=1, ids=P, nb=8, T=5, V=100, D=64, scale=1.0, K=2, rows=_rows(0, 2, 5), dw=_ptrs(P, P + (1 << 30)), wt=1, acc=0,
             ws=P, size=1 << 40, stream=None)
 
 
@@ -70,6 +70,17 @@ SUMS = dict(dy=P, ld=64, dt=1, ids=P, nb=8, T=5, V=100, D=64, scale=1.0, K=2, ro
                                  dict(ws=None), dict(ws=P + 128), dict(V=1 << 20, D=1 << 20, ld=1 << 20)])
 def test_embedding_backward_refuses(bad):
     assert _call(bk.load().bkmoo_embedding_backward, SUMS, bad) == INVALID
+
+
+def test_gradients_that_overlap_are_refused():
+    """Two languages that add to one place would lose each other's sums."""
+    fn, grads = bk.load().bkmoo_embedding_backward, lambda d: dict(dw=_ptrs(P, P + d), size=0)
+    assert _call(fn, SUMS, grads(0)) == INVALID and _call(fn, SUMS, grads(100 * 64 * 2 - 2)) == INVALID
+    assert _call(fn, SUMS, grads(100 * 64 * 2)) == WS and _call(fn, SUMS, dict(wt=0, **grads(100 * 64 * 2))) == INVALID
+    fn = bk.load().bkmoo_qk_norm_backward
+    for q, k in (((P, P), (P + 256, P + 512)), ((P, P + 256), (P + 512, P + 126)), ((P, P + 256), (P, P + 512))):
+        assert _call(fn, BACK, dict(dwq=_ptrs(*q), dwk=_ptrs(*k), size=0)) == INVALID
+    assert _call(fn, BACK, dict(size=0)) == WS
 
 
 def test_embedding_backward_needs_its_workspace():
@@ -108,7 +119,7 @@ def test_qk_norm_forward_without_rows_does_nothing():
 
 BACK = dict(dqo=P, ld1=512, dko=P, ld2=512, q=P, ldq=512, k=P, ldk=512, wq=P, wk=P, wt=1, T=5, hq=4, hk=2, hd=64, pos=P, nb=8,
             freq=_freq(*[0.5] * 32), rot=64, inter=0, eps=1e-6, K=2, rows=_rows(0, 2, 5), dq=P + (1 << 30), ld3=512,
-            dk=P + (1 << 30), ld4=512, dwq=_ptrs(P, P), dwk=_ptrs(P, P), dt=1, acc=0, ws=P, size=1 << 40, stream=None)
+            dk=P + (1 << 30), ld4=512, dwq=_ptrs(P, P + 128), dwk=_ptrs(P + 256, P + 384), dt=1, acc=0, ws=P, size=1 << 40, stream=None)
 
 
 @pytest.mark.parametrize("bad", BAD_NORM + [dict(dqo=None), dict(dko=P + 8), dict(ld1=248), dict(ld2=516), dict(dq=None),
