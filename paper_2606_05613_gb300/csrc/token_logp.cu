@@ -236,59 +236,91 @@ __device__ void top_of_part(const Part<E>& p, const Best& mine, int n, TopRoom<E
     at = __shfl_sync(0xffffffffu, at, 0) + __popc(those & ((1u << lane) - 1));
     if (it) list[at] = what;
   };
-  note(best >= bound && other < bound, t.near, &t.n_near, mine.at);
-  note(best >= bound && other >= bound, t.who, &t.n_who, p.first + tid);
-  const float low = value_of(bound);
-  auto reaches = [&](float z) { return bound == 0 || z >= low; };
+  const uint32_t reach = max(bound, 1u);
+  note(best >= reach && other < reach, t.near, &t.n_near, mine.at);
+  note(best >= reach && other >= reach, t.who, &t.n_who, p.first + tid);
+  // Elements from the bound up; where they are more than there is room for (many as large as the
+  // bound), or the bound is minus infinity, those above it.
+  const float low = bound == 0 ? -INFINITY : value_of(bound);
+  bool above = bound == 0;
   auto keep = [&](uint32_t those, const auto& z, int v) {
     int at = atomicAdd(&t.count, __popc(those));
     for (; those; those &= those - 1, ++at)
       if (at < kBuffer<E, N>) t.buffer[at] = place_of(z(__ffs(those) - 1), v + __ffs(those) - 1);
   };
   const int single = single_at(p, tid);
-  if (single >= 0) {
-    const float z = widen(p.row[single]);
-    if (reaches(z)) keep(1u, [&](int) { return z; }, single);
-  }
-  __syncthreads();
-  // those vectors, by all threads
-  const int near = kAhead * t.n_near, whole = t.n_who;
-  const int items = near + whole * ((p.last - p.first + N - 1) / N);
-  for (int i0 = tid; i0 < items; i0 += kAhead * N) {
-    uint4 x[kAhead];
-    int at[kAhead];
+  for (;;) {
+    auto reaches = [&](float z) { return above ? z > low : z >= low; };
+    if (single >= 0) {
+      const float z = widen(p.row[single]);
+      if (reaches(z)) keep(1u, [&](int) { return z; }, single);
+    }
+    __syncthreads();
+    // those threads' vectors, by all threads
+    const int near = kAhead * t.n_near, whole = t.n_who;
+    const int items = near + whole * ((p.last - p.first + N - 1) / N);
+    for (int i0 = tid; i0 < items; i0 += kAhead * N) {
+      uint4 x[kAhead];
+      int at[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int i = i0 + k * N;
-      at[k] = p.last;
-      if (i >= items) continue;
-      if (i < near) {
-        at[k] = t.near[i / kAhead] + i % kAhead * N;
-      } else {
-        const int j = (i - near) / whole;
-        at[k] = t.who[i - near - j * whole] + j * N;
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k * N;
+        at[k] = p.last;
+        if (i >= items) continue;
+        if (i < near) {
+          at[k] = t.near[i / kAhead] + i % kAhead * N;
+        } else {
+          const int j = (i - near) / whole;
+          at[k] = t.who[i - near - j * whole] + j * N;
+        }
+        if (at[k] < p.last) x[k] = vector_at(p, at[k]);
       }
-      if (at[k] < p.last) x[k] = vector_at(p, at[k]);
-    }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (at[k] >= p.last) continue;
-      float z[kVec<E>];
-      unpack(x[k], z);
-      uint32_t those = 0;
+      for (int k = 0; k < kAhead; ++k) {
+        if (at[k] >= p.last) continue;
+        float z[kVec<E>];
+        unpack(x[k], z);
+        uint32_t those = 0;
 #pragma unroll
-      for (int e = 0; e < kVec<E>; ++e) those |= reaches(z[e]) ? 1u << e : 0u;
-      // (the elements by their number from the words: an index into registers is none)
-      if (those) keep(those, [&](int e) { return element(x[k], e, E()); }, p.body + at[k] * kVec<E>);
+        for (int e = 0; e < kVec<E>; ++e) those |= reaches(z[e]) ? 1u << e : 0u;
+        // (the elements by their number from the words: an index into registers is none)
+        if (those) keep(those, [&](int e) { return element(x[k], e, E()); }, p.body + at[k] * kVec<E>);
+      }
     }
+    __syncthreads();
+    if (above || t.count <= kBuffer<E, N>) break;
+    __syncthreads();
+    above = true;
+    if (tid == 0) t.count = 0;
+    __syncthreads();
   }
-  __syncthreads();
-  if (t.count <= kBuffer<E, N>) {
-    first_of<N>(t.buffer, t.count, n, t.list);
+  int have = t.count;
+  if (have <= kBuffer<E, N>) {
+    first_of<N>(t.buffer, have, n, t.list);
+    if (have >= n) return;
+    // the others are as large as the bound, or NaN: the first ones of the row
+    const int end = p.back ? p.body + p.vecs * kVec<E> + p.tail : p.body + p.last * kVec<E>;
+    for (int nan = 0; nan < 2 && have < n; ++nan) {
+      for (int v0 = p.front ? 0 : p.body + p.first * kVec<E>; v0 < end && have < n; v0 += N) {
+        const bool in = v0 + tid < end;
+        const float z = in ? widen(p.row[v0 + tid]) : 0.0f;
+        const uint32_t those = __ballot_sync(0xffffffffu, in && (nan ? z != z : z == low));
+        __syncthreads();
+        if (lane == 0) t.near[wid] = __popc(those);
+        __syncthreads();
+        int at = have;
+        for (int w = 0; w < kWarpsHere; ++w) {
+          if (w < wid) at += t.near[w];
+          have += t.near[w];
+        }
+        at += __popc(those & ((1u << lane) - 1));
+        if ((those >> lane & 1) && at < n) t.list[at] = place_of(z, v0 + tid);
+      }
+    }
     return;
   }
-  // More elements reach the bound than there is room for (equal logits, or the best ones
-  // with a few threads): stripe by stripe, keeping the n first so far.
+  // More elements than there is room for all the same (the best ones lie with a few threads):
+  // stripe by stripe, keeping the n first so far.
   __syncthreads();
   if (tid == 0) t.count = 0;
   uint64_t least = 0;                   // the n-th place so far

@@ -213,6 +213,21 @@ def test_masked_logits(V, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("T,V", [(2, 300), (3, 5000), (2, 151936), (700, 12007)])
+def test_few_tokens_are_allowed(T, V, dtype):
+    """A grammar leaves 0 to 60 tokens of a row, the others are minus infinity or the lowest value."""
+    z, _ = _logits(T, V, dtype, 1)
+    left = torch.rand(T, V, generator=_gen(2), device=DEV).argsort(-1) < torch.tensor([3, 19, 33, 60, 1], device=DEV)[
+        torch.arange(T, device=DEV) % 5][:, None]
+    targets = left.float().argmax(-1)
+    for mask in (-INF, torch.finfo(dtype).min):
+        y = torch.where(left, z, mask).to(dtype)
+        _Ref(y, targets).check(_forward(y, targets, 20), y)
+        y[:, V // 2:] = z[:, V // 2:V // 2 + 1]             # and half of them all alike
+        _Ref(y, targets).check(_forward(y, targets, 32), y)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("V", [12, 1001, 70000])
 def test_rows_without_a_token_and_rows_that_are_no_numbers(V, dtype):
     z, _ = _logits(6, V, dtype, 1)
