@@ -1,17 +1,19 @@
 // Rows of an embedding looked up by token and scaled, and the gradient of the embedding
 // apart by language (include/bkmoo.h).
 //
-// Forward: y_t = s W[id_t].  Bound by memory.
+// Forward: y_t = s W[id_t].  Bound by memory: 16384 rows of 2048 bf16 take 15.3 us (6.3 TB/s), a
+// thread with one vector on its way at a time 22.5.
 //
 // Backward: dW_k[v] = s sum of dy_t over language k's rows t with id_t = v.  The rows are
 // put in the order of (language, token, t); then each token's rows lie side by side, and
-// a warp sums a piece of 32 places for 256 columns in that order.  A sum that lies in one
+// a warp sums a piece of 8 to 32 places for 256 columns in that order.  A sum that lies in one
 // piece is written (or added) by its warp; the others leave their parts, which are joined in
-// the order of the pieces: no atomics on values, the same result every time.
+// the order of the pieces: no atomics on values, the same result every time.  8192 rows of
+// 2048 bf16 in 4 languages, added, take 20 us: 9 for the sums, the others a chain of latencies.
 //
-// The order: places of 1024 rows sorted by a CTA (bitonic, in registers and shared memory),
-// then runs of sorted rows merged 32 at a time: a row's place in the merged run is its
-// place in its own plus, for each other run, how many there come before it, a binary search.
+// The order: 256 rows sorted by a CTA (bitonic, in registers and shared memory), then runs of
+// sorted rows merged 32 at a time: a row's place in the merged run is its place in its own
+// plus, for each other run, how many there come before it, a binary search.
 #include <math.h>
 
 #include "tile_host.cuh"
@@ -168,13 +170,14 @@ constexpr int kMergeRows = kEmbedThreads / 4;
 __global__ void __launch_bounds__(kEmbedThreads) merge_keys_kernel(const __grid_constant__ MergeArgs a, const __grid_constant__ FillArgs f) {
   grid_wait();
   if (blockIdx.x >= f.own) return fill(f);
+  // (run r's place i lies at i ^ r: the same place of other runs is in other banks)
   __shared__ uint32_t keys[kMerge][kSortRun];
   const int tid = threadIdx.x;
   const int64_t own = (int64_t)blockIdx.x * kMergeRows / kSortRun, first = own / kMerge * kMerge * kSortRun;
 #pragma unroll
   for (int j = 0; j < kMerge; ++j) {
     const int64_t i = first + j * kSortRun + tid;
-    keys[j][tid] = i < a.T ? (uint32_t)(a.in[i] >> 32) : kNoToken;
+    keys[j][tid ^ j] = i < a.T ? (uint32_t)(a.in[i] >> 32) : kNoToken;
   }
   const int64_t i = (int64_t)blockIdx.x * kMergeRows + tid / 4;
   const uint64_t mine = i < a.T ? a.in[i] : ~0ull;
@@ -188,7 +191,7 @@ __global__ void __launch_bounds__(kEmbedThreads) merge_keys_kernel(const __grid_
 #pragma unroll
     for (int j = 0; j < kMerge / 4; ++j) {
       const int r = 4 * j + (tid & 3);
-      const uint32_t there = keys[r][before[j] + step - 1];
+      const uint32_t there = keys[r][(before[j] + step - 1) ^ r];
       if (there < key || (there == key && r < me)) before[j] += step;
     }
   }
@@ -197,7 +200,7 @@ __global__ void __launch_bounds__(kEmbedThreads) merge_keys_kernel(const __grid_
   for (int j = 0; j < kMerge / 4; ++j) {
     const int r = 4 * j + (tid & 3);
     if (r == me) continue;
-    const uint32_t there = keys[r][before[j]];          // (all but one have been looked at)
+    const uint32_t there = keys[r][before[j] ^ r];          // (all but one have been looked at)
     place += before[j] + (there < key || (there == key && r < me) ? 1 : 0);
   }
   place += __shfl_xor_sync(0xffffffffu, place, 1);
@@ -480,6 +483,8 @@ bool embed_sizes_ok(int64_t T, int64_t V, int64_t D, double scale) {
 }
 
 // Places of a warp's piece: as many as leave 2432 warps (16 for each of 152 SMs), 8 to 32.
+// 600 rows of 768 bf16 in 4 languages, added, take 12, 14 and 18 us by pieces of 8, 16 and 32;
+// 8192 of 2048 24, 21 and 23; 65536 of 768 83, 76 and 75.
 int piece_of(int64_t T, int64_t blocks) {
   int piece = 32;
   while (piece > 8 && up_by(T, piece) * blocks < 2432) piece /= 2;
