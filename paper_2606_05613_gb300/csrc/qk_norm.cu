@@ -20,8 +20,8 @@ namespace {
 constexpr int kQkThreads = 128;
 constexpr int kQkWarps = kQkThreads / 32;
 constexpr int kMaxHead = 256;
-constexpr int kForwardCtas = 6, kBackwardCtas = 4;     // on an SM
-constexpr int kAhead = 4;               // steps of a warp whose loads are on their way
+constexpr int kForwardCtas = 5, kBackwardCtas = 4;     // on an SM
+constexpr int kAhead = 3;               // steps of a warp whose loads are on their way
 
 struct QkSide {
   const __nv_bfloat16 *x, *dout;
@@ -40,71 +40,74 @@ struct QkArgs {
   uint64_t turn[kMaxHead / 2];          // 2^64 f / 2 pi
 };
 
-// The angles of a token's pairs, [2][rot / 2], by a warp.
-__device__ __forceinline__ void angles(const QkArgs& a, uint64_t pos, int lane, float (*room)[kMaxHead / 2]) {
+// 16 numbers of each of a head's lanes, four by four, those of neighbouring lanes side by side:
+// eight lanes read 128 bytes in a row.
+struct Numbers {
+  float4 v[4][16];
+  __device__ __forceinline__ float& at(int l, int j) { return reinterpret_cast<float*>(&v[j >> 2][l])[j & 3]; }
+  __device__ __forceinline__ void get(int l, float (&x)[16]) const {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 f = v[q][l];
+      x[4 * q] = f.x, x[4 * q + 1] = f.y, x[4 * q + 2] = f.z, x[4 * q + 3] = f.w;
+    }
+  }
+};
+// The cos and sin of a token's pairs (8 a lane), by a warp.
+__device__ __forceinline__ void angles(const QkArgs& a, uint64_t pos, int lane, Numbers& room) {
   __syncwarp();
   for (int i = lane; i < a.rot / 2; i += 32) {
     // half turns in [-1, 1)
     const float half = __int2float_rn((int32_t)((pos * a.turn[i] + 0x80000000ull) >> 32)) * 0x1p-31f;
-    float s, c;
-    sincospif(half, &s, &c);
-    room[0][i] = c;
-    room[1][i] = s;
+    sincospif(half, &room.at(i >> 3, 8 + (i & 7)), &room.at(i >> 3, i & 7));
   }
   __syncwarp();
+}
+// What is not turned, once.
+__device__ __forceinline__ void no_angles(const QkArgs& a, int lane, Numbers& room) {
+  for (int i = a.rot / 2 + lane; i < kMaxHead / 2; i += 32) room.at(i >> 3, i & 7) = 1.0f, room.at(i >> 3, 8 + (i & 7)) = 0.0f;
 }
 
 // Where a lane's 16 elements of a head lie: two vectors of 8.
 struct Place {
-  int lo, hi, pair;                     // columns; its first pair
-  bool live, turns;
+  int lo, hi;                           // columns
+  bool live;
 };
 template <bool NEIGHBOURS>
 __device__ __forceinline__ Place place_of_lane(const QkArgs& a, int l) {
   Place p;
   p.live = 16 * l < a.hd;
-  p.turns = 16 * l < a.rot;
-  p.pair = 8 * l;
   p.lo = 16 * l;
   p.hi = p.lo + 8;
-  if (!NEIGHBOURS && p.turns) {
+  if (!NEIGHBOURS && 16 * l < a.rot) {
     p.lo = 8 * l;
     p.hi = p.lo + a.rot / 2;
   }
   return p;
 }
-struct Angles {
-  float c[8], s[8];
-};
-__device__ __forceinline__ void eight(const float* p, float* x) {      // p: on 16 bytes
-  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-}
-__device__ __forceinline__ Angles angles_of(const Place& p, float (*room)[kMaxHead / 2]) {
-  Angles g;
-  if (p.turns) {
-    eight(&room[0][p.pair], g.c);
-    eight(&room[1][p.pair], g.s);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g.c[j] = 1.0f, g.s[j] = 0.0f;
-  }
-  return g;
-}
-// y: the lane's elements, the vector at lo and then the one at hi.  BACK: the other way.
-template <bool NEIGHBOURS, bool BACK>
-__device__ __forceinline__ void rotate(float (&y)[16], const Angles& g) {
+// y: the lane's elements, the vector at lo and then the one at hi, turned back by g, 8 cos and
+// 8 sin.
+template <bool NEIGHBOURS>
+__device__ __forceinline__ void turn_back(float (&y)[16], const float (&g)[16]) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float& a = y[NEIGHBOURS ? 2 * j : j];
     float& b = y[NEIGHBOURS ? 2 * j + 1 : j + 8];
-    const float s = BACK ? -g.s[j] : g.s[j], x = a;
-    a = fmaf(-b, s, x * g.c[j]);
-    b = fmaf(x, s, b * g.c[j]);
+    const float x = a;
+    a = fmaf(b, g[j + 8], x * g[j]);
+    b = fmaf(-x, g[j + 8], b * g[j]);
   }
 }
 __device__ __forceinline__ float weight_at(const QkArgs& a, const void* w, int c) {
   return a.w_f32 ? static_cast<const float*>(w)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(w)[c]);
+}
+template <bool NEIGHBOURS>
+__device__ __forceinline__ void get_weights(const QkArgs& a, const void* w, Numbers& to) {
+  for (int i = threadIdx.x; i < 256; i += kQkThreads) {
+    const int l = i >> 4, j = i & 15;
+    const Place p = place_of_lane<NEIGHBOURS>(a, l);
+    to.at(l, j) = p.live ? weight_at(a, w, (j < 8 ? p.lo : p.hi) + (j & 7)) : 0.0f;
+  }
 }
 // Loads go to shared memory, each lane's to a place of its own that only it reads: a copy
 // that is on its way holds no register.
@@ -155,14 +158,15 @@ struct Way {
   E* at;
 };
 
-// G lanes a head.  A warp takes a run of steps.
+// G lanes a head.  A warp takes a run of steps.  Bound by memory: 8192 tokens of 32 + 8 heads of
+// 128 take 30 us (5.6 TB/s), and 29 in a copy of this kernel that copies and computes nothing.
+// 5 CTAs on an SM and 3 steps ahead: 6 and 7 CTAs 30.3 and 31.9, 6 steps 30.5.
 template <int G, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const __grid_constant__ QkArgs a, const int64_t each) {
   grid_wait();
   grid_release();
-  __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ Numbers room[kQkWarps], weights[2];
   __shared__ Pair ring[kQkWarps][kAhead];
-  __shared__ __align__(16) float weights[2][kMaxHead];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int per = a.side[0].steps + a.side[1].steps, step_elems = 32 / G * a.hd;
   const int64_t total = a.T * per, from = ((int64_t)blockIdx.x * kQkWarps + wid) * each;
@@ -204,10 +208,8 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
   };
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
-  for (int i = threadIdx.x; i < 2 * a.hd; i += kQkThreads) {
-    const int k = i >= a.hd, c = i - (k ? a.hd : 0);
-    weights[k][c] = weight_at(a, a.side[k].w, c);
-  }
+  for (int k = 0; k < 2; ++k) get_weights<NEIGHBOURS>(a, a.side[k].w, weights[k]);
+  no_angles(a, lane, room[wid]);
   __syncthreads();
   int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, here.t) : 0;
   bool begins = true, new_token = true;
@@ -220,17 +222,16 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
         angles(a, (uint64_t)pos, lane, room[wid]);
         if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
       }
-      const Angles g = angles_of(p, room[wid]);
-      float w[16];
-      eight(&weights[here.k][p.live ? p.lo : 0], w);
-      eight(&weights[here.k][p.live ? p.hi : 0], w + 8);
+      float g[16], w[16];
+      room[wid].get(lane % G, g);
+      weights[here.k].get(lane % G, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float wa = w[NEIGHBOURS ? 2 * j : j], wb = w[NEIGHBOURS ? 2 * j + 1 : j + 8];
-        ca[j] = wa * g.c[j];
-        sa[j] = wa * g.s[j];
-        cb[j] = wb * g.c[j];
-        sb[j] = wb * g.s[j];
+        ca[j] = wa * g[j];
+        sa[j] = wa * g[j + 8];
+        cb[j] = wb * g[j];
+        sb[j] = wb * g[j + 8];
       }
     }
     copies_wait();
@@ -256,7 +257,11 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
   copies_wait_all();
 }
 
-// The backward pass by CTAs that each take a run of one side's and one language's steps.
+// The backward pass by CTAs that each take a run of one side's and one language's steps, and leave
+// their sums of the weights' gradients.  8192 tokens of 32 + 8 heads of 128 in 4 languages take
+// 46 us (5.5 TB/s), of which 3 are the sums' kernel; 5 CTAs on an SM 53, for which registers go to
+// memory, 3 CTAs 55.  w and the angles are read from shared memory for every step: the
+// registers hold the sums.  Runs of neighbouring steps: tokens dealt out in turn take 53.
 struct QkRuns {
   int32_t K, weights;
   int32_t first[2 * kMaxK + 1];         // CTAs of (side, language), side by side
@@ -268,9 +273,8 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
                                                                   const __grid_constant__ QkRuns q) {
   grid_wait();
   grid_release();
-  __shared__ __align__(16) float room[kQkWarps][2][kMaxHead / 2];
+  __shared__ Numbers room[kQkWarps], weights;
   __shared__ Pair ring[kQkWarps][kAhead][2];             // x, dout
-  __shared__ __align__(16) float weights[kMaxHead];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, l = lane % G;
   int run = 0;
   while ((int)blockIdx.x >= q.first[run + 1]) ++run;
@@ -305,28 +309,27 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
   };
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
-  for (int c = threadIdx.x; c < a.hd; c += kQkThreads) weights[c] = weight_at(a, s.w, c);
+  get_weights<NEIGHBOURS>(a, s.w, weights);
+  no_angles(a, lane, room[wid]);
   __syncthreads();
   float dw[16] = {};
   int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, t) : 0;
   bool new_token = true;
-  Angles g;
   for (int i = 0; i < steps; ++i) {
     fetch();
     if (new_token) {
       angles(a, (uint64_t)pos, lane, room[wid]);
-      g = angles_of(p, room[wid]);
       if (t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, t + 1);
     }
     const bool live = live_at(step);
     copies_wait();
     const Pair* v = ring[wid][i % kAhead];
     float x[16], d[16], w[16], sum = 0.0f, dot = 0.0f;
-    eight(&weights[p.live ? p.lo : 0], w);
-    eight(&weights[p.live ? p.hi : 0], w + 8);
-    get_pair(v[0], lane, x);
     get_pair(v[1], lane, d);
-    rotate<NEIGHBOURS, true>(d, g);
+    room[wid].get(l, w);                // (w and the angles stay in shared memory: registers are short)
+    turn_back<NEIGHBOURS>(d, w);
+    get_pair(v[0], lane, x);
+    weights.get(l, w);
 #pragma unroll
     for (int j = 0; j < 16; ++j) {
       sum = fmaf(x[j], x[j], sum);
@@ -563,9 +566,11 @@ extern "C" int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, con
   int ctas = 0;
   if (tile_sms(&ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
   ctas *= kBackwardCtas;
-  // one CTA more for each part that is not whole
-  const int most = kMostCtas - 2 * kMaxK;
-  if (ctas > most) ctas = most;
+  // A side's and a language's last CTA is not full.  With those all are to be on the card at
+  // once: the few that were not would begin when the others end.
+  if (ctas > kMostCtas) ctas = kMostCtas;
+  ctas -= 2 * K;
+  if (ctas < 1) ctas = 1;
   QkRuns r = {};
   r.K = K;
   r.weights = weights;
