@@ -585,10 +585,11 @@ extern "C" int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t 
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return BKMOO_ERR_CUDA;
-  // Few rows: by more CTAs, while all are on the card at once and have 4096 logits each (300 x
-  // 32000 bf16: 7.3 us by one, 5.9 by two, 7.2 by four; 1 x 151936: 5.0 by four, 4.0 by eight).
+  // Few rows: by more CTAs, up to 4 an SM, while each has 4096 logits (200 x 128256 bf16: 11.5 us by
+  // one, 9.9 by two, 10.2 by four; 400: 20.5, 19.0 and 19.8, with the 20 likeliest 28, 31 and 35;
+  // 1 x 151936: 5.0 by four, 4.0 by eight).
   int parts = 1;
-  while (parts < kMaxCluster && T * parts * 2 <= 8 * sms && V / (2 * parts) >= 4096) parts *= 2;
+  while (parts < kMaxCluster && T * parts * 2 <= 4 * sms && V / (2 * parts) >= 4096) parts *= 2;
   if (T * parts > 0x7fffffffll) return BKMOO_ERR_INVALID;
   LogpArgs a = {logits, ld, T, (int32_t)V, targets, id_bytes, n_top, logp,
                 reinterpret_cast<float2*>(stats), entropy, top_ids, top_logp};
