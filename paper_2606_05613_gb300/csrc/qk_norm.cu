@@ -125,6 +125,7 @@ __device__ __forceinline__ void copy_pair(Pair& to, const __nv_bfloat16* head, c
   copy16(&to.lo[lane], live ? head + p.lo : any, live);
   copy16(&to.hi[lane], live ? head + p.hi : any, live);
 }
+__device__ __forceinline__ int next_slot(int slot) { return slot == kAhead - 1 ? 0 : slot + 1; }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 // All but the newest kAhead - 1 steps' copies have come.
@@ -198,11 +199,12 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
     if (w.k == 0) ++w.t;
     return true;
   };
-  int ahead = 0;
+  int ahead = 0, slot = 0, slot_there = 0;
   auto fetch = [&]() {
     const bool live = there.over > 0 && ahead < steps;
-    copy_pair(ring[wid][ahead % kAhead], there.at, a.side[0].x, p, lane, live);
+    copy_pair(ring[wid][slot_there], there.at, a.side[0].x, p, lane, live);
     copies_end();
+    slot_there = next_slot(slot_there);
     if (next(there)) set(there, a.side[there.k].x, a.side[there.k].ld, 0);
     ++ahead;
   };
@@ -236,7 +238,8 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
     }
     copies_wait();
     float x[16], sum = 0.0f;
-    get_pair(ring[wid][i % kAhead], lane, x);
+    get_pair(ring[wid][slot], lane, x);
+    slot = next_slot(slot);
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum = fmaf(x[j], x[j], sum);
     const float r = rsqrtf(fmaf(over_head<G>(sum), a.inv_hd, a.eps));
@@ -292,11 +295,12 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
   const int64_t back = (int64_t)(s.steps - 1) * step_elems, in = (int64_t)(step0 * (32 / G) + head0) * a.hd;
   const __nv_bfloat16 *at_x = s.x + t0 * s.ld + in, *at_d = s.dout + t0 * s.ld_dout + in;
   __nv_bfloat16* at_out = s.out + t0 * s.ld_out + in;
-  int step = step0, step_there = step0, ahead = 0;
+  int step = step0, step_there = step0, ahead = 0, slot = 0, slot_there = 0;
   int64_t t = t0;
   auto live_at = [&](int step) { return p.live && step * (32 / G) + head0 < s.heads; };
   auto fetch = [&]() {
-    Pair* r = ring[wid][ahead % kAhead];
+    Pair* r = ring[wid][slot_there];
+    slot_there = next_slot(slot_there);
     const bool live = ahead < steps && live_at(step_there);
     copy_pair(r[0], at_x, s.x, p, lane, live);
     copy_pair(r[1], at_d, s.x, p, lane, live);
@@ -323,7 +327,8 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
     }
     const bool live = live_at(step);
     copies_wait();
-    const Pair* v = ring[wid][i % kAhead];
+    const Pair* v = ring[wid][slot];
+    slot = next_slot(slot);
     float x[16], d[16], w[16], sum = 0.0f, dot = 0.0f;
     get_pair(v[1], lane, d);
     room[wid].get(l, w);                // (w and the angles stay in shared memory: registers are short)
