@@ -17,9 +17,10 @@ activations are bfloat16 on a GPU (an embedding's and the logits of
 token_log_probs may be float32); the products that no language splits
 (y = x W^T and its dx of LanguageLinear) are torch's.
 
-A captured step (torch.cuda.graph) has begin_batch(), the forward and the
-backward pass all in the capture, and no graph of an eager pass over the same
-weights may be alive then: autograd would tie the capture to that pass's stream.
+The forward and the backward pass may be captured (torch.cuda.graph) on
+begin_batch()'s stream, between it and finish(); a step is then begin_batch(),
+a replay there and finish().  No graph of an eager pass over the same weights
+may be alive during the capture: autograd would tie it to that pass's stream.
 """
 from __future__ import annotations
 

@@ -72,7 +72,8 @@ def _batch(seed=1):
 
 
 def _relative(a, b):
-    return float((a.detach().double() - b.double()).norm() / b.double().norm())
+    a, b = a.detach().double(), b.detach().double()
+    return float((a - b).norm() / b.norm())
 
 
 def test_gradients_come_apart_by_language():
@@ -206,6 +207,32 @@ def test_a_captured_pass():
         got = {n: [g.clone() for g in ps] for n, ps in places.items()}
         step()
         assert all(torch.equal(u, v) for n in got for u, v in zip(got[n], places[n]))
+
+
+def test_steps_with_a_captured_pass():
+    """begin_batch(), a replay on its stream and finish(): the directions of eager steps, bit for bit."""
+    m = _Model()
+    moo = BucketMOO(m.parameters(), K, 1 << 14, rule="mean")
+    batch, stream = _batch(), torch.cuda.Stream()
+    want = []
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        for seed in (1, 2, 3):
+            moo.begin_batch()
+            new = _batch(seed)
+            _loss(m(new[0], new[1], ROWS), new[2], new[3]).backward()
+            want.append(moo.finish().clone())
+        moo.begin_batch()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            _loss(m(batch[0], batch[1], ROWS), batch[2], batch[3]).backward()
+        for seed, d in zip((1, 2, 3), want):
+            for t, new in zip(batch, _batch(seed)):
+                t.copy_(new)
+            moo.begin_batch()
+            graph.replay()
+            assert torch.equal(moo.finish(), d)
+    torch.cuda.synchronize()
 
 
 def _example():
