@@ -53,22 +53,27 @@ struct Numbers {
     }
   }
 };
-// The cos and sin of a token's pairs (8 a lane), by a warp.
+// The cos and sin of a token's pairs, 8 a lane, by a warp.
+template <bool NEIGHBOURS>
 __device__ __forceinline__ void angles(const QkArgs& a, uint64_t pos, int lane, Numbers& room) {
   __syncwarp();
   for (int i = lane; i < a.rot / 2; i += 32) {
     // half turns in [-1, 1)
     const float half = __int2float_rn((int32_t)((pos * a.turn[i] + 0x80000000ull) >> 32)) * 0x1p-31f;
-    sincospif(half, &room.at(i >> 3, 8 + (i & 7)), &room.at(i >> 3, i & 7));
+    // where the lane that has the pair keeps it (Place)
+    const bool second = NEIGHBOURS && i >= a.hd / 4;
+    const int k = second ? i - a.hd / 4 : i, l = NEIGHBOURS ? k >> 2 : k >> 3, j = NEIGHBOURS ? (second ? 4 : 0) + (k & 3) : k & 7;
+    sincospif(half, &room.at(l, 8 + j), &room.at(l, j));
   }
   __syncwarp();
 }
-// What is not turned, once.
-__device__ __forceinline__ void no_angles(const QkArgs& a, int lane, Numbers& room) {
-  for (int i = a.rot / 2 + lane; i < kMaxHead / 2; i += 32) room.at(i >> 3, i & 7) = 1.0f, room.at(i >> 3, 8 + (i & 7)) = 0.0f;
+// None is turned, at first.
+__device__ __forceinline__ void no_angles(int lane, Numbers& room) {
+  for (int i = lane; i < 128; i += 32) room.at(i >> 3, i & 7) = 1.0f, room.at(i >> 3, 8 + (i & 7)) = 0.0f;
 }
 
-// Where a lane's 16 elements of a head lie: two vectors of 8.
+// Where a lane's 16 elements of a head lie: two vectors of 8, whose pairs are between them or within
+// each.  Neighbouring lanes' vectors are neighbours: a line of memory is asked for once.
 struct Place {
   int lo, hi;                           // columns
   bool live;
@@ -77,11 +82,15 @@ template <bool NEIGHBOURS>
 __device__ __forceinline__ Place place_of_lane(const QkArgs& a, int l) {
   Place p;
   p.live = 16 * l < a.hd;
-  p.lo = 16 * l;
-  p.hi = p.lo + 8;
-  if (!NEIGHBOURS && 16 * l < a.rot) {
+  if (NEIGHBOURS) {
+    p.lo = 8 * l;
+    p.hi = p.lo + a.hd / 2;
+  } else if (16 * l < a.rot) {
     p.lo = 8 * l;
     p.hi = p.lo + a.rot / 2;
+  } else {
+    p.lo = a.rot / 2 + 8 * l;
+    p.hi = p.lo + (a.hd - a.rot) / 2;
   }
   return p;
 }
@@ -211,7 +220,7 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
   for (int k = 0; k < 2; ++k) get_weights<NEIGHBOURS>(a, a.side[k].w, weights[k]);
-  no_angles(a, lane, room[wid]);
+  no_angles(lane, room[wid]);
   __syncthreads();
   int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, here.t) : 0;
   bool begins = true, new_token = true;
@@ -221,7 +230,7 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
     fetch();
     if (begins) {
       if (new_token) {
-        angles(a, (uint64_t)pos, lane, room[wid]);
+        angles<NEIGHBOURS>(a, (uint64_t)pos, lane, room[wid]);
         if (here.t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, here.t + 1);
       }
       float g[16], w[16];
@@ -314,7 +323,7 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
 #pragma unroll
   for (int j = 0; j < kAhead - 1; ++j) fetch();
   get_weights<NEIGHBOURS>(a, s.w, weights);
-  no_angles(a, lane, room[wid]);
+  no_angles(lane, room[wid]);
   __syncthreads();
   float dw[16] = {};
   int64_t pos = steps > 0 ? load_id(a.pos, a.id_bytes, t) : 0;
@@ -322,7 +331,7 @@ __global__ void __launch_bounds__(kQkThreads, kBackwardCtas) qk_norm_grad_kernel
   for (int i = 0; i < steps; ++i) {
     fetch();
     if (new_token) {
-      angles(a, (uint64_t)pos, lane, room[wid]);
+      angles<NEIGHBOURS>(a, (uint64_t)pos, lane, room[wid]);
       if (t + 1 < a.T) pos = load_id(a.pos, a.id_bytes, t + 1);
     }
     const bool live = live_at(step);
@@ -580,14 +589,15 @@ extern "C" int bkmoo_qk_norm_backward(const void* dq_out, int64_t ld_dq_out, con
   r.K = K;
   r.weights = weights;
   r.part = static_cast<float*>(ws);
-  const int64_t total = T * (a.side[0].steps + a.side[1].steps);
-  int64_t budget = (total + ctas - 1) / ctas;            // steps of a CTA
-  if (budget < kQkWarps) budget = kQkWarps;
+  // A token costs its steps and its angles, of which 256 are about as long as a step: 8680 tokens of
+  // 16 + 2 heads of 256 took 81 us with CTAs dealt out by steps alone.
+  int64_t cost[2];
+  for (int i = 0; i < 2; ++i) cost[i] = 256 * a.side[i].steps + rot;
+  int64_t budget = (T * (cost[0] + cost[1]) + ctas - 1) / ctas;          // of a CTA
+  if (budget < 256 * kQkWarps) budget = 256 * kQkWarps;
   for (int i = 0; i < 2; ++i)
-    for (int l = 0; l < K; ++l) {
-      const int64_t steps = (rows[l + 1] - rows[l]) * a.side[i].steps;
-      r.first[i * K + l + 1] = r.first[i * K + l] + (int32_t)((steps + budget - 1) / budget);
-    }
+    for (int l = 0; l < K; ++l)
+      r.first[i * K + l + 1] = r.first[i * K + l] + (int32_t)(((rows[l + 1] - rows[l]) * cost[i] + budget - 1) / budget);
   for (int l = 0; l <= K; ++l) r.rows[l] = rows[l];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int grid = r.first[2 * K];
