@@ -35,59 +35,43 @@ struct LookupArgs {
   void* y;
   int64_t ld, ld_y, T, V;
   int32_t id_bytes;
-  uint32_t D, per;                      // columns; threads' pieces of a row
+  uint32_t D, per;                      // columns; pieces of a row: vectors, or kColumns columns
   float scale;
 };
-// VEC: 16 bytes a thread at a time, else an element.  A thread has AHEAD of them on their way
-// at once: 4 where there are more than the card holds threads.
-template <class E, bool VEC, int AHEAD>
+// 16 bytes a thread at a time.  A thread has AHEAD of them on their way at once: 4 where there are
+// more than the card holds threads.
+template <class E, int AHEAD>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(const __grid_constant__ LookupArgs a) {
   grid_wait();
-  constexpr int N = VEC ? kVec<E> : 1;
   const int64_t n = a.T * a.per;
   for (int64_t i0 = (int64_t)blockIdx.x * (kEmbedThreads * AHEAD) + threadIdx.x; i0 < n;
        i0 += (int64_t)gridDim.x * (kEmbedThreads * AHEAD)) {
     int64_t t[AHEAD], c[AHEAD], id[AHEAD];
     uint4 v[AHEAD];
-    float x[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       const int64_t i = i0 + j * kEmbedThreads;
       id[j] = -1;
       if (i >= n) continue;
       t[j] = n < (1ll << 32) ? (uint32_t)i / a.per : i / a.per;
-      c[j] = (i - t[j] * a.per) * N;
+      c[j] = (i - t[j] * a.per) * kVec<E>;
       id[j] = load_id(a.ids, a.id_bytes, t[j]);
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
-      const bool none = id[j] < 0 || id[j] >= a.V;
-      const E* from = static_cast<const E*>(a.table) + (none ? 0 : id[j] * a.ld + c[j]);
       v[j] = make_uint4(0, 0, 0, 0);
-      x[j] = 0.0f;
-      if (VEC && !none) v[j] = *reinterpret_cast<const uint4*>(from);
-      if (!VEC && !none) x[j] = widen(*from);
+      if (id[j] >= 0 && id[j] < a.V) v[j] = *reinterpret_cast<const uint4*>(static_cast<const E*>(a.table) + id[j] * a.ld + c[j]);
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (i0 + j * kEmbedThreads >= n) break;
-      E* to = static_cast<E*>(a.y) + t[j] * a.ld_y + c[j];
-      if (VEC) {
-        float y[kVec<E>];
-        unpack(v[j], y);
+      float y[kVec<E>];
+      unpack(v[j], y);
 #pragma unroll
-        for (int e = 0; e < kVec<E>; ++e) y[e] *= a.scale;
-        *reinterpret_cast<uint4*>(to) = repack(y);
-      } else {
-        *to = narrow<E>(x[j] * a.scale);
-      }
+      for (int e = 0; e < kVec<E>; ++e) y[e] *= a.scale;
+      *reinterpret_cast<uint4*>(static_cast<E*>(a.y) + t[j] * a.ld_y + c[j]) = repack(y);
     }
   }
-}
-template <class E>
-const void* embed_fn(bool vec, bool ahead) {
-  return vec ? ahead ? (const void*)embed_kernel<E, true, 4> : (const void*)embed_kernel<E, true, 1>
-             : ahead ? (const void*)embed_kernel<E, false, 4> : (const void*)embed_kernel<E, false, 1>;
 }
 
 // ---- order -----------------------------------------------------------------
@@ -302,6 +286,32 @@ struct Eight<E, false> {
       if (c0 + lane + 32 * j < D) row[c0 + lane + 32 * j] = narrow<E>(x[j]);
   }
 };
+// Rows looked up that do not all start on 16 bytes: a warp for 256 columns of one.
+template <class E>
+__global__ void __launch_bounds__(kEmbedThreads) embed_odd_kernel(const __grid_constant__ LookupArgs a) {
+  grid_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t n = a.T * a.per;
+  for (int64_t i = (int64_t)blockIdx.x * (kEmbedThreads / 32) + (threadIdx.x >> 5); i < n;
+       i += (int64_t)gridDim.x * (kEmbedThreads / 32)) {
+    const int64_t t = n < (1ll << 32) ? (uint32_t)i / a.per : i / a.per, c0 = (i - t * a.per) * kColumns;
+    const int64_t id = load_id(a.ids, a.id_bytes, t);
+    float x[8] = {};
+    if (id >= 0 && id < a.V) {
+      Eight<E, false> v;
+      v.load(static_cast<const E*>(a.table) + id * a.ld, c0, lane, a.D);
+      v.get(x);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] *= a.scale;
+    Eight<E, false>::store(static_cast<E*>(a.y) + t * a.ld_y, c0, lane, a.D, x);
+  }
+}
+template <class E>
+const void* embed_fn(bool vec, bool ahead) {
+  return !vec ? (const void*)embed_odd_kernel<E> : ahead ? (const void*)embed_kernel<E, 4> : (const void*)embed_kernel<E, 1>;
+}
+
 using Part8 = Eight<float, true>;       // (a lane's 8 columns side by side, whichever they are)
 
 template <class W>
@@ -526,11 +536,11 @@ extern "C" int bkmoo_embedding_forward(const void* table, int64_t ld_table, int3
   if (T == 0) return BKMOO_OK;
   if (!matrix_ok(y, dtype, T, D, ldy) || !aligned_at(ids, id_bytes)) return BKMOO_ERR_INVALID;
   const bool vec = on_vectors(table, dtype, D, ld_table) && on_vectors(y, dtype, D, ldy);
-  const int n = vec ? (int)(16 / float_bytes(dtype)) : 1;
-  LookupArgs a = {table, ids, y, ld_table, ldy, T, V, id_bytes, (uint32_t)D, (uint32_t)(D / n), (float)scale};
-  const bool ahead = T * a.per > 152 * 2048;
+  const int64_t per = vec ? D * (int64_t)float_bytes(dtype) / 16 : up_by(D, kColumns);
+  LookupArgs a = {table, ids, y, ld_table, ldy, T, V, id_bytes, (uint32_t)D, (uint32_t)per, (float)scale};
+  const bool ahead = vec && T * per > 152 * 2048;
   const void* fn = dtype == BKMOO_F32 ? embed_fn<float>(vec, ahead) : embed_fn<__nv_bfloat16>(vec, ahead);
-  const int64_t ctas = up_by(T * a.per, kEmbedThreads * (ahead ? 4 : 1)), most = 1 << 20;
+  const int64_t ctas = up_by(T * per, vec ? kEmbedThreads * (ahead ? 4 : 1) : kEmbedThreads / 32), most = 1 << 20;
   void* list[] = {&a};
   return launch_behind(fn, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kEmbedThreads), list, 0,
                        static_cast<cudaStream_t>(stream), true) == cudaSuccess
