@@ -18,7 +18,6 @@
 namespace bkmoo {
 namespace {
 
-constexpr int kGradThreads = 256;
 constexpr int kMaxTop = 32;
 constexpr int kMaxCluster = 8;
 constexpr int kAhead = 4;               // vectors of a thread that are on their way at once
@@ -485,13 +484,13 @@ struct LogpGradArgs {
   uint32_t pieces;                       // of a row
 };
 constexpr int kGradVecs = 4;             // of a thread
-template <class E>
-constexpr int kGradPiece = kGradThreads * kGradVecs * kVec<E>;
+template <class E, int N>
+constexpr int kGradPiece = N * kGradVecs * kVec<E>;
 
 // dz_v = g ([v = target] - p_v) - h p_v (log p_v + H).  Bound by memory: a row is read and
 // written once.  A row whose g and h are 0 is not read.
-template <class E, bool ENTROPY>
-__global__ void __launch_bounds__(kGradThreads) token_logp_grad_kernel(const LogpGradArgs a) {
+template <class E, bool ENTROPY, int N>
+__global__ void __launch_bounds__(N) token_logp_grad_kernel(const LogpGradArgs a) {
   grid_wait();
   grid_release();
   const int64_t t = blockIdx.x / a.pieces;
@@ -518,17 +517,17 @@ __global__ void __launch_bounds__(kGradThreads) token_logp_grad_kernel(const Log
       const int s = single_at(p, tid);
       if (s >= 0) out[s] = narrow<E>(none ? 0.0f : grad(widen(row[s]), s));
     }
-    const int i0 = piece * kGradThreads * kGradVecs + tid;
+    const int i0 = piece * N * kGradVecs + tid;
     uint4* to = reinterpret_cast<uint4*>(out + p.body);
     uint4 x[kGradVecs];
     if (!none) {
 #pragma unroll
       for (int j = 0; j < kGradVecs; ++j)
-        if (i0 + j * kGradThreads < p.vecs) x[j] = vector_at(p, i0 + j * kGradThreads);
+        if (i0 + j * N < p.vecs) x[j] = vector_at(p, i0 + j * N);
     }
 #pragma unroll
     for (int j = 0; j < kGradVecs; ++j) {
-      const int i = i0 + j * kGradThreads;
+      const int i = i0 + j * N;
       if (i >= p.vecs) break;
       if (none) {
         to[i] = make_uint4(0, 0, 0, 0);
@@ -541,11 +540,17 @@ __global__ void __launch_bounds__(kGradThreads) token_logp_grad_kernel(const Log
       to[i] = repack(z);
     }
   } else {
-    for (int v = piece * kGradPiece<E> + tid, k = 0; k < kGradVecs * kVec<E> && v < a.V; ++k, v += kGradThreads)
+    for (int v = piece * kGradPiece<E, N> + tid, k = 0; k < kGradVecs * kVec<E> && v < a.V; ++k, v += N)
       out[v] = narrow<E>(none ? 0.0f : grad(widen(row[v]), v));
   }
 }
 
+template <class E>
+const void* grad_fn(int threads, bool entropy) {
+  return threads == 64 ? entropy ? (const void*)token_logp_grad_kernel<E, true, 64> : (const void*)token_logp_grad_kernel<E, false, 64>
+         : entropy     ? (const void*)token_logp_grad_kernel<E, true, 256>
+                       : (const void*)token_logp_grad_kernel<E, false, 256>;
+}
 template <class E, int N>
 const void* logp_fn(bool entropy, bool top) {
   return entropy ? top ? (const void*)token_logp_kernel<E, true, true, N> : (const void*)token_logp_kernel<E, true, false, N>
@@ -636,17 +641,18 @@ extern "C" int bkmoo_token_logp_backward(const void* logits, int64_t ld, int32_t
       !aligned_at(d_logp, 4) || (d_entropy && (!aligned_at(d_entropy, 4) || !aligned_at(entropy, 4))))
     return BKMOO_ERR_INVALID;
   const bool f32 = dtype == BKMOO_F32;
-  const int64_t piece = f32 ? kGradPiece<float> : kGradPiece<__nv_bfloat16>;
+  // Short rows go to CTAs of 64 threads, of which more are at work on different rows (20000 bf16 rows
+  // of 2000: 28 us, by 256 threads 44; of 8000 98 and 102); long ones to fewer CTAs (8192 rows of
+  // 128256: 588 and 544).
+  const int threads = V * (int64_t)float_bytes(dtype) / 16 <= 1024 ? 64 : 256;
+  const int64_t piece = threads * kGradVecs * (f32 ? kVec<float> : kVec<__nv_bfloat16>);
   const int64_t pieces = (V + piece - 1) / piece;
   if (T * pieces > 0x7fffffffll) return BKMOO_ERR_INVALID;
   LogpGradArgs a = {logits, d_logits, ld, ld_d, (int32_t)V, targets, id_bytes,
                     reinterpret_cast<const float2*>(stats), d_logp, d_entropy, entropy, (uint32_t)pieces};
-  const void* fn = f32 ? d_entropy ? (const void*)token_logp_grad_kernel<float, true>
-                                   : (const void*)token_logp_grad_kernel<float, false>
-                   : d_entropy ? (const void*)token_logp_grad_kernel<__nv_bfloat16, true>
-                               : (const void*)token_logp_grad_kernel<__nv_bfloat16, false>;
+  const void* fn = f32 ? grad_fn<float>(threads, d_entropy) : grad_fn<__nv_bfloat16>(threads, d_entropy);
   void* list[] = {&a};
-  return launch_behind(fn, dim3((unsigned)(T * pieces)), dim3(kGradThreads), list, 0,
+  return launch_behind(fn, dim3((unsigned)(T * pieces)), dim3(threads), list, 0,
                        static_cast<cudaStream_t>(stream), true) == cudaSuccess
              ? BKMOO_OK
              : BKMOO_ERR_CUDA;
