@@ -159,12 +159,12 @@ __device__ __forceinline__ float over_head(float v) {
   return v;
 }
 
-// A warp's way through steps: groups of 32 / G heads, the queries' of a token and then its
-// keys', token after token.  at: the lane's head in one array, behind the last of them no matter where.
+// A warp's way through steps: 32 / G heads of a token, its queries' and then its keys', token after
+// token.  at: the lane's head in one array; over: the heads from there on, 0 or less behind the last.
 template <class E>
 struct Way {
   int64_t t;
-  int k, left, over;                    // the side, its steps from here, its heads from the lane's
+  int step, over;
   E* at;
 };
 
@@ -177,35 +177,36 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
   grid_release();
   __shared__ Numbers room[kQkWarps], weights[2];
   __shared__ Pair ring[kQkWarps][kAhead];
+  constexpr int kHeads = 32 / G;
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const int per = a.side[0].steps + a.side[1].steps, step_elems = 32 / G * a.hd;
+  const int queries = a.side[0].heads, heads = queries + a.side[1].heads, per = (heads + kHeads - 1) / kHeads;
+  // the first steps with a key and without a query
+  const int some = queries / kHeads, none = (queries + kHeads - 1) / kHeads, step_elems = kHeads * a.hd;
   const int64_t total = a.T * per, from = ((int64_t)blockIdx.x * kQkWarps + wid) * each;
   const int64_t to = from + each < total ? from + each : total;
   const int steps = from < to ? (int)(to - from) : 0;
   const Place p = place_of_lane<NEIGHBOURS>(a, lane % G);
-  // to step i of a side of a token
-  auto set = [&](auto& w, auto* const x, int64_t ld, int i) {
-    const int head = i * (32 / G) + lane / G;
-    w.left = a.side[w.k].steps - i;
-    w.over = p.live ? a.side[w.k].heads - head : 0;
-    w.at = x + w.t * ld + (int64_t)head * a.hd;
+  auto side_of = [&](int step) { return step * kHeads + lane / G >= queries; };
+  auto set = [&](auto& w, auto* const x, int64_t ld) {       // to its token's and step's head
+    const int head = w.step * kHeads + lane / G;
+    w.over = p.live ? heads - head : 0;
+    w.at = x + w.t * ld + (int64_t)(head >= queries ? head - queries : head) * a.hd;
   };
+  auto set_in = [&](Way<const __nv_bfloat16>& w) { set(w, a.side[side_of(w.step)].x, a.side[side_of(w.step)].ld); };
+  auto set_out = [&](Way<__nv_bfloat16>& w) { set(w, a.side[side_of(w.step)].out, a.side[side_of(w.step)].ld_out); };
   Way<const __nv_bfloat16> there;
   Way<__nv_bfloat16> here;
-  {
-    const int step = (int)(from % per), k = step >= a.side[0].steps, i = step - (k ? a.side[0].steps : 0);
-    here.t = there.t = from / per;
-    here.k = there.k = k;
-    set(there, a.side[k].x, a.side[k].ld, i);
-    set(here, a.side[k].out, a.side[k].ld_out, i);
-  }
-  // whether the side ends
+  here.t = there.t = from / per;
+  here.step = there.step = (int)(from % per);
+  set_in(there);
+  set_out(here);
+  // whether a token begins, or its keys
   auto next = [&](auto& w) {
-    w.over -= 32 / G;
+    w.over -= kHeads;
     w.at += step_elems;
-    if (--w.left > 0) return false;
-    w.k ^= 1;
-    if (w.k == 0) ++w.t;
+    if (++w.step < per) return w.step == some || w.step == none;
+    w.step = 0;
+    ++w.t;
     return true;
   };
   int ahead = 0, slot = 0, slot_there = 0;
@@ -214,7 +215,7 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
     copy_pair(ring[wid][slot_there], there.at, a.side[0].x, p, lane, live);
     copies_end();
     slot_there = next_slot(slot_there);
-    if (next(there)) set(there, a.side[there.k].x, a.side[there.k].ld, 0);
+    if (next(there)) set_in(there);
     ++ahead;
   };
 #pragma unroll
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
       }
       float g[16], w[16];
       room[wid].get(lane % G, g);
-      weights[here.k].get(lane % G, w);
+      weights[side_of(here.step)].get(lane % G, w);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float wa = w[NEIGHBOURS ? 2 * j : j], wb = w[NEIGHBOURS ? 2 * j + 1 : j + 8];
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
     if (here.over > 0) store_pair(here.at, p, x);
     const int64_t t = here.t;
     begins = next(here);
-    if (begins) set(here, a.side[here.k].out, a.side[here.k].ld_out, 0);
+    if (begins) set_out(here);
     new_token = here.t != t;
   }
   copies_wait_all();
@@ -504,7 +505,8 @@ extern "C" int bkmoo_qk_norm_forward(const void* q, int64_t ldq, const void* k, 
   int ctas = 0;
   if (tile_sms(&ctas) != BKMOO_OK) return BKMOO_ERR_CUDA;
   ctas *= kForwardCtas;
-  const int64_t total = T * (a.side[0].steps + a.side[1].steps);
+  const int at_once = 32 / g;
+  const int64_t total = T * ((q_heads + k_heads + at_once - 1) / at_once);
   int64_t each = (total + (int64_t)ctas * kQkWarps - 1) / ((int64_t)ctas * kQkWarps);
   const int64_t grid = (total + each * kQkWarps - 1) / (each * kQkWarps);
   void* list[] = {&a, &each};
