@@ -272,9 +272,9 @@ __global__ void __launch_bounds__(kQkThreads, kForwardCtas) qk_norm_kernel(const
 
 // The backward pass by CTAs that each take a run of one side's and one language's steps, and leave
 // their sums of the weights' gradients.  8192 tokens of 32 + 8 heads of 128 in 4 languages take
-// 46 us (5.5 TB/s), of which 3 are the sums' kernel; 5 CTAs on an SM 53, for which registers go to
-// memory, 3 CTAs 55.  w and the angles are read from shared memory for every step: the
-// registers hold the sums.  Runs of neighbouring steps: tokens dealt out in turn take 53.
+// 44 us (5.8 TB/s), of which 3 are the sums' kernel.  4 CTAs on an SM: when it took 46, 5 CTAs, whose
+// registers go to memory, took 53, 3 CTAs 55, and tokens dealt out in turn instead of in runs 53.
+// w and the angles are read from shared memory for every step: the registers hold the sums.
 struct QkRuns {
   int32_t K, weights;
   int32_t first[2 * kMaxK + 1];         // CTAs of (side, language), side by side
