@@ -25,6 +25,7 @@ may be alive during the capture: autograd would tie it to that pass's stream.
 from __future__ import annotations
 
 import collections
+import ctypes
 import functools
 
 import torch
@@ -291,28 +292,48 @@ class Embedding(torch.nn.Module):
         return _Embedding.apply(ids, self.weight, self.scale, rows)
 
 
-_frequencies = functools.lru_cache(maxsize=None)(native.rope_frequencies)
+# Arrays that kernels read; no caller is handed one.
+_frequencies = functools.lru_cache(maxsize=64)(native.rope_frequencies)
+
+
+@functools.lru_cache(maxsize=64)
+def _given_frequencies(inv_freq):
+    return (ctypes.c_double * len(inv_freq))(*inv_freq)
 
 
 class QueryKeyNorm(torch.nn.Module):
     """Queries [..., heads, width] and keys [..., key heads, width] normed head by head, scaled by
-    a weight each and their first `rotated` elements turned by the token's position."""
+    a weight each and their first `rotated` elements turned by the token's position: by
+    base^(-2i / rotated) radians a position, or by `inv_freq`, rotated / 2 numbers of the layer's own."""
 
-    def __init__(self, width: int, rotated=None, base: float = 10000.0, interleaved=False, eps: float = 1e-6, device="cuda"):
+    _given = None
+
+    def __init__(self, width: int, rotated=None, base: float = 10000.0, interleaved=False, eps: float = 1e-6, device="cuda",
+                 inv_freq=None):
         super().__init__()
         self.eps, self.interleaved = eps, interleaved
-        self.rotated, self.base = width if rotated is None else rotated, base
+        if inv_freq is not None:
+            self._given = tuple(float(f) for f in inv_freq)
+            rotated = 2 * len(self._given) if rotated is None else rotated
+            if 2 * len(self._given) != rotated:
+                raise ValueError("inv_freq must be rotated / 2 numbers, %d rotated, got %d" % (rotated, len(self._given)))
+        rotated = width if rotated is None else rotated
+        self.rotated, self.base = rotated, base
         self.w_q, self.w_k = (torch.nn.Parameter(torch.ones(width, device=device, dtype=torch.bfloat16)) for _ in range(2))
+
+    def _array(self):
+        return _frequencies(self.rotated, self.base) if self._given is None else _given_frequencies(self._given)
 
     @property
     def inv_freq(self):
-        return _frequencies(self.rotated, self.base)
+        """The frequencies, a copy."""
+        return tuple(self._array())
 
     def forward(self, q, k, positions, rows=None):
         if q.shape[:-2] != k.shape[:-2] or positions.shape != q.shape[:-2]:
             raise ValueError("queries, keys and positions must have the same tokens, got %s, %s and %s"
                              % (tuple(q.shape[:-2]), tuple(k.shape[:-2]), tuple(positions.shape)))
-        return _QueryKeyNorm.apply(q, k, self.w_q, self.w_k, positions, self.inv_freq, self.eps, self.interleaved, rows)
+        return _QueryKeyNorm.apply(q, k, self.w_q, self.w_k, positions, self._array(), self.eps, self.interleaved, rows)
 
 
 class LanguageLinear(torch.nn.Module):

@@ -1,0 +1,42 @@
+"""CPU: more of what the layers of test_language_model_cpu.py do around the kernels."""
+import copy
+import pickle
+
+import pytest
+import torch
+
+from paper_2606_05613_gb300 import native
+from paper_2606_05613_gb300.language import QueryKeyNorm
+from test_language_model_cpu import _plain, _qk      # noqa: F401 (a fixture)
+
+
+def test_a_layers_frequencies_are_its_own():
+    """What a layer hands out cannot be written into another layer, or into a pass whose
+    backward is still to come."""
+    a, fused, q, k, pos = _qk()
+    b = QueryKeyNorm(32, rotated=16, device="cpu")
+    want = [10000.0 ** (-i / 8) for i in range(8)]
+    qo, ko = a(q, k, pos)
+    (ref,) = torch.autograd.grad((qo.float().sum() + ko.float().sum()), fused, retain_graph=True)
+    with pytest.raises(TypeError):
+        a.inv_freq[3] = 9.0
+    assert list(a.inv_freq) == want and list(b.inv_freq) == want
+    (again,) = torch.autograd.grad((qo.float().sum() + ko.float().sum()), fused)
+    assert torch.equal(again, ref)
+
+
+def test_a_layer_takes_frequencies():
+    base, fused, q, k, pos = _qk()
+    slow = [f / 4 for f in base.inv_freq]
+    layer = QueryKeyNorm(32, device="cpu", inv_freq=slow)
+    layer.load_state_dict(base.state_dict())
+    slow[0] = 7.0                                 # (the caller's list stays the caller's)
+    assert layer.rotated == 16 and layer.inv_freq == tuple(f / 4 for f in base.inv_freq)
+    # a quarter of the frequency is the same turn at four times the position
+    got, want = layer(q, k, 4 * pos), base(q, k, pos)
+    assert all(torch.equal(u, v) for u, v in zip(got, want))
+    for other in (pickle.loads(pickle.dumps(layer)), copy.deepcopy(layer)):
+        assert other.inv_freq == layer.inv_freq
+    for bad in (dict(rotated=32), dict(rotated=15)):
+        with pytest.raises(ValueError, match="inv_freq"):
+            QueryKeyNorm(32, device="cpu", inv_freq=layer.inv_freq, **bad)
