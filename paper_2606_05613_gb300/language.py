@@ -318,6 +318,8 @@ class QueryKeyNorm(torch.nn.Module):
             if 2 * len(self._given) != rotated:
                 raise ValueError("inv_freq must be rotated / 2 numbers, %d rotated, got %d" % (rotated, len(self._given)))
         rotated = width if rotated is None else rotated
+        if rotated % 16 or not 0 <= rotated <= width:
+            raise ValueError("rotated must be a multiple of 16 from 0 to the width, %d, got %s" % (width, rotated))
         self.rotated, self.base = rotated, base
         self.w_q, self.w_k = (torch.nn.Parameter(torch.ones(width, device=device, dtype=torch.bfloat16)) for _ in range(2))
 

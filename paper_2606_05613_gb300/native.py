@@ -687,6 +687,8 @@ def bkmoo_embedding_backward(dy, ids, rows, dw, scale=1.0, accumulate=False, ws=
 def rope_frequencies(rot: int, base: float):
     """The rotation's frequencies base^(-2i / rot), radians a position, for the calls below
     (which take any sequence of them)."""
+    if rot < 0 or rot % 2:
+        raise ValueError("rot must be even and not negative, got %s" % rot)
     n = rot // 2
     return (ctypes.c_double * n)(*[base ** (-2.0 * i / rot) for i in range(n)])
 

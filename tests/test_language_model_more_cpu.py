@@ -40,3 +40,18 @@ def test_a_layer_takes_frequencies():
     for bad in (dict(rotated=32), dict(rotated=15)):
         with pytest.raises(ValueError, match="inv_freq"):
             QueryKeyNorm(32, device="cpu", inv_freq=layer.inv_freq, **bad)
+
+
+@pytest.mark.parametrize("rotated", [17, 33, 8, 24, -16, 48])
+def test_widths_that_cannot_be_rotated_are_refused(rotated):
+    """17 elements were turned as 16 of them, by the frequencies of 17."""
+    with pytest.raises(ValueError, match="rotated must be"):
+        QueryKeyNorm(32, rotated=rotated, device="cpu")
+    layer, _, q, k, pos = _qk()
+    if rotated % 2:
+        with pytest.raises(ValueError, match="even"):
+            native.rope_frequencies(rotated, 1e4)
+        layer.rotated = rotated                   # (an attribute that may be set)
+        with pytest.raises(ValueError, match="even"):
+            layer(q, k, pos)
+    assert len(native.rope_frequencies(0, 1e4)) == 0 and QueryKeyNorm(32, rotated=0, device="cpu").inv_freq == ()
