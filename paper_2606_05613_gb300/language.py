@@ -213,13 +213,13 @@ class _QueryKeyNorm(torch.autograd.Function):
 
         for t in to:
             _enter(t)
-        if all(to) and (to[0][2] is None) == (to[1][2] is None):
+        if all(to) and (to[0][2] is None) == (to[1][2] is None) and to[0][0] is not to[1][0]:
             call(to[0][1], to[0][0], to[1][0])
         elif not any(to):
             call([0, T])
         else:
-            # one of them is frozen, or they are apart by different bounds: each with a place
-            # beside it for what the other one would get
+            # one of them is frozen, they are apart by different bounds, or they are one parameter:
+            # each with a place beside it for what the other one would get
             for i, t in enumerate(to):
                 if t is not None:
                     other = [torch.zeros_like(g) for g in t[0]]

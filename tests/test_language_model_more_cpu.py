@@ -7,7 +7,7 @@ import torch
 
 from paper_2606_05613_gb300 import native
 from paper_2606_05613_gb300.language import QueryKeyNorm
-from test_language_model_cpu import _plain, _qk      # noqa: F401 (a fixture)
+from test_language_model_cpu import ROWS, _close, _places, _plain, _qk      # noqa: F401 (a fixture)
 
 
 def test_a_layers_frequencies_are_its_own():
@@ -55,3 +55,33 @@ def test_widths_that_cannot_be_rotated_are_refused(rotated):
         with pytest.raises(ValueError, match="even"):
             layer(q, k, pos)
     assert len(native.rope_frequencies(0, 1e4)) == 0 and QueryKeyNorm(32, rotated=0, device="cpu").inv_freq == ()
+
+
+@pytest.mark.parametrize("apart", [True, False])
+def test_one_weight_for_both_norms(monkeypatch, apart):
+    """Queries' and keys' gradients of it add up; the call itself takes no places that overlap."""
+    real = native.bkmoo_qk_norm_backward
+
+    def strict(*a, **k):
+        places = [*(a[11] or ()), *(a[12] or ())]
+        assert len({p.data_ptr() for p in places}) == len(places)
+        return real(*a, **k)
+
+    monkeypatch.setattr(native, "bkmoo_qk_norm_backward", strict)
+    layer, fused, q, k, pos = _qk()
+    apart_layer, fused2, q2, k2, _ = _qk()
+    layer.w_k = layer.w_q
+    with torch.no_grad():
+        apart_layer.w_k.copy_(apart_layer.w_q)
+    if apart:
+        for w in (layer.w_q, apart_layer.w_q, apart_layer.w_k):
+            _places(w)
+    for m, a, b in ((layer, q, k), (apart_layer, q2, k2)):
+        qo, ko = m(a, b, pos, ROWS)
+        (qo.float().square().sum() + ko.float().square().sum()).backward()
+    assert torch.equal(fused.grad, fused2.grad)
+    got = layer.w_q.language_grads if apart else [layer.w_q.grad]
+    each = zip(apart_layer.w_q.language_grads, apart_layer.w_k.language_grads) if apart else [(apart_layer.w_q.grad, apart_layer.w_k.grad)]
+    for g, (u, v) in zip(got, each):
+        # each part is rounded to bf16, and their sum
+        assert float((g.double() - (u.double() + v.double())).norm()) <= 2.0 ** -8 * float(u.double().norm() + v.double().norm() + g.double().norm())
