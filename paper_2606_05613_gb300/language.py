@@ -99,14 +99,14 @@ class _Gate(torch.autograd.Function):
               for w, need in zip((w_gate, w_up), ctx.needs_input_grad[1:3])]
         for t in to:
             _enter(t)
-        if all(to) and (to[0][2] is None) == (to[1][2] is None):
+        if all(to) and (to[0][2] is None) == (to[1][2] is None) and to[0][0] is not to[1][0]:
             native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, to[0][1], dx, to[0][0], to[1][0],
                                        accumulate=True)
         elif not any(to):
             native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, [0, T], dx)
         else:
-            # one of them is frozen, or they are apart by different bounds: da and db, which
-            # the call leaves in its workspace, and each weight's gradients from its own
+            # one of them is frozen, they are apart by different bounds, or they are one parameter:
+            # da and db, which the call leaves in its workspace, and each weight's gradients from its own
             ws = m.new_empty(native.bkmoo_gate_backward_workspace_size(T, F), dtype=torch.uint8)
             native.bkmoo_gate_backward(dh, a, b, m, g, u, ctx.act, [0, T],
                                        dx if dx is not None else _room(m, T, D), ws=ws)
