@@ -474,13 +474,17 @@ class _Room:
     def __init__(self, torch, nbytes: int, dev: int, stream):
         self.at = None
         if nbytes:
-            raw, alloc = _raw_stream(torch, stream, dev), torch._C._cuda_cudaCachingAllocator_raw_alloc
-            if torch.cuda.current_device() == dev:
+            # (both are private names of torch: where they are gone, its public ones)
+            raw, c = _raw_stream(torch, stream, dev), torch._C
+            alloc = getattr(c, "_cuda_cudaCachingAllocator_raw_alloc", None)
+            self.free = getattr(c, "_cuda_cudaCachingAllocator_raw_delete", None) or torch.cuda.caching_allocator_delete
+            if alloc is None:
+                self.at = torch.cuda.caching_allocator_alloc(nbytes, dev, raw)
+            elif torch.cuda.current_device() == dev:
                 self.at = alloc(nbytes, raw)
             else:
                 with torch.cuda.device(dev):
                     self.at = alloc(nbytes, raw)
-            self.free = torch._C._cuda_cudaCachingAllocator_raw_delete
 
     def __del__(self):
         if self.at is not None:

@@ -1,6 +1,7 @@
 """CPU: more of what the layers of test_language_model_cpu.py do around the kernels."""
 import copy
 import pickle
+import types
 
 import pytest
 import torch
@@ -85,3 +86,26 @@ def test_one_weight_for_both_norms(monkeypatch, apart):
     for g, (u, v) in zip(got, each):
         # each part is rounded to bf16, and their sum
         assert float((g.double() - (u.double() + v.double())).norm()) <= 2.0 ** -8 * float(u.double().norm() + v.double().norm() + g.double().norm())
+
+
+@pytest.mark.parametrize("private", [True, False])
+def test_workspaces_from_the_allocators_public_entries(monkeypatch, private):
+    """The quicker entries that torch does not document are taken where they are there."""
+    notes, names = [], ["_cuda_cudaCachingAllocator_raw_alloc", "_cuda_cudaCachingAllocator_raw_delete"]
+    for name in names:
+        monkeypatch.setattr(torch._C, name, None, raising=False)
+        monkeypatch.delattr(torch._C, name)
+    if private:
+        monkeypatch.setattr(torch._C, names[0], lambda size, stream: notes.append((size, stream)) or 512, raising=False)
+        monkeypatch.setattr(torch._C, names[1], lambda at: notes.append(at), raising=False)
+    else:
+        monkeypatch.setattr(torch.cuda, "caching_allocator_alloc",
+                            lambda size, device=None, stream=None: notes.append((size, stream)) or (512 if device == 0 else 0))
+        monkeypatch.setattr(torch.cuda, "caching_allocator_delete", lambda at: notes.append(at))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    stream = types.SimpleNamespace(cuda_stream=7)
+    room = native._Room(torch, 100, 0, stream)
+    assert room.at == 512
+    del room
+    native._Room(torch, 0, 0, stream)
+    assert notes == [(100, 7), 512]
