@@ -103,6 +103,20 @@ __device__ __forceinline__ void take(Sums& r, const float (&z)[N]) {
     if (ENTROPY) r.u = fmaf(e, fmaxf(x, kLowest), r.u);
   }
 }
+// Where a thread has more than kLongBatches batches of a row (2048 bf16 logits, 1024 fp32 ones), its sums
+// so far are put aside after as many, and begin again: in one fp32 sum of n terms each of them may be off
+// by n 2^-24 of itself, and all to the same side where the logits are alike.  A row of 2^27 fp32 logits
+// of two values was 9e-4 off in log s.  A kernel of its own: 600 bf16 rows of 2^21 take 425 us with it and
+// 417 without, and the same steps in the kernel for the other rows cost those 1%.
+constexpr int kLongBatches = 64;
+constexpr int kLongVecs = kLongBatches * kAhead * 256;       // of a CTA
+template <bool ENTROPY>
+__device__ __forceinline__ void put_aside(Sums& r, Sums& aside) {
+  raise<ENTROPY>(aside, r.m);            // (r's maximum is never the lower one)
+  aside.s += r.s;
+  if (ENTROPY) aside.u += r.u;
+  r.s = r.u = 0.0f;
+}
 // The largest of a vector, NaN aside.
 __device__ __forceinline__ float largest(const uint4& v, float) {
   return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
@@ -369,7 +383,7 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 // 128256 bf16 294 us (7.1 TB/s), with the entropy 296, with the 20 likeliest too 350; 1531 x
 // 50257 fp32 52, 50 and 59 us.  One row of 151936 takes 4.0 us and 6.8, a chain of latencies.
 // 6 CTAs of 256 to an SM leave 40 registers: at 5, 1531 rows are two rounds and a little.
-template <class E, bool ENTROPY, bool TOP, int N>
+template <class E, bool ENTROPY, bool TOP, int N, bool LONG = false>
 __global__ void __launch_bounds__(N, N == 32 ? 32 : 1536 / N) token_logp_kernel(const LogpArgs a, const int parts) {
   grid_wait();
   grid_release();
@@ -381,28 +395,41 @@ __global__ void __launch_bounds__(N, N == 32 ? 32 : 1536 / N) token_logp_kernel(
   const int64_t target = load_id(a.targets, a.id_bytes, t);
   Sums r = {-INFINITY, 0.0f, 0.0f};
   Best best = {-INFINITY, -INFINITY, p.first + tid};
-  for (int i = p.first + tid; i < p.last; i += kAhead * N) {
-    uint4 v[kAhead];
-    float top = -INFINITY;
+  auto batches = [&](int i0, int end) {
+    for (int i = i0; i < end; i += kAhead * N) {
+      uint4 v[kAhead];
+      float top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (i + j * N < p.last) v[j] = vector_at(p, i + j * N);
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j * N < p.last) v[j] = vector_at(p, i + j * N);
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (i + j * N < p.last) top = fmaxf(top, largest(v[j], E()));
-    const float old = r.m;
-    if (raise<ENTROPY>(r, top)) {
-      if (TOP) best.second = old, best.at = i;
-    } else if (TOP) {
-      best.second = fmaxf(best.second, top);
+      for (int j = 0; j < kAhead; ++j)
+        if (i + j * N < p.last) top = fmaxf(top, largest(v[j], E()));
+      const float old = r.m;
+      if (raise<ENTROPY>(r, top)) {
+        if (TOP) best.second = old, best.at = i;
+      } else if (TOP) {
+        best.second = fmaxf(best.second, top);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i + j * N >= p.last) break;
+        float z[kVec<E>];
+        unpack(v[j], z);
+        take<ENTROPY>(r, z);
+      }
     }
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (i + j * N >= p.last) break;
-      float z[kVec<E>];
-      unpack(v[j], z);
-      take<ENTROPY>(r, z);
+  };
+  if (LONG) {
+    __shared__ Sums aside[N];
+    aside[tid] = r;
+    for (int from = p.first; from < p.last; from += kLongVecs) {
+      batches(from + tid, min(from + kLongVecs, p.last));
+      put_aside<ENTROPY>(r, aside[tid]);
     }
+    r = aside[tid];
+  } else {
+    batches(p.first + tid, p.last);
   }
   best.first = r.m;
   const int single = single_at(p, tid);
@@ -551,17 +578,18 @@ const void* grad_fn(int threads, bool entropy) {
          : entropy     ? (const void*)token_logp_grad_kernel<E, true, 256>
                        : (const void*)token_logp_grad_kernel<E, false, 256>;
 }
-template <class E, int N>
+template <class E, int N, bool LONG = false>
 const void* logp_fn(bool entropy, bool top) {
-  return entropy ? top ? (const void*)token_logp_kernel<E, true, true, N> : (const void*)token_logp_kernel<E, true, false, N>
-         : top   ? (const void*)token_logp_kernel<E, false, true, N>
-                 : (const void*)token_logp_kernel<E, false, false, N>;
+  return entropy ? top ? (const void*)token_logp_kernel<E, true, true, N, LONG> : (const void*)token_logp_kernel<E, true, false, N, LONG>
+         : top   ? (const void*)token_logp_kernel<E, false, true, N, LONG>
+                 : (const void*)token_logp_kernel<E, false, false, N, LONG>;
 }
 template <class E>
-const void* logp_fn(int threads, bool entropy, bool top, size_t* room) {
+const void* logp_fn(int threads, bool is_long, bool entropy, bool top, size_t* room) {
   *room = !top ? 0 : threads == 32 ? sizeof(TopRoom<E, 32>) : threads == 128 ? sizeof(TopRoom<E, 128>) : sizeof(TopRoom<E, 256>);
   return threads == 32    ? logp_fn<E, 32>(entropy, top)
          : threads == 128 ? logp_fn<E, 128>(entropy, top)
+         : is_long        ? logp_fn<E, 256, true>(entropy, top)
                           : logp_fn<E, 256>(entropy, top);
 }
 
@@ -608,8 +636,9 @@ extern "C" int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t 
   const bool many = T * parts >= 8 * sms;
   const int threads = vecs < (many ? 768 : 256) ? 32 : vecs < (many ? 6000 : 1024) ? 128 : 256;
   size_t room = 0;
-  const void* fn = f32 ? logp_fn<float>(threads, entropy, n_top > 0, &room)
-                       : logp_fn<__nv_bfloat16>(threads, entropy, n_top > 0, &room);
+  const bool is_long = vecs > kLongVecs;
+  const void* fn = f32 ? logp_fn<float>(threads, is_long, entropy, n_top > 0, &room)
+                       : logp_fn<__nv_bfloat16>(threads, is_long, entropy, n_top > 0, &room);
   void* list[] = {&a, &parts};
   cudaLaunchConfig_t cfg = {};
   // (the kernel waits at its top for the one ahead of it: launch_behind)
