@@ -479,9 +479,10 @@ int bkmoo_language_wgrad(const void* dy, int64_t ld_dy, const void* x, int64_t l
  * embedding at its front, the norms of queries and keys, and the log probabilities at its
  * end.  Common to the calls below: `ids`, `positions` and `targets` are device arrays
  * [T] of int32 (id_bytes 4) or int64 (8).  rows, dw pointers, dw_dtype and accumulate
- * are those of bkmoo_gate_backward.  Sums are fp32 in an order fixed by the sizes and
- * bounds: the same call gives the same bits.  Results are rounded once.  T = 0 queues
- * nothing (gradients that are not added to are set to 0).
+ * are those of bkmoo_gate_backward.  Sums are fp32 in an order fixed by the sizes, the
+ * bounds and, but for the embedding, the device's number of SMs: the same call on the same
+ * kind of device gives the same bits.  Results are rounded once.  T = 0 queues nothing
+ * (gradients that are not added to are set to 0).
  *
  * bkmoo_embedding_forward -- y_t = scale W[id_t].  table: [V][D] of dtype (fp32 or bf16)
  * with rows of ld_table elements, y: [T][D] of the same with rows of ldy, both at any
@@ -522,9 +523,10 @@ int bkmoo_embedding_backward(const void* dy, int64_t ld_dy, int32_t dtype, const
  * head_dim: a multiple of 16 up to 256; rot: a multiple of 16 up to head_dim, 0 for none.
  * q_out may be q, with the same stride, and k_out k; otherwise nothing overlaps.  w_q, w_k:
  * [head_dim] of w_dtype (fp32 or bf16).  inv_freq: host, rot / 2 radians a position (read
- * before the call returns); positions may be negative or as far as 2^40: the angle's
- * fraction of a turn is exact to 2^-32 (and to the rounding of inv_freq).  Squares are summed
- * in fp32, so elements beyond 1.8e19 leave nothing of their head.
+ * before the call returns); positions may be negative.  An angle is off by at most 2^-26 of
+ * a turn and, for every position, by 2^-64 of a turn and 2^-52 of its own inv_freq / 2 pi (inv_freq
+ * = 1: 2^-34 at position 2^20, 2^-14 at 2^40).  Squares are summed in fp32, so elements beyond 1.8e19
+ * leave nothing of their head.
  */
 int bkmoo_qk_norm_forward(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* w_q,
                           const void* w_k, int32_t w_dtype, int64_t T, int64_t q_heads,

@@ -340,6 +340,7 @@ __device__ __forceinline__ float* part_row(const SumArgs& a, int64_t piece, int 
 // A warp's piece: places a.piece * piece and on, 256 columns from c0.  What begins before the
 // piece goes to its first part, what goes on behind it to its second.  kRowsAhead rows, and
 // the places that they are added to, are on their way at once.
+// (8 CTAs an SM leave 64 registers: of bf16 sums by vectors 28 bytes a thread go to memory.)
 constexpr int kSumThreads = 128;
 constexpr int kRowsAhead = 4;
 template <class E, class W, bool VEC>
@@ -494,7 +495,7 @@ bool embed_sizes_ok(int64_t T, int64_t V, int64_t D, double scale) {
 
 // Places of a warp's piece: as many as leave 2432 warps (16 for each of 152 SMs), 8 to 32.
 // 600 rows of 768 bf16 in 4 languages, added, take 12, 14 and 18 us by pieces of 8, 16 and 32;
-// 8192 of 2048 24, 21 and 23; 65536 of 768 83, 76 and 75.
+// 8192 of 2048 23, 21 and 22; 65536 of 768 79, 72 and 71.
 int piece_of(int64_t T, int64_t blocks) {
   int piece = 32;
   while (piece > 8 && up_by(T, piece) * blocks < 2432) piece /= 2;

@@ -8,7 +8,9 @@
 //
 // A position's angle in turns is pos f / 2 pi, of which only the fraction counts.  The
 // frequency is kept as a 64-bit fraction of a turn, so that the product modulo 2^64 is that
-// fraction, exact however far the position is, without a number of 64 bits' precision.
+// fraction, without floating point in 64 bits.  The product is exact; the angle is off by what
+// the frequency is, times the position: f / 2 pi has two roundings in 64-bit floating point (2^-52 of
+// itself) and is cut to 2^-64 of a turn; and by 2^-26 of a turn where the fraction becomes fp32.
 #include <math.h>
 
 #include "tile_host.cuh"

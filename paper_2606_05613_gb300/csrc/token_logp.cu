@@ -380,9 +380,10 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 // A row by a cluster of CTAs (one, two, four or eight), each a part of it.  Memory-bound: 8192 x
-// 128256 bf16 294 us (7.1 TB/s), with the entropy 296, with the 20 likeliest too 350; 1531 x
-// 50257 fp32 52, 50 and 59 us.  One row of 151936 takes 4.0 us and 6.8, a chain of latencies.
-// 6 CTAs of 256 to an SM leave 40 registers: at 5, 1531 rows are two rounds and a little.
+// 128256 bf16 291 to 295 us (7.2 TB/s), with the entropy 299, with the 20 likeliest too 353; 1531 x
+// 50257 fp32 51, 49 and 59 us.  One row of 151936 takes 3.8 us and 7, a chain of latencies.
+// 6 CTAs of 256 to an SM leave 40 registers (of fp32 with entropy and likeliest 12 bytes go to memory):
+// at 5, 1531 rows are two rounds and a little.
 template <class E, bool ENTROPY, bool TOP, int N, bool LONG = false>
 __global__ void __launch_bounds__(N, N == 32 ? 32 : 1536 / N) token_logp_kernel(const LogpArgs a, const int parts) {
   grid_wait();
@@ -514,8 +515,11 @@ constexpr int kGradVecs = 4;             // of a thread
 template <class E, int N>
 constexpr int kGradPiece = N * kGradVecs * kVec<E>;
 
-// dz_v = g ([v = target] - p_v) - h p_v (log p_v + H).  Bound by memory: a row is read and
-// written once.  A row whose g and h are 0 is not read.
+// dz_v = g ([v = target] - p_v) - h p_v (log p_v + H).  A row is read and written once; one whose g
+// and h are 0 is not read.  Bound by memory where a row of the result starts at the same place of
+// 16 bytes as the logits': 8192 x 50257 bf16 256 us, 4096 fp32 233.  Others go element by element, a load
+// on its way at a time: 702 and 380 us with rows of the result padded to 50264, of which 7 of 8 (fp32:
+// 3 of 4) start elsewhere.
 template <class E, bool ENTROPY, int N>
 __global__ void __launch_bounds__(N) token_logp_grad_kernel(const LogpGradArgs a) {
   grid_wait();
@@ -631,8 +635,9 @@ extern "C" int bkmoo_token_logp_forward(const void* logits, int64_t ld, int32_t 
   // Threads a row (a warp alone, 128 or 256): the fewer, the less of a row's time goes into what
   // its threads do together, but a long row by few is slow.  20000 bf16 rows of 2000: 15, 27 and
   // 45 us, the 20 likeliest 48, 83 and 143; 4096 of 10007: 14, 14.5 and 18 (31, 29, 40); 1500
-  // fp32 of 262144: 359, 219 and 240 (750, 273, 256).  Where rows are few, latency counts:
-  // 20 rows of 4000 3.2, 2.2 and 2.3 (8.4, 4.5, 4.2).
+  // fp32 of 262144: 359, 219 and 240 (750, 273, 256): there 256 is the better choice with the
+  // likeliest only, as 1500 rows fit the card once by 128 threads and not by 256, which this does not
+  // look at.  Where rows are few, latency counts: 20 rows of 4000 3.2, 2.2 and 2.3 (8.4, 4.5, 4.2).
   const bool many = T * parts >= 8 * sms;
   const int threads = vecs < (many ? 768 : 256) ? 32 : vecs < (many ? 6000 : 1024) ? 128 : 256;
   size_t room = 0;
