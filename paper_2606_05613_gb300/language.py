@@ -164,11 +164,12 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ids, weight, scale, rows):
         flat = ids.reshape(-1).contiguous()
-        y = weight.new_empty(flat.numel(), weight.shape[1])
-        native.bkmoo_embedding_forward(_matrix(weight), flat, y, scale)
+        # (results are no views, here and below: they may be changed in place)
+        y = weight.new_empty(*ids.shape, weight.shape[1])
+        native.bkmoo_embedding_forward(_matrix(weight), flat, y.view(-1, weight.shape[1]), scale)
         ctx.save_for_backward(flat, weight)
         ctx.scale, ctx.rows = scale, rows
-        return y.view(*ids.shape, weight.shape[1])
+        return y
 
     @staticmethod
     @once_differentiable
@@ -189,12 +190,12 @@ class _QueryKeyNorm(torch.autograd.Function):
         a, b = _on_heads(q), _on_heads(k)
         u, v = w_q.contiguous(), w_k.contiguous()
         pos = positions.reshape(-1).contiguous()
-        qo, ko = torch.empty(a.shape, dtype=a.dtype, device=a.device), torch.empty(b.shape, dtype=b.dtype, device=b.device)
-        native.bkmoo_qk_norm_forward(a, b, u, v, pos, inv_freq, qo, ko, eps, interleaved)
+        qo, ko = torch.empty(q.shape, dtype=a.dtype, device=a.device), torch.empty(k.shape, dtype=b.dtype, device=b.device)
+        native.bkmoo_qk_norm_forward(a, b, u, v, pos, inv_freq, qo.view(a.shape), ko.view(b.shape), eps, interleaved)
         ctx.save_for_backward(a, b, w_q, w_k, pos)
         ctx.fixed = inv_freq, eps, interleaved
         ctx.rows, ctx.shapes = rows, (q.shape, k.shape)
-        return qo.view(q.shape), ko.view(k.shape)
+        return qo, ko
 
     @staticmethod
     @once_differentiable
@@ -236,19 +237,20 @@ class _TokenLogProbs(torch.autograd.Function):
         z, lead = _matrix(logits), logits.shape[:-1]
         t = targets.reshape(-1).contiguous()
         T = z.shape[0]
-        logp, stats = torch.empty(T, device=z.device), torch.empty(T, 2, device=z.device)
-        H = torch.empty(T, device=z.device) if entropy else None
-        ids = torch.empty(T, top, dtype=torch.int64, device=z.device) if top else None
-        best = torch.empty(T, top, device=z.device) if top else None
-        native.bkmoo_token_logp_forward(z, t, logp, stats, H, ids, best)
+        logp, stats = torch.empty(lead, device=z.device), torch.empty(T, 2, device=z.device)
+        H = torch.empty(lead, device=z.device) if entropy else None
+        ids = torch.empty(*lead, top, dtype=torch.int64, device=z.device) if top else None
+        best = torch.empty(*lead, top, device=z.device) if top else None
+        native.bkmoo_token_logp_forward(z, t, logp.view(T), stats, None if H is None else H.view(T),
+                                        *((ids.view(T, top), best.view(T, top)) if top else ()))
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(z, t, stats, H)
         ctx.shape = logits.shape
-        out = [logp.view(lead)]
+        out = [logp]
         if entropy:
-            out.append(H.view(lead))
+            out.append(H)
         if top:
-            out += [ids.view(*lead, top), best.view(*lead, top)]
+            out += [ids, best]
             ctx.mark_non_differentiable(*out[-2:])
         return tuple(out)
 
@@ -259,7 +261,8 @@ class _TokenLogProbs(torch.autograd.Function):
         h = more[0] if H is not None else None
         g = torch.zeros(z.shape[0], device=z.device) if g is None else g.reshape(-1).contiguous()
         dz = _room(z, *z.shape)
-        native.bkmoo_token_logp_backward(z, t, stats, g, dz, H, None if h is None else h.reshape(-1).contiguous())
+        native.bkmoo_token_logp_backward(z, t, stats, g, dz, None if H is None else H.view(-1),
+                                         None if h is None else h.reshape(-1).contiguous())
         return dz.reshape(ctx.shape), None, None, None
 
 
@@ -270,7 +273,8 @@ def token_log_probs(logits, targets, entropy=False, top=0):
     """Log probability of each row's target (0 where it is outside the vocabulary: padding), and
     where asked for the rows' entropy and their `top` (32 at most) most likely tokens with their
     log probabilities.  logits [..., vocabulary], float32 or bfloat16; targets [...], int64
-    or int32.  logp and entropy have gradients."""
+    or int32.  logp and entropy have gradients; the backward pass reads entropy, so it is not to be
+    changed in place ahead of that."""
     if targets.shape != logits.shape[:-1]:
         raise ValueError("one target for each row of logits, got %s and %s" % (tuple(targets.shape), tuple(logits.shape)))
     out = list(_TokenLogProbs.apply(logits, targets, entropy, top))

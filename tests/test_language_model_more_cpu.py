@@ -7,8 +7,8 @@ import pytest
 import torch
 
 from paper_2606_05613_gb300 import native
-from paper_2606_05613_gb300.language import QueryKeyNorm
-from test_language_model_cpu import ROWS, _close, _places, _plain, _qk      # noqa: F401 (a fixture)
+from paper_2606_05613_gb300.language import QueryKeyNorm, token_log_probs
+from test_language_model_cpu import ROWS, _embedding, _gen, _places, _plain, _qk      # noqa: F401 (a fixture)
 
 
 def test_a_layers_frequencies_are_its_own():
@@ -109,3 +109,29 @@ def test_workspaces_from_the_allocators_public_entries(monkeypatch, private):
     del room
     native._Room(torch, 0, 0, stream)
     assert notes == [(100, 7), 512]
+
+
+@pytest.mark.parametrize("lead", [(2, 5), (10,), (0, 5)])
+def test_results_may_be_changed_in_place(lead):
+    """x = embedding(ids); x += positions, and the like: the gradients are those of x = x + positions."""
+    got = []
+    for place in (True, False):
+        emb, ids = _embedding(scale=2.0)
+        x = emb(ids.reshape(-1)[:torch.Size(lead).numel()].view(lead))
+        d = torch.randn(x.shape, generator=_gen(1)).bfloat16()
+        x = x.add_(d) if place else x + d
+        (x.float() ** 2).sum().backward()
+        norm, fused, q, k, pos = _qk()
+        q, k, pos = (t.flatten(0, 1)[:torch.Size(lead).numel()].view(*lead, *t.shape[2:]) for t in (q, k, pos))
+        a, b = norm(q, k, pos)
+        a, b = (a.mul_(0.5), b.add_(1.0)) if place else (a * 0.5, b + 1.0)
+        ((a.float() ** 2).sum() + (b.float() ** 2).sum()).backward()
+        z = torch.randn(*lead, 13, generator=_gen(2)).requires_grad_()
+        t = torch.randint(0, 13, lead, generator=_gen(3))
+        out = token_log_probs(z, t, entropy=True, top=2)
+        skip = t < 4
+        lp = out.logp.masked_fill_(skip, 0.0) if place else out.logp.masked_fill(skip, 0.0)
+        assert lp.shape == out.entropy.shape == lead and out.top_ids.shape == (*lead, 2)
+        ((lp ** 2).sum() + out.entropy.sum()).backward()
+        got.append([x, emb.weight.grad, a, b, fused.grad, norm.w_q.grad, norm.w_k.grad, lp, z.grad])
+    assert all(torch.equal(u, v) for u, v in zip(*got))
