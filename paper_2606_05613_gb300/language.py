@@ -237,10 +237,11 @@ class _TokenLogProbs(torch.autograd.Function):
         z, lead = _matrix(logits), logits.shape[:-1]
         t = targets.reshape(-1).contiguous()
         T = z.shape[0]
-        logp, stats = torch.empty(lead, device=z.device), torch.empty(T, 2, device=z.device)
-        H = torch.empty(lead, device=z.device) if entropy else None
+        f32 = dict(dtype=torch.float32, device=z.device)
+        logp, stats = torch.empty(lead, **f32), torch.empty(T, 2, **f32)
+        H = torch.empty(lead, **f32) if entropy else None
         ids = torch.empty(*lead, top, dtype=torch.int64, device=z.device) if top else None
-        best = torch.empty(*lead, top, device=z.device) if top else None
+        best = torch.empty(*lead, top, **f32) if top else None
         native.bkmoo_token_logp_forward(z, t, logp.view(T), stats, None if H is None else H.view(T),
                                         *((ids.view(T, top), best.view(T, top)) if top else ()))
         ctx.set_materialize_grads(False)
@@ -259,7 +260,7 @@ class _TokenLogProbs(torch.autograd.Function):
     def backward(ctx, g, *more):
         z, t, stats, H = ctx.saved_tensors
         h = more[0] if H is not None else None
-        g = torch.zeros(z.shape[0], device=z.device) if g is None else g.reshape(-1).contiguous()
+        g = torch.zeros(z.shape[0], dtype=torch.float32, device=z.device) if g is None else g.reshape(-1).contiguous()
         dz = _room(z, *z.shape)
         native.bkmoo_token_logp_backward(z, t, stats, g, dz, None if H is None else H.view(-1),
                                          None if h is None else h.reshape(-1).contiguous())

@@ -135,3 +135,17 @@ def test_results_may_be_changed_in_place(lead):
         ((lp ** 2).sum() + out.entropy.sum()).backward()
         got.append([x, emb.weight.grad, a, b, fused.grad, norm.w_q.grad, norm.w_k.grad, lp, z.grad])
     assert all(torch.equal(u, v) for u, v in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float64])
+def test_log_probs_are_32_bit_under_any_default(dtype):
+    z = torch.randn(5, 13, generator=_gen(2)).requires_grad_()
+    t = torch.randint(0, 13, (5,), generator=_gen(3))
+    torch.set_default_dtype(dtype)
+    try:
+        out = token_log_probs(z, t, entropy=True, top=2)
+        assert all(v.dtype is torch.float32 for v in (out.logp, out.entropy, out.top_logp))
+        out.entropy.sum().backward()
+    finally:
+        torch.set_default_dtype(torch.float32)
+    assert z.grad.dtype is torch.float32
